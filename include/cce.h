@@ -71,7 +71,8 @@ enum {
 
 enum {
     CCE_STATUS_BAD_LABEL = 1,  /* some label was outside [0, V) and not ignore_index */
-    CCE_STATUS_ROW_BOUND = 2   /* cce_*_compact: more valid rows than max_valid_rows; results are incomplete */
+    CCE_STATUS_ROW_BOUND = 2,  /* cce_*_compact: more valid rows than max_valid_rows; results are incomplete */
+    CCE_STATUS_BAD_TOKEN = 4   /* cce_embedding_*: some token was outside [0, V) and not ignore_index */
 };
 
 /* Library version, "major.minor.patch". Host only. */

@@ -21,6 +21,8 @@ CCE_ERR_HIP = -3
 CCE_ERR_TOO_LARGE = -4
 STATIC_SCRATCH_BYTES = 16 << 20
 CCE_STATUS_BAD_LABEL = 1
+CCE_STATUS_BAD_TOKEN = 4
+STATE8_BLOCK = 128
 
 EXPORTED_SYMBOLS = [
     "cce_version", "cce_strerror", "cce_last_hip_error", "cce_workspace_bytes",
@@ -42,10 +44,22 @@ EXPORTED_SYMBOLS = [
     "cce_get_row_skipping", "cce_set_row_skipping", "cce_get_compact_tiling",
     # include/cce_fp8.h
     "cce_fp8_scale_bytes", "cce_quantize_e4m3", "cce_fp8_forward", "cce_fp8_backward",
+    # include/cce_embed.h
+    "cce_embedding_forward", "cce_embedding_workspace_bytes", "cce_embedding_backward",
+    # include/cce_optim.h
+    "cce_sumsq_multi_workspace_bytes", "cce_grad_sumsq_multi", "cce_adamw_multi_step", "cce_adamw_state8_read",
 ]
 KERNEL_FAMILIES = ["lse_partial_kernel", "grad_tile_kernel", "grad_gemm_kernel"]
 
 _lib = None
+
+
+class _OptimTensor(ctypes.Structure):
+    """cce_optim_tensor of include/cce_optim.h."""
+    _fields_ = [("param", ctypes.c_void_p), ("param_bf16", ctypes.c_void_p), ("grad", ctypes.c_void_p),
+                ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("lr_scale", ctypes.c_float), ("weight_decay", ctypes.c_float),
+                ("grad_bf16", ctypes.c_int32), ("state8", ctypes.c_int32)]
 
 
 class CCEError(RuntimeError):
@@ -164,6 +178,20 @@ def lib() -> ctypes.CDLL:
     L.cce_fp8_forward.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i32, vp, vp, vp, sz, vp]
     L.cce_fp8_backward.restype = ctypes.c_int
     L.cce_fp8_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i32, vp, vp, ctypes.c_int, vp, sz, vp]
+    L.cce_embedding_forward.restype = ctypes.c_int
+    L.cce_embedding_forward.argtypes = [vp, vp, i64, i64, i64, i32, f32, vp, vp, vp]
+    L.cce_embedding_workspace_bytes.restype = sz
+    L.cce_embedding_workspace_bytes.argtypes = [i64, i64, i64]
+    L.cce_embedding_backward.restype = ctypes.c_int
+    L.cce_embedding_backward.argtypes = [vp, vp, i64, i64, i64, i32, f32, vp, ctypes.c_int, vp, vp, sz, vp]
+    L.cce_sumsq_multi_workspace_bytes.restype = sz
+    L.cce_sumsq_multi_workspace_bytes.argtypes = [i64]
+    L.cce_grad_sumsq_multi.restype = ctypes.c_int
+    L.cce_grad_sumsq_multi.argtypes = [vp, i64, vp, ctypes.c_int, f32, f32, vp, vp, sz, vp]
+    L.cce_adamw_multi_step.restype = ctypes.c_int
+    L.cce_adamw_multi_step.argtypes = [vp, i64, f32, f32, f32, f32, i64, vp, ctypes.c_uint32, vp]
+    L.cce_adamw_state8_read.restype = ctypes.c_int
+    L.cce_adamw_state8_read.argtypes = [vp, vp, i64, ctypes.c_int, vp, vp]
     _lib = L
     return L
 
@@ -922,3 +950,243 @@ def cce_backward_compact_ex(hidden: torch.Tensor, weight: torch.Tensor, labels: 
                                       d_hidden.data_ptr(), d_weight.data_ptr(), 1 if accumulate_dw else 0,
                                       workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)), "cce_backward_compact_ex")
     return d_hidden, d_weight
+
+
+# ---------------------------------------------------------------- include/cce_embed.h
+
+def _check_on(device: torch.device, t: torch.Tensor, dtype, shape, name):
+    _check(t, dtype, shape, name)
+    if t.device != device:
+        raise ValueError(f"{name}: expected a tensor on {device}, got one on {t.device}")
+
+
+def _new(shape, dtype, device: torch.device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """A tensor whose memory belongs to the stream that the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _call(where: str, fn, device: torch.device, stream: Optional[torch.cuda.Stream], *args) -> None:
+    """fn(*args, stream) with `device` current; the stream is the given one or the device's current one."""
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    elif stream.device != device:
+        raise ValueError(f"stream: expected one of {device}, got one of {stream.device}")
+    if torch.cuda.current_device() == device.index:
+        rc = fn(*args, stream.cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, stream.cuda_stream)
+    if rc != CCE_OK:
+        raise CCEError(rc, where)
+
+
+def cce_embedding_forward(tokens: torch.Tensor, weight: torch.Tensor, ignore_index: int = -100, *, scale: float = 1.0,
+                          out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """bf16 [N, D]: scale * weight[tokens]; zero rows for ignore_index and for tokens outside the matrix (the
+    latter OR CCE_STATUS_BAD_TOKEN into `status`, int32 [1], if given)."""
+    N, = tokens.shape
+    V, D = weight.shape
+    device = weight.device
+    _check_on(device, tokens, torch.int32, (N,), "tokens")
+    _check(weight, torch.bfloat16, (V, D), "weight")
+    if out is None:
+        out = _new((N, D), torch.bfloat16, device, stream)
+    else:
+        _check_on(device, out, torch.bfloat16, (N, D), "out")
+    if status is not None:
+        _check_on(device, status, torch.int32, (1,), "status")
+    _call("cce_embedding_forward", lib().cce_embedding_forward, device, stream, tokens.data_ptr(), weight.data_ptr(), N, D, V,
+          ignore_index, scale, out.data_ptr(), status.data_ptr() if status is not None else None)
+    return out
+
+
+def embedding_workspace_bytes(N: int, D: int, V: int) -> int:
+    return int(lib().cce_embedding_workspace_bytes(N, D, V))
+
+
+def cce_embedding_backward(tokens: torch.Tensor, d_out: torch.Tensor, V: int, ignore_index: int = -100, *,
+                           scale: float = 1.0, d_weight: Optional[torch.Tensor] = None, accumulate_dw: bool = False,
+                           status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                           stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """dW fp32 [V, D] of cce_embedding_forward for the gradient d_out bf16 [N, D] of its output; with accumulate_dw
+    it is added to d_weight (tied embeddings: the dW of cce_backward)."""
+    N, D = d_out.shape
+    device = d_out.device
+    _check(d_out, torch.bfloat16, (N, D), "d_out")
+    _check_on(device, tokens, torch.int32, (N,), "tokens")
+    if d_weight is None:
+        if accumulate_dw:
+            raise ValueError("accumulate_dw needs an existing d_weight")
+        d_weight = _new((V, D), torch.float32, device, stream)
+    else:
+        _check_on(device, d_weight, torch.float32, (V, D), "d_weight")
+    if status is not None:
+        _check_on(device, status, torch.int32, (1,), "status")
+    if workspace is None:
+        n = embedding_workspace_bytes(N, D, V)
+        if n == 0:
+            raise CCEError(CCE_ERR_UNSUPPORTED, "cce_embedding_workspace_bytes")
+        workspace = _new((n,), torch.uint8, device, stream)
+    else:
+        _check_on(device, workspace, torch.uint8, (workspace.numel(),), "workspace")
+    _call("cce_embedding_backward", lib().cce_embedding_backward, device, stream, tokens.data_ptr(), d_out.data_ptr(), N, D, V,
+          ignore_index, scale, d_weight.data_ptr(), 1 if accumulate_dw else 0,
+          status.data_ptr() if status is not None else None, workspace.data_ptr(), workspace.numel())
+    return d_weight
+
+
+# ---------------------------------------------------------------- include/cce_optim.h
+
+class OptimTensors:
+    """The tensors of an optimizer step, made once and given to every step (it keeps them alive).
+
+    grads             fp32 or bf16, of any shape, contiguous; the other lists are parallel to it
+    params, m, v      fp32 parameters and moments, of as many values; moments in 8 bits are uint8 and have a scale
+                      byte per STATE8_BLOCK values in m_scales and v_scales (zeros before the first step)
+    params_bf16       None, or the bf16 copies to keep (None for a tensor without one)
+    lr_scale, weight_decay   a number, or one for each tensor
+    params, m and v may be left out for cce_grad_sumsq_multi alone.  Memory that a step writes may not overlap any
+    other of the list."""
+
+    def __init__(self, grads, params=None, m=None, v=None, *, params_bf16=None, m_scales=None, v_scales=None,
+                 lr_scale=1.0, weight_decay=0.0):
+        count = len(grads)
+        if count == 0:
+            raise ValueError("grads: expected at least one tensor")
+        if (params is None) != (m is None) or (params is None) != (v is None):
+            raise ValueError("params, m and v: expected all three or none")
+        self.steps = params is not None
+        self.device = grads[0].device
+        self._array = (_OptimTensor * count)()
+        lists = {"params": params, "m": m, "v": v, "params_bf16": params_bf16, "m_scales": m_scales, "v_scales": v_scales}
+        lists = {name: [None] * count if x is None else list(x) for name, x in lists.items()}
+        rates = {name: list(x) if hasattr(x, "__len__") else [x] * count
+                 for name, x in (("lr_scale", lr_scale), ("weight_decay", weight_decay))}
+        for name, x in [*lists.items(), *rates.items()]:
+            if len(x) != count:
+                raise ValueError(f"{name}: expected {count} entries, got {len(x)}")
+        self._keep = lists
+        self._take_grads(grads, [g.numel() for g in grads])
+        if not self.steps:
+            return
+        for i, entry in enumerate(self._array):
+            n, blocks = entry.n, (entry.n + STATE8_BLOCK - 1) // STATE8_BLOCK
+            state = lists["m"][i].dtype if lists["m"][i] is not None else None
+            if state not in (torch.float32, torch.uint8):
+                raise ValueError(f"m[{i}]: expected float32 or uint8, got {state}")
+            entry.state8 = int(state == torch.uint8)
+            wanted = [("param", "params", torch.float32, n), ("m", "m", state, n), ("v", "v", state, n)]
+            if lists["params_bf16"][i] is not None:
+                wanted.append(("param_bf16", "params_bf16", torch.bfloat16, n))
+            if entry.state8:
+                wanted += [("m_scale", "m_scales", torch.uint8, blocks), ("v_scale", "v_scales", torch.uint8, blocks)]
+            for field, name, dtype, values in wanted:
+                setattr(entry, field, self._pointer(name, i, lists[name][i], dtype, values))
+            entry.lr_scale, entry.weight_decay = rates["lr_scale"][i], rates["weight_decay"][i]
+
+    def __len__(self):
+        return len(self._array)
+
+    def _pointer(self, name, i, t, dtype, n):
+        if t is None or t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != self.device:
+            got = "None" if t is None else f"{t.dtype} of {t.numel()} contiguous={t.is_contiguous()} on {t.device}"
+            raise ValueError(f"{name}[{i}]: expected a contiguous {dtype} tensor of {n} elements on {self.device}, got {got}")
+        return t.data_ptr()
+
+    def _take_grads(self, grads, sizes):
+        for i, g in enumerate(grads):
+            if g.dtype not in (torch.float32, torch.bfloat16) or not g.is_cuda:
+                raise ValueError(f"grads[{i}]: expected a cuda float32 or bfloat16 tensor, got {g.dtype} on {g.device}")
+        pointers = [self._pointer("grads", i, g, g.dtype, n) for i, (g, n) in enumerate(zip(grads, sizes))]
+        self._keep["grads"] = list(grads)
+        self._check_overlap()
+        for entry, g, pointer, n in zip(self._array, grads, pointers, sizes):
+            entry.grad, entry.n, entry.grad_bf16 = pointer, n, int(g.dtype == torch.bfloat16)
+
+    def set_grads(self, grads):
+        """Other gradients for the same parameters (a step whose gradients lie elsewhere)."""
+        if len(grads) != len(self):
+            raise ValueError(f"grads: expected {len(self)} tensors, got {len(grads)}")
+        old = self._keep["grads"]
+        try:
+            self._take_grads(grads, [entry.n for entry in self._array])
+        except ValueError:
+            self._keep["grads"] = old
+            raise
+
+    def _check_overlap(self):
+        spans = []
+        for name, tensors in self._keep.items():
+            spans += [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), name != "grads", f"{name}[{i}]")
+                      for i, t in enumerate(tensors) if t is not None and t.numel()]
+        spans.sort()
+        last = written = (0, 0, False, "")                 # of the spans so far those that end last, of all and of the written ones
+        for span in spans:
+            other = last if span[2] else written
+            if span[0] < other[1]:
+                raise ValueError(f"{span[3]} overlaps {other[3]}")
+            last = max(last, span, key=lambda s: s[1])
+            written = max(written, span, key=lambda s: s[1]) if span[2] else written
+
+
+def cce_grad_sumsq_multi(tensors: OptimTensors, sumsq: Optional[torch.Tensor] = None, accumulate: bool = False, *,
+                         max_norm: Optional[float] = None, eps_norm: float = 1e-6, clip_coef: Optional[torch.Tensor] = None,
+                         workspace: Optional[torch.Tensor] = None,
+                         stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """(device fp64 [1]: sum of squares of all gradients, added to `sumsq` when accumulate; device fp32 [1]: the clipping
+    coefficient for max_norm, or None without one)."""
+    device = tensors.device
+    if sumsq is None:
+        if accumulate:
+            raise ValueError("accumulate needs an existing sumsq")
+        sumsq = _new((1,), torch.float64, device, stream)
+    else:
+        _check_on(device, sumsq, torch.float64, (1,), "sumsq")
+    if max_norm is None:
+        if clip_coef is not None:
+            raise ValueError("clip_coef needs max_norm")
+    elif clip_coef is None:
+        clip_coef = _new((1,), torch.float32, device, stream)
+    else:
+        _check_on(device, clip_coef, torch.float32, (1,), "clip_coef")
+    if workspace is None:
+        workspace = _new((int(lib().cce_sumsq_multi_workspace_bytes(len(tensors))),), torch.uint8, device, stream)
+    else:
+        _check_on(device, workspace, torch.uint8, (workspace.numel(),), "workspace")
+    _call("cce_grad_sumsq_multi", lib().cce_grad_sumsq_multi, device, stream, tensors._array, len(tensors), sumsq.data_ptr(),
+          1 if accumulate else 0, max_norm if max_norm is not None else 0.0, eps_norm,
+          clip_coef.data_ptr() if clip_coef is not None else None, workspace.data_ptr(), workspace.numel())
+    return sumsq, clip_coef
+
+
+def cce_adamw_multi_step(tensors: OptimTensors, step: int, *, lr: float, beta1: float = 0.9, beta2: float = 0.999,
+                         eps: float = 1e-8, clip_coef: Optional[torch.Tensor] = None, seed: int = 0,
+                         stream: Optional[torch.cuda.Stream] = None) -> None:
+    """In-place AdamW step on all tensors of the list; `seed` of the rounding of moments in 8 bits."""
+    if not tensors.steps:
+        raise ValueError("tensors: the list has gradients alone")
+    if clip_coef is not None:
+        _check_on(tensors.device, clip_coef, torch.float32, (1,), "clip_coef")
+    _call("cce_adamw_multi_step", lib().cce_adamw_multi_step, tensors.device, stream, tensors._array, len(tensors), lr, beta1, beta2,
+          eps, step, clip_coef.data_ptr() if clip_coef is not None else None, seed & 0xFFFFFFFF)
+
+
+def cce_adamw_state8_read(codes: torch.Tensor, scales: torch.Tensor, *, second: bool = False,
+                          out: Optional[torch.Tensor] = None,
+                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """fp32, shaped like `codes` (uint8): the first moment that 8-bit codes stand for, or the second one."""
+    device = codes.device
+    _check(codes, torch.uint8, codes.shape, "codes")
+    n = codes.numel()
+    _check_on(device, scales, torch.uint8, ((n + STATE8_BLOCK - 1) // STATE8_BLOCK,), "scales")
+    if out is None:
+        out = _new(codes.shape, torch.float32, device, stream)
+    else:
+        _check_on(device, out, torch.float32, codes.shape, "out")
+    _call("cce_adamw_state8_read", lib().cce_adamw_state8_read, device, stream, codes.data_ptr(), scales.data_ptr(), n,
+          1 if second else 0, out.data_ptr())
+    return out

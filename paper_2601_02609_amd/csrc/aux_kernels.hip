@@ -12,42 +12,14 @@
 #include "../../include/cce_aux.h"
 #include "../../include/cce_fp8.h"
 #include "host_util.h"
+#include "vec_util.h"
 
 namespace cce {
-
-typedef __attribute__((ext_vector_type(4))) unsigned int au32x4;
-typedef __attribute__((ext_vector_type(4))) float af32x4;
 
 constexpr int kNormMaxChunks = 16;      // 16-byte chunks per lane and row: D <= 16 * 64 * 8 = 8192
 constexpr int kNormBackwardBlocks = 512;        // D <= 1024: four rows in flight per workgroup
 constexpr int kNormBackwardBlocksWide = 1024;   // wider rows: two rows or one
 constexpr int kSumsqBlocks = 1024;
-
-__device__ __forceinline__ void unpack8(const au32x4& p, float (&f)[8]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(p[i] << 16);
-        f[2 * i + 1] = __uint_as_float(p[i] & 0xffff0000u);
-    }
-}
-
-__device__ __forceinline__ au32x4 pack8(const float (&f)[8]) {
-    au32x4 p;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        union { __bf16 h[2]; unsigned int u; } cv;
-        cv.h[0] = (__bf16)f[2 * i];
-        cv.h[1] = (__bf16)f[2 * i + 1];
-        p[i] = cv.u;
-    }
-    return p;
-}
-
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o);
-    return x;
-}
 
 // ------------------------------------------------------------------------------------------
 // RMSNorm forward (RMSNorm definition; fused forward kernel: one pass, rstd cached).

@@ -1,0 +1,199 @@
+"""GPU parity of the embedding lookup and its gradient with the fp64 oracle.
+
+Tolerances, from the arithmetic: the lookup is one fp32 product rounded to bf16, the same bits as NumPy's.  A sum of
+n fp32 terms in any order is off by at most (n - 1) 2^-24 of the sum of their magnitudes; the scale and the
+addition to dW round once more each: (n + 2) 2^-24 of what the oracle calls the size."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import embedding_oracle as E
+from paper_2601_02609_amd import inputs as I
+from tests.gpu_util import bf16_dev
+
+pytestmark = pytest.mark.gpu
+IGN = -100
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2601_02609_amd import binding
+    binding.lib()
+    return binding
+
+
+def _bits(x):
+    return I.f32_to_bf16_bits(np.asarray(x, dtype=np.float32))
+
+
+def _tokens(rng, N, V, kind, ignore):
+    if kind == "zipf":
+        p = np.arange(1, V + 1) ** -1.2
+        t = rng.choice(V, N, p=p / p.sum())
+    elif kind == "one":
+        t = np.full(N, V - 1)
+    elif kind == "runs":                                                    # every token 31 times: sums that end inside any piece
+        t = rng.permutation(np.arange(N) // 31 % V)
+    else:
+        t = rng.integers(0, V, N)
+    t = t.astype(np.int32)
+    t[rng.random(N) < ignore] = IGN
+    return t
+
+
+def _guarded(shape, dtype):
+    """A tensor in the middle of a larger one, and a check that its surroundings are as they were."""
+    n = int(np.prod(shape))
+    whole = torch.full((n + 2048,), 7.0, dtype=dtype, device="cuda")
+    return whole[1024:1024 + n].view(shape), lambda: bool((whole[:1024] == 7).all() and (whole[1024 + n:] == 7).all())
+
+
+@pytest.mark.parametrize("N,D,V,kind,ignore,scale", [
+    (1, 8, 1, "uniform", 0.0, 1.0), (1, 896, 5000, "uniform", 0.0, 29.933), (3, 24, 7, "zipf", 0.4, -0.5), (257, 64, 1000, "uniform", 0.1, 1.0),
+    (1000, 896, 3001, "zipf", 0.15, 29.933), (63, 4096, 100, "zipf", 0.3, 64.0), (5, 65536, 3, "uniform", 0.0, 2.0), (2049, 1032, 33, "one", 0.2, 1.0),
+    (100, 72, 50, "uniform", 1.0, 3.0)])
+def test_lookup_is_the_rounded_product(B, N, D, V, kind, ignore, scale):
+    rng = np.random.default_rng(N + D)
+    w, t = _bits(rng.standard_normal((V, D))), _tokens(rng, N, V, kind, ignore)
+    print(f"[lookup] N={N} D={D} V={V}", flush=True)
+    out, intact = _guarded((N, D), torch.bfloat16)
+    B.cce_embedding_forward(torch.from_numpy(t).cuda(), bf16_dev(w), IGN, scale=scale, out=out)
+    got = out.view(torch.int16).cpu().numpy().view(np.uint16)
+    want = np.zeros((N, D), dtype=np.uint16)
+    ok = E.takes_part(t, V, IGN)
+    want[ok] = _bits(np.float32(scale) * I.bf16_bits_to_f32(w[t[ok]]))
+    assert np.array_equal(got, want) and intact()
+    assert np.array_equal(E.forward(I.bf16_bits_to_f32(w[:, :8]).astype(np.float64), t, IGN, 1.0)[ok], I.bf16_bits_to_f32(w[t[ok], :8]))
+
+
+def _gradient_case(B, N, D, V, kind, ignore, scale, accumulate, seed=0):
+    rng = np.random.default_rng(N + D + V + seed)
+    t = _tokens(rng, N, V, kind, ignore)
+    dy = _bits(rng.standard_normal((N, D)) * np.exp(rng.uniform(-3, 3, (N, 1))))
+    ok = E.takes_part(t, V, IGN)
+    dy[~ok] = 0x7FC0                                                        # NaN where no token takes part
+    dw0 = rng.standard_normal((V, D)).astype(np.float32)
+    dw, intact = _guarded((V, D), torch.float32)
+    dw.copy_(torch.from_numpy(dw0) if accumulate else torch.full((V, D), float("nan")))
+    print(f"[gradient] N={N} D={D} V={V} {kind} accumulate={accumulate}", flush=True)
+    B.cce_embedding_backward(torch.from_numpy(t).cuda(), bf16_dev(dy), V, IGN, scale=scale, d_weight=dw, accumulate_dw=accumulate)
+    got = dw.cpu().numpy()
+    want, size = E.backward(I.bf16_bits_to_f32(dy).astype(np.float64), t, V, IGN, float(np.float32(scale)), dw0 if accumulate else None)
+    count = np.bincount(t[ok], minlength=V)
+    assert np.all(np.abs(got - want) <= (count[:, None] + 2) * 2.0 ** -24 * size)
+    assert intact()
+    assert np.array_equal(got[count == 0], (dw0 if accumulate else np.zeros_like(dw0))[count == 0])
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("N,D,V,kind,ignore,scale", [
+    (1, 8, 1, "uniform", 0.0, 1.0), (2, 8, 300, "one", 0.0, 1.0), (257, 64, 1000, "uniform", 0.1, 1.0), (63, 16, 5, "zipf", 0.3, 0.5),
+    (64, 72, 7, "uniform", 0.0, 1.0), (1000, 24, 9, "zipf", 0.1, -1.5), (5000, 896, 3001, "zipf", 0.15, 29.933), (2048, 128, 151936, "zipf", 0.0, 1.0),
+    (4097, 1032, 1, "one", 0.05, 1.0), (3000, 512, 40, "zipf", 0.0, 1.0), (300, 8192, 50, "zipf", 0.2, 1.0), (7, 65536, 3, "uniform", 0.0, 1.0),
+    (1500, 256, 4000, "runs", 0.0, 1.0), (10000, 520, 257, "uniform", 0.5, 1.0), (100, 64, 50, "uniform", 1.0, 1.0), (2500, 1024, 300, "runs", 0.4, 1.0),
+    (40000, 40, 20000, "zipf", 0.1, 1.0), (33000, 8, 2, "uniform", 0.0, 1.0), (1025, 3584, 600000 // 512, "zipf", 0.0, 1.0)])
+def test_gradient_matches_oracle(B, N, D, V, kind, ignore, scale, accumulate):
+    _gradient_case(B, N, D, V, kind, ignore, scale, accumulate)
+
+
+@pytest.mark.parametrize("V", [255, 256, 257, 511, 512, 262143, 262144, 262145, 600001])
+def test_gradient_at_vocabulary_borders(B, V):
+    _gradient_case(B, 700, 16, V, "uniform", 0.1, 1.0, True)
+    _gradient_case(B, 700, 16, V, "one", 0.1, 1.0, False)
+
+
+def test_tokens_outside_the_matrix_are_reported(B):
+    V, D = 30, 64
+    t = np.array([0, 30, 29, -1, IGN, 5, 2 ** 31 - 1, -2 ** 31], dtype=np.int32)
+    rng = np.random.default_rng(5)
+    w, dy = _bits(rng.standard_normal((V, D))), _bits(rng.standard_normal((len(t), D)))
+    status = torch.full((1,), 64, dtype=torch.int32, device="cuda")
+    td = torch.from_numpy(t).cuda()
+    out = B.cce_embedding_forward(td, bf16_dev(w), IGN, status=status)
+    assert int(status) == 64 | B.CCE_STATUS_BAD_TOKEN                       # OR-ed in, nothing cleared
+    ok = E.takes_part(t, V, IGN)
+    assert ok.tolist() == [True, False, True, False, False, True, False, False]
+    assert torch.equal(out.cpu()[torch.from_numpy(~ok)], torch.zeros((~ok).sum(), D, dtype=torch.bfloat16))
+    status.zero_()
+    dw = B.cce_embedding_backward(td, bf16_dev(dy), V, IGN, status=status)
+    assert int(status) == B.CCE_STATUS_BAD_TOKEN
+    want, _ = E.backward(I.bf16_bits_to_f32(dy).astype(np.float64), t, V, IGN)
+    assert np.array_equal(dw.cpu().numpy(), want)                           # single rows: no rounding
+    status.zero_()
+    good = torch.from_numpy(np.array([IGN, 3, 29], dtype=np.int32)).cuda()
+    B.cce_embedding_forward(good, bf16_dev(w), IGN, status=status)
+    B.cce_embedding_backward(good, bf16_dev(dy[:3]), V, IGN, status=status)
+    assert int(status) == 0
+    B.cce_embedding_forward(td, bf16_dev(w), IGN)                           # no status word: nothing to report to
+    # an ignore_index inside the vocabulary takes its token out
+    out = B.cce_embedding_forward(good, bf16_dev(w), 29, status=status)
+    assert int(status) == B.CCE_STATUS_BAD_TOKEN and not bool(out[2].any()) and bool(out[1].any())
+
+
+def test_gradient_is_the_same_in_every_run_and_with_any_workspace(B):
+    rng = np.random.default_rng(6)
+    N, D, V = 6000, 256, 500
+    t = torch.from_numpy(_tokens(rng, N, V, "zipf", 0.1)).cuda()
+    dy = torch.randn(N, D, device="cuda").bfloat16()
+    a = B.cce_embedding_backward(t, dy, V, IGN)
+    need = B.embedding_workspace_bytes(N, D, V)
+    for fill, extra in ((0, 0), (255, 0), (127, 4096)):
+        ws = torch.full((need + extra,), fill, dtype=torch.uint8, device="cuda")
+        assert torch.equal(a, B.cce_embedding_backward(t, dy, V, IGN, workspace=ws))
+    # a larger batch's workspace serves a smaller one
+    big = torch.full((B.embedding_workspace_bytes(20000, D, V),), 255, dtype=torch.uint8, device="cuda")
+    assert torch.equal(a, B.cce_embedding_backward(t, dy, V, IGN, workspace=big))
+
+
+def test_gradient_of_the_lookup_against_differences(B):
+    """<dy, y(W + h P) - y(W - h P)> / 2h = <dW, P>: the lookup is linear, so differences of exact bf16 values are exact
+    up to the fp32 sums (2^-24 of each term, N D terms)."""
+    rng = np.random.default_rng(7)
+    N, D, V = 300, 64, 40
+    t = torch.from_numpy(_tokens(rng, N, V, "zipf", 0.1)).cuda()
+    w = torch.randint(-8, 9, (V, D), device="cuda").bfloat16()
+    p = torch.randint(-8, 9, (V, D), device="cuda").bfloat16()
+    dy = torch.randint(-8, 9, (N, D), device="cuda").bfloat16()
+    up, down = (B.cce_embedding_forward(t, w + s * p, IGN, scale=2.0).double() for s in (1, -1))
+    dw = B.cce_embedding_backward(t, dy, V, IGN, scale=2.0).double()
+    assert float(((up - down) / 2 * dy.double()).sum()) == float((dw * p.double()).sum())
+
+
+def test_rows_beyond_32_bit_offsets(B):
+    """2.2 G values of dW and of W: the last rows' offsets pass 2^31 values and 2^32 bytes."""
+    D, V = 8192, 270000
+    w = torch.zeros(V, D, dtype=torch.bfloat16, device="cuda")
+    w[V - 1] = torch.randn(D, device="cuda").bfloat16()
+    t = torch.tensor([V - 1, 0, V - 1, V - 2], dtype=torch.int32, device="cuda")
+    out = B.cce_embedding_forward(t, w)
+    assert torch.equal(out[0], w[V - 1]) and torch.equal(out[2], w[V - 1]) and not bool(out[1].any())
+    del w
+    dw = torch.full((V, D), 3.0, device="cuda")
+    B.cce_embedding_backward(t, out, V, d_weight=dw)
+    assert torch.equal(dw[V - 1], 2 * out[0].float()) and not bool(dw[:V - 1].any())
+
+
+def test_binding_refuses(B):
+    t = torch.zeros(4, dtype=torch.int32, device="cuda")
+    w = torch.zeros(10, 64, dtype=torch.bfloat16, device="cuda")
+    dy = torch.zeros(4, 64, dtype=torch.bfloat16, device="cuda")
+    for bad in (t.long(), t[::2], t.view(2, 2)):
+        with pytest.raises(ValueError):
+            B.cce_embedding_forward(bad, w)
+    for bad in (w.float(), w[:, ::2], w.t()):
+        with pytest.raises(ValueError):
+            B.cce_embedding_forward(t, bad)
+    with pytest.raises(ValueError):
+        B.cce_embedding_forward(t, w, out=torch.empty(4, 64, device="cuda"))
+    with pytest.raises(ValueError):
+        B.cce_embedding_backward(t, dy, 10, accumulate_dw=True)
+    with pytest.raises(ValueError):
+        B.cce_embedding_backward(t, dy, 10, d_weight=torch.empty(9, 64, device="cuda"))
+    with pytest.raises(ValueError):
+        B.cce_embedding_backward(t, dy, 10, status=torch.zeros(1, device="cuda"))
+    with pytest.raises(B.CCEError):
+        B.cce_embedding_backward(t, dy, 10, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(B.CCEError):                                         # rows of 12 values are not 16-byte chunks
+        B.cce_embedding_forward(t, torch.zeros(10, 12, dtype=torch.bfloat16, device="cuda"))
+    with pytest.raises(B.CCEError):
+        B.cce_embedding_backward(t[:0], dy[:0], 10)

@@ -1,0 +1,268 @@
+"""GPU parity of the optimizer steps over many tensors with their oracles in 64 bits.
+
+Tolerances, from the arithmetic (u = 2^-24, half a step of fp32):
+    sum of squares   fp64 products are exact, sums of n terms off by at most n 2^-53 of the (positive) result
+    m                two products, a sum, the clipping product and 1 - beta1: 4 u (|beta1 m| + |(1 - beta1) g|)
+    v                positive terms of at most five roundings each: 6 u v
+    param            decay and the last sum 3 u |p|, update 12 u of itself, m's error through it
+    8-bit moments    formed in fp64 on both sides: the same codes.  param as above with m and v rounded once
+    bf16 copies      the rounding of the fp32 parameters that the step wrote, bit for bit"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import adamw_oracle as A
+from oracle import state8_oracle as S
+from paper_2601_02609_amd import inputs as I
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+SIZES = [1, 3, 7, 8, 9, 127, 128, 129, 255, 2047, 2048, 2049, 5000, 100003, 0, 2056]
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2601_02609_amd import binding
+    binding.lib()
+    return binding
+
+
+def _flat(sizes, dtype, fill=0):
+    """Tensors in the middle of one buffer, 128 values apart at least, and a check of what lies between them."""
+    starts = np.cumsum([128] + [(n + 127) // 128 * 128 + 128 for n in sizes])
+    whole = torch.full((int(starts[-1]),), 7, dtype=dtype, device="cuda")
+    views = [whole[a:a + n] for a, n in zip(starts, sizes)]
+    for x in views:
+        x.fill_(fill)
+    gaps = torch.ones(len(whole), dtype=torch.bool, device="cuda")
+    for a, n in zip(starts, sizes):
+        gaps[a:a + n] = False
+    return views, lambda: bool((whole[gaps] == 7).all())
+
+
+class _Tensors:
+    """Parameters, gradients and moments of a list of tensors, in the library's form and in the oracle's."""
+
+    def __init__(self, B, sizes, state8, bf16, seed=0, copies=True):
+        rng = np.random.default_rng(seed)
+        self.sizes, self.state8, self.bf16 = sizes, state8, bf16
+        self.p = [(rng.standard_normal(n) * 0.1).astype(np.float32) for n in sizes]
+        pd, ok_p = _flat(sizes, torch.float32)
+        pb, ok_b = _flat(sizes, torch.bfloat16)
+        m32, ok_m = _flat(sizes, torch.float32)
+        v32, ok_v = _flat(sizes, torch.float32)
+        m8, ok_m8 = _flat(sizes, torch.uint8)
+        v8, ok_v8 = _flat(sizes, torch.uint8)
+        ms, ok_ms = _flat([(n + 127) // 128 for n in sizes], torch.uint8)
+        vs, ok_vs = _flat([(n + 127) // 128 for n in sizes], torch.uint8)
+        for d, p in zip(pd, self.p):
+            d.copy_(torch.from_numpy(p))
+        self.intact = lambda: all(f() for f in (ok_p, ok_b, ok_m, ok_v, ok_m8, ok_v8, ok_ms, ok_vs))
+        self.pd, self.pb = pd, pb if copies else [None] * len(sizes)
+        self.md = [m8[i] if e else m32[i] for i, e in enumerate(state8)]
+        self.vd = [v8[i] if e else v32[i] for i, e in enumerate(state8)]
+        self.ms, self.vs = ms, vs
+        self.lr_scale = [16.0 if i % 3 == 1 else 1.0 for i in range(len(sizes))]
+        self.wd = [0.0 if i % 4 == 2 else 0.1 for i in range(len(sizes))]
+        self.rng = rng
+        self.new_grads()
+        self.list = B.OptimTensors(self.gd, self.pd, self.md, self.vd, params_bf16=self.pb, m_scales=ms, v_scales=vs,
+                                   lr_scale=self.lr_scale, weight_decay=self.wd)
+
+    def new_grads(self):
+        self.g = [(self.rng.standard_normal(n) * np.exp(self.rng.uniform(-9, -2, n))).astype(np.float32) for n in self.sizes]
+        self.g = [I.bf16_bits_to_f32(I.f32_to_bf16_bits(g)) if b else g for g, b in zip(self.g, self.bf16)]
+        self.gd = [torch.from_numpy(g).cuda().to(torch.bfloat16 if b else torch.float32) for g, b in zip(self.g, self.bf16)]
+
+    def host(self, i):
+        return [x.cpu().numpy() for x in (self.pd[i], self.md[i], self.ms[i], self.vd[i], self.vs[i])]
+
+
+def _check_step(T, before, clip, step, seed, hp):
+    f32 = lambda x: float(np.float32(x))
+    b1, b2, eps = f32(hp["beta1"]), f32(hp["beta2"]), f32(hp["eps"])
+    for i, n in enumerate(T.sizes):
+        if n == 0:
+            continue
+        p0, m0, ms0, v0, vs0 = before[i]
+        p1, m1, ms1, v1, vs1 = T.host(i)
+        lr, wd = float(np.float32(hp["lr"]) * np.float32(T.lr_scale[i])), f32(T.wd[i])
+        if T.state8[i]:
+            p, state, m, v = S.step(p0, T.g[i], (m0, ms0, v0, vs0), step, seed, lr, b1, b2, eps, wd, clip=clip)
+            for name, got, want in zip(("m", "m scale", "v", "v scale"), (m1, ms1, v1, vs1), state):
+                assert np.array_equal(got, want), (i, n, name, int((got != want).sum()))
+            em = U * np.abs(m)
+        else:
+            p, m, v = A.adamw_step(p0, T.g[i], m0, v0, step, lr, b1, b2, eps, wd, clip=clip)
+            em = 4 * U * (np.abs(b1 * m0) + np.abs((1 - b1) * clip * T.g[i].astype(np.float64)))
+            assert np.all(np.abs(m1 - m) <= em + 1e-45), i
+            assert np.all(np.abs(v1 - v) <= 6 * U * v + 1e-45), i
+        den = np.sqrt(v / (1 - b2 ** step)) + eps
+        update = lr * (m / (1 - b1 ** step)) / den
+        tol = 3 * U * (np.abs(p0) + np.abs(p)) + 12 * U * np.abs(update) + lr * em / (1 - b1 ** step) / den
+        assert np.all(np.abs(p1 - p) <= tol), (i, n, float((np.abs(p1 - p) / tol).max()))
+        if T.pb[i] is not None:
+            assert np.array_equal(T.pb[i].view(torch.int16).cpu().numpy().view(np.uint16), I.f32_to_bf16_bits(p1)), i
+
+
+@pytest.mark.parametrize("state8", ["32", "8", "both"])
+@pytest.mark.parametrize("grads", ["fp32", "bf16", "both"])
+def test_steps_match_the_oracle(B, state8, grads):
+    """Three steps from zero moments, each checked from the state that the one before left, over odd sizes."""
+    sizes = SIZES + [130 + i for i in range(60)]                            # more than one launch holds
+    flags = {"32": lambda i: 0, "fp32": lambda i: 0, "8": lambda i: 1, "bf16": lambda i: 1, "both": lambda i: (i // 2) % 2}
+    T = _Tensors(B, sizes, [flags[state8](i) for i in range(len(sizes))], [flags[grads](i + 1) for i in range(len(sizes))], seed=11)
+    hp = dict(lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8)
+    for step in (1, 2, 3):
+        before = [T.host(i) for i in range(len(sizes))]
+        clip = 0.37 if step == 2 else 1.0
+        cd = torch.tensor([clip], device="cuda") if step == 2 else None
+        print(f"[adamw multi] {state8} {grads} step {step}", flush=True)
+        B.cce_adamw_multi_step(T.list, step, clip_coef=cd, seed=99, **hp)
+        torch.cuda.synchronize()
+        _check_step(T, before, float(np.float32(clip)), step, 99, hp)
+        T.new_grads()
+        T.list.set_grads(T.gd)
+    assert T.intact()
+
+
+@pytest.mark.parametrize("state8", [0, 1])
+def test_large_tensor_and_no_copy(B, state8):
+    T = _Tensors(B, [896 * 1201 + 3, 5], [state8] * 2, [0, 1], seed=12, copies=False)
+    hp = dict(lr=3e-4, beta1=0.9, beta2=0.999, eps=1e-8)
+    before = [T.host(i) for i in range(2)]
+    B.cce_adamw_multi_step(T.list, 1000, seed=3, **hp)
+    _check_step(T, before, 1.0, 1000, 3, hp)
+    assert T.intact()
+
+
+def test_step_of_one_tensor_equals_the_single_step(B):
+    """Within the two calls' roundings of cce_adamw_step on the same tensor."""
+    n = 100001
+    T = _Tensors(B, [n], [0], [0], seed=13)
+    p, m, v = (torch.from_numpy(T.p[0]).cuda(), torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"))
+    hp = dict(lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8)
+    T.list = B.OptimTensors(T.gd, T.pd, T.md, T.vd, weight_decay=0.1)
+    B.cce_adamw_multi_step(T.list, 1, **hp)
+    B.cce_adamw_step(p, T.gd[0], m, v, 1, weight_decay=0.1, **hp)
+    assert float((T.md[0] - m).abs().max()) <= 8 * U * float(m.abs().max())
+    assert float((T.vd[0] - v).abs().max()) <= 12 * U * float(v.abs().max())
+    assert float((T.pd[0] - p).abs().max()) <= 6 * U * float(p.abs().max()) + 48 * U * 1e-3
+
+
+def test_state8_values_without_a_code_and_extremes(B):
+    """NaN and infinite gradients spoil their own value only; zeros, the smallest and the largest values keep a scale."""
+    n = 640
+    T = _Tensors(B, [n], [1], [0], seed=14)
+    g = T.g[0].copy()
+    g[3], g[7], g[9] = np.nan, np.inf, -np.inf
+    g[128:256] = 0.0
+    g[256:384] = np.float32(1e-38) * np.arange(1, 129)
+    g[384:512] = np.float32(3e37)
+    g[512:520] = np.float32(1e-45)
+    T.g[0] = g
+    T.gd[0].copy_(torch.from_numpy(g))
+    hp = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8)
+    before = T.host(0)
+    B.cce_adamw_multi_step(T.list, 1, seed=5, **hp)
+    p1, m1, ms1, v1, vs1 = T.host(0)
+    _, state, _, _ = S.step(before[0], g, (before[1], before[2], before[3], before[4]), 1, 5, 1e-3, float(np.float32(0.9)),
+                            float(np.float32(0.999)), float(np.float32(1e-8)), 0.1)
+    bad = ~np.isfinite(g)
+    for got, want in zip((m1, v1), (state[0], state[2])):
+        assert np.array_equal(got, want)
+    assert np.array_equal(ms1, state[1]) and np.array_equal(vs1, state[3])
+    assert np.isnan(p1[bad]).all() and np.isfinite(p1[:384][~bad[:384]]).all()
+    m = B.cce_adamw_state8_read(T.md[0], T.ms[0])
+    assert np.array_equal(np.isnan(m.cpu().numpy()), bad)
+
+
+@pytest.mark.parametrize("n", [1, 7, 8, 127, 128, 129, 2049, 100003])
+def test_state8_read_is_what_the_codes_stand_for(B, n):
+    rng = np.random.default_rng(n)
+    codes = rng.integers(0, 256, n).astype(np.uint8)
+    scales = rng.integers(87, 168, (n + 127) // 128).astype(np.uint8)
+    c, s = torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda()
+    (out,), intact = _flat([n], torch.float32)
+    B.cce_adamw_state8_read(c, s, out=out)
+    assert np.array_equal(out.cpu().numpy(), S.decode(codes, scales, S.M).astype(np.float32), equal_nan=True) and intact()
+    B.cce_adamw_state8_read(c, s, second=True, out=out)
+    assert np.array_equal(out.cpu().numpy(), (S.decode(codes, scales, S.R) ** 2).astype(np.float32), equal_nan=True) and intact()
+
+
+def test_seed_and_step_choose_the_random_numbers(B):
+    def run(seed, step):
+        T = _Tensors(B, [5000, 300], [1, 1], [0, 0], seed=15)
+        B.cce_adamw_multi_step(T.list, step, lr=1e-3, seed=seed)
+        return torch.cat([T.md[0], T.vd[0], T.md[1]])
+    a = run(1, 4)
+    assert torch.equal(a, run(1, 4)) and not torch.equal(a, run(2, 4)) and torch.equal(a, run(1 + (1 << 32), 4))
+
+
+@pytest.mark.parametrize("sizes,bf16", [([1], 0), ([3, 0, 8, 2049], 0), (SIZES, 2), ([100 + i for i in range(400)], 2), ([3_000_001, 17], 1), ([0, 0], 0)])
+def test_sumsq_multi_and_clip(B, sizes, bf16):
+    rng = np.random.default_rng(len(sizes))
+    g = [(rng.standard_normal(n) * 0.05).astype(np.float32) for n in sizes]
+    kinds = [bf16 if bf16 < 2 else i % 2 for i in range(len(sizes))]
+    g = [I.bf16_bits_to_f32(I.f32_to_bf16_bits(x)) if k else x for x, k in zip(g, kinds)]
+    T = B.OptimTensors([torch.from_numpy(x).cuda().to(torch.bfloat16 if k else torch.float32) for x, k in zip(g, kinds)])
+    want = float(sum((x.astype(np.longdouble) ** 2).sum() for x in g))
+    tol = (sum(sizes) + 4) * 2.0 ** -53 * want
+    s, none = B.cce_grad_sumsq_multi(T)
+    assert none is None and abs(float(s) - want) <= tol
+    again, _ = B.cce_grad_sumsq_multi(T)
+    assert torch.equal(s, again)
+    for max_norm in (0.5, 1e6):
+        s2, c = B.cce_grad_sumsq_multi(T, s.clone(), True, max_norm=max_norm, eps_norm=1e-6)
+        assert abs(float(s2) - 2 * want) <= 3 * tol
+        ref = min(1.0, max_norm / (np.sqrt(2 * want) + float(np.float32(1e-6))))
+        assert abs(float(c) - ref) <= 2 * U * ref
+    single = B.cce_clip_coef(s2, 1e6)
+    assert float(single) == float(c)
+
+
+def test_sumsq_of_non_finite_gradients(B):
+    g = torch.ones(5000, device="cuda")
+    g[4321] = float("inf")
+    s, c = B.cce_grad_sumsq_multi(B.OptimTensors([g]), max_norm=1.0)
+    assert float(s) == float("inf") and float(c) == 0.0
+    g[4321] = 1e30                                                          # whose square fp32 does not hold
+    s, _ = B.cce_grad_sumsq_multi(B.OptimTensors([g]))
+    assert abs(float(s) / 1e60 - 1.0) <= 1e-6
+
+
+def test_list_refuses(B):
+    def new(**change):
+        f = lambda dtype=torch.float32, n=300: [torch.zeros(n, dtype=dtype, device="cuda"), torch.zeros(8, dtype=dtype, device="cuda")]
+        a = dict(grads=f(), params=f(), m=f(), v=f()) | change
+        return B.OptimTensors(a.pop("grads"), a.pop("params"), a.pop("m"), a.pop("v"), **a)
+    new()
+    z = lambda n, dtype=torch.float32: torch.zeros(n, dtype=dtype, device="cuda")
+    for change in (dict(params=[z(300)]), dict(params=[z(300), z(9)]), dict(params=None), dict(m=[z(300, torch.float16), z(8, torch.float16)]),
+                   dict(grads=[z(300, torch.float16), z(8)]), dict(v=[z(600)[::2], z(8)]), dict(m=[z(300, torch.uint8), z(8)]),
+                   dict(m=[z(300, torch.uint8), z(8)], v=[z(300, torch.uint8), z(8)]), dict(params_bf16=[z(300), None]),
+                   dict(weight_decay=[0.1]), dict(lr_scale=[1.0, 1.0, 1.0]), dict(params=[z(300), None])):
+        with pytest.raises(ValueError):
+            new(**change)
+    whole = z(400)
+    for change in (dict(params=[whole[:300], whole[292:300]]), dict(params=[whole[:300], z(8)], m=[z(300), whole[100:108]]),
+                   dict(grads=[whole[:300], z(8)], v=[z(300), whole[:8]])):
+        with pytest.raises(ValueError, match="overlaps"):
+            new(**change)
+    T = new(params_bf16=[None, z(8, torch.bfloat16)])
+    with pytest.raises(ValueError):
+        T.set_grads([z(300)])
+    with pytest.raises(ValueError):
+        T.set_grads([z(300), z(9)])
+    T.set_grads([z(300, torch.bfloat16), z(8)])
+    B.cce_adamw_multi_step(T, 1, lr=1e-3)
+    with pytest.raises(ValueError):
+        B.cce_adamw_multi_step(B.OptimTensors([z(5)]), 1, lr=1e-3)
+    with pytest.raises(ValueError):
+        B.cce_grad_sumsq_multi(T, accumulate=True)
+    with pytest.raises(ValueError):
+        B.cce_grad_sumsq_multi(T, clip_coef=z(1))
+    with pytest.raises(B.CCEError):
+        B.cce_adamw_multi_step(T, 0, lr=1e-3)
+    with pytest.raises(B.CCEError):                                         # rows that do not start at 16 bytes
+        B.cce_grad_sumsq_multi(B.OptimTensors([z(9)[1:]]))
