@@ -15,7 +15,8 @@
  * on an error.
  *
  * Sizes: N >= 1 tokens (below 2^31), V >= 1 rows (at most 2^24), D a positive multiple of 8 (at
- * most 65536): CCE_ERR_INVALID for sizes <= 0, CCE_ERR_UNSUPPORTED for the other limits.
+ * most 65536), V * D at most 2^37: CCE_ERR_INVALID for sizes <= 0, CCE_ERR_UNSUPPORTED for the
+ * other limits.
  *
  * A token equal to `ignore_index` (padding) or outside [0, V) takes no part: its row of y is zero,
  * its row of dy is never read (it may hold NaN) and no row of dW changes by it.  A token outside
