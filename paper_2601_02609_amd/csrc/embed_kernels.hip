@@ -24,21 +24,43 @@ __device__ __forceinline__ bool token_takes_part(int token, int V, int ignore_in
     return false;
 }
 
-// y_i = scale * W[t_i]: a thread per 16 bytes of y.
+// y_i = scale * W[t_i]: four chunks of 16 bytes of y a thread, 4 KB of the workgroup apart, whose tokens, rows and
+// stores are in flight together.  A chunk's row within the workgroup's 16 KB by multiplication: `inverse` is
+// ceil(2^32 / row_chunks), exact for the numbers below 2^17 that occur.
+constexpr int kLookupChunks = 1024;
+
 __global__ __launch_bounds__(256) void embedding_forward_kernel(
-        const int32_t* __restrict__ tokens, const uint16_t* __restrict__ weight, int64_t chunks, int row_chunks, int V,
-        int ignore_index, float scale, uint16_t* __restrict__ out, int32_t* status) {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < chunks; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / row_chunks;
-        const int c = (int)(i - row * row_chunks);
-        const int token = tokens[row];
-        float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (token_takes_part(token, V, ignore_index, c == 0 ? status : nullptr)) {
-            unpack8(((const au32x4*)weight)[(size_t)token * row_chunks + c], f);
+        const int32_t* __restrict__ tokens, const uint16_t* __restrict__ weight, int64_t chunks, int row_chunks, uint64_t inverse,
+        int V, int ignore_index, float scale, uint16_t* __restrict__ out, int32_t* status) {
+    for (int64_t first = (int64_t)blockIdx.x * kLookupChunks; first < chunks; first += (int64_t)gridDim.x * kLookupChunks) {
+        const int64_t row0 = first / row_chunks;
+        const int c0 = (int)(first - row0 * row_chunks);
+        const int live = chunks - first < kLookupChunks ? (int)(chunks - first) : kLookupChunks;
+        int token[4], c[4];
+        bool ok[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = u * 256 + (int)threadIdx.x;
+            const uint32_t o = (uint32_t)(c0 + (i < live ? i : 0));
+            const int row = (int)(((uint64_t)o * inverse) >> 32);
+            c[u] = (int)o - row * row_chunks;
+            token[u] = tokens[row0 + row];
+        }
+        au32x4 v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            ok[u] = token_takes_part(token[u], V, ignore_index, c[u] == 0 ? status : nullptr);
+            if (ok[u]) v[u] = ((const au32x4*)weight)[(size_t)token[u] * row_chunks + c[u]];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = u * 256 + (int)threadIdx.x;
+            float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (ok[u]) unpack8(v[u], f);
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] *= scale;
+            if (i < live) ((au32x4*)out)[first + i] = ok[u] ? pack8(f) : au32x4{0u, 0u, 0u, 0u};
         }
-        ((au32x4*)out)[i] = pack8(f);
     }
 }
 
@@ -51,11 +73,14 @@ __global__ __launch_bounds__(256) void embedding_forward_kernel(
 //   join    the partial rows of the groups that cross, in order
 // The order of all sums follows from the tokens and the sizes.
 // ------------------------------------------------------------------------------------------
-constexpr int kSliceKeys = 768;                 // rows of the matrix that an order workgroup counts: 48 KB of LDS
+constexpr int kSliceKeys = 640;                 // rows of the matrix that an order workgroup counts: 40 KB of LDS
 constexpr int kOrderWaves = 16;
+constexpr int kOrderLoads = 8;                  // loads of tokens in flight, and as many ahead
+constexpr int kFound = 640;                     // positions that a wavefront notes: 20 KB of LDS
 constexpr int kJoinWaves = 8;
-constexpr int kMinPiece = 16;                   // rows of a piece, more where that makes over kMaxPieces
-constexpr int kMaxPieces = 2048;
+constexpr int kJoinShort = 16;                  // pieces of a group that one wavefront joins, and one more
+constexpr int kSumWaves = 4096;                 // wavefronts that the sum is cut into, if there are rows for them
+constexpr int kMaxPiece = 128;
 
 // Slices of the vocabulary: token t is key t / slices of slice t % slices (a power of two).  The frequent tokens, which
 // tokenizers number first, are spread over the slices.
@@ -78,11 +103,13 @@ struct EmbedBackward {
     float scale;
 };
 
-// A workgroup per slice looks through all tokens twice (they stay in the L2s): its wavefronts, each with a range of
-// positions, count their keys in LDS; after a scan over keys and wavefronts they go through their ranges again, 64
-// positions at a time, and give the positions of one key consecutive places.
+// A workgroup per slice looks through all tokens (which stay in the L2s): its wavefronts, each with a range of positions,
+// count their keys in LDS and note what they found there; after a scan over keys and wavefronts they give the positions
+// of one key consecutive places.  64 tokens that none is in the slice of cost a handful of instructions, most of them
+// scalar: all slices together do that 256 N / 64 times, which is what bounds the kernel.
 __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const EmbedBackward a) {
     __shared__ uint32_t count[kOrderWaves * kSliceKeys];
+    __shared__ uint16_t found[kOrderWaves][kFound];          // places in the wavefront's range
     __shared__ uint32_t wave_total[kOrderWaves], wave_below[kOrderWaves];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int slice = blockIdx.x, mask = (1 << a.bits) - 1;
@@ -92,21 +119,41 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const
 
     const int64_t range = ((int64_t)a.N + 64 * kOrderWaves - 1) / (64 * kOrderWaves) * 64;
     const int64_t begin = w * range, end = begin + range < a.N ? begin + range : a.N;
-    uint32_t below = 0u;
-    for (int64_t i = begin; i < end; i += 256) {
-        int token[4];
+    const unsigned long long lanes_below = (1ull << lane) - 1ull;
+    if (slice == 0 && a.status)
+        for (int64_t i = begin + lane; i < end; i += 64) token_takes_part(a.tokens[i], a.V, a.ignore_index, a.status);
+    auto load = [&](int64_t i, int (&token)[kOrderLoads]) {
+        if (i + 64 * kOrderLoads <= end) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) token[u] = i + 64 * u + lane < end ? a.tokens[i + 64 * u + lane] : a.ignore_index;
+            for (int u = 0; u < kOrderLoads; ++u) token[u] = a.tokens[i + 64 * u + lane];
+        } else {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (!token_takes_part(token[u], a.V, a.ignore_index, slice == 0 ? a.status : nullptr)) continue;
+            for (int u = 0; u < kOrderLoads; ++u) token[u] = i + 64 * u + lane < end ? a.tokens[i + 64 * u + lane] : -1;
+        }
+    };
+    auto valid = [&](int token) { return (unsigned)token < (unsigned)a.V && token != a.ignore_index; };
+    uint32_t below = 0u, n = 0u;                             // tokens of slices below and of this one, in scalar registers
+    int token[kOrderLoads], next[kOrderLoads];
+    load(begin, token);
+    for (int64_t i = begin; i < end; i += 64 * kOrderLoads) {
+        load(i + 64 * kOrderLoads, next);
+#pragma unroll
+        for (int u = 0; u < kOrderLoads; ++u) {
             const int s = token[u] & mask;
-            below += s < slice ? 1u : 0u;
-            if (s == slice) atomicAdd(&own[token[u] >> a.bits], 1u);
+            const unsigned long long ok = __ballot(valid(token[u]));
+            below += (uint32_t)__popcll(__ballot(s < slice) & ok);
+            const unsigned long long mine = __ballot(s == slice) & ok;
+            if (mine != 0ull) {
+                if (mine >> lane & 1ull) {
+                    const uint32_t place = n + (uint32_t)__popcll(mine & lanes_below);
+                    atomicAdd(&own[token[u] >> a.bits], 1u);
+                    if (place < (uint32_t)kFound) found[w][place] = (uint16_t)((i - begin) + 64 * u + lane);
+                }
+                n += (uint32_t)__popcll(mine);
+            }
+            token[u] = next[u];
         }
     }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) below += (uint32_t)__shfl_xor((int)below, o);
     if (lane == 0) wave_below[w] = below;
     __syncthreads();
 
@@ -131,35 +178,55 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const
     if (key <= a.keys) a.starts[(size_t)slice * (a.keys + 1) + key] = (int32_t)at;
     if (key < a.keys)
         for (int i = 0; i < kOrderWaves; ++i) {
-            const uint32_t n = count[i * a.keys + key];
+            const uint32_t here = count[i * a.keys + key];
             count[i * a.keys + key] = at;
-            at += n;
+            at += here;
         }
     __syncthreads();
 
-    for (int64_t i = begin; i < end; i += 256) {
-        int token[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) token[u] = i + 64 * u + lane < end ? a.tokens[i + 64 * u + lane] : a.ignore_index;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const bool mine = token_takes_part(token[u], a.V, a.ignore_index, nullptr) && (token[u] & mask) == slice;
-            unsigned long long left = __ballot(mine);
-            while (left) {                                   // a trip per key among the 64
-                const int leader = __ffsll(left) - 1;
-                const int t = __builtin_amdgcn_readlane(token[u], leader);
-                const unsigned long long same = __ballot(mine && token[u] == t);
-                int place = 0;
-                if (lane == leader) place = (int)atomicAdd(&own[t >> a.bits], (uint32_t)__popcll(same));
-                place = __builtin_amdgcn_readlane(place, leader);
-                if (mine && token[u] == t) {
-                    place += __popcll(same & ((1ull << lane) - 1ull));
-                    a.order[place] = (int32_t)(i + 64 * u + lane);
-                    a.sorted[place] = t;
-                }
-                left &= ~same;
+    // 64 positions, those of `mine` in ascending order with keys of this slice: lanes of one key find each other bit by bit
+    auto place_them = [&](unsigned long long mine, uint32_t k, int64_t position) {
+        unsigned long long same = mine;
+        for (int b = 0; (a.keys - 1) >> b != 0; ++b) {
+            const unsigned long long ones = __ballot(k >> b & 1u);
+            same &= k >> b & 1u ? ones : ~ones;
+        }
+        if (mine >> lane & 1ull) {
+            const int leader = __ffsll(same) - 1;
+            uint32_t to = 0u;
+            if (lane == leader) to = atomicAdd(&own[k], (uint32_t)__popcll(same));
+            to = (uint32_t)__shfl((int)to, leader) + (uint32_t)__popcll(same & lanes_below);
+            a.order[to] = (int32_t)position;
+            a.sorted[to] = (int32_t)(k << a.bits) + slice;
+        }
+    };
+    auto place_found = [&](uint32_t many, int64_t from) {    // what found[w] holds, as places behind `from`
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        for (uint32_t i = 0; i < many; i += 64) {
+            const int64_t position = from + (i + lane < many ? found[w][i + lane] : 0);
+            const int t = a.tokens[position];
+            place_them(__ballot(i + lane < many), (uint32_t)t >> a.bits, position);
+        }
+    };
+    if (n <= (uint32_t)kFound && range <= 65536) {
+        place_found(n, begin);
+        return;
+    }
+    // more than was noted: through the range again, noting as many as fit
+    for (int64_t from = begin; from < end; from += 32768) {
+        const int64_t to = from + 32768 < end ? from + 32768 : end;
+        uint32_t many = 0u;
+        for (int64_t i = from; i < to; i += 64) {
+            const int t = i + lane < to ? a.tokens[i + lane] : -1;
+            const unsigned long long mine = __ballot(valid(t) && (t & mask) == slice);
+            if (mine >> lane & 1ull) found[w][many + (uint32_t)__popcll(mine & lanes_below)] = (uint16_t)(i - from + lane);
+            many += (uint32_t)__popcll(mine);
+            if (many > (uint32_t)kFound - 64u) {
+                place_found(many, from);
+                many = 0u;
             }
         }
+        place_found(many, from);
     }
 }
 
@@ -199,10 +266,11 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbedBackward 
     const bool live = c < a.row_chunks;
     if (!live) c = 0;                                        // reads along with the first chunk's lane, stores nothing
     const int64_t first = piece * a.piece;
+    if (first >= a.N) return;
+    const int before = first > 0 ? a.sorted[first - 1] : -1, at_first = a.sorted[first];       // beside the load of M
     if (first >= M) return;
     const int64_t last = first + a.piece < M ? first + a.piece : M;
-    const int before = first > 0 ? a.sorted[first - 1] : -1;
-    bool begun = before == a.sorted[first];                  // the present group began in front of the piece
+    bool begun = before == at_first;                         // the present group began in front of the piece
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     float* partial = a.partial + ((size_t)piece * 2 * a.row_chunks + c) * 8;
     auto store_partial = [&](int which) {
@@ -271,47 +339,88 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbedBackward 
 // wavefronts share the group's partial rows: the last one of the piece where it begins, the first ones of the others.
 __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(const EmbedBackward a, int strips) {
     __shared__ af32x4 red[kJoinWaves][64];
+    __shared__ int crossing[kSliceKeys][3];                  // key, first and last piece
+    __shared__ int groups;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int slice = blockIdx.x / strips;
     const int quads = a.row_chunks * 2, c = ((int)blockIdx.x - slice * strips) * 64 + lane;
     const int32_t* starts = a.starts + (size_t)slice * (a.keys + 1);
     const af32x4* partial = (const af32x4*)a.partial;
-    for (int first = 0; first < a.keys; first += 64) {
-        const int key = first + lane;
-        const int from = key < a.keys ? starts[key] : 0, to = key < a.keys ? starts[key + 1] : 0;
-        unsigned long long crossing = __ballot(to > from && from / a.piece != (to - 1) / a.piece);
-        while (crossing) {                                   // the same for all wavefronts of the workgroup
-            const int k = __ffsll(crossing) - 1;
-            crossing &= crossing - 1;
-            const int p = __builtin_amdgcn_readlane(from, k) / a.piece, q = (__builtin_amdgcn_readlane(to, k) - 1) / a.piece;
-            af32x4 sum = {0.f, 0.f, 0.f, 0.f};
-            if (c < quads) {
-                for (int i = p + w; i <= q; i += kJoinWaves) sum += partial[((size_t)i * 2 + (i == p ? 1 : 0)) * quads + c];
-            }
-            red[w][lane] = sum;
-            __syncthreads();
-            if (w == 0 && c < quads) {
-#pragma unroll
-                for (int i = 1; i < kJoinWaves; ++i) sum += red[i][lane];
-                af32x4* at = (af32x4*)a.dW + (size_t)(((int64_t)(first + k) << a.bits) + slice) * quads + c;
-                const af32x4 r = a.scale * sum;
-                at[0] = a.accumulate ? at[0] + r : r;
-            }
-            __syncthreads();
+    if (threadIdx.x == 0) groups = 0;
+    __syncthreads();
+    for (int key = threadIdx.x; key < a.keys; key += 64 * kJoinWaves) {
+        const int from = starts[key], to = starts[key + 1];
+        const int p = from / a.piece, q = (to - 1) / a.piece;
+        if (to > from && p != q) {                           // in whatever order: no sum is over two groups
+            const int g = atomicAdd(&groups, 1);
+            crossing[g][0] = key;
+            crossing[g][1] = p;
+            crossing[g][2] = q;
         }
+    }
+    __syncthreads();
+    // short groups: a wavefront each; long ones: the wavefronts share the partial rows
+    const int n = groups;
+    auto rows_of = [&](int p, int q, int step, int from) {
+        af32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        for (int first = p + from; first <= q; first += 8 * step) {
+            af32x4 x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int i = first + u * step;
+                x[u] = af32x4{0.f, 0.f, 0.f, 0.f};
+                if (i <= q) x[u] = partial[((size_t)i * 2 + (i == p ? 1 : 0)) * quads + c];
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) sum += x[u];
+        }
+        return sum;
+    };
+    auto row_at = [&](int key) { return (af32x4*)a.dW + (size_t)(((int64_t)key << a.bits) + slice) * quads + c; };
+    for (int g = w; g < n; g += kJoinWaves) {
+        const int p = crossing[g][1], q = crossing[g][2];
+        if (q - p >= kJoinShort || c >= quads) continue;
+        af32x4* at = row_at(crossing[g][0]);
+        af32x4 old = {0.f, 0.f, 0.f, 0.f};
+        if (a.accumulate) old = at[0];
+        at[0] = old + a.scale * rows_of(p, q, 1, 0);
+    }
+    for (int g = 0; g < n; ++g) {
+        const int p = crossing[g][1], q = crossing[g][2];
+        if (q - p < kJoinShort) continue;                    // the same for all
+        af32x4* at = row_at(crossing[g][0]);
+        af32x4 sum = {0.f, 0.f, 0.f, 0.f}, old = sum;
+        if (c < quads) {
+            if (w == 0 && a.accumulate) old = at[0];
+            sum = rows_of(p, q, kJoinWaves, w);
+        }
+        red[w][lane] = sum;
+        __syncthreads();
+        if (w == 0 && c < quads) {
+#pragma unroll
+            for (int i = 1; i < kJoinWaves; ++i) sum += red[i][lane];
+            at[0] = old + a.scale * sum;
+        }
+        __syncthreads();
     }
 }
 
-// Rows of a piece.
-static int embed_piece(int64_t N) {
-    const int64_t rows = (N + kMaxPieces - 1) / kMaxPieces;
-    return (int)(rows <= kMinPiece ? kMinPiece : (rows + 7) / 8 * 8);
+// Lanes that share a row, and the rest of a row's chunks in further strips.
+static int embed_lanes(int64_t D) { return D <= 64 ? 8 : D <= 128 ? 16 : D <= 256 ? 32 : 64; }
+
+// Rows of a piece, a multiple of eight (what a wavefront has in flight): as many as leave kSumWaves wavefronts.
+static int64_t embed_piece(int64_t N, int64_t D) {
+    const int64_t lanes = embed_lanes(D), strips = (D / 8 + lanes - 1) / lanes;
+    const int64_t rows = (N * strips * lanes / 64 + kSumWaves - 1) / kSumWaves;
+    return rows <= 8 ? 8 : rows >= kMaxPiece ? kMaxPiece : (rows + 7) / 8 * 8;
 }
 
-// At most this many pieces for N rows or fewer.
-static int64_t embed_pieces(int64_t N) {
-    const int64_t n = (N + kMinPiece - 1) / kMinPiece;
-    return n < kMaxPieces ? n : kMaxPieces;
+// No N' <= N rows have more pieces.
+static int64_t embed_pieces(int64_t N, int64_t D) {
+    const int64_t lanes = embed_lanes(D), strips = (D / 8 + lanes - 1) / lanes;
+    const int64_t most = kSumWaves * 64 / (strips * lanes) + 1, short_ones = (N + 7) / 8, long_ones = (N + kMaxPiece - 1) / kMaxPiece;
+    const int64_t n = short_ones < most ? short_ones : most;
+    return n > long_ones ? n : long_ones;
 }
 
 static int embed_shape(int64_t N, int64_t D, int64_t V) {
@@ -332,10 +441,11 @@ int cce_embedding_forward(const int32_t* tokens, const void* weight, int64_t N, 
     const int rc = embed_shape(N, D, V);
     if (rc != CCE_OK) return rc;
     if ((((uintptr_t)weight | (uintptr_t)out) & 15) || (((uintptr_t)tokens | (uintptr_t)status) & 3)) return CCE_ERR_INVALID;
-    const int64_t chunks = N * (D / 8), want = (chunks + 255) / 256;
+    const int64_t row_chunks = D / 8, chunks = N * row_chunks, want = (chunks + kLookupChunks - 1) / kLookupChunks;
     (void)hipGetLastError();
     hipLaunchKernelGGL(embedding_forward_kernel, dim3((unsigned)(want < kMaxBlocks ? want : kMaxBlocks)), dim3(256), 0, (hipStream_t)stream_,
-                       tokens, (const uint16_t*)weight, chunks, (int)(D / 8), (int)V, ignore_index, scale, (uint16_t*)out, status);
+                       tokens, (const uint16_t*)weight, chunks, (int)row_chunks, (((uint64_t)1 << 32) + row_chunks - 1) / row_chunks,
+                       (int)V, ignore_index, scale, (uint16_t*)out, status);
     return hip_ok(hipGetLastError()) ? CCE_OK : CCE_ERR_HIP;
 }
 
@@ -343,7 +453,7 @@ size_t cce_embedding_workspace_bytes(int64_t N, int64_t D, int64_t V) {
     if (embed_shape(N, D, V) != CCE_OK) return 0;
     const int bits = slice_bits(V);
     const int64_t starts = (((V + (1 << bits) - 1) >> bits) + 1) << bits;
-    return (size_t)(round_up(starts * 4, 256) + 2 * round_up(N * 4, 256) + embed_pieces(N) * 2 * D * 4);
+    return (size_t)(round_up(starts * 4, 256) + 2 * round_up(N * 4, 256) + embed_pieces(N, D) * 2 * D * 4);
 }
 
 int cce_embedding_backward(const int32_t* tokens, const void* d_out, int64_t N, int64_t D, int64_t V,
@@ -365,7 +475,7 @@ int cce_embedding_backward(const int32_t* tokens, const void* d_out, int64_t N, 
     a.bits = slice_bits(V);
     a.keys = (int)((V + (1 << a.bits) - 1) >> a.bits);
     a.row_chunks = (int)(D / 8);
-    a.piece = embed_piece(N);
+    a.piece = (int)embed_piece(N, D);
     a.accumulate = accumulate_dW ? 1 : 0;
     a.scale = scale;
     const int slices = 1 << a.bits;
@@ -376,7 +486,7 @@ int cce_embedding_backward(const int32_t* tokens, const void* d_out, int64_t N, 
     a.partial = (float*)at;
     hipLaunchKernelGGL(embedding_order_kernel, dim3((unsigned)slices), dim3(64 * kOrderWaves), 0, stream, a);
 
-    const int lanes = D <= 64 ? 8 : D <= 128 ? 16 : D <= 256 ? 32 : 64;
+    const int lanes = embed_lanes(D);
     a.strips = (a.row_chunks + lanes - 1) / lanes;
     const int64_t pieces = (N + a.piece - 1) / a.piece;
     const int sum_blocks = (int)((pieces * a.strips * lanes + 255) / 256);

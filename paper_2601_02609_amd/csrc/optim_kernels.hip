@@ -22,7 +22,8 @@ constexpr int64_t kMaxTensor = (int64_t)1 << 34;       // values of a tensor
 constexpr int64_t kMaxGrid = (1 << 24) - 1;            // of 256 threads: a launch has fewer than 2^32 threads
 constexpr int kStepTensors = 44;                       // tensors of a launch: kernel arguments hold 4 KB
 constexpr int kNormTensors = 160;
-constexpr int kNormBlocks = 1024;                      // workgroups of a launch, each with one partial sum
+constexpr int kNormBlocks = 2048;                      // workgroups of a launch, each with one partial sum
+constexpr int kNormChunk = 4096;                       // values of a workgroup's trip
 
 struct StepTensor {
     float* param;
@@ -34,14 +35,14 @@ struct StepTensor {
     uint8_t* v_scale;
     int64_t n;
     float lr, decay;                                   // decay: 1 - lr * weight_decay
-    uint32_t first;                                    // its first workgroup
-    uint32_t grad_bf16;
+    uint64_t grad_bf16;
 };
 
 struct StepArgs {
     StepTensor t[kStepTensors];
+    uint32_t first[kStepTensors];                      // a tensor's first workgroup
     const float* clip_coef;
-    float beta1, beta2, eps, inv_bc1, inv_bc2;
+    float beta1, beta2, eps, inv_bc1, inv_bc2, root_inv_bc2;
     uint32_t key, count;
 };
 static_assert(sizeof(StepArgs) <= 4096, "kernel arguments hold 4 KB");
@@ -49,26 +50,25 @@ static_assert(sizeof(StepArgs) <= 4096, "kernel arguments hold 4 KB");
 struct NormTensor {
     const void* grad;
     int64_t n;
-    uint32_t first;                                    // its first chunk
-    uint32_t grad_bf16;
 };
 
 struct NormArgs {
     NormTensor t[kNormTensors];
+    uint32_t first[kNormTensors];                      // a tensor's first chunk; twice that, plus 1 if it is bf16
     double* partials;
     uint32_t count, chunks;
 };
 static_assert(sizeof(NormArgs) <= 4096, "kernel arguments hold 4 KB");
 
-// Which tensor of the table workgroup (or chunk) `b` belongs to: the last one that begins at or before it.
-template <class Tensor>
-__device__ __forceinline__ int tensor_of(const Tensor* t, int count, uint32_t b) {
-    int low = 0, high = count - 1;
-    while (low < high) {
-        const int mid = (low + high + 1) >> 1;
-        if (t[mid].first <= b) low = mid; else high = mid - 1;
+// Which tensor of the table workgroup (or chunk) `b` belongs to: the last one that begins at or before it.  Every lane
+// looks at one entry: one load instead of the chain of a binary search.
+__device__ __forceinline__ int tensor_of(const uint32_t* first, int count, uint32_t b) {
+    int n = 0;
+    for (int base = 0; base < count; base += 64) {
+        const int i = base + (int)(threadIdx.x & 63);
+        n += (int)__popcll(__ballot(i < count && first[i] <= b));
     }
-    return low;
+    return __builtin_amdgcn_readfirstlane(n - 1);
 }
 
 // Eight gradient values from `at` on, of which `live` exist; zeros behind them.
@@ -119,13 +119,41 @@ __global__ __launch_bounds__(256) void norm_partial_kernel(const NormArgs a) {
     __shared__ double red[4];
     double sum = 0.0;
     for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
-        const int i = tensor_of(a.t, (int)a.count, c);
-        const int64_t at = (int64_t)(c - a.t[i].first) * kBlockValues + threadIdx.x * 8, left = a.t[i].n - at;
-        if (left <= 0) continue;
-        float g[8];
-        load_grad(a.t[i].grad, a.t[i].grad_bf16 != 0, at, left < 8 ? (int)left : 8, g);
+        const int i = tensor_of(a.first, (int)a.count, 2 * c + 1);
+        const int64_t at = (int64_t)(c - (a.first[i] >> 1)) * kNormChunk, left = a.t[i].n - at;
+        if (a.first[i] & 1u) {
+            const uint16_t* g = (const uint16_t*)a.t[i].grad + at;
+            if (left >= kNormChunk) {
+                au32x4 v[kNormChunk / 2048];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fma((double)g[e], (double)g[e], sum);
+                for (int u = 0; u < kNormChunk / 2048; ++u) v[u] = ((const au32x4*)g)[u * 256 + threadIdx.x];
+#pragma unroll
+                for (int u = 0; u < kNormChunk / 2048; ++u) {
+                    float f[8];
+                    unpack8(v[u], f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum = fma((double)f[e], (double)f[e], sum);
+                }
+            } else {
+                for (int64_t j = threadIdx.x; j < left; j += 256) {
+                    const double x = (double)__uint_as_float((uint32_t)g[j] << 16);
+                    sum = fma(x, x, sum);
+                }
+            }
+        } else {
+            const float* g = (const float*)a.t[i].grad + at;
+            if (left >= kNormChunk) {
+                af32x4 v[kNormChunk / 1024];
+#pragma unroll
+                for (int u = 0; u < kNormChunk / 1024; ++u) v[u] = ((const af32x4*)g)[u * 256 + threadIdx.x];
+#pragma unroll
+                for (int u = 0; u < kNormChunk / 1024; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum = fma((double)v[u][e], (double)v[u][e], sum);
+            } else {
+                for (int64_t j = threadIdx.x; j < left; j += 256) sum = fma((double)g[j], (double)g[j], sum);
+            }
+        }
     }
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
@@ -155,34 +183,71 @@ __global__ __launch_bounds__(1024) void norm_final_kernel(const double* __restri
 }
 
 // ------------------------------------------------------------------------------------------
-// AdamW.  The parameter's part of a step, from its new moments: decoupled decay, bias corrections, update.
+// AdamW: clip, moments, bias corrections, decoupled decay and update.
 // ------------------------------------------------------------------------------------------
-__device__ __forceinline__ float adamw_param(float p, float m, float v, float lr, float decay, const StepArgs& a) {
-    return p * decay - lr * ((m * a.inv_bc1) / (sqrtf(v * a.inv_bc2) + a.eps));
+__device__ __forceinline__ void adamw_one(float& p, float g, float& m, float& v, float lr, float decay, const StepArgs& a) {
+    m = a.beta1 * m + (1.f - a.beta1) * g;
+    v = a.beta2 * v + (1.f - a.beta2) * g * g;
+    p = p * decay - lr * ((m * a.inv_bc1) / (sqrtf(v * a.inv_bc2) + a.eps));
 }
 
+// Every value is touched once: streaming accesses, two groups of 16 bytes of a tensor a thread.
 __global__ __launch_bounds__(256) void adamw_multi_kernel(const StepArgs a) {
-    const StepTensor& t = a.t[tensor_of(a.t, (int)a.count, blockIdx.x)];
-    const int64_t at = (int64_t)(blockIdx.x - t.first) * kBlockValues + threadIdx.x * 8, left = t.n - at;
-    if (left <= 0) return;
-    const int live = left < 8 ? (int)left : 8;
+    const int i = tensor_of(a.first, (int)a.count, blockIdx.x);
+    const StepTensor& t = a.t[i];
+    const int64_t at = (int64_t)(blockIdx.x - a.first[i]) * kBlockValues, left = t.n - at;
     const float clip = a.clip_coef ? a.clip_coef[0] : 1.f;
-    float p[8], g[8], m[8], v[8];
-    load_f32(t.param, at, live, p);
-    load_grad(t.grad, t.grad_bf16 != 0, at, live, g);
-    load_f32((const float*)t.m, at, live, m);
-    load_f32((const float*)t.v, at, live, v);
+    float* p = t.param + at;
+    float* m = (float*)t.m + at;
+    float* v = (float*)t.v + at;
+    uint16_t* copy = t.param_bf16 ? t.param_bf16 + at : nullptr;
+    const float* g32 = (const float*)t.grad + at;
+    const uint16_t* g16 = (const uint16_t*)t.grad + at;
+    const float lr = t.lr, decay = t.decay;
+    const bool bf16 = t.grad_bf16 != 0;
+    if (left >= kBlockValues) {
+        af32x4 pv[2], mv[2], vv[2], gv[2];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float ge = g[e] * clip;
-        m[e] = a.beta1 * m[e] + (1.f - a.beta1) * ge;
-        v[e] = a.beta2 * v[e] + (1.f - a.beta2) * ge * ge;
-        p[e] = adamw_param(p[e], m[e], v[e], t.lr, t.decay, a);
+        for (int u = 0; u < 2; ++u) {
+            const int q = u * 256 + (int)threadIdx.x;
+            pv[u] = __builtin_nontemporal_load((const af32x4*)p + q);
+            mv[u] = __builtin_nontemporal_load((const af32x4*)m + q);
+            vv[u] = __builtin_nontemporal_load((const af32x4*)v + q);
+            if (bf16) {
+                const ou32x2 h = __builtin_nontemporal_load((const ou32x2*)g16 + q);
+                gv[u] = af32x4{__uint_as_float(h[0] << 16), __uint_as_float(h[0] & 0xffff0000u),
+                               __uint_as_float(h[1] << 16), __uint_as_float(h[1] & 0xffff0000u)};
+            } else {
+                gv[u] = __builtin_nontemporal_load((const af32x4*)g32 + q);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int q = u * 256 + (int)threadIdx.x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float pe = pv[u][e], me = mv[u][e], ve = vv[u][e];
+                adamw_one(pe, gv[u][e] * clip, me, ve, lr, decay, a);
+                pv[u][e] = pe; mv[u][e] = me; vv[u][e] = ve;
+            }
+            __builtin_nontemporal_store(pv[u], (af32x4*)p + q);
+            __builtin_nontemporal_store(mv[u], (af32x4*)m + q);
+            __builtin_nontemporal_store(vv[u], (af32x4*)v + q);
+            if (copy) {
+                union { __bf16 h[4]; ou32x2 u; } cv;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) cv.h[e] = (__bf16)pv[u][e];
+                *((ou32x2*)copy + q) = cv.u;
+            }
+        }
+        return;
     }
-    store_f32(t.param, at, live, p);
-    store_f32((float*)t.m, at, live, m);
-    store_f32((float*)t.v, at, live, v);
-    if (t.param_bf16) store_bf16(t.param_bf16, at, live, p);
+    for (int j = threadIdx.x; j < left; j += 256) {
+        float pe = p[j], me = m[j], ve = v[j];
+        adamw_one(pe, (bf16 ? __uint_as_float((uint32_t)g16[j] << 16) : g32[j]) * clip, me, ve, lr, decay, a);
+        p[j] = pe; m[j] = me; v[j] = ve;
+        if (copy) { union { __bf16 h; uint16_t u; } cv; cv.h = (__bf16)pe; copy[j] = cv.u; }
+    }
 }
 
 // Moments in 8 bits.  BITS mantissa bits: 3 for m (E4M3, signed), 4 for sqrt(v) (unsigned), bias 7 in both.
@@ -195,46 +260,68 @@ __device__ __forceinline__ uint32_t mix32(uint32_t h) {
     return h ^ (h >> 16);
 }
 
+// What a code stands for, without its scale.  Its fields are moved into fp32's, whose bias is 120 larger:
+// subnormal codes become subnormal values.
 template <int BITS>
-__device__ __forceinline__ double decode8(uint32_t code, int scale) {
+__device__ __forceinline__ float decode8(uint32_t code) {
     const uint32_t mag = BITS == 3 ? code & 0x7fu : code;
-    // the code's fields moved into fp32's, whose bias is 120 larger: subnormal codes become subnormal values
     float x = __uint_as_float(mag << (23 - BITS)) * 0x1p120f;
     if (mag == (BITS == 3 ? 0x7fu : 0xffu)) x = __uint_as_float(0x7fc00000u);
-    if (BITS == 3 && code > 0x7fu) x = -x;
-    return ldexp((double)x, scale - 127);
+    return BITS == 3 && code > 0x7fu ? -x : x;
 }
 
-// The high word of |x|, one more if its low word is not 0, for the block's largest; 0 if x is not finite.
-__device__ __forceinline__ uint32_t high_word_up(double x) {
-    const uint64_t w = (uint64_t)__double_as_longlong(x) & 0x7fffffffffffffffull;
-    const uint32_t high = (uint32_t)(w >> 32);
-    return high >= 0x7ff00000u ? 0u : high + ((uint32_t)w != 0u ? 1u : 0u);
+__device__ __forceinline__ double power_of_two(int e) { return __longlong_as_double((long long)(1023 + e) << 52); }
+
+__device__ __forceinline__ uint32_t high_word(double x) { return (uint32_t)((uint64_t)__double_as_longlong(x) >> 32); }
+
+// sqrt of x >= 0 from the hardware's reciprocal root (2^-27 or so) and one correction of it: good to some 2^-52.
+// Infinite x gives NaN, as its code is.
+__device__ __forceinline__ double root(double x) {
+    const double y = __builtin_amdgcn_rsq(fmax(x, 1e-290)), s = x * y;
+    return fma(0.5 * s, fma(-s, y, 1.0), s);
 }
 
-// e = ceil(log2(amax / top)), top = 1.75 * 2^8 or 1.875 * 2^8, of the largest high_word_up: rounding the
-// words up keeps which side of a border (a value with a low word of 0) they are on.
+__device__ __forceinline__ uint32_t row16_max(uint32_t x) {
+    auto step = [&](uint32_t other) { x = other > x ? other : x; };
+    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, false));       // row_ror:8, 4, 2, 1
+    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xf, 0xf, false));
+    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x122, 0xf, 0xf, false));
+    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x121, 0xf, 0xf, false));
+    return x;
+}
+
+// The exponent of the scale of a block of which this lane has eight values: e = ceil(log2(amax / top)), top = 1.75 * 2^8
+// or 1.875 * 2^8, of the largest finite magnitude.  High words are enough if they are rounded up: that keeps which side
+// of a border (a value whose low word is 0) they are on.
 template <int BITS>
-__device__ __forceinline__ int scale_exponent(uint32_t amax) {
+__device__ __forceinline__ int scale_exponent(const double (&x)[8]) {
+    double top = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmax(top, fabs(x[i]));                               // of a NaN and a number the number
+    if (top == INFINITY) {
+        top = 0.0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fabs(x[i]) < INFINITY ? fmax(top, fabs(x[i])) : top;
+    }
+    const uint32_t amax = row16_max(high_word(top) + ((uint32_t)__double_as_longlong(top) != 0u ? 1u : 0u));
     if (amax == 0u) return 0;
     const int e = (int)(amax >> 20) - 1023 - 8 + ((amax & 0xfffffu) > (BITS == 3 ? 0xc0000u : 0xe0000u) ? 1 : 0);
     return e < -100 ? -100 : (e > 120 ? 120 : e);
 }
 
-// y = |x| 2^-e rounded down after `dither` steps of 2^-(20 - BITS) of a code's step: the high word of a
-// normal y has the code's bits in front of those that the dither meets; below 2^-6, y + 2^-6 has the
-// subnormal codes' step.
+// The code of y = |x| 2^-e, rounded down after `dither` steps of 2^-(20 - BITS) of a code's step.  The high word of a normal y
+// has the code's bits in front of those that the dither meets, with a bias 1016 larger; below 2^-6 codes have the step of
+// that binade, and the significand is moved down to it.
 template <int BITS>
 __device__ __forceinline__ uint32_t encode8(double x, int e, uint32_t dither) {
-    const double a = fabs(x);
-    if (!(a < INFINITY)) return BITS == 3 ? 0x7fu : 0xffu;
-    const double y = ldexp(a, -e);
-    const bool low = y < 0x1p-6;
-    const uint32_t high = (uint32_t)((uint64_t)__double_as_longlong(low ? y + 0x1p-6 : y) >> 32);
-    uint32_t code = ((high + dither) >> (20 - BITS)) - ((low ? 1017u : 1016u) << BITS);
-    if (BITS == 3) { if (x < 0.0) code |= 0x80u; }
-    else if (x > 0.0 && code == 0u) code = 1u;
-    return code;
+    const uint32_t word = high_word(x) & 0x7fffffffu;
+    const int y = (int)(word - ((uint32_t)e << 20));
+    const int down = 1017 - (y >> 20);
+    const uint32_t small = (((uint32_t)y & 0xfffffu) | 0x100000u) >> (down < 31 ? down : 31);
+    uint32_t code = down > 0 ? (small + dither) >> (20 - BITS) : (((uint32_t)y + dither) >> (20 - BITS)) - (1016u << BITS);
+    if (BITS == 4 && code == 0u && x > 0.0) code = 1u;
+    if (BITS == 3 && x < 0.0) code |= 0x80u;
+    return word >= 0x7ff00000u ? (BITS == 3 ? 0x7fu : 0xffu) : code;
 }
 
 __device__ __forceinline__ ou32x2 load_codes(const void* codes, int64_t at, int live) {
@@ -256,41 +343,37 @@ __device__ __forceinline__ void store_codes(void* codes, int64_t at, int live, c
 }
 
 // 16 lanes share a block of 128 values, eight each.  The moments are formed in fp64, so that which way a
-// value next to a border goes does not depend on the order or the fusing of the operations.
+// value next to a border goes does not depend on the order or the fusing of the operations.  The update takes
+// sqrt(v / bc2) from the root that is stored, and reciprocals to one unit in the last place.
 __global__ __launch_bounds__(256) void adamw_multi8_kernel(const StepArgs a) {
-    const StepTensor& t = a.t[tensor_of(a.t, (int)a.count, blockIdx.x)];
-    const int64_t at = (int64_t)(blockIdx.x - t.first) * kBlockValues + threadIdx.x * 8, left = t.n - at;
+    const int i = tensor_of(a.first, (int)a.count, blockIdx.x);
+    const StepTensor& t = a.t[i];
+    const int64_t at = (int64_t)(blockIdx.x - a.first[i]) * kBlockValues + threadIdx.x * 8, left = t.n - at;
     const int live = left < 8 ? (left > 0 ? (int)left : 0) : 8;         // lanes without a value take part in the block's largest
     const int64_t block = at / CCE_STATE8_BLOCK;
     const double clip = a.clip_coef ? (double)a.clip_coef[0] : 1.0;
-    const double b1 = (double)a.beta1, b2 = (double)a.beta2;
     float p[8], g[8];
     load_f32(t.param, at, live, p);
     load_grad(t.grad, t.grad_bf16 != 0, at, live, g);
     const ou32x2 mc = load_codes(t.m, at, live), vc = load_codes(t.v, at, live);
     const int ms = live > 0 ? t.m_scale[block] : 127, vs = live > 0 ? t.v_scale[block] : 127;
+    const double b1 = (double)a.beta1, b2 = (double)a.beta2;
+    const double keep_m = b1 * power_of_two(ms - 127), keep_v = b2 * power_of_two(2 * (vs - 127));
+    const double take_m = (1.0 - b1) * clip, take_v = (1.0 - b2) * clip * clip;
+    const float rate = t.lr * a.inv_bc1;
     double m[8], r[8];
-    uint32_t mtop = 0u, rtop = 0u;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const double ge = (double)g[e] * clip;
-        const double r0 = decode8<4>((vc[e >> 2] >> (8 * (e & 3))) & 0xffu, vs);
-        m[e] = b1 * decode8<3>((mc[e >> 2] >> (8 * (e & 3))) & 0xffu, ms) + (1.0 - b1) * ge;
-        const double v = b2 * (r0 * r0) + ((1.0 - b2) * ge) * ge;
-        r[e] = sqrt(v);
-        p[e] = adamw_param(p[e], (float)m[e], (float)v, t.lr, t.decay, a);
-        const uint32_t mw = high_word_up(m[e]), rw = high_word_up(r[e]);
-        mtop = mw > mtop ? mw : mtop;
-        rtop = rw > rtop ? rw : rtop;
+        const double ge = (double)g[e];
+        const float r0 = decode8<4>((vc[e >> 2] >> (8 * (e & 3))) & 0xffu);             // whose square has ten bits
+        m[e] = fma((double)decode8<3>((mc[e >> 2] >> (8 * (e & 3))) & 0xffu), keep_m, ge * take_m);
+        r[e] = root(fma((double)(r0 * r0), keep_v, ge * ge * take_v));
+        const float rf = (float)r[e], under = fmaxf(fmaf(rf, a.root_inv_bc2, a.eps), 0x1p-126f);
+        const float update = rate * (float)m[e] * __builtin_amdgcn_rcpf(under);
+        p[e] = fmaf(p[e], t.decay, rf == rf ? -update : rf);
     }
-#pragma unroll
-    for (int o = 1; o <= 8; o <<= 1) {
-        const uint32_t mo = (uint32_t)__shfl_xor((int)mtop, o), ro = (uint32_t)__shfl_xor((int)rtop, o);
-        mtop = mo > mtop ? mo : mtop;
-        rtop = ro > rtop ? ro : rtop;
-    }
+    const int em = scale_exponent<3>(m), er = scale_exponent<4>(r);
     if (live == 0) return;
-    const int em = scale_exponent<3>(mtop), er = scale_exponent<4>(rtop);
     ou32x2 mo = {0u, 0u}, vo = {0u, 0u};
     const uint32_t base = (uint32_t)at + (uint32_t)((uint64_t)at >> 32) * 32310901u + a.key;
 #pragma unroll
@@ -315,12 +398,12 @@ __global__ __launch_bounds__(256) void state8_read_kernel(const uint8_t* __restr
     for (int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; at < n; at += (int64_t)gridDim.x * kBlockValues) {
         const int live = n - at < 8 ? (int)(n - at) : 8;
         const ou32x2 c = load_codes(codes, at, live);
-        const int scale = scales[at / CCE_STATE8_BLOCK];
+        const double power = power_of_two((BITS == 4 ? 2 : 1) * (scales[at / CCE_STATE8_BLOCK] - 127));
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const double d = decode8<BITS>((c[e >> 2] >> (8 * (e & 3))) & 0xffu, scale);
-            x[e] = (float)(BITS == 4 ? d * d : d);
+            const float d = decode8<BITS>((c[e >> 2] >> (8 * (e & 3))) & 0xffu);
+            x[e] = (float)((double)(BITS == 4 ? d * d : d) * power);
         }
         store_f32(out, at, live, x);
     }
@@ -344,7 +427,7 @@ static int check_gradients(const cce_optim_tensor* tensors, int64_t count) {
         if (t.n < 0) return CCE_ERR_INVALID;
         if (t.n == 0) continue;
         blocks += t.n / kBlockValues + 1;
-        if (t.n > kMaxTensor || blocks > 0x7fffffff) return CCE_ERR_UNSUPPORTED;
+        if (t.n > kMaxTensor || blocks > 0x3fffffff) return CCE_ERR_UNSUPPORTED;
         if (!t.grad || misaligned(t.grad, 16) || (t.grad_bf16 != 0 && t.grad_bf16 != 1)) return CCE_ERR_INVALID;
     }
     return CCE_OK;
@@ -379,8 +462,9 @@ int cce_grad_sumsq_multi(const cce_optim_tensor* tensors, int64_t count, double*
         for (; i < count && a.count < (uint32_t)kNormTensors; ++i) {
             const cce_optim_tensor& t = tensors[i];
             if (t.n == 0) continue;
-            a.t[a.count++] = NormTensor{t.grad, t.n, (uint32_t)chunks, (uint32_t)t.grad_bf16};
-            chunks += (t.n + kBlockValues - 1) / kBlockValues;
+            a.first[a.count] = 2 * (uint32_t)chunks + (uint32_t)t.grad_bf16;
+            a.t[a.count++] = NormTensor{t.grad, t.n};
+            chunks += (t.n + kNormChunk - 1) / kNormChunk;
         }
         if (a.count == 0) continue;
         const int blocks = (int)(chunks < kNormBlocks ? chunks : kNormBlocks);
@@ -415,6 +499,7 @@ int cce_adamw_multi_step(const cce_optim_tensor* tensors, int64_t count, float l
     a.beta1 = beta1; a.beta2 = beta2; a.eps = eps;
     a.inv_bc1 = (float)(1.0 / (1.0 - pow((double)beta1, (double)step)));
     a.inv_bc2 = (float)(1.0 / (1.0 - pow((double)beta2, (double)step)));
+    a.root_inv_bc2 = (float)sqrt(1.0 / (1.0 - pow((double)beta2, (double)step)));
     a.key = mix32_host(seed + mix32_host((uint32_t)step));
     for (int state8 = 0; state8 < 2; ++state8) {
         for (int64_t i = 0; i < count;) {
@@ -426,8 +511,9 @@ int cce_adamw_multi_step(const cce_optim_tensor* tensors, int64_t count, float l
                 const int64_t own = (t.n + kBlockValues - 1) / kBlockValues;
                 if (blocks + own > kMaxGrid) break;
                 const float rate = lr * t.lr_scale;
+                a.first[a.count] = (uint32_t)blocks;
                 a.t[a.count++] = StepTensor{t.param, (uint16_t*)t.param_bf16, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.n,
-                                            rate, 1.f - rate * t.weight_decay, (uint32_t)blocks, (uint32_t)t.grad_bf16};
+                                            rate, 1.f - rate * t.weight_decay, (uint64_t)t.grad_bf16};
                 blocks += own;
             }
             if (a.count == 0) continue;

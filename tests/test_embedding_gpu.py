@@ -102,6 +102,27 @@ def test_gradient_at_vocabulary_borders(B, V):
     _gradient_case(B, 700, 16, V, "one", 0.1, 1.0, False)
 
 
+@pytest.mark.parametrize("N,D,V,hot", [(1_100_003, 8, 70000, 0.5), (300_001, 64, 700, 0.0), (70_000, 264, 200_000, 0.9), (1_048_577, 16, 1, 0.0)])
+def test_gradient_of_many_tokens(B, N, D, V, hot):
+    """Ranges of a wavefront beyond 16 bits, and more of a slice's tokens in one than it notes: whole numbers, whose sums
+    fp32 holds."""
+    rng = np.random.default_rng(N)
+    t = rng.integers(0, V, N).astype(np.int32)
+    t[rng.random(N) < hot] = min(5, V - 1)
+    t[rng.random(N) < 0.05] = IGN
+    dy = rng.integers(-4, 5, (N, D))
+    ok = E.takes_part(t, V, IGN)
+    want = np.stack([np.bincount(t[ok], weights=dy[ok, j], minlength=V) for j in range(D)], axis=1)
+    assert np.abs(dy).sum(0).max() < 2 ** 24
+    print(f"[gradient] N={N} D={D} V={V}", flush=True)
+    td, dyd = torch.from_numpy(t).cuda(), torch.from_numpy(dy).cuda().bfloat16()
+    for accumulate in (False, True):
+        dw, intact = _guarded((V, D), torch.float32)
+        dw.fill_(3.0)
+        B.cce_embedding_backward(td, dyd, V, IGN, scale=2.0, d_weight=dw, accumulate_dw=accumulate)
+        assert np.array_equal(dw.cpu().numpy(), 2.0 * want + (3.0 if accumulate else 0.0)) and intact()
+
+
 def test_tokens_outside_the_matrix_are_reported(B):
     V, D = 30, 64
     t = np.array([0, 30, 29, -1, IGN, 5, 2 ** 31 - 1, -2 ** 31], dtype=np.int32)
