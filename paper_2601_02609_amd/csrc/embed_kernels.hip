@@ -74,13 +74,19 @@ __global__ __launch_bounds__(256) void embedding_forward_kernel(
 // The order of all sums follows from the tokens and the sizes.
 // ------------------------------------------------------------------------------------------
 constexpr int kSliceKeys = 640;                 // rows of the matrix that an order workgroup counts: 40 KB of LDS
+constexpr int kKeyBits = 10;
+static_assert(kSliceKeys <= 1 << kKeyBits, "bits of a key");
 constexpr int kOrderWaves = 16;
 constexpr int kOrderLoads = 8;                  // loads of tokens in flight, and as many ahead
 constexpr int kFound = 640;                     // positions that a wavefront notes: 20 KB of LDS
+constexpr int kSmallTokens = 1024;              // one launch takes: a thread each
+constexpr int kSmallRows = 2048;                // and rows of strips, which one workgroup may have all of
+constexpr int kSmallShare = 16;                 // rows of a key that one wavefront adds up
 constexpr int kJoinWaves = 8;
 constexpr int kJoinShort = 16;                  // pieces of a group that one wavefront joins, and one more
 constexpr int kSumWaves = 4096;                 // wavefronts that the sum is cut into, if there are rows for them
 constexpr int kMaxPiece = 128;
+constexpr int64_t kStreamBytes = (int64_t)128 << 20;      // half of the last-level cache
 
 // Slices of the vocabulary: token t is key t / slices of slice t % slices (a power of two).  The frequent tokens, which
 // tokenizers number first, are spread over the slices.
@@ -103,6 +109,18 @@ struct EmbedBackward {
     float scale;
 };
 
+// Of the lanes `among`, those that have this lane's key: they find each other bit by bit.
+__device__ __forceinline__ unsigned long long lanes_of_key(unsigned long long among, uint32_t key) {
+    unsigned long long same = among;
+#pragma unroll
+    for (int b = 0; b < kKeyBits; ++b) {
+        const uint32_t bit = 0u - (key >> b & 1u);
+        const unsigned long long ones = __ballot(bit != 0u);
+        same &= ~(ones ^ ((unsigned long long)bit << 32 | bit));
+    }
+    return same;
+}
+
 // A workgroup per slice looks through all tokens (which stay in the L2s): its wavefronts, each with a range of positions,
 // count their keys in LDS and note what they found there; after a scan over keys and wavefronts they give the positions
 // of one key consecutive places.  64 tokens that none is in the slice of cost a handful of instructions, most of them
@@ -111,30 +129,28 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const
     __shared__ uint32_t count[kOrderWaves * kSliceKeys];
     __shared__ uint16_t found[kOrderWaves][kFound];          // places in the wavefront's range
     __shared__ uint32_t wave_total[kOrderWaves], wave_below[kOrderWaves];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int slice = blockIdx.x, mask = (1 << a.bits) - 1;
     uint32_t* own = count + w * a.keys;
-    for (int i = threadIdx.x; i < kOrderWaves * a.keys; i += 64 * kOrderWaves) count[i] = 0u;
-    __syncthreads();
-
     const int64_t range = ((int64_t)a.N + 64 * kOrderWaves - 1) / (64 * kOrderWaves) * 64;
     const int64_t begin = w * range, end = begin + range < a.N ? begin + range : a.N;
     const unsigned long long lanes_below = (1ull << lane) - 1ull;
     if (slice == 0 && a.status)
         for (int64_t i = begin + lane; i < end; i += 64) token_takes_part(a.tokens[i], a.V, a.ignore_index, a.status);
-    auto load = [&](int64_t i, int (&token)[kOrderLoads]) {
-        if (i + 64 * kOrderLoads <= end) {
+    auto load = [&](int64_t i, int (&token)[kOrderLoads]) {  // -1 behind the end; every load is made, none waits for another
+        const int64_t from = i < a.N ? i : 0;
+        const int left = i < end ? (end - i < 64 * kOrderLoads ? (int)(end - i) : 64 * kOrderLoads) : 0;
 #pragma unroll
-            for (int u = 0; u < kOrderLoads; ++u) token[u] = a.tokens[i + 64 * u + lane];
-        } else {
+        for (int u = 0; u < kOrderLoads; ++u) token[u] = a.tokens[from + (64 * u + lane < left ? 64 * u + lane : 0)];
 #pragma unroll
-            for (int u = 0; u < kOrderLoads; ++u) token[u] = i + 64 * u + lane < end ? a.tokens[i + 64 * u + lane] : -1;
-        }
+        for (int u = 0; u < kOrderLoads; ++u) token[u] = 64 * u + lane < left ? token[u] : -1;
     };
     auto valid = [&](int token) { return (unsigned)token < (unsigned)a.V && token != a.ignore_index; };
     uint32_t below = 0u, n = 0u;                             // tokens of slices below and of this one, in scalar registers
     int token[kOrderLoads], next[kOrderLoads];
     load(begin, token);
+    for (int i = threadIdx.x; i < kOrderWaves * a.keys; i += 64 * kOrderWaves) count[i] = 0u;
+    __syncthreads();
     for (int64_t i = begin; i < end; i += 64 * kOrderLoads) {
         load(i + 64 * kOrderLoads, next);
 #pragma unroll
@@ -146,7 +162,7 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const
             if (mine != 0ull) {
                 if (mine >> lane & 1ull) {
                     const uint32_t place = n + (uint32_t)__popcll(mine & lanes_below);
-                    atomicAdd(&own[token[u] >> a.bits], 1u);
+                    atomicAdd(&own[(uint32_t)token[u] >> a.bits], 1u);
                     if (place < (uint32_t)kFound) found[w][place] = (uint16_t)((i - begin) + 64 * u + lane);
                 }
                 n += (uint32_t)__popcll(mine);
@@ -184,13 +200,9 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const
         }
     __syncthreads();
 
-    // 64 positions, those of `mine` in ascending order with keys of this slice: lanes of one key find each other bit by bit
+    // 64 positions, those of `mine` in ascending order with keys of this slice
     auto place_them = [&](unsigned long long mine, uint32_t k, int64_t position) {
-        unsigned long long same = mine;
-        for (int b = 0; (a.keys - 1) >> b != 0; ++b) {
-            const unsigned long long ones = __ballot(k >> b & 1u);
-            same &= k >> b & 1u ? ones : ~ones;
-        }
+        const unsigned long long same = lanes_of_key(mine, k);
         if (mine >> lane & 1ull) {
             const int leader = __ffsll(same) - 1;
             uint32_t to = 0u;
@@ -202,10 +214,18 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const
     };
     auto place_found = [&](uint32_t many, int64_t from) {    // what found[w] holds, as places behind `from`
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        for (uint32_t i = 0; i < many; i += 64) {
-            const int64_t position = from + (i + lane < many ? found[w][i + lane] : 0);
-            const int t = a.tokens[position];
-            place_them(__ballot(i + lane < many), (uint32_t)t >> a.bits, position);
+        for (uint32_t i = 0; i < many; i += 256) {
+            int64_t position[4];
+            int t[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t j = i + 64 * u + lane;
+                position[u] = from + (j < many ? found[w][j] : 0);
+                t[u] = a.tokens[position[u]];
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (i + 64 * u < many) place_them(__ballot(i + 64 * u + lane < many), (uint32_t)t[u] >> a.bits, position[u]);
         }
     };
     if (n <= (uint32_t)kFound && range <= 65536) {
@@ -239,7 +259,9 @@ __device__ __forceinline__ int of_lane(int x, int j) {
 
 // LPR lanes share a row (a strip of 512 columns of it if D > 512), 16 bytes each, and take one piece.  Eight rows, and
 // the rows of dW that they end at, are in flight.
-template <int LPR>
+// STREAM: d_out of kStreamBytes or more, read past the caches, which keep more of dW then: 140 -> 123 us for 32768 x 3584 added to
+// dW, 93 -> 85 for 32768 x 2048 (128 MiB); below, rows that the launch before left there are worth more (16384 x 2048 45 -> 50).
+template <int LPR, bool STREAM>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbedBackward a, int sum_blocks) {
     const int slices = 1 << a.bits;
     if ((int)blockIdx.x >= sum_blocks) {                     // zeros: 64 keys of a slice for each workgroup
@@ -254,7 +276,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbedBackward 
             const int64_t v = ((int64_t)(first + __ffsll(none) - 1) << a.bits) + slice;
             none &= none - 1;
             af32x4* to = (af32x4*)a.dW + (size_t)v * width;
-            for (int i = threadIdx.x; i < width; i += 256) to[i] = af32x4{0.f, 0.f, 0.f, 0.f};
+            for (int i = threadIdx.x; i < width; i += 256) __builtin_nontemporal_store(af32x4{0.f, 0.f, 0.f, 0.f}, to + i);
         }
         return;
     }
@@ -293,7 +315,10 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbedBackward 
         bool inside = begun;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (j < rows) x[j] = ((const au32x4*)a.d_out)[(size_t)of_lane<LPR>(pos, j) * a.row_chunks + c];
+            if (j < rows) {
+                const au32x4* from = (const au32x4*)a.d_out + (size_t)of_lane<LPR>(pos, j) * a.row_chunks + c;
+                x[j] = STREAM ? __builtin_nontemporal_load(from) : *from;
+            }
         if (a.accumulate) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -405,6 +430,139 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(const E
     }
 }
 
+// ------------------------------------------------------------------------------------------
+// Few tokens: one launch.  A workgroup per slice finds its positions among all N <= kSmallTokens in order, then a wavefront
+// sums a key's rows (a strip of 512 columns of them) by itself, or all of them share the rows of a key that has many.
+// Bound by latency, launches above all.  Against the three launches: 257 x 64 into a new dW 13.1 -> 4.9 us; added to dW, 512 x 896
+// 15.9 -> 6.1, 1024 x 896 16.9 -> 7.5, 256 x 4096 17.1 -> 8.9.  kSmallRows bounds what one workgroup may have to sum if all tokens
+// are the same: 14.5 -> 24.4 us for 1024 x 896 then, 15.0 -> 46.9 for 1024 x 2048, which takes three launches.
+// ------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(64 * kOrderWaves) void embedding_small_kernel(const EmbedBackward a) {
+    __shared__ uint32_t mine[kSmallTokens];                  // this slice's positions, ascending, and their keys in the upper 16 bits
+    __shared__ uint16_t rows[kSmallTokens];                  // the positions, those of a key together
+    __shared__ uint32_t first[kSliceKeys], many[kSliceKeys]; // of each key: its first place in `mine`, how many it has
+    __shared__ uint32_t begin[kSliceKeys];                   // where its rows begin, then where the next one goes
+    __shared__ uint32_t keys_here[kSmallTokens];
+    __shared__ uint32_t wave_count[kOrderWaves], keys_found, rows_given;
+    __shared__ float red[kOrderWaves][512];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int slice = blockIdx.x, mask = (1 << a.bits) - 1;
+    const int token = (int)threadIdx.x < a.N ? a.tokens[threadIdx.x] : a.ignore_index;
+    const bool ok = token_takes_part(token, a.V, a.ignore_index, slice == 0 ? a.status : nullptr);
+    const unsigned long long hits = __ballot(ok && (token & mask) == slice);
+    if (lane == 0) wave_count[w] = (uint32_t)__popcll(hits);
+    if ((int)threadIdx.x < a.keys) { first[threadIdx.x] = 0xffffffffu; many[threadIdx.x] = 0u; }
+    if (threadIdx.x == 0) keys_found = rows_given = 0u;
+    __syncthreads();
+    uint32_t at = 0u, n = 0u;
+#pragma unroll
+    for (int i = 0; i < kOrderWaves; ++i) {
+        at += i < w ? wave_count[i] : 0u;
+        n += wave_count[i];
+    }
+    if (hits >> lane & 1ull) {
+        const uint32_t key = (uint32_t)token >> a.bits;
+        at += (uint32_t)__popcll(hits & ((1ull << lane) - 1ull));
+        mine[at] = key << 16 | threadIdx.x;
+        atomicMin(&first[key], at);
+        atomicAdd(&many[key], 1u);
+    }
+    __syncthreads();
+    const uint32_t own = threadIdx.x < n ? mine[threadIdx.x] : 0u, key = own >> 16;
+    if (threadIdx.x < n && first[key] == threadIdx.x) {      // keys in whatever order: no sum is over two of them
+        keys_here[atomicAdd(&keys_found, 1u)] = key;
+        begin[key] = atomicAdd(&rows_given, many[key]);
+    }
+    __syncthreads();
+    const unsigned long long live = __ballot(threadIdx.x < n);
+    const unsigned long long same = lanes_of_key(live, key);
+    const int leader = live >> lane & 1ull ? __ffsll(same) - 1 : lane;
+    for (uint32_t turn = 0; turn * 64u < n; ++turn) {        // one wavefront after the other, so that positions stay in order
+        if (w == (int)turn) {
+            uint32_t to = 0u;
+            if (lane == leader && threadIdx.x < n) to = atomicAdd(&begin[key], (uint32_t)__popcll(same));
+            to = (uint32_t)__shfl((int)to, leader) + (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
+            if (threadIdx.x < n) rows[to] = (uint16_t)own;
+        }
+        __syncthreads();
+    }
+    const int found = (int)keys_found;                       // and begin is where a key's rows end now
+
+    // the rows `from` up to `to` of this slice's, one chunk a lane, eight rows in flight
+    auto sum_rows = [&](uint32_t from, uint32_t to, int c, float (&sum)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+        for (uint32_t i = from; i < to; i += 8) {
+            au32x4 x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const size_t row = rows[i + j < to ? i + j : i];
+                x[j] = ((const au32x4*)a.d_out)[row * a.row_chunks + c];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (i + j >= to) continue;
+                float f[8];
+                unpack8(x[j], f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += f[e];
+            }
+        }
+    };
+    auto row_at = [&](uint32_t k, int c) { return (af32x4*)a.dW + ((((size_t)k << a.bits) + slice) * a.row_chunks + c) * 2; };
+    auto add_to_row = [&](af32x4* to, const af32x4 (&old)[2], const float (&sum)[8]) {
+        to[0] = old[0] + af32x4{a.scale * sum[0], a.scale * sum[1], a.scale * sum[2], a.scale * sum[3]};
+        to[1] = old[1] + af32x4{a.scale * sum[4], a.scale * sum[5], a.scale * sum[6], a.scale * sum[7]};
+    };
+    for (int item = w; item < found * a.strips; item += kOrderWaves) {
+        const uint32_t k = keys_here[item / a.strips], to = begin[k], from = to - many[k];
+        const int c = item % a.strips * 64 + lane;
+        if (to - from > (uint32_t)kSmallShare || c >= a.row_chunks) continue;
+        af32x4* at_row = row_at(k, c);
+        af32x4 old[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        if (a.accumulate) { old[0] = at_row[0]; old[1] = at_row[1]; }
+        float sum[8];
+        sum_rows(from, to, c, sum);
+        add_to_row(at_row, old, sum);
+    }
+    // a key with many rows: the wavefronts take `side` strips side by side and `parts` parts of the rows
+    int side = 1;
+    while (side < a.strips && side < kOrderWaves) side <<= 1;
+    const int parts = kOrderWaves / side;
+    for (int g = 0; g < found; ++g) {
+        const uint32_t k = keys_here[g], to = begin[k], from = to - many[k];
+        if (to - from <= (uint32_t)kSmallShare) continue;    // the same for all
+        const uint32_t part = (to - from + parts - 1) / parts;
+        for (int strip = 0; strip < a.strips; strip += side) {
+            const int c = (strip + w % side) * 64 + lane;
+            const uint32_t low = from + (w / side) * part, high = low + part < to ? low + part : to;
+            float sum[8];
+            sum_rows(low, c < a.row_chunks ? high : low, c, sum);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) red[w][lane * 8 + e] = sum[e];
+            __syncthreads();
+            if (w < side && c < a.row_chunks) {
+                af32x4* at_row = row_at(k, c);
+                af32x4 old[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+                if (a.accumulate) { old[0] = at_row[0]; old[1] = at_row[1]; }
+                for (int i = 1; i < parts; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[e] += red[i * side + w][lane * 8 + e];
+                add_to_row(at_row, old, sum);
+            }
+            __syncthreads();
+        }
+    }
+    if (a.accumulate) return;
+    const int width = a.row_chunks * 2;
+    for (int k = w; k < a.keys; k += kOrderWaves) {
+        const int64_t v = ((int64_t)k << a.bits) + slice;
+        if (many[k] != 0u || v >= a.V) continue;
+        af32x4* to = (af32x4*)a.dW + (size_t)v * width;
+        for (int i = lane; i < width; i += 64) __builtin_nontemporal_store(af32x4{0.f, 0.f, 0.f, 0.f}, to + i);
+    }
+}
+
 // Lanes that share a row, and the rest of a row's chunks in further strips.
 static int embed_lanes(int64_t D) { return D <= 64 ? 8 : D <= 128 ? 16 : D <= 256 ? 32 : 64; }
 
@@ -484,6 +642,11 @@ int cce_embedding_backward(const int32_t* tokens, const void* d_out, int64_t N, 
     a.order = (int32_t*)at; at += round_up(N * 4, 256);
     a.sorted = (int32_t*)at; at += round_up(N * 4, 256);
     a.partial = (float*)at;
+    if (N <= kSmallTokens && N * ((a.row_chunks + 63) / 64) <= kSmallRows) {
+        a.strips = (a.row_chunks + 63) / 64;
+        hipLaunchKernelGGL(embedding_small_kernel, dim3((unsigned)slices), dim3(64 * kOrderWaves), 0, stream, a);
+        return hip_ok(hipGetLastError()) ? CCE_OK : CCE_ERR_HIP;
+    }
     hipLaunchKernelGGL(embedding_order_kernel, dim3((unsigned)slices), dim3(64 * kOrderWaves), 0, stream, a);
 
     const int lanes = embed_lanes(D);
@@ -492,10 +655,11 @@ int cce_embedding_backward(const int32_t* tokens, const void* d_out, int64_t N, 
     const int sum_blocks = (int)((pieces * a.strips * lanes + 255) / 256);
     const int zero_blocks = a.accumulate ? 0 : (a.keys + 63) / 64 * slices;
     const dim3 grid((unsigned)(sum_blocks + zero_blocks));
-    if (lanes == 8) hipLaunchKernelGGL(embedding_sum_kernel<8>, grid, dim3(256), 0, stream, a, sum_blocks);
-    else if (lanes == 16) hipLaunchKernelGGL(embedding_sum_kernel<16>, grid, dim3(256), 0, stream, a, sum_blocks);
-    else if (lanes == 32) hipLaunchKernelGGL(embedding_sum_kernel<32>, grid, dim3(256), 0, stream, a, sum_blocks);
-    else hipLaunchKernelGGL(embedding_sum_kernel<64>, grid, dim3(256), 0, stream, a, sum_blocks);
+    const bool stream_rows = N * D * 2 >= kStreamBytes;
+#define CCE_EMBED_SUM(LPR, STREAM) hipLaunchKernelGGL((embedding_sum_kernel<LPR, STREAM>), grid, dim3(256), 0, stream, a, sum_blocks)
+    if (lanes == 8) CCE_EMBED_SUM(8, false); else if (lanes == 16) CCE_EMBED_SUM(16, false); else if (lanes == 32) CCE_EMBED_SUM(32, false);
+    else if (stream_rows) CCE_EMBED_SUM(64, true); else CCE_EMBED_SUM(64, false);
+#undef CCE_EMBED_SUM
 
     if (pieces > 1) {
         const int strips = (int)((D + 255) / 256);
