@@ -10,7 +10,7 @@
  *
  * `tensors` is a HOST array, read before the call returns and not kept: addresses may change from
  * call to call.  count >= 1.  A tensor of n = 0 values takes no part and its pointers are not looked
- * at; n is at most 2^34, all together 2^41 (CCE_ERR_UNSUPPORTED beyond).  The memory of no two entries
+ * at; n is at most 2^33, all together 2^40 (CCE_ERR_UNSUPPORTED beyond).  The memory of no two entries
  * may overlap.
  */
 #ifndef CCE_OPTIM_H_

@@ -64,7 +64,7 @@ def encode(x, u, bits: int):
             code = np.where((x[at] > 0.0) & (code == 0), 1, code)
         code = np.where(fine, code, NAN[bits])
         if bits == M:
-            code = code + np.where(fine & (x[at] < 0.0), 128, 0)
+            code = code + np.where(fine & np.signbit(x[at]), 128, 0)
         codes[at] = code
         scales[b] = e + 127
     return codes, scales

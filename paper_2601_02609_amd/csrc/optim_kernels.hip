@@ -2,7 +2,7 @@
 // moments in fp32 or in 8 bits.  C ABI declared in include/cce_optim.h.
 //
 // The tensors of a launch are a table in the kernel's arguments (nothing to copy, nothing to keep): a
-// tensor's values are cut into blocks of kBlockValues and the workgroups are numbered through all of them.
+// tensor's values are cut into blocks of kStepValues (kNormChunk) and the workgroups are numbered through all of them.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stddef.h>
@@ -16,9 +16,11 @@
 namespace cce {
 
 typedef __attribute__((ext_vector_type(2))) unsigned int ou32x2;
+typedef __attribute__((ext_vector_type(2))) float of32x2;
 
-constexpr int kBlockValues = 2048;                     // values of a workgroup: eight a thread
-constexpr int64_t kMaxTensor = (int64_t)1 << 34;       // values of a tensor
+constexpr int kStepValues = 1024;                      // values of a workgroup of a step: four a thread
+constexpr int kReadValues = 2048;                      // of a workgroup that reads 8-bit moments
+constexpr int64_t kMaxTensor = (int64_t)1 << 33;       // values of a tensor
 constexpr int64_t kMaxGrid = (1 << 24) - 1;            // of 256 threads: a launch has fewer than 2^32 threads
 constexpr int kStepTensors = 44;                       // tensors of a launch: kernel arguments hold 4 KB
 constexpr int kNormTensors = 160;
@@ -71,44 +73,23 @@ __device__ __forceinline__ int tensor_of(const uint32_t* first, int count, uint3
     return __builtin_amdgcn_readfirstlane(n - 1);
 }
 
-// Eight gradient values from `at` on, of which `live` exist; zeros behind them.
-__device__ __forceinline__ void load_grad(const void* grad, bool bf16, int64_t at, int live, float (&g)[8]) {
-    if (live >= 8) {
-        if (bf16) {
-            unpack8(*(const au32x4*)((const uint16_t*)grad + at), g);
-        } else {
-            const af32x4 a = *(const af32x4*)((const float*)grad + at), b = *(const af32x4*)((const float*)grad + at + 4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { g[e] = a[e]; g[4 + e] = b[e]; }
-        }
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        g[e] = 0.f;
-        if (e < live) g[e] = bf16 ? __uint_as_float((uint32_t)((const uint16_t*)grad)[at + e] << 16) : ((const float*)grad)[at + e];
-    }
+__device__ __forceinline__ float grad_at(const void* grad, bool bf16, int64_t i) {
+    return bf16 ? __uint_as_float((uint32_t)((const uint16_t*)grad)[i] << 16) : ((const float*)grad)[i];
 }
 
-__device__ __forceinline__ void load_f32(const float* p, int64_t at, int live, float (&x)[8]) { load_grad(p, false, at, live, x); }
-
-__device__ __forceinline__ void store_f32(float* p, int64_t at, int live, const float (&x)[8]) {
-    if (live >= 8) {
-        *(af32x4*)(p + at) = af32x4{x[0], x[1], x[2], x[3]};
-        *(af32x4*)(p + at + 4) = af32x4{x[4], x[5], x[6], x[7]};
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < live) p[at + e] = x[e];
+// Group q of four gradient values behind `base`.
+__device__ __forceinline__ af32x4 load_grad4(const void* grad, bool bf16, int64_t base, int q) {
+    if (!bf16) return __builtin_nontemporal_load((const af32x4*)((const float*)grad + base) + q);
+    const ou32x2 h = __builtin_nontemporal_load((const ou32x2*)((const uint16_t*)grad + base) + q);
+    return af32x4{__uint_as_float(h[0] << 16), __uint_as_float(h[0] & 0xffff0000u),
+                  __uint_as_float(h[1] << 16), __uint_as_float(h[1] & 0xffff0000u)};
 }
 
-__device__ __forceinline__ void store_bf16(uint16_t* p, int64_t at, int live, const float (&x)[8]) {
-    const au32x4 packed = pack8(x);
-    if (live >= 8) { *(au32x4*)(p + at) = packed; return; }
+__device__ __forceinline__ ou32x2 pack4(const af32x4& x) {
+    union { __bf16 h[4]; ou32x2 u; } cv;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < live) p[at + e] = (uint16_t)(packed[e >> 1] >> (16 * (e & 1)));
+    for (int e = 0; e < 4; ++e) cv.h[e] = (__bf16)x[e];
+    return cv.u;
 }
 
 // ------------------------------------------------------------------------------------------
@@ -191,62 +172,39 @@ __device__ __forceinline__ void adamw_one(float& p, float g, float& m, float& v,
     p = p * decay - lr * ((m * a.inv_bc1) / (sqrtf(v * a.inv_bc2) + a.eps));
 }
 
-// Every value is touched once: streaming accesses, two groups of 16 bytes of a tensor a thread.
+// Every value is touched once: streaming accesses of 16 bytes, one group of a tensor a thread.  Bound by HBM: 411 M values at
+// the rate of a copy of as many bytes.  Two groups a thread took 2.6 % longer, four 1.3 %; 32 bytes of a thread in a row 3.5 %.
 __global__ __launch_bounds__(256) void adamw_multi_kernel(const StepArgs a) {
     const int i = tensor_of(a.first, (int)a.count, blockIdx.x);
     const StepTensor& t = a.t[i];
-    const int64_t at = (int64_t)(blockIdx.x - a.first[i]) * kBlockValues, left = t.n - at;
+    const int64_t base = (int64_t)(blockIdx.x - a.first[i]) * kStepValues, left = t.n - base;
     const float clip = a.clip_coef ? a.clip_coef[0] : 1.f;
-    float* p = t.param + at;
-    float* m = (float*)t.m + at;
-    float* v = (float*)t.v + at;
-    uint16_t* copy = t.param_bf16 ? t.param_bf16 + at : nullptr;
-    const float* g32 = (const float*)t.grad + at;
-    const uint16_t* g16 = (const uint16_t*)t.grad + at;
-    const float lr = t.lr, decay = t.decay;
+    float* p = t.param + base;
+    float* m = (float*)t.m + base;
+    float* v = (float*)t.v + base;
     const bool bf16 = t.grad_bf16 != 0;
-    if (left >= kBlockValues) {
-        af32x4 pv[2], mv[2], vv[2], gv[2];
+    const int q = threadIdx.x;
+    if (left >= kStepValues) {
+        af32x4 pv = __builtin_nontemporal_load((const af32x4*)p + q), mv = __builtin_nontemporal_load((const af32x4*)m + q),
+               vv = __builtin_nontemporal_load((const af32x4*)v + q);
+        const af32x4 gv = load_grad4(t.grad, bf16, base, q);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int q = u * 256 + (int)threadIdx.x;
-            pv[u] = __builtin_nontemporal_load((const af32x4*)p + q);
-            mv[u] = __builtin_nontemporal_load((const af32x4*)m + q);
-            vv[u] = __builtin_nontemporal_load((const af32x4*)v + q);
-            if (bf16) {
-                const ou32x2 h = __builtin_nontemporal_load((const ou32x2*)g16 + q);
-                gv[u] = af32x4{__uint_as_float(h[0] << 16), __uint_as_float(h[0] & 0xffff0000u),
-                               __uint_as_float(h[1] << 16), __uint_as_float(h[1] & 0xffff0000u)};
-            } else {
-                gv[u] = __builtin_nontemporal_load((const af32x4*)g32 + q);
-            }
+        for (int e = 0; e < 4; ++e) {
+            float pe = pv[e], me = mv[e], ve = vv[e];
+            adamw_one(pe, gv[e] * clip, me, ve, t.lr, t.decay, a);
+            pv[e] = pe; mv[e] = me; vv[e] = ve;
         }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int q = u * 256 + (int)threadIdx.x;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float pe = pv[u][e], me = mv[u][e], ve = vv[u][e];
-                adamw_one(pe, gv[u][e] * clip, me, ve, lr, decay, a);
-                pv[u][e] = pe; mv[u][e] = me; vv[u][e] = ve;
-            }
-            __builtin_nontemporal_store(pv[u], (af32x4*)p + q);
-            __builtin_nontemporal_store(mv[u], (af32x4*)m + q);
-            __builtin_nontemporal_store(vv[u], (af32x4*)v + q);
-            if (copy) {
-                union { __bf16 h[4]; ou32x2 u; } cv;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) cv.h[e] = (__bf16)pv[u][e];
-                *((ou32x2*)copy + q) = cv.u;
-            }
-        }
+        __builtin_nontemporal_store(pv, (af32x4*)p + q);
+        __builtin_nontemporal_store(mv, (af32x4*)m + q);
+        __builtin_nontemporal_store(vv, (af32x4*)v + q);
+        if (t.param_bf16) *((ou32x2*)(t.param_bf16 + base) + q) = pack4(pv);
         return;
     }
-    for (int j = threadIdx.x; j < left; j += 256) {
+    for (int j = q; j < left; j += 256) {
         float pe = p[j], me = m[j], ve = v[j];
-        adamw_one(pe, (bf16 ? __uint_as_float((uint32_t)g16[j] << 16) : g32[j]) * clip, me, ve, lr, decay, a);
+        adamw_one(pe, grad_at(t.grad, bf16, base + j) * clip, me, ve, t.lr, t.decay, a);
         p[j] = pe; m[j] = me; v[j] = ve;
-        if (copy) { union { __bf16 h; uint16_t u; } cv; cv.h = (__bf16)pe; copy[j] = cv.u; }
+        if (t.param_bf16) t.param_bf16[base + j] = (uint16_t)pack4(af32x4{pe, 0.f, 0.f, 0.f})[0];
     }
 }
 
@@ -281,131 +239,182 @@ __device__ __forceinline__ double root(double x) {
     return fma(0.5 * s, fma(-s, y, 1.0), s);
 }
 
-__device__ __forceinline__ uint32_t row16_max(uint32_t x) {
-    auto step = [&](uint32_t other) { x = other > x ? other : x; };
-    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, false));       // row_ror:8, 4, 2, 1
-    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xf, 0xf, false));
-    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x122, 0xf, 0xf, false));
-    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x121, 0xf, 0xf, false));
+// The largest of 32 lanes.
+__device__ __forceinline__ uint32_t half_max(uint32_t x) {
+    auto step = [&](int other) { x = (uint32_t)other > x ? (uint32_t)other : x; };
+    step(__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, false));                 // row_ror:8, 4, 2, 1
+    step(__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, (int)x, 0x122, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, (int)x, 0x121, 0xf, 0xf, false));
+    step(__builtin_amdgcn_ds_swizzle((int)x, 0x401f));                                    // lane ^ 16
     return x;
 }
 
-// The exponent of the scale of a block of which this lane has eight values: e = ceil(log2(amax / top)), top = 1.75 * 2^8
-// or 1.875 * 2^8, of the largest finite magnitude.  High words are enough if they are rounded up: that keeps which side
-// of a border (a value whose low word is 0) they are on.
+// What four values of a block need to become codes: the high words of their magnitudes, and the block's exponent
+// e = ceil(log2(amax / top)), top = 1.75 * 2^8 or 1.875 * 2^8, of the largest finite magnitude.  High words decide it, but
+// where the largest one is top's own: then whether a low word is not 0.
+constexpr uint32_t kNotFinite = 0x7ff00000u;
 template <int BITS>
-__device__ __forceinline__ int scale_exponent(const double (&x)[8]) {
-    double top = 0.0;
+__device__ __forceinline__ int scale_exponent(const double (&x)[4], uint32_t (&word)[4], bool& finite) {
+    constexpr uint32_t border = BITS == 3 ? 0xc0000u : 0xe0000u;
+    uint32_t top = 0u;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmax(top, fabs(x[i]));                               // of a NaN and a number the number
-    if (top == INFINITY) {
-        top = 0.0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = fabs(x[i]) < INFINITY ? fmax(top, fabs(x[i])) : top;
+    for (int i = 0; i < 4; ++i) {
+        word[i] = BITS == 3 ? high_word(x[i]) & 0x7fffffffu : high_word(x[i]);
+        top = word[i] > top ? word[i] : top;
     }
-    const uint32_t amax = row16_max(high_word(top) + ((uint32_t)__double_as_longlong(top) != 0u ? 1u : 0u));
-    if (amax == 0u) return 0;
-    const int e = (int)(amax >> 20) - 1023 - 8 + ((amax & 0xfffffu) > (BITS == 3 ? 0xc0000u : 0xe0000u) ? 1 : 0);
+    finite = top < kNotFinite;
+    if (!finite) {
+        top = 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = word[i] < kNotFinite && word[i] > top ? word[i] : top;
+    }
+    if ((top & 0xfffffu) == border) {
+        uint32_t low = 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) low |= word[i] == top ? (uint32_t)__double_as_longlong(x[i]) : 0u;
+        top += low != 0u ? 1u : 0u;
+    }
+    top = half_max(top);
+    if (top == 0u) return 0;
+    const int e = (int)(top >> 20) - 1023 - 8 + ((top & 0xfffffu) > border ? 1 : 0);
     return e < -100 ? -100 : (e > 120 ? 120 : e);
 }
 
-// The code of y = |x| 2^-e, rounded down after `dither` steps of 2^-(20 - BITS) of a code's step.  The high word of a normal y
-// has the code's bits in front of those that the dither meets, with a bias 1016 larger; below 2^-6 codes have the step of
-// that binade, and the significand is moved down to it.
+// The code of y = |x| 2^-e, rounded down after `dither` steps of 2^-(20 - BITS) of a code's step.  The high word of y, its
+// exponent rebased, has the code's bits in front of those that the dither meets; below 2^-6 codes have the step of that
+// binade, and the significand is moved down to it.  `rebase`: (e + 1016) << 20.
 template <int BITS>
-__device__ __forceinline__ uint32_t encode8(double x, int e, uint32_t dither) {
-    const uint32_t word = high_word(x) & 0x7fffffffu;
-    const int y = (int)(word - ((uint32_t)e << 20));
-    const int down = 1017 - (y >> 20);
-    const uint32_t small = (((uint32_t)y & 0xfffffu) | 0x100000u) >> (down < 31 ? down : 31);
-    uint32_t code = down > 0 ? (small + dither) >> (20 - BITS) : (((uint32_t)y + dither) >> (20 - BITS)) - (1016u << BITS);
-    if (BITS == 4 && code == 0u && x > 0.0) code = 1u;
-    if (BITS == 3 && x < 0.0) code |= 0x80u;
-    return word >= 0x7ff00000u ? (BITS == 3 ? 0x7fu : 0xffu) : code;
+__device__ __forceinline__ uint32_t encode8(uint32_t word, uint32_t rebase, uint32_t dither) {
+    const int y = (int)(word - rebase), down = 1 - (y >> 20);
+    const uint32_t small = (((uint32_t)y & 0xfffffu) | 0x100000u) >> ((down < 31 ? down : 31) & 31);
+    const uint32_t code = ((down > 0 ? small : (uint32_t)y) + dither) >> (20 - BITS);
+    const uint32_t least = word < 1u ? word : 1u;            // a root above 0 does not become 0
+    return BITS == 4 && code < least ? least : code;
 }
 
-__device__ __forceinline__ ou32x2 load_codes(const void* codes, int64_t at, int live) {
-    const uint8_t* c = (const uint8_t*)codes + at;
-    if (live >= 8) return *(const ou32x2*)c;
-    ou32x2 r = {0u, 0u};
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < live) r[e >> 2] |= (uint32_t)c[e] << (8 * (e & 3));
-    return r;
-}
-
-__device__ __forceinline__ void store_codes(void* codes, int64_t at, int live, const ou32x2& r) {
-    uint8_t* c = (uint8_t*)codes + at;
-    if (live >= 8) { *(ou32x2*)c = r; return; }
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < live) c[e] = (uint8_t)(r[e >> 2] >> (8 * (e & 3)));
-}
-
-// 16 lanes share a block of 128 values, eight each.  The moments are formed in fp64, so that which way a
-// value next to a border goes does not depend on the order or the fusing of the operations.  The update takes
-// sqrt(v / bc2) from the root that is stored, and reciprocals to one unit in the last place.
+// 32 lanes share a block of 128 values, four each.  The moments are formed in fp64, so that which way a value next to a
+// border goes does not depend on the order or the fusing of the operations.  The update takes sqrt(v / bc2) from the root
+// that is stored, and reciprocals to one unit in the last place.
 __global__ __launch_bounds__(256) void adamw_multi8_kernel(const StepArgs a) {
     const int i = tensor_of(a.first, (int)a.count, blockIdx.x);
     const StepTensor& t = a.t[i];
-    const int64_t at = (int64_t)(blockIdx.x - a.first[i]) * kBlockValues + threadIdx.x * 8, left = t.n - at;
-    const int live = left < 8 ? (left > 0 ? (int)left : 0) : 8;         // lanes without a value take part in the block's largest
-    const int64_t block = at / CCE_STATE8_BLOCK;
+    const int64_t base = (int64_t)(blockIdx.x - a.first[i]) * kStepValues;
+    const int q = threadIdx.x;
+    const int64_t at = base + 4 * q, left = t.n - at;
+    const bool whole = left >= 4, bf16 = t.grad_bf16 != 0;
+    uint8_t* ms = t.m_scale + at / CCE_STATE8_BLOCK;
+    uint8_t* vs = t.v_scale + at / CCE_STATE8_BLOCK;
+    uint8_t* mcode = (uint8_t*)t.m + at;
+    uint8_t* vcode = (uint8_t*)t.v + at;
+    af32x4 p = {0.f, 0.f, 0.f, 0.f}, g = p;                   // zeros behind the end: they take part in the block's largest
+    uint32_t mc = 0u, vc = 0u;
+    int sm = 127, sv = 127;
+    if (whole) {
+        p = __builtin_nontemporal_load((const af32x4*)(t.param + base) + q);
+        g = load_grad4(t.grad, bf16, base, q);
+        mc = *(const uint32_t*)mcode;
+        vc = *(const uint32_t*)vcode;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e) {
+            if (e >= left) continue;
+            p[e] = t.param[at + e];
+            g[e] = grad_at(t.grad, bf16, at + e);
+            mc |= (uint32_t)mcode[e] << (8 * e);
+            vc |= (uint32_t)vcode[e] << (8 * e);
+        }
+    }
+    if (left > 0) { sm = ms[0]; sv = vs[0]; }
     const double clip = a.clip_coef ? (double)a.clip_coef[0] : 1.0;
-    float p[8], g[8];
-    load_f32(t.param, at, live, p);
-    load_grad(t.grad, t.grad_bf16 != 0, at, live, g);
-    const ou32x2 mc = load_codes(t.m, at, live), vc = load_codes(t.v, at, live);
-    const int ms = live > 0 ? t.m_scale[block] : 127, vs = live > 0 ? t.v_scale[block] : 127;
     const double b1 = (double)a.beta1, b2 = (double)a.beta2;
-    const double keep_m = b1 * power_of_two(ms - 127), keep_v = b2 * power_of_two(2 * (vs - 127));
     const double take_m = (1.0 - b1) * clip, take_v = (1.0 - b2) * clip * clip;
+    const double keep_m = b1 * power_of_two(sm - 127), keep_v = b2 * power_of_two(2 * (sv - 127));
     const float rate = t.lr * a.inv_bc1;
-    double m[8], r[8];
+    const of32x2 m0[2] = {__builtin_amdgcn_cvt_pk_f32_fp8((int)mc, false), __builtin_amdgcn_cvt_pk_f32_fp8((int)mc, true)};
+    double m[4], r[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < 4; ++e) {
         const double ge = (double)g[e];
-        const float r0 = decode8<4>((vc[e >> 2] >> (8 * (e & 3))) & 0xffu);             // whose square has ten bits
-        m[e] = fma((double)decode8<3>((mc[e >> 2] >> (8 * (e & 3))) & 0xffu), keep_m, ge * take_m);
+        const float r0 = decode8<4>(vc >> (8 * e) & 0xffu);                              // whose square has ten bits
+        m[e] = fma((double)m0[e >> 1][e & 1], keep_m, ge * take_m);
         r[e] = root(fma((double)(r0 * r0), keep_v, ge * ge * take_v));
-        const float rf = (float)r[e], under = fmaxf(fmaf(rf, a.root_inv_bc2, a.eps), 0x1p-126f);
-        const float update = rate * (float)m[e] * __builtin_amdgcn_rcpf(under);
-        p[e] = fmaf(p[e], t.decay, rf == rf ? -update : rf);
+        float under = fmaf((float)r[e], a.root_inv_bc2, a.eps);
+        under = under < 0x1p-126f ? 0x1p-126f : under;                                   // a NaN stays one
+        p[e] = fmaf(-rate * (float)m[e], __builtin_amdgcn_rcpf(under), p[e] * t.decay);
     }
-    const int em = scale_exponent<3>(m), er = scale_exponent<4>(r);
-    if (live == 0) return;
-    ou32x2 mo = {0u, 0u}, vo = {0u, 0u};
-    const uint32_t base = (uint32_t)at + (uint32_t)((uint64_t)at >> 32) * 32310901u + a.key;
+    uint32_t mw[4], rw[4], cm[4], cr[4];
+    bool m_finite, r_finite;
+    const int em = scale_exponent<3>(m, mw, m_finite), er = scale_exponent<4>(r, rw, r_finite);
+    const uint32_t key = (uint32_t)at + (uint32_t)((uint64_t)at >> 32) * 32310901u + a.key;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t h = mix32(base + e);
-        mo[e >> 2] |= encode8<3>(m[e], em, h >> 15) << (8 * (e & 3));
-        vo[e >> 2] |= encode8<4>(r[e], er, h & 0xffffu) << (8 * (e & 3));
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t h = mix32(key + (uint32_t)e);
+        cm[e] = (high_word(m[e]) >> 24 & 0x80u) | encode8<3>(mw[e], (uint32_t)(em + 1016) << 20, h >> 15);
+        cr[e] = encode8<4>(rw[e], (uint32_t)(er + 1016) << 20, h & 0xffffu);
     }
-    store_f32(t.param, at, live, p);
-    if (t.param_bf16) store_bf16(t.param_bf16, at, live, p);
-    store_codes(t.m, at, live, mo);
-    store_codes(t.v, at, live, vo);
-    if ((threadIdx.x & 15) == 0) {
-        t.m_scale[block] = (uint8_t)(em + 127);
-        t.v_scale[block] = (uint8_t)(er + 127);
+    if (!m_finite || !r_finite) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            cm[e] = mw[e] >= kNotFinite ? 0x7fu : cm[e];
+            cr[e] = rw[e] >= kNotFinite ? 0xffu : cr[e];
+        }
+    }
+    if (left <= 0) return;
+    const uint32_t mo = cm[0] | cm[1] << 8 | cm[2] << 16 | cm[3] << 24, vo = cr[0] | cr[1] << 8 | cr[2] << 16 | cr[3] << 24;
+    const ou32x2 copy = pack4(p);
+    if (whole) {
+        __builtin_nontemporal_store(p, (af32x4*)(t.param + base) + q);
+        if (t.param_bf16) *((ou32x2*)(t.param_bf16 + base) + q) = copy;
+        *(uint32_t*)mcode = mo;
+        *(uint32_t*)vcode = vo;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e) {
+            if (e >= left) continue;
+            t.param[at + e] = p[e];
+            if (t.param_bf16) t.param_bf16[at + e] = (uint16_t)(copy[e >> 1] >> (16 * (e & 1)));
+            mcode[e] = (uint8_t)(mo >> (8 * e));
+            vcode[e] = (uint8_t)(vo >> (8 * e));
+        }
+    }
+    if ((q & 31) == 0) {
+        ms[0] = (uint8_t)(em + 127);
+        vs[0] = (uint8_t)(er + 127);
     }
 }
 
+// Four values a thread, two groups of them 1024 values apart.
 template <int BITS>
 __global__ __launch_bounds__(256) void state8_read_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                           int64_t n, float* __restrict__ out) {
-    for (int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; at < n; at += (int64_t)gridDim.x * kBlockValues) {
-        const int live = n - at < 8 ? (int)(n - at) : 8;
-        const ou32x2 c = load_codes(codes, at, live);
-        const double power = power_of_two((BITS == 4 ? 2 : 1) * (scales[at / CCE_STATE8_BLOCK] - 127));
-        float x[8];
+    auto value = [&](uint32_t code, double power) {
+        const float d = decode8<BITS>(code);
+        return (float)((double)(BITS == 4 ? d * d : d) * power);
+    };
+    for (int64_t base = (int64_t)blockIdx.x * kReadValues; base < n; base += (int64_t)gridDim.x * kReadValues) {
+        uint32_t c[2];
+        int scale[2];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float d = decode8<BITS>((c[e >> 2] >> (8 * (e & 3))) & 0xffu);
-            x[e] = (float)((double)(BITS == 4 ? d * d : d) * power);
+        for (int u = 0; u < 2; ++u) {
+            const int64_t at = base + 1024 * u + 4 * (int)threadIdx.x;
+            if (at + 4 <= n) c[u] = __builtin_nontemporal_load((const uint32_t*)(codes + at));
+            if (at < n) scale[u] = scales[at / CCE_STATE8_BLOCK];
         }
-        store_f32(out, at, live, x);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int64_t at = base + 1024 * u + 4 * (int)threadIdx.x;
+            if (at >= n) continue;
+            const double power = power_of_two((BITS == 4 ? 2 : 1) * (scale[u] - 127));
+            if (at + 4 <= n) {
+                af32x4 x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = value(c[u] >> (8 * e) & 0xffu, power);
+                __builtin_nontemporal_store(x, (af32x4*)(out + at));
+            } else {
+                for (int64_t j = at; j < n; ++j) out[j] = value(codes[j], power);
+            }
+        }
     }
 }
 
@@ -426,7 +435,7 @@ static int check_gradients(const cce_optim_tensor* tensors, int64_t count) {
         const cce_optim_tensor& t = tensors[i];
         if (t.n < 0) return CCE_ERR_INVALID;
         if (t.n == 0) continue;
-        blocks += t.n / kBlockValues + 1;
+        blocks += t.n / kStepValues + 1;
         if (t.n > kMaxTensor || blocks > 0x3fffffff) return CCE_ERR_UNSUPPORTED;
         if (!t.grad || misaligned(t.grad, 16) || (t.grad_bf16 != 0 && t.grad_bf16 != 1)) return CCE_ERR_INVALID;
     }
@@ -508,7 +517,7 @@ int cce_adamw_multi_step(const cce_optim_tensor* tensors, int64_t count, float l
             for (; i < count && a.count < (uint32_t)kStepTensors; ++i) {
                 const cce_optim_tensor& t = tensors[i];
                 if (t.n == 0 || t.state8 != state8) continue;
-                const int64_t own = (t.n + kBlockValues - 1) / kBlockValues;
+                const int64_t own = (t.n + kStepValues - 1) / kStepValues;
                 if (blocks + own > kMaxGrid) break;
                 const float rate = lr * t.lr_scale;
                 a.first[a.count] = (uint32_t)blocks;
@@ -527,7 +536,7 @@ int cce_adamw_multi_step(const cce_optim_tensor* tensors, int64_t count, float l
 int cce_adamw_state8_read(const void* codes, const uint8_t* scales, int64_t n, int second, float* out, void* stream_) {
     if (!codes || !scales || !out || n <= 0 || (second != 0 && second != 1)) return CCE_ERR_INVALID;
     if (misaligned(codes, 8) || misaligned(out, 16)) return CCE_ERR_INVALID;
-    const int64_t want = (n + kBlockValues - 1) / kBlockValues;
+    const int64_t want = (n + kReadValues - 1) / kReadValues;
     const dim3 grid((unsigned)(want < kMaxGrid ? want : kMaxGrid));
     hipStream_t stream = (hipStream_t)stream_;
     (void)hipGetLastError();
