@@ -45,6 +45,7 @@ struct StepArgs {
     uint32_t first[kStepTensors];                      // a tensor's first workgroup
     const float* clip_coef;
     float beta1, beta2, eps, inv_bc1, inv_bc2, root_inv_bc2;
+    double keep_m, take_m, keep_v, take_v;             // the betas and 1 - beta, exact
     uint32_t key, count;
 };
 static_assert(sizeof(StepArgs) <= 4096, "kernel arguments hold 4 KB");
@@ -281,16 +282,15 @@ __device__ __forceinline__ int scale_exponent(const double (&x)[4], uint32_t (&w
     return e < -100 ? -100 : (e > 120 ? 120 : e);
 }
 
-// The code of y = |x| 2^-e, rounded down after `dither` steps of 2^-(20 - BITS) of a code's step.  The high word of y, its
-// exponent rebased, has the code's bits in front of those that the dither meets; below 2^-6 codes have the step of that
-// binade, and the significand is moved down to it.  `rebase`: (e + 1016) << 20.
+// The code of x 2^-e, rounded down after `dither` steps of 2^-(20 - BITS) of a code's step.  Scaled by 2^-1016 more, what the
+// formats' bias of 7 has as exponent field is fp64's own: its high word has the code's bits in front of those that the
+// dither meets, and subnormal codes are subnormal numbers.  `word`: of |x|, not NaN or infinite.
 template <int BITS>
-__device__ __forceinline__ uint32_t encode8(uint32_t word, uint32_t rebase, uint32_t dither) {
-    const int y = (int)(word - rebase), down = 1 - (y >> 20);
-    const uint32_t small = (((uint32_t)y & 0xfffffu) | 0x100000u) >> ((down < 31 ? down : 31) & 31);
-    const uint32_t code = ((down > 0 ? small : (uint32_t)y) + dither) >> (20 - BITS);
-    const uint32_t least = word < 1u ? word : 1u;            // a root above 0 does not become 0
-    return BITS == 4 && code < least ? least : code;
+__device__ __forceinline__ uint32_t encode8(double x, uint32_t word, int e, uint32_t dither) {
+    const uint32_t y = high_word(ldexp(x, -1016 - e)) + dither;
+    if (BITS == 3) return (y >> 17 & 0x7fu) | (y >> 24 & 0x80u);
+    const uint32_t code = y >> 16, least = word < 1u ? word : 1u;                        // a root above 0 does not become 0
+    return code < least ? least : code;
 }
 
 // 32 lanes share a block of 128 values, four each.  The moments are formed in fp64, so that which way a value next to a
@@ -327,9 +327,8 @@ __global__ __launch_bounds__(256) void adamw_multi8_kernel(const StepArgs a) {
     }
     if (left > 0) { sm = ms[0]; sv = vs[0]; }
     const double clip = a.clip_coef ? (double)a.clip_coef[0] : 1.0;
-    const double b1 = (double)a.beta1, b2 = (double)a.beta2;
-    const double take_m = (1.0 - b1) * clip, take_v = (1.0 - b2) * clip * clip;
-    const double keep_m = b1 * power_of_two(sm - 127), keep_v = b2 * power_of_two(2 * (sv - 127));
+    const double take_m = a.take_m * clip, take_v = a.take_v * clip * clip;
+    const double keep_m = ldexp(a.keep_m, sm - 127), keep_v = ldexp(a.keep_v, 2 * (sv - 127));
     const float rate = t.lr * a.inv_bc1;
     const of32x2 m0[2] = {__builtin_amdgcn_cvt_pk_f32_fp8((int)mc, false), __builtin_amdgcn_cvt_pk_f32_fp8((int)mc, true)};
     double m[4], r[4];
@@ -350,8 +349,8 @@ __global__ __launch_bounds__(256) void adamw_multi8_kernel(const StepArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const uint32_t h = mix32(key + (uint32_t)e);
-        cm[e] = (high_word(m[e]) >> 24 & 0x80u) | encode8<3>(mw[e], (uint32_t)(em + 1016) << 20, h >> 15);
-        cr[e] = encode8<4>(rw[e], (uint32_t)(er + 1016) << 20, h & 0xffffu);
+        cm[e] = encode8<3>(m[e], mw[e], em, h >> 15);
+        cr[e] = encode8<4>(r[e], rw[e], er, h & 0xffffu);
     }
     if (!m_finite || !r_finite) {
 #pragma unroll
@@ -509,6 +508,8 @@ int cce_adamw_multi_step(const cce_optim_tensor* tensors, int64_t count, float l
     a.inv_bc1 = (float)(1.0 / (1.0 - pow((double)beta1, (double)step)));
     a.inv_bc2 = (float)(1.0 / (1.0 - pow((double)beta2, (double)step)));
     a.root_inv_bc2 = (float)sqrt(1.0 / (1.0 - pow((double)beta2, (double)step)));
+    a.keep_m = (double)beta1; a.take_m = 1.0 - a.keep_m;
+    a.keep_v = (double)beta2; a.take_v = 1.0 - a.keep_v;
     a.key = mix32_host(seed + mix32_host((uint32_t)step));
     for (int state8 = 0; state8 < 2; ++state8) {
         for (int64_t i = 0; i < count;) {
