@@ -14,6 +14,7 @@ namespace cce {
 constexpr int64_t kEmbedMaxRows = (int64_t)1 << 24;      // V
 constexpr int64_t kEmbedMaxDim = 65536;                  // D
 constexpr int64_t kEmbedMaxValues = (int64_t)1 << 37;    // V * D: half a terabyte of dW
+constexpr int64_t kStreamOut = (int64_t)192 << 20;        // bytes of an output that the last-level cache (256 MB) cannot keep
 constexpr int64_t kMaxBlocks = (1 << 24) - 1;            // of 256 threads: a launch has fewer than 2^32 threads
 
 // Whether a token names a row; a bad one that is not ignore_index is reported.
@@ -24,11 +25,16 @@ __device__ __forceinline__ bool token_takes_part(int token, int V, int ignore_in
     return false;
 }
 
-// y_i = scale * W[t_i]: four chunks of 16 bytes of y a thread, 4 KB of the workgroup apart, whose tokens, rows and
-// stores are in flight together.  A chunk's row within the workgroup's 16 KB by multiplication: `inverse` is
-// ceil(2^32 / row_chunks), exact for the numbers below 2^17 that occur.
-constexpr int kLookupChunks = 1024;
+// y_i = scale * W[t_i]: two chunks of 16 bytes of y a thread, 4 KB of the workgroup apart, whose tokens, rows and stores are
+// in flight together (four: 3.0 -> 3.3 us for one token, 3 % longer for large outputs; one, a division each: 86 us at 32768 x
+// 3584 against 69).  A chunk's row within the workgroup's 8 KB by multiplication: `inverse` is ceil(2^32 / row_chunks),
+// exact for the numbers below 2^17 that occur.
+// STREAM: y of kStreamOut or more is written past the caches, which could not keep it for the kernel that reads it and do keep
+// rows of W then: 32768 x 3584 (224 MiB) 69 -> 48 us, with the final norm behind it 175 -> 170; smaller ones, that kernel finds in
+// the caches: 32768 x 2048 (128 MiB) with the norm 87 against 92 us.
+constexpr int kLookupChunks = 512;
 
+template <bool STREAM>
 __global__ __launch_bounds__(256) void embedding_forward_kernel(
         const int32_t* __restrict__ tokens, const uint16_t* __restrict__ weight, int64_t chunks, int row_chunks, uint64_t inverse,
         int V, int ignore_index, float scale, uint16_t* __restrict__ out, int32_t* status) {
@@ -36,30 +42,32 @@ __global__ __launch_bounds__(256) void embedding_forward_kernel(
         const int64_t row0 = first / row_chunks;
         const int c0 = (int)(first - row0 * row_chunks);
         const int live = chunks - first < kLookupChunks ? (int)(chunks - first) : kLookupChunks;
-        int token[4], c[4];
-        bool ok[4];
+        int token[2], c[2];
+        bool ok[2];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < 2; ++u) {
             const int i = u * 256 + (int)threadIdx.x;
             const uint32_t o = (uint32_t)(c0 + (i < live ? i : 0));
             const int row = (int)(((uint64_t)o * inverse) >> 32);
             c[u] = (int)o - row * row_chunks;
             token[u] = tokens[row0 + row];
         }
-        au32x4 v[4];
+        au32x4 v[2];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < 2; ++u) {
             ok[u] = token_takes_part(token[u], V, ignore_index, c[u] == 0 ? status : nullptr);
             if (ok[u]) v[u] = ((const au32x4*)weight)[(size_t)token[u] * row_chunks + c[u]];
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < 2; ++u) {
             const int i = u * 256 + (int)threadIdx.x;
             float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (ok[u]) unpack8(v[u], f);
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] *= scale;
-            if (i < live) ((au32x4*)out)[first + i] = ok[u] ? pack8(f) : au32x4{0u, 0u, 0u, 0u};
+            const au32x4 y = ok[u] ? pack8(f) : au32x4{0u, 0u, 0u, 0u};
+            if (i >= live) continue;
+            if (STREAM) __builtin_nontemporal_store(y, (au32x4*)out + first + i); else ((au32x4*)out)[first + i] = y;
         }
     }
 }
@@ -87,6 +95,9 @@ constexpr int kJoinShort = 16;                  // pieces of a group that one wa
 constexpr int kSumWaves = 4096;                 // wavefronts that the sum is cut into, if there are rows for them
 constexpr int kMaxPiece = 128;
 constexpr int64_t kStreamBytes = (int64_t)128 << 20;      // half of the last-level cache
+// A dW of this size or more gets its zeros past the caches: 500 MiB with 16384 x 4096 rows 149 -> 133 us; smaller ones what reads
+// dW next finds there: the sum of squares of 219 MiB with the gradient in front of it 85 against 102 us.
+constexpr int64_t kStreamZeros = (int64_t)256 << 20;
 
 // Slices of the vocabulary: token t is key t / slices of slice t % slices (a power of two).  The frequent tokens, which
 // tokenizers number first, are spread over the slices.
@@ -105,7 +116,7 @@ struct EmbedBackward {
     int32_t* order;           // [N] positions
     int32_t* sorted;          // [N] their tokens
     float* partial;           // [pieces][2][D]: of the group a piece begins within, of the one that it begins and does not end
-    int N, V, ignore_index, bits, keys, row_chunks, piece, strips, accumulate;
+    int N, V, ignore_index, bits, keys, row_chunks, piece, strips, accumulate, stream_zeros;
     float scale;
 };
 
@@ -276,7 +287,11 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbedBackward 
             const int64_t v = ((int64_t)(first + __ffsll(none) - 1) << a.bits) + slice;
             none &= none - 1;
             af32x4* to = (af32x4*)a.dW + (size_t)v * width;
-            for (int i = threadIdx.x; i < width; i += 256) __builtin_nontemporal_store(af32x4{0.f, 0.f, 0.f, 0.f}, to + i);
+            if (a.stream_zeros) {
+                for (int i = threadIdx.x; i < width; i += 256) __builtin_nontemporal_store(af32x4{0.f, 0.f, 0.f, 0.f}, to + i);
+            } else {
+                for (int i = threadIdx.x; i < width; i += 256) to[i] = af32x4{0.f, 0.f, 0.f, 0.f};
+            }
         }
         return;
     }
@@ -559,7 +574,7 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_small_kernel(const
         const int64_t v = ((int64_t)k << a.bits) + slice;
         if (many[k] != 0u || v >= a.V) continue;
         af32x4* to = (af32x4*)a.dW + (size_t)v * width;
-        for (int i = lane; i < width; i += 64) __builtin_nontemporal_store(af32x4{0.f, 0.f, 0.f, 0.f}, to + i);
+        for (int i = lane; i < width; i += 64) to[i] = af32x4{0.f, 0.f, 0.f, 0.f};
     }
 }
 
@@ -601,9 +616,13 @@ int cce_embedding_forward(const int32_t* tokens, const void* weight, int64_t N, 
     if ((((uintptr_t)weight | (uintptr_t)out) & 15) || (((uintptr_t)tokens | (uintptr_t)status) & 3)) return CCE_ERR_INVALID;
     const int64_t row_chunks = D / 8, chunks = N * row_chunks, want = (chunks + kLookupChunks - 1) / kLookupChunks;
     (void)hipGetLastError();
-    hipLaunchKernelGGL(embedding_forward_kernel, dim3((unsigned)(want < kMaxBlocks ? want : kMaxBlocks)), dim3(256), 0, (hipStream_t)stream_,
-                       tokens, (const uint16_t*)weight, chunks, (int)row_chunks, (((uint64_t)1 << 32) + row_chunks - 1) / row_chunks,
-                       (int)V, ignore_index, scale, (uint16_t*)out, status);
+    const dim3 grid((unsigned)(want < kMaxBlocks ? want : kMaxBlocks));
+    const uint64_t inverse = (((uint64_t)1 << 32) + row_chunks - 1) / row_chunks;
+    hipStream_t stream = (hipStream_t)stream_;
+#define CCE_EMBED_LOOKUP(STREAM) hipLaunchKernelGGL(embedding_forward_kernel<STREAM>, grid, dim3(256), 0, stream, tokens, \
+        (const uint16_t*)weight, chunks, (int)row_chunks, inverse, (int)V, ignore_index, scale, (uint16_t*)out, status)
+    if (N * D * 2 >= kStreamOut) CCE_EMBED_LOOKUP(true); else CCE_EMBED_LOOKUP(false);
+#undef CCE_EMBED_LOOKUP
     return hip_ok(hipGetLastError()) ? CCE_OK : CCE_ERR_HIP;
 }
 
@@ -635,6 +654,7 @@ int cce_embedding_backward(const int32_t* tokens, const void* d_out, int64_t N, 
     a.row_chunks = (int)(D / 8);
     a.piece = (int)embed_piece(N, D);
     a.accumulate = accumulate_dW ? 1 : 0;
+    a.stream_zeros = V * D * 4 >= kStreamZeros ? 1 : 0;
     a.scale = scale;
     const int slices = 1 << a.bits;
     char* at = (char*)workspace;

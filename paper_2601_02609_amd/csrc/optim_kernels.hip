@@ -22,7 +22,7 @@ constexpr int kStepValues = 1024;                      // values of a workgroup 
 constexpr int kReadValues = 2048;                      // of a workgroup that reads 8-bit moments
 constexpr int64_t kMaxTensor = (int64_t)1 << 33;       // values of a tensor
 constexpr int64_t kMaxGrid = (1 << 24) - 1;            // of 256 threads: a launch has fewer than 2^32 threads
-constexpr int kStepTensors = 44;                       // tensors of a launch: kernel arguments hold 4 KB
+constexpr int kStepTensors = 64, kStepTensors8 = 52;   // tensors of a launch: kernel arguments hold 4 KB
 constexpr int kNormTensors = 160;
 constexpr int kNormBlocks = 2048;                      // workgroups of a launch, each with one partial sum
 constexpr int kNormChunk = 4096;                       // values of a workgroup's trip
@@ -33,22 +33,28 @@ struct StepTensor {
     const void* grad;
     void* m;
     void* v;
-    uint8_t* m_scale;
-    uint8_t* v_scale;
     int64_t n;
     float lr, decay;                                   // decay: 1 - lr * weight_decay
-    uint64_t grad_bf16;
 };
 
+struct StepTensor8 : StepTensor {
+    uint8_t* m_scale;
+    uint8_t* v_scale;
+};
+
+template <class Tensor, int COUNT>
 struct StepArgs {
-    StepTensor t[kStepTensors];
-    uint32_t first[kStepTensors];                      // a tensor's first workgroup
+    static constexpr int kCount = COUNT;
+    Tensor t[COUNT];
+    uint32_t first[COUNT];                             // twice a tensor's first workgroup, plus 1 if its gradient is bf16
     const float* clip_coef;
-    float beta1, beta2, eps, inv_bc1, inv_bc2, root_inv_bc2;
     double keep_m, take_m, keep_v, take_v;             // the betas and 1 - beta, exact
+    float beta1, beta2, eps, inv_bc1, inv_bc2, root_inv_bc2;
     uint32_t key, count;
 };
-static_assert(sizeof(StepArgs) <= 4096, "kernel arguments hold 4 KB");
+using StepArgs32 = StepArgs<StepTensor, kStepTensors>;
+using StepArgs8 = StepArgs<StepTensor8, kStepTensors8>;
+static_assert(sizeof(StepArgs32) <= 4096 && sizeof(StepArgs8) <= 4096, "kernel arguments hold 4 KB");
 
 struct NormTensor {
     const void* grad;
@@ -63,8 +69,8 @@ struct NormArgs {
 };
 static_assert(sizeof(NormArgs) <= 4096, "kernel arguments hold 4 KB");
 
-// Which tensor of the table workgroup (or chunk) `b` belongs to: the last one that begins at or before it.  Every lane
-// looks at one entry: one load instead of the chain of a binary search.
+// Which tensor of the table workgroup (or chunk) w belongs to, b = 2 w + 1: the last one that begins at or before it.  Every
+// lane looks at one entry: one load instead of the chain of a binary search.
 __device__ __forceinline__ int tensor_of(const uint32_t* first, int count, uint32_t b) {
     int n = 0;
     for (int base = 0; base < count; base += 64) {
@@ -167,7 +173,7 @@ __global__ __launch_bounds__(1024) void norm_final_kernel(const double* __restri
 // ------------------------------------------------------------------------------------------
 // AdamW: clip, moments, bias corrections, decoupled decay and update.
 // ------------------------------------------------------------------------------------------
-__device__ __forceinline__ void adamw_one(float& p, float g, float& m, float& v, float lr, float decay, const StepArgs& a) {
+__device__ __forceinline__ void adamw_one(float& p, float g, float& m, float& v, float lr, float decay, const StepArgs32& a) {
     m = a.beta1 * m + (1.f - a.beta1) * g;
     v = a.beta2 * v + (1.f - a.beta2) * g * g;
     p = p * decay - lr * ((m * a.inv_bc1) / (sqrtf(v * a.inv_bc2) + a.eps));
@@ -175,15 +181,15 @@ __device__ __forceinline__ void adamw_one(float& p, float g, float& m, float& v,
 
 // Every value is touched once: streaming accesses of 16 bytes, one group of a tensor a thread.  Bound by HBM: 411 M values at
 // the rate of a copy of as many bytes.  Two groups a thread took 2.6 % longer, four 1.3 %; 32 bytes of a thread in a row 3.5 %.
-__global__ __launch_bounds__(256) void adamw_multi_kernel(const StepArgs a) {
-    const int i = tensor_of(a.first, (int)a.count, blockIdx.x);
+__global__ __launch_bounds__(256) void adamw_multi_kernel(const StepArgs32 a) {
+    const int i = tensor_of(a.first, (int)a.count, 2 * blockIdx.x + 1);
     const StepTensor& t = a.t[i];
-    const int64_t base = (int64_t)(blockIdx.x - a.first[i]) * kStepValues, left = t.n - base;
+    const int64_t base = (int64_t)(blockIdx.x - (a.first[i] >> 1)) * kStepValues, left = t.n - base;
     const float clip = a.clip_coef ? a.clip_coef[0] : 1.f;
     float* p = t.param + base;
     float* m = (float*)t.m + base;
     float* v = (float*)t.v + base;
-    const bool bf16 = t.grad_bf16 != 0;
+    const bool bf16 = (a.first[i] & 1u) != 0u;
     const int q = threadIdx.x;
     if (left >= kStepValues) {
         af32x4 pv = __builtin_nontemporal_load((const af32x4*)p + q), mv = __builtin_nontemporal_load((const af32x4*)m + q),
@@ -296,13 +302,13 @@ __device__ __forceinline__ uint32_t encode8(double x, uint32_t word, int e, uint
 // 32 lanes share a block of 128 values, four each.  The moments are formed in fp64, so that which way a value next to a
 // border goes does not depend on the order or the fusing of the operations.  The update takes sqrt(v / bc2) from the root
 // that is stored, and reciprocals to one unit in the last place.
-__global__ __launch_bounds__(256) void adamw_multi8_kernel(const StepArgs a) {
-    const int i = tensor_of(a.first, (int)a.count, blockIdx.x);
-    const StepTensor& t = a.t[i];
-    const int64_t base = (int64_t)(blockIdx.x - a.first[i]) * kStepValues;
+__global__ __launch_bounds__(256) void adamw_multi8_kernel(const StepArgs8 a) {
+    const int i = tensor_of(a.first, (int)a.count, 2 * blockIdx.x + 1);
+    const StepTensor8& t = a.t[i];
+    const int64_t base = (int64_t)(blockIdx.x - (a.first[i] >> 1)) * kStepValues;
     const int q = threadIdx.x;
     const int64_t at = base + 4 * q, left = t.n - at;
-    const bool whole = left >= 4, bf16 = t.grad_bf16 != 0;
+    const bool whole = left >= 4, bf16 = (a.first[i] & 1u) != 0u;
     uint8_t* ms = t.m_scale + at / CCE_STATE8_BLOCK;
     uint8_t* vs = t.v_scale + at / CCE_STATE8_BLOCK;
     uint8_t* mcode = (uint8_t*)t.m + at;
@@ -425,6 +431,18 @@ static uint32_t mix32_host(uint32_t h) {
     return h ^ (h >> 16);
 }
 
+static void fill_tensor(StepTensor& to, const cce_optim_tensor& t, float rate) {
+    to.param = t.param; to.param_bf16 = (uint16_t*)t.param_bf16; to.grad = t.grad; to.m = t.m; to.v = t.v; to.n = t.n;
+    to.lr = rate;
+    to.decay = 1.f - rate * t.weight_decay;
+}
+
+static void fill_tensor(StepTensor8& to, const cce_optim_tensor& t, float rate) {
+    fill_tensor(static_cast<StepTensor&>(to), t, rate);
+    to.m_scale = t.m_scale;
+    to.v_scale = t.v_scale;
+}
+
 static bool misaligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
 
 static int check_gradients(const cce_optim_tensor* tensors, int64_t count) {
@@ -502,34 +520,41 @@ int cce_adamw_multi_step(const cce_optim_tensor* tensors, int64_t count, float l
     }
     hipStream_t stream = (hipStream_t)stream_;
     (void)hipGetLastError();
-    StepArgs a;
-    a.clip_coef = clip_coef;
-    a.beta1 = beta1; a.beta2 = beta2; a.eps = eps;
-    a.inv_bc1 = (float)(1.0 / (1.0 - pow((double)beta1, (double)step)));
-    a.inv_bc2 = (float)(1.0 / (1.0 - pow((double)beta2, (double)step)));
-    a.root_inv_bc2 = (float)sqrt(1.0 / (1.0 - pow((double)beta2, (double)step)));
-    a.keep_m = (double)beta1; a.take_m = 1.0 - a.keep_m;
-    a.keep_v = (double)beta2; a.take_v = 1.0 - a.keep_v;
-    a.key = mix32_host(seed + mix32_host((uint32_t)step));
-    for (int state8 = 0; state8 < 2; ++state8) {
+    // the tensors with moments of one kind, as many a launch as its table and a grid hold
+    auto run = [&](auto& a, int state8, auto launch) {
+        a.clip_coef = clip_coef;
+        a.beta1 = beta1; a.beta2 = beta2; a.eps = eps;
+        a.keep_m = (double)beta1; a.take_m = 1.0 - a.keep_m;
+        a.keep_v = (double)beta2; a.take_v = 1.0 - a.keep_v;
+        a.inv_bc1 = (float)(1.0 / (1.0 - pow((double)beta1, (double)step)));
+        a.inv_bc2 = (float)(1.0 / (1.0 - pow((double)beta2, (double)step)));
+        a.root_inv_bc2 = (float)sqrt(1.0 / (1.0 - pow((double)beta2, (double)step)));
+        a.key = mix32_host(seed + mix32_host((uint32_t)step));
         for (int64_t i = 0; i < count;) {
             a.count = 0;
             int64_t blocks = 0;
-            for (; i < count && a.count < (uint32_t)kStepTensors; ++i) {
+            for (; i < count && a.count < (uint32_t)a.kCount; ++i) {
                 const cce_optim_tensor& t = tensors[i];
                 if (t.n == 0 || t.state8 != state8) continue;
                 const int64_t own = (t.n + kStepValues - 1) / kStepValues;
                 if (blocks + own > kMaxGrid) break;
                 const float rate = lr * t.lr_scale;
-                a.first[a.count] = (uint32_t)blocks;
-                a.t[a.count++] = StepTensor{t.param, (uint16_t*)t.param_bf16, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.n,
-                                            rate, 1.f - rate * t.weight_decay, (uint64_t)t.grad_bf16};
+                a.first[a.count] = 2 * (uint32_t)blocks + (uint32_t)t.grad_bf16;
+                fill_tensor(a.t[a.count++], t, rate);
                 blocks += own;
             }
-            if (a.count == 0) continue;
-            if (state8) hipLaunchKernelGGL(adamw_multi8_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a);
-            else hipLaunchKernelGGL(adamw_multi_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a);
+            if (a.count != 0) launch(a, (unsigned)blocks);
         }
+    };
+    bool any32 = false, any8 = false;
+    for (int64_t i = 0; i < count; ++i) (tensors[i].state8 ? any8 : any32) = true;
+    if (any32) {
+        StepArgs32 a;
+        run(a, 0, [&](const StepArgs32& x, unsigned blocks) { hipLaunchKernelGGL(adamw_multi_kernel, dim3(blocks), dim3(256), 0, stream, x); });
+    }
+    if (any8) {
+        StepArgs8 a;
+        run(a, 1, [&](const StepArgs8& x, unsigned blocks) { hipLaunchKernelGGL(adamw_multi8_kernel, dim3(blocks), dim3(256), 0, stream, x); });
     }
     return hip_ok(hipGetLastError()) ? CCE_OK : CCE_ERR_HIP;
 }
