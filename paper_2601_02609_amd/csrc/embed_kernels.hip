@@ -92,8 +92,11 @@ constexpr int kSmallRows = 2048;                // and rows of strips, which one
 constexpr int kSmallShare = 16;                 // rows of a key that one wavefront adds up
 constexpr int kJoinWaves = 8;
 constexpr int kJoinShort = 16;                  // pieces of a group that one wavefront joins, and one more
-constexpr int kSumWaves = 4096;                 // wavefronts that the sum is cut into, if there are rows for them
-constexpr int kMaxPiece = 128;
+// Wavefronts that the sum is cut into, if there are rows for them.  Added to dW, the pieces take unequal times (rows of dW are read
+// where groups end) and more of them even out: 32768 x 3584 124 -> 118 us, 32768 x 1024 of uniform tokens 72 -> 67; overwriting,
+// they cost: 16384 x 2048 101 -> 108.
+constexpr int64_t kSumWaves = 4096, kSumWavesAdd = 8192;
+constexpr int64_t kMaxPieces = 4096;            // more make the join of a frequent token's partial rows long
 constexpr int64_t kStreamBytes = (int64_t)128 << 20;      // half of the last-level cache
 // A dW of this size or more gets its zeros past the caches: 500 MiB with 16384 x 4096 rows 149 -> 133 us; smaller ones what reads
 // dW next finds there: the sum of squares of 219 MiB with the gradient in front of it 85 against 102 us.
@@ -120,6 +123,11 @@ struct EmbedBackward {
     float scale;
 };
 
+// How many of the lanes in front of this one are in `mask`.
+__device__ __forceinline__ uint32_t lanes_in_front(unsigned long long mask) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
+}
+
 // Of the lanes `among`, those that have this lane's key: they find each other bit by bit.
 __device__ __forceinline__ unsigned long long lanes_of_key(unsigned long long among, uint32_t key) {
     unsigned long long same = among;
@@ -145,7 +153,6 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const
     uint32_t* own = count + w * a.keys;
     const int64_t range = ((int64_t)a.N + 64 * kOrderWaves - 1) / (64 * kOrderWaves) * 64;
     const int64_t begin = w * range, end = begin + range < a.N ? begin + range : a.N;
-    const unsigned long long lanes_below = (1ull << lane) - 1ull;
     if (slice == 0 && a.status)
         for (int64_t i = begin + lane; i < end; i += 64) token_takes_part(a.tokens[i], a.V, a.ignore_index, a.status);
     auto load = [&](int64_t i, int (&token)[kOrderLoads]) {  // -1 behind the end; every load is made, none waits for another
@@ -171,8 +178,8 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const
             below += (uint32_t)__popcll(__ballot(s < slice) & ok);
             const unsigned long long mine = __ballot(s == slice) & ok;
             if (mine != 0ull) {
-                if (mine >> lane & 1ull) {
-                    const uint32_t place = n + (uint32_t)__popcll(mine & lanes_below);
+                if (s == slice && valid(token[u])) {
+                    const uint32_t place = n + lanes_in_front(mine);
                     atomicAdd(&own[(uint32_t)token[u] >> a.bits], 1u);
                     if (place < (uint32_t)kFound) found[w][place] = (uint16_t)((i - begin) + 64 * u + lane);
                 }
@@ -218,7 +225,7 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const
             const int leader = __ffsll(same) - 1;
             uint32_t to = 0u;
             if (lane == leader) to = atomicAdd(&own[k], (uint32_t)__popcll(same));
-            to = (uint32_t)__shfl((int)to, leader) + (uint32_t)__popcll(same & lanes_below);
+            to = (uint32_t)__shfl((int)to, leader) + lanes_in_front(same);
             a.order[to] = (int32_t)position;
             a.sorted[to] = (int32_t)(k << a.bits) + slice;
         }
@@ -250,7 +257,7 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const
         for (int64_t i = from; i < to; i += 64) {
             const int t = i + lane < to ? a.tokens[i + lane] : -1;
             const unsigned long long mine = __ballot(valid(t) && (t & mask) == slice);
-            if (mine >> lane & 1ull) found[w][many + (uint32_t)__popcll(mine & lanes_below)] = (uint16_t)(i - from + lane);
+            if (mine >> lane & 1ull) found[w][many + lanes_in_front(mine)] = (uint16_t)(i - from + lane);
             many += (uint32_t)__popcll(mine);
             if (many > (uint32_t)kFound - 64u) {
                 place_found(many, from);
@@ -304,7 +311,18 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbedBackward 
     if (!live) c = 0;                                        // reads along with the first chunk's lane, stores nothing
     const int64_t first = piece * a.piece;
     if (first >= a.N) return;
-    const int before = first > 0 ? a.sorted[first - 1] : -1, at_first = a.sorted[first];       // beside the load of M
+    // positions and tokens of eight rows, and the token behind each; entries from M on say nothing, but may be loaded with it
+    const int j0 = threadIdx.x & 7;
+    int pos = 0, token = -1, next = -1;
+    auto load_rows = [&](int64_t b) {
+        if (b + j0 < a.N) {
+            pos = a.order[b + j0];
+            token = a.sorted[b + j0];
+        }
+        if (b + j0 + 1 < a.N) next = a.sorted[b + j0 + 1];
+    };
+    load_rows(first);
+    const int before = first > 0 ? a.sorted[first - 1] : -1, at_first = a.sorted[first];
     if (first >= M) return;
     const int64_t last = first + a.piece < M ? first + a.piece : M;
     bool begun = before == at_first;                         // the present group began in front of the piece
@@ -317,28 +335,23 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbedBackward 
         to[1] = af32x4{sum[4], sum[5], sum[6], sum[7]};
     };
     for (int64_t b = first; b < last; b += 8) {
-        const int j0 = threadIdx.x & 7;
         const int rows = last - b < 8 ? (int)(last - b) : 8;
-        int pos = 0, token = -1, next = -1;
-        if (j0 < rows) {
-            pos = a.order[b + j0];
-            token = a.sorted[b + j0];
-            if (b + j0 + 1 < M) next = a.sorted[b + j0 + 1];
-        }
+        const int row = pos, of = token, behind = b + j0 + 1 < M ? next : -1;
+        if (b + 8 < last) load_rows(b + 8);
         au32x4 x[8];
         af32x4 w[8][2];
         bool inside = begun;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j < rows) {
-                const au32x4* from = (const au32x4*)a.d_out + (size_t)of_lane<LPR>(pos, j) * a.row_chunks + c;
+                const au32x4* from = (const au32x4*)a.d_out + (size_t)of_lane<LPR>(row, j) * a.row_chunks + c;
                 x[j] = STREAM ? __builtin_nontemporal_load(from) : *from;
             }
         if (a.accumulate) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int t = of_lane<LPR>(token, j);
-                if (j < rows && t != of_lane<LPR>(next, j)) {
+                const int t = of_lane<LPR>(of, j);
+                if (j < rows && t != of_lane<LPR>(behind, j)) {
                     if (!inside) {
                         const af32x4* from = (const af32x4*)a.dW + ((size_t)t * a.row_chunks + c) * 2;
                         w[j][0] = from[0];
@@ -355,8 +368,8 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbedBackward 
             unpack8(x[j], f);
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] += f[e];
-            const int t = of_lane<LPR>(token, j);
-            if (t == of_lane<LPR>(next, j)) continue;
+            const int t = of_lane<LPR>(of, j);
+            if (t == of_lane<LPR>(behind, j)) continue;
             if (begun) {
                 store_partial(0);
             } else if (live) {
@@ -477,7 +490,7 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_small_kernel(const
     }
     if (hits >> lane & 1ull) {
         const uint32_t key = (uint32_t)token >> a.bits;
-        at += (uint32_t)__popcll(hits & ((1ull << lane) - 1ull));
+        at += lanes_in_front(hits);
         mine[at] = key << 16 | threadIdx.x;
         atomicMin(&first[key], at);
         atomicAdd(&many[key], 1u);
@@ -496,7 +509,7 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_small_kernel(const
         if (w == (int)turn) {
             uint32_t to = 0u;
             if (lane == leader && threadIdx.x < n) to = atomicAdd(&begin[key], (uint32_t)__popcll(same));
-            to = (uint32_t)__shfl((int)to, leader) + (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
+            to = (uint32_t)__shfl((int)to, leader) + lanes_in_front(same);
             if (threadIdx.x < n) rows[to] = (uint16_t)own;
         }
         __syncthreads();
@@ -581,19 +594,19 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_small_kernel(const
 // Lanes that share a row, and the rest of a row's chunks in further strips.
 static int embed_lanes(int64_t D) { return D <= 64 ? 8 : D <= 128 ? 16 : D <= 256 ? 32 : 64; }
 
-// Rows of a piece, a multiple of eight (what a wavefront has in flight): as many as leave kSumWaves wavefronts.
-static int64_t embed_piece(int64_t N, int64_t D) {
+// Rows of a piece, a multiple of eight (what a wavefront has in flight): as many as leave `waves` wavefronts and kMaxPieces pieces.
+static int64_t embed_piece(int64_t N, int64_t D, int64_t waves) {
     const int64_t lanes = embed_lanes(D), strips = (D / 8 + lanes - 1) / lanes;
-    const int64_t rows = (N * strips * lanes / 64 + kSumWaves - 1) / kSumWaves;
-    return rows <= 8 ? 8 : rows >= kMaxPiece ? kMaxPiece : (rows + 7) / 8 * 8;
+    const int64_t by_waves = (N * strips * lanes / 64 + waves - 1) / waves, by_pieces = (N + kMaxPieces - 1) / kMaxPieces;
+    const int64_t rows = by_waves > by_pieces ? by_waves : by_pieces;
+    return rows <= 8 ? 8 : (rows + 7) / 8 * 8;
 }
 
 // No N' <= N rows have more pieces.
 static int64_t embed_pieces(int64_t N, int64_t D) {
-    const int64_t lanes = embed_lanes(D), strips = (D / 8 + lanes - 1) / lanes;
-    const int64_t most = kSumWaves * 64 / (strips * lanes) + 1, short_ones = (N + 7) / 8, long_ones = (N + kMaxPiece - 1) / kMaxPiece;
-    const int64_t n = short_ones < most ? short_ones : most;
-    return n > long_ones ? n : long_ones;
+    const int64_t lanes = embed_lanes(D), strips = (D / 8 + lanes - 1) / lanes, short_ones = (N + 7) / 8;
+    const int64_t by_waves = kSumWavesAdd * 64 / (strips * lanes) + 1, most = by_waves < kMaxPieces ? by_waves : kMaxPieces;
+    return short_ones < most ? short_ones : most;
 }
 
 static int embed_shape(int64_t N, int64_t D, int64_t V) {
@@ -652,8 +665,8 @@ int cce_embedding_backward(const int32_t* tokens, const void* d_out, int64_t N, 
     a.bits = slice_bits(V);
     a.keys = (int)((V + (1 << a.bits) - 1) >> a.bits);
     a.row_chunks = (int)(D / 8);
-    a.piece = (int)embed_piece(N, D);
     a.accumulate = accumulate_dW ? 1 : 0;
+    a.piece = (int)embed_piece(N, D, a.accumulate ? kSumWavesAdd : kSumWaves);
     a.stream_zeros = V * D * 4 >= kStreamZeros ? 1 : 0;
     a.scale = scale;
     const int slices = 1 << a.bits;
