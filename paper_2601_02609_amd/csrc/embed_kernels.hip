@@ -86,7 +86,7 @@ constexpr int kKeyBits = 10;
 static_assert(kSliceKeys <= 1 << kKeyBits, "bits of a key");
 constexpr int kOrderWaves = 16;
 constexpr int kOrderLoads = 8;                  // loads of tokens in flight, and as many ahead
-constexpr int kFound = 640;                     // positions that a wavefront notes: 20 KB of LDS
+constexpr int kFound = 1024;                    // positions that a wavefront notes: 32 KB of LDS (two workgroups fit a CU)
 constexpr int kSmallTokens = 1024;              // one launch takes: a thread each
 constexpr int kSmallRows = 2048;                // and rows of strips, which one workgroup may have all of
 constexpr int kSmallShare = 16;                 // rows of a key that one wavefront adds up
@@ -251,21 +251,32 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const
         return;
     }
     // more than was noted: through the range again, noting as many as fit
-    for (int64_t from = begin; from < end; from += 32768) {
-        const int64_t to = from + 32768 < end ? from + 32768 : end;
-        uint32_t many = 0u;
-        for (int64_t i = from; i < to; i += 64) {
-            const int t = i + lane < to ? a.tokens[i + lane] : -1;
-            const unsigned long long mine = __ballot(valid(t) && (t & mask) == slice);
-            if (mine >> lane & 1ull) found[w][many + lanes_in_front(mine)] = (uint16_t)(i - from + lane);
-            many += (uint32_t)__popcll(mine);
-            if (many > (uint32_t)kFound - 64u) {
-                place_found(many, from);
-                many = 0u;
+    uint32_t many = 0u;
+    int64_t from = begin;                                    // what the noted places are counted from
+    load(begin, token);
+    for (int64_t i = begin; i < end; i += 64 * kOrderLoads) {
+        load(i + 64 * kOrderLoads, next);
+#pragma unroll
+        for (int u = 0; u < kOrderLoads; ++u) {
+            const bool is_mine = valid(token[u]) && (token[u] & mask) == slice;
+            const unsigned long long mine = __ballot(is_mine);
+            if (mine != 0ull) {
+                if (is_mine) found[w][many + lanes_in_front(mine)] = (uint16_t)((i - from) + 64 * u + lane);
+                many += (uint32_t)__popcll(mine);
+                if (many > (uint32_t)kFound - 64u) {
+                    place_found(many, from);
+                    many = 0u;
+                }
             }
+            token[u] = next[u];
         }
-        place_found(many, from);
+        if (i + 2 * 64 * kOrderLoads - from > 65536) {       // the next ones' places would pass 16 bits
+            place_found(many, from);
+            many = 0u;
+            from = i + 64 * kOrderLoads;
+        }
     }
+    place_found(many, from);
 }
 
 // A value of lane j of each group of eight lanes.  Wavefronts that work on one row have it in a scalar register.
