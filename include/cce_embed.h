@@ -10,9 +10,10 @@
  *
  * Conventions are those of cce.h: DEVICE pointers owned by the caller, dense row-major, 16-byte
  * aligned (tokens, status: 4-byte); bf16 tensors are raw 16-bit patterns (void*); `stream` is a
- * hipStream_t as void*; nothing is allocated, freed or synchronised, and a stream under HIP graph
- * capture may call them; CCE_OK or a negative CCE_ERR_* code is returned and nothing is enqueued
- * on an error.
+ * hipStream_t as void*; nothing is allocated, freed or synchronised: the calls consist of kernel
+ * launches only, and a stream under HIP graph capture may make them once each has been made once on
+ * the device outside a capture; CCE_OK or a negative CCE_ERR_* code is returned and nothing is
+ * enqueued on an error (CCE_ERR_HIP: as in cce.h).
  *
  * Sizes: N >= 1 tokens (below 2^31), V >= 1 rows (at most 2^24), D a positive multiple of 8 (at
  * most 65536), V * D at most 2^37: CCE_ERR_INVALID for sizes <= 0, CCE_ERR_UNSUPPORTED for the

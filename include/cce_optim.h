@@ -4,9 +4,11 @@
  * tensors of a model in a few launches, with moments in 32 or in 8 bits.
  *
  * Conventions are those of cce.h: tensor pointers are DEVICE pointers owned by the caller; `stream` is
- * a hipStream_t as void*; nothing is allocated, freed or synchronised, and a stream under HIP graph
- * capture may call them (a replay repeats the captured step: its bias corrections, its random
- * numbers); CCE_OK or a negative CCE_ERR_* code is returned and nothing is enqueued on an error.
+ * a hipStream_t as void*; nothing is allocated, freed or synchronised: the calls consist of kernel
+ * launches only, and a stream under HIP graph capture may make them once each has been made once on
+ * the device outside a capture (a replay repeats the captured step: its tensors, its bias
+ * corrections, its random numbers); CCE_OK or a negative CCE_ERR_* code is returned and nothing is
+ * enqueued on an error (CCE_ERR_HIP: as in cce.h).
  *
  * `tensors` is a HOST array, read before the call returns and not kept: addresses may change from
  * call to call.  count >= 1.  A tensor of n = 0 values takes no part and its pointers are not looked
@@ -46,7 +48,8 @@ size_t cce_sumsq_multi_workspace_bytes(int64_t count);
 /*
  * Sum of squares of all gradients and the clipping coefficient of their global norm (gradient-clipping
  * strategies).  Of `tensors` it reads grad, n and grad_bf16.
- *   sumsq      i/o fp64 [1] device, 8-byte aligned: accumulate == 0: set, != 0: added to
+ *   sumsq      i/o fp64 [1] device, 8-byte aligned: accumulate == 0: set, != 0: added to (not finite if a
+ *              gradient is not; the coefficient of a NaN is 1, as cce_clip_coef's)
  *   clip_coef  out fp32 [1] device, may be NULL: min(1, max_norm / (sqrt(sumsq) + eps_norm)) of the new
  *              sumsq; max_norm > 0 and eps_norm >= 0 are looked at only then
  *   workspace  at least cce_sumsq_multi_workspace_bytes(count) bytes, 256-byte aligned
@@ -68,8 +71,9 @@ int cce_grad_sumsq_multi(const cce_optim_tensor* tensors, int64_t count, double*
  * 2^(s - 127) is the smallest power of two, from 2^-100 to 2^120, with which the block's largest finite
  * |m| (sqrt(v)) is at most 448 (480), 1 for a block of zeros; a value between two codes goes up with the
  * probability of its place between them, in steps of 2^-17 (2^-16), and a sqrt(v) > 0 never to 0.  NaN and
- * infinite values get a NaN code.  Rounded to nearest, v could not follow a beta2 near 1: 0.1 % of it a
- * step is far below half the distance of two codes.
+ * infinite values get a NaN code.  sqrt(v / bias correction) + eps is at least 2^-126 in the update.
+ * Rounded to nearest, v could not follow a beta2 near 1: 0.1 % of it a step is far below half the
+ * distance of two codes.
  * The random numbers are a hash of `seed`, `step` and the value's place in its tensor: the same call gives
  * the same bits.  `seed` is not used for moments in fp32, whose arithmetic is fp32 as in cce_adamw_step.
  */

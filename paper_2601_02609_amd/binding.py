@@ -1049,7 +1049,8 @@ def cce_embedding_backward(tokens: torch.Tensor, d_out: torch.Tensor, V: int, ig
 # ---------------------------------------------------------------- include/cce_optim.h
 
 class OptimTensors:
-    """The tensors of an optimizer step, made once and given to every step (it keeps them alive).
+    """The tensors of an optimizer step, made once and given to every step.  It keeps the tensors alive and works on the memory
+    that they have now: give it other gradients with set_grads, and make it anew for parameters or moments that move.
 
     grads             fp32 or bf16, of any shape, contiguous; the other lists are parallel to it
     params, m, v      fp32 parameters and moments, of as many values; moments in 8 bits are uint8 and have a scale
@@ -1128,16 +1129,18 @@ class OptimTensors:
     def _check_overlap(self):
         spans = []
         for name, tensors in self._keep.items():
-            spans += [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), name != "grads", f"{name}[{i}]")
-                      for i, t in enumerate(tensors) if t is not None and t.numel()]
+            for i, x in enumerate(tensors):
+                if x is not None:
+                    start = x.data_ptr()
+                    spans.append((start, start + x.numel() * x.element_size(), name != "grads", name, i))
         spans.sort()
-        last = written = (0, 0, False, "")                 # of the spans so far those that end last, of all and of the written ones
-        for span in spans:
-            other = last if span[2] else written
-            if span[0] < other[1]:
-                raise ValueError(f"{span[3]} overlaps {other[3]}")
-            last = max(last, span, key=lambda s: s[1])
-            written = max(written, span, key=lambda s: s[1]) if span[2] else written
+        end = end_written = 0                              # where the spans so far end, all of them and the written ones
+        for start, stop, writes, name, i in spans:
+            if start < (end if writes else end_written) and stop > start:
+                raise ValueError(f"{name}[{i}] overlaps another tensor of the list")
+            end = max(end, stop)
+            if writes:
+                end_written = max(end_written, stop)
 
 
 def cce_grad_sumsq_multi(tensors: OptimTensors, sumsq: Optional[torch.Tensor] = None, accumulate: bool = False, *,

@@ -136,6 +136,29 @@ def test_large_tensor_and_no_copy(B, state8):
     assert T.intact()
 
 
+@pytest.mark.parametrize("hp,step", [(dict(lr=1e-2, beta1=0.0, beta2=0.0, eps=1e-8), 3), (dict(lr=0.0, beta1=0.9, beta2=0.999, eps=1e-8), 1),
+                                     (dict(lr=1e-3, beta1=0.99, beta2=0.9999, eps=1e-3), 100000), (dict(lr=1e-3, beta1=0.5, beta2=0.5, eps=0.0), 2)])
+@pytest.mark.parametrize("state8", [0, 1])
+def test_other_hyperparameters(B, hp, step, state8):
+    T = _Tensors(B, [3000, 129], [state8] * 2, [0, 0], seed=16)
+    for k in (step, step + 1):
+        before = [T.host(i) for i in range(2)]
+        B.cce_adamw_multi_step(T.list, k, seed=8, **hp)
+        _check_step(T, before, 1.0, k, 8, hp)
+        T.new_grads()
+        T.list.set_grads(T.gd)
+
+
+def test_zero_gradient_and_eps_with_8_bit_moments(B):
+    """0 / max(0, 2^-126): the parameters decay and nothing else, the moments stay zero."""
+    T = _Tensors(B, [500], [1], [0], seed=17)
+    T.gd[0].zero_()
+    B.cce_adamw_multi_step(T.list, 1, lr=1e-3, eps=0.0)
+    decay = np.float32(1) - np.float32(1e-3) * np.float32(0.1)
+    assert np.array_equal(T.pd[0].cpu().numpy(), T.p[0] * decay)
+    assert not bool(T.md[0].any()) and not bool(T.vd[0].any()) and bool((T.ms[0] == 127).all())
+
+
 def test_step_of_one_tensor_equals_the_single_step(B):
     """Within the two calls' roundings of cce_adamw_step on the same tensor."""
     n = 100001
