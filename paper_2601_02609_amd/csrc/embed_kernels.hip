@@ -90,7 +90,6 @@ constexpr int kFound = 1024;                    // positions that a wavefront no
 constexpr int kSmallTokens = 1024;              // one launch takes: a thread each
 constexpr int kSmallRows = 2048;                // and rows of strips, which one workgroup may have all of
 constexpr int kSmallShare = 16;                 // rows of a key that one wavefront adds up
-constexpr int kJoinWaves = 8;
 constexpr int kJoinShort = 16;                  // pieces of a group that one wavefront joins, and one more
 // Wavefronts that the sum is cut into, if there are rows for them.  Added to dW, the pieces take unequal times (rows of dW are read
 // where groups end) and more of them even out: 32768 x 3584 124 -> 118 us, 32768 x 1024 of uniform tokens 72 -> 67; overwriting,
@@ -401,8 +400,12 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbedBackward 
 
 // A workgroup per slice and 256 columns: of its slice's keys it takes those whose group crosses a piece's end, and its
 // wavefronts share the group's partial rows: the last one of the piece where it begins, the first ones of the others.
-__global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(const EmbedBackward a, int strips) {
-    __shared__ af32x4 red[kJoinWaves][64];
+// WAVES of a workgroup: four where more workgroups are than fit the card at a time (32768 x 3584 117.9 -> 115.1 us in all, 2048 x
+// 4096 24.8 -> 22.9), sixteen for one strip, where a frequent token's partial rows are the time (65536 x 64 45.2 -> 42.8),
+// eight between (8192 x 896 with four 22.1 -> 23.8).
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void embedding_join_kernel(const EmbedBackward a, int strips) {
+    __shared__ af32x4 red[WAVES][64];
     __shared__ int crossing[kSliceKeys][3];                  // key, first and last piece
     __shared__ int groups;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -412,7 +415,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(const E
     const af32x4* partial = (const af32x4*)a.partial;
     if (threadIdx.x == 0) groups = 0;
     __syncthreads();
-    for (int key = threadIdx.x; key < a.keys; key += 64 * kJoinWaves) {
+    for (int key = threadIdx.x; key < a.keys; key += 64 * WAVES) {
         const int from = starts[key], to = starts[key + 1];
         const int p = from / a.piece, q = (to - 1) / a.piece;
         if (to > from && p != q) {                           // in whatever order: no sum is over two groups
@@ -441,7 +444,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(const E
         return sum;
     };
     auto row_at = [&](int key) { return (af32x4*)a.dW + (size_t)(((int64_t)key << a.bits) + slice) * quads + c; };
-    for (int g = w; g < n; g += kJoinWaves) {
+    for (int g = w; g < n; g += WAVES) {
         const int p = crossing[g][1], q = crossing[g][2];
         if (q - p >= kJoinShort || c >= quads) continue;
         af32x4* at = row_at(crossing[g][0]);
@@ -456,13 +459,13 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(const E
         af32x4 sum = {0.f, 0.f, 0.f, 0.f}, old = sum;
         if (c < quads) {
             if (w == 0 && a.accumulate) old = at[0];
-            sum = rows_of(p, q, kJoinWaves, w);
+            sum = rows_of(p, q, WAVES, w);
         }
         red[w][lane] = sum;
         __syncthreads();
         if (w == 0 && c < quads) {
 #pragma unroll
-            for (int i = 1; i < kJoinWaves; ++i) sum += red[i][lane];
+            for (int i = 1; i < WAVES; ++i) sum += red[i][lane];
             at[0] = old + a.scale * sum;
         }
         __syncthreads();
@@ -706,8 +709,10 @@ int cce_embedding_backward(const int32_t* tokens, const void* d_out, int64_t N, 
 #undef CCE_EMBED_SUM
 
     if (pieces > 1) {
-        const int strips = (int)((D + 255) / 256);
-        hipLaunchKernelGGL(embedding_join_kernel, dim3((unsigned)(slices * strips)), dim3(64 * kJoinWaves), 0, stream, a, strips);
+        const int strips = (int)((D + 255) / 256), groups = slices * strips;
+#define CCE_EMBED_JOIN(WAVES) hipLaunchKernelGGL(embedding_join_kernel<WAVES>, dim3((unsigned)groups), dim3(64 * WAVES), 0, stream, a, strips)
+        if (groups > 2048) CCE_EMBED_JOIN(4); else if (strips > 1) CCE_EMBED_JOIN(8); else CCE_EMBED_JOIN(16);
+#undef CCE_EMBED_JOIN
     }
     return hip_ok(hipGetLastError()) ? CCE_OK : CCE_ERR_HIP;
 }

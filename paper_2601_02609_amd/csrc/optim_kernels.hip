@@ -154,7 +154,13 @@ __global__ __launch_bounds__(1024) void norm_final_kernel(const double* __restri
                                                           int accumulate, float max_norm, float eps_norm, float* __restrict__ clip_coef) {
     __shared__ double red[16];
     double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < count; i += 1024) sum += partials[i];
+    for (int64_t i = threadIdx.x; i < count; i += 8192) {      // eight loads of a thread in flight
+        double x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[u] = i + 1024 * u < count ? partials[i + 1024 * u] : 0.0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) sum += x[u];
+    }
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
