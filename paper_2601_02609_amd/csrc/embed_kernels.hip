@@ -152,8 +152,8 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const
     uint32_t* own = count + w * a.keys;
     const int64_t range = ((int64_t)a.N + 64 * kOrderWaves - 1) / (64 * kOrderWaves) * 64;
     const int64_t begin = w * range, end = begin + range < a.N ? begin + range : a.N;
-    if (slice == 0 && a.status)
-        for (int64_t i = begin + lane; i < end; i += 64) token_takes_part(a.tokens[i], a.V, a.ignore_index, a.status);
+    const bool report = slice == 0 && a.status != nullptr;
+    unsigned long long bad = 0ull;
     auto load = [&](int64_t i, int (&token)[kOrderLoads]) {  // -1 behind the end; every load is made, none waits for another
         const int64_t from = i < a.N ? i : 0;
         const int left = i < end ? (end - i < 64 * kOrderLoads ? (int)(end - i) : 64 * kOrderLoads) : 0;
@@ -174,6 +174,7 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const
         for (int u = 0; u < kOrderLoads; ++u) {
             const int s = token[u] & mask;
             const unsigned long long ok = __ballot(valid(token[u]));
+            if (report) bad |= __ballot(token[u] != a.ignore_index && i + 64 * u + lane < end) & ~ok;
             below += (uint32_t)__popcll(__ballot(s < slice) & ok);
             const unsigned long long mine = __ballot(s == slice) & ok;
             if (mine != 0ull) {
@@ -187,6 +188,7 @@ __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const
             token[u] = next[u];
         }
     }
+    if (bad != 0ull && lane == 0) atomicOr(a.status, CCE_STATUS_BAD_TOKEN);
     if (lane == 0) wave_below[w] = below;
     __syncthreads();
 

@@ -151,6 +151,25 @@ def test_tokens_outside_the_matrix_are_reported(B):
     assert int(status) == B.CCE_STATUS_BAD_TOKEN and not bool(out[2].any()) and bool(out[1].any())
 
 
+@pytest.mark.parametrize("N", [1, 64, 700, 1025, 5000, 40001])
+@pytest.mark.parametrize("bad", [-1, 100, -2 ** 31, 2 ** 31 - 1])
+def test_one_bad_token_anywhere_is_reported(B, N, bad):
+    """In one launch and in three, at either end: by both calls, and not without one."""
+    V, D = 100, 64
+    dy = torch.ones(N, D, dtype=torch.bfloat16, device="cuda")
+    w = torch.ones(V, D, dtype=torch.bfloat16, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for at in (None, 0, N // 2, N - 1):
+        t = torch.full((N,), IGN, dtype=torch.int32, device="cuda")
+        t[N // 3] = 7
+        if at is not None:
+            t[at] = bad
+        for call in (lambda: B.cce_embedding_forward(t, w, IGN, status=status), lambda: B.cce_embedding_backward(t, dy, V, IGN, status=status)):
+            status.zero_()
+            call()
+            assert int(status) == (0 if at is None else B.CCE_STATUS_BAD_TOKEN), at
+
+
 def test_gradient_is_the_same_in_every_run_and_with_any_workspace(B):
     rng = np.random.default_rng(6)
     N, D, V = 6000, 256, 500

@@ -213,6 +213,29 @@ def test_state8_read_is_what_the_codes_stand_for(B, n):
     assert np.array_equal(out.cpu().numpy(), (S.decode(codes, scales, S.R) ** 2).astype(np.float32), equal_nan=True) and intact()
 
 
+def test_places_beyond_32_bits(B):
+    """A tensor of over 2^32 values: its last ones, whose random numbers and addresses take the upper word in."""
+    n, tail = (1 << 32) + 300, 1000
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    m, v = torch.zeros(n, dtype=torch.uint8, device="cuda"), torch.zeros(n, dtype=torch.uint8, device="cuda")
+    ms, vs = (torch.zeros((n + 127) // 128, dtype=torch.uint8, device="cuda") for _ in range(2))
+    rng = np.random.default_rng(18)
+    first = (n - tail) // 128 * 128
+    gt = I.f32_to_bf16_bits((rng.standard_normal(n - first) * 1e-2).astype(np.float32))
+    g[first:] = torch.from_numpy(gt.view(np.int16)).cuda().view(torch.bfloat16)
+    T = B.OptimTensors([g], [p], [m], [v], m_scales=[ms], v_scales=[vs])
+    s, _ = B.cce_grad_sumsq_multi(T)
+    gf = I.bf16_bits_to_f32(gt).astype(np.float64)
+    assert abs(float(s) / float((gf ** 2).sum()) - 1.0) <= 1e-12
+    B.cce_adamw_multi_step(T, 2, lr=1e-3, beta2=0.99, seed=21)
+    um, ur = S.dither(n - first, 21, 2, first=first)
+    b1, b2 = float(np.float32(0.9)), float(np.float32(0.99))
+    for codes, scales, want in ((m, ms, S.encode((1 - b1) * gf, um, S.M)), (v, vs, S.encode(np.sqrt((1 - b2) * gf * gf), ur, S.R))):
+        assert np.array_equal(codes[first:].cpu().numpy(), want[0]) and np.array_equal(scales[first // 128:].cpu().numpy(), want[1])
+        assert not bool(codes[:first].any())
+    assert bool((p[first:] != 0).any()) and not bool(p[:first].any())
+
+
 def test_seed_and_step_choose_the_random_numbers(B):
     def run(seed, step):
         T = _Tensors(B, [5000, 300], [1, 1], [0, 0], seed=15)
