@@ -56,7 +56,7 @@ size_t cce_embedding_workspace_bytes(int64_t N, int64_t D, int64_t V);
  *                             accumulate_dW != 0: added to, other rows are neither read nor written
  *   workspace  at least cce_embedding_workspace_bytes(N, D, V) bytes, 256-byte aligned; calls that may
  *              run at the same time need one each
- * Sums are fp32 in an order that depends on the tokens alone: the same bits in every run.
+ * Sums are fp32 in an order that the arguments decide: the same call gives the same bits.
  */
 int cce_embedding_backward(const int32_t* tokens, const void* d_out, int64_t N, int64_t D, int64_t V,
                            int32_t ignore_index, float scale, float* dW, int accumulate_dW, int32_t* status,

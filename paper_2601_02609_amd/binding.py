@@ -10,6 +10,7 @@ import ctypes
 import os
 from typing import Optional, Tuple
 
+import numpy as np
 import torch
 
 from . import build as _build
@@ -956,7 +957,7 @@ def cce_backward_compact_ex(hidden: torch.Tensor, weight: torch.Tensor, labels: 
 
 # The calls below take a few microseconds on the GPU at their smallest: what the host does for one counts.  This is
 # torch.cuda.current_stream(device).cuda_stream without the objects in between (2 us of 10).
-_current_stream_ptr = torch._C._cuda_getCurrentRawStream
+_current_stream_ptr = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _check_on(device: torch.device, t: torch.Tensor, dtype, shape: tuple, name):
@@ -1069,78 +1070,92 @@ class OptimTensors:
             raise ValueError("params, m and v: expected all three or none")
         self.steps = params is not None
         self.device = grads[0].device
-        self._array = (_OptimTensor * count)()
+        self._table = np.zeros(count, dtype=np.dtype(_OptimTensor))
+        self._address = self._table.ctypes.data
         lists = {"params": params, "m": m, "v": v, "params_bf16": params_bf16, "m_scales": m_scales, "v_scales": v_scales}
         lists = {name: [None] * count if x is None else list(x) for name, x in lists.items()}
-        rates = {name: list(x) if hasattr(x, "__len__") else [x] * count
-                 for name, x in (("lr_scale", lr_scale), ("weight_decay", weight_decay))}
-        for name, x in [*lists.items(), *rates.items()]:
+        rates = {"lr_scale": lr_scale, "weight_decay": weight_decay}
+        for name, x in [*lists.items(), *((name, x) for name, x in rates.items() if hasattr(x, "__len__"))]:
             if len(x) != count:
                 raise ValueError(f"{name}: expected {count} entries, got {len(x)}")
         self._keep = lists
-        self._take_grads(grads, [g.numel() for g in grads])
-        if not self.steps:
-            return
-        for i, entry in enumerate(self._array):
-            n, blocks = entry.n, (entry.n + STATE8_BLOCK - 1) // STATE8_BLOCK
-            state = lists["m"][i].dtype if lists["m"][i] is not None else None
-            if state not in (torch.float32, torch.uint8):
-                raise ValueError(f"m[{i}]: expected float32 or uint8, got {state}")
-            entry.state8 = int(state == torch.uint8)
-            wanted = [("param", "params", torch.float32, n), ("m", "m", state, n), ("v", "v", state, n)]
-            if lists["params_bf16"][i] is not None:
-                wanted.append(("param_bf16", "params_bf16", torch.bfloat16, n))
-            if entry.state8:
-                wanted += [("m_scale", "m_scales", torch.uint8, blocks), ("v_scale", "v_scales", torch.uint8, blocks)]
-            for field, name, dtype, values in wanted:
-                setattr(entry, field, self._pointer(name, i, lists[name][i], dtype, values))
-            entry.lr_scale, entry.weight_decay = rates["lr_scale"][i], rates["weight_decay"][i]
+        sizes = [g.numel() for g in grads]
+        self._table["n"] = sizes
+        if self.steps:
+            states = [x.dtype if x is not None else None for x in lists["m"]]
+            for i, state in enumerate(states):
+                if state not in (torch.float32, torch.uint8):
+                    raise ValueError(f"m[{i}]: expected float32 or uint8, got {state}")
+            eight = [state == torch.uint8 for state in states]
+            if not any(eight):
+                lists["m_scales"] = lists["v_scales"] = [None] * count
+            blocks = [(n + STATE8_BLOCK - 1) // STATE8_BLOCK for n in sizes]
+            all_of = [True] * count
+            for field, name, dtypes, values, wanted in (
+                    ("param", "params", [torch.float32] * count, sizes, all_of), ("m", "m", states, sizes, all_of),
+                    ("v", "v", states, sizes, all_of), ("m_scale", "m_scales", [torch.uint8] * count, blocks, eight),
+                    ("v_scale", "v_scales", [torch.uint8] * count, blocks, eight),
+                    ("param_bf16", "params_bf16", [torch.bfloat16] * count, sizes, [x is not None for x in lists["params_bf16"]])):
+                self._table[field] = self._pointers(name, lists[name], dtypes, values, wanted)
+            self._table["state8"] = eight
+            self._table["lr_scale"] = lr_scale
+            self._table["weight_decay"] = weight_decay
+        self._take_grads(list(grads), sizes)
 
     def __len__(self):
-        return len(self._array)
+        return len(self._table)
 
-    def _pointer(self, name, i, t, dtype, n):
-        if t is None or t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != self.device:
-            got = "None" if t is None else f"{t.dtype} of {t.numel()} contiguous={t.is_contiguous()} on {t.device}"
-            raise ValueError(f"{name}[{i}]: expected a contiguous {dtype} tensor of {n} elements on {self.device}, got {got}")
-        return t.data_ptr()
+    def _pointers(self, name, tensors, dtypes, sizes, wanted):
+        device, pointers = self.device, []
+        for i, (t, dtype, n, want) in enumerate(zip(tensors, dtypes, sizes, wanted)):
+            if not want:
+                pointers.append(0)
+            elif t is None or t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != device:
+                got = "None" if t is None else f"{t.dtype} of {t.numel()} contiguous={t.is_contiguous()} on {t.device}"
+                raise ValueError(f"{name}[{i}]: expected a contiguous {dtype} tensor of {n} elements on {device}, got {got}")
+            else:
+                pointers.append(t.data_ptr())
+        return pointers
 
     def _take_grads(self, grads, sizes):
-        for i, g in enumerate(grads):
-            if g.dtype not in (torch.float32, torch.bfloat16) or not g.is_cuda:
-                raise ValueError(f"grads[{i}]: expected a cuda float32 or bfloat16 tensor, got {g.dtype} on {g.device}")
-        pointers = [self._pointer("grads", i, g, g.dtype, n) for i, (g, n) in enumerate(zip(grads, sizes))]
-        self._keep["grads"] = list(grads)
-        self._check_overlap()
-        for entry, g, pointer, n in zip(self._array, grads, pointers, sizes):
-            entry.grad, entry.n, entry.grad_bf16 = pointer, n, int(g.dtype == torch.bfloat16)
+        dtypes = [g.dtype for g in grads]
+        for i, (g, dtype) in enumerate(zip(grads, dtypes)):
+            if dtype not in (torch.float32, torch.bfloat16) or not g.is_cuda:
+                raise ValueError(f"grads[{i}]: expected a cuda float32 or bfloat16 tensor, got {dtype} on {g.device}")
+        pointers = self._pointers("grads", grads, dtypes, sizes, [True] * len(grads))
+        before = self._table[["grad", "grad_bf16"]].copy()
+        self._table["grad"] = pointers
+        self._table["grad_bf16"] = [dtype == torch.bfloat16 for dtype in dtypes]
+        if self.steps:
+            try:
+                self._check_overlap()
+            except ValueError:
+                self._table[["grad", "grad_bf16"]] = before
+                raise
+        self._keep["grads"] = grads
 
     def set_grads(self, grads):
         """Other gradients for the same parameters (a step whose gradients lie elsewhere)."""
         if len(grads) != len(self):
             raise ValueError(f"grads: expected {len(self)} tensors, got {len(grads)}")
-        old = self._keep["grads"]
-        try:
-            self._take_grads(grads, [entry.n for entry in self._array])
-        except ValueError:
-            self._keep["grads"] = old
-            raise
+        self._take_grads(list(grads), self._table["n"].tolist())
 
     def _check_overlap(self):
-        spans = []
-        for name, tensors in self._keep.items():
-            for i, x in enumerate(tensors):
-                if x is not None:
-                    start = x.data_ptr()
-                    spans.append((start, start + x.numel() * x.element_size(), name != "grads", name, i))
-        spans.sort()
-        end = end_written = 0                              # where the spans so far end, all of them and the written ones
-        for start, stop, writes, name, i in spans:
-            if start < (end if writes else end_written) and stop > start:
-                raise ValueError(f"{name}[{i}] overlaps another tensor of the list")
-            end = max(end, stop)
-            if writes:
-                end_written = max(end_written, stop)
+        t, n = self._table, self._table["n"]
+        moment, blocks = n * np.where(t["state8"] != 0, 1, 4), (n + STATE8_BLOCK - 1) // STATE8_BLOCK
+        columns = [("param", "params", n * 4), ("param_bf16", "params_bf16", n * 2), ("m", "m", moment), ("v", "v", moment),
+                   ("m_scale", "m_scales", blocks), ("v_scale", "v_scales", blocks), ("grad", "grads", n * np.where(t["grad_bf16"] != 0, 2, 4))]
+        starts = np.concatenate([t[field].astype(np.int64) for field, _, _ in columns])
+        ends = starts + np.concatenate([size for _, _, size in columns])
+        writes = np.arange(len(starts)) < 6 * len(n)
+        order = np.argsort(starts, kind="stable")
+        order = order[(starts[order] != 0) & (ends[order] > starts[order])]
+        start, end, written = starts[order], np.maximum.accumulate(ends[order]), np.maximum.accumulate(np.where(writes[order], ends[order], 0))
+        # what is written begins behind the end of everything in front of it, a gradient behind that of what is written
+        over = start[1:] < np.where(writes[order][1:], end[:-1], written[:-1])
+        if over.any():
+            at = int(order[1 + int(np.argmax(over))])
+            raise ValueError(f"{columns[at // len(n)][1]}[{at % len(n)}] overlaps another tensor of the list")
 
 
 def cce_grad_sumsq_multi(tensors: OptimTensors, sumsq: Optional[torch.Tensor] = None, accumulate: bool = False, *,
@@ -1167,7 +1182,7 @@ def cce_grad_sumsq_multi(tensors: OptimTensors, sumsq: Optional[torch.Tensor] = 
         workspace = _new((int(lib().cce_sumsq_multi_workspace_bytes(len(tensors))),), torch.uint8, device, stream)
     else:
         _check_on(device, workspace, torch.uint8, (workspace.numel(),), "workspace")
-    _call("cce_grad_sumsq_multi", lib().cce_grad_sumsq_multi, device, stream, tensors._array, len(tensors), sumsq.data_ptr(),
+    _call("cce_grad_sumsq_multi", lib().cce_grad_sumsq_multi, device, stream, tensors._address, len(tensors), sumsq.data_ptr(),
           1 if accumulate else 0, max_norm if max_norm is not None else 0.0, eps_norm,
           clip_coef.data_ptr() if clip_coef is not None else None, workspace.data_ptr(), workspace.numel())
     return sumsq, clip_coef
@@ -1181,7 +1196,7 @@ def cce_adamw_multi_step(tensors: OptimTensors, step: int, *, lr: float, beta1: 
         raise ValueError("tensors: the list has gradients alone")
     if clip_coef is not None:
         _check_on(tensors.device, clip_coef, torch.float32, (1,), "clip_coef")
-    _call("cce_adamw_multi_step", lib().cce_adamw_multi_step, tensors.device, stream, tensors._array, len(tensors), lr, beta1, beta2,
+    _call("cce_adamw_multi_step", lib().cce_adamw_multi_step, tensors.device, stream, tensors._address, len(tensors), lr, beta1, beta2,
           eps, step, clip_coef.data_ptr() if clip_coef is not None else None, seed & 0xFFFFFFFF)
 
 

@@ -291,6 +291,7 @@ def test_list_refuses(B):
         with pytest.raises(ValueError):
             new(**change)
     whole = z(400)
+    new(grads=[whole[:300], whole[292:300]])                                # gradients are only read
     for change in (dict(params=[whole[:300], whole[292:300]]), dict(params=[whole[:300], z(8)], m=[z(300), whole[100:108]]),
                    dict(grads=[whole[:300], z(8)], v=[z(300), whole[:8]])):
         with pytest.raises(ValueError, match="overlaps"):
@@ -300,6 +301,8 @@ def test_list_refuses(B):
         T.set_grads([z(300)])
     with pytest.raises(ValueError):
         T.set_grads([z(300), z(9)])
+    with pytest.raises(ValueError, match="overlaps"):                       # and the gradients stay those that were
+        T.set_grads([T._keep["params"][0], z(8)])
     T.set_grads([z(300, torch.bfloat16), z(8)])
     B.cce_adamw_multi_step(T, 1, lr=1e-3)
     with pytest.raises(ValueError):
