@@ -691,6 +691,8 @@ int cce_embedding_backward(const int32_t* tokens, const void* d_out, int64_t N, 
     a.order = (int32_t*)at; at += round_up(N * 4, 256);
     a.sorted = (int32_t*)at; at += round_up(N * 4, 256);
     a.partial = (float*)at;
+    const int64_t pieces = (N + a.piece - 1) / a.piece;
+    if ((size_t)(at - (char*)workspace) + (size_t)pieces * 2 * D * 4 > workspace_bytes) return CCE_ERR_INVALID;
     if (N <= kSmallTokens && N * ((a.row_chunks + 63) / 64) <= kSmallRows) {
         a.strips = (a.row_chunks + 63) / 64;
         hipLaunchKernelGGL(embedding_small_kernel, dim3((unsigned)slices), dim3(64 * kOrderWaves), 0, stream, a);
@@ -700,7 +702,6 @@ int cce_embedding_backward(const int32_t* tokens, const void* d_out, int64_t N, 
 
     const int lanes = embed_lanes(D);
     a.strips = (a.row_chunks + lanes - 1) / lanes;
-    const int64_t pieces = (N + a.piece - 1) / a.piece;
     const int sum_blocks = (int)((pieces * a.strips * lanes + 255) / 256);
     const int zero_blocks = a.accumulate ? 0 : (a.keys + 63) / 64 * slices;
     const dim3 grid((unsigned)(sum_blocks + zero_blocks));

@@ -76,7 +76,11 @@ def _gradient_case(B, N, D, V, kind, ignore, scale, accumulate, seed=0):
     dw, intact = _guarded((V, D), torch.float32)
     dw.copy_(torch.from_numpy(dw0) if accumulate else torch.full((V, D), float("nan")))
     print(f"[gradient] N={N} D={D} V={V} {kind} accumulate={accumulate}", flush=True)
-    B.cce_embedding_backward(torch.from_numpy(t).cuda(), bf16_dev(dy), V, IGN, scale=scale, d_weight=dw, accumulate_dw=accumulate)
+    need = B.embedding_workspace_bytes(N, D, V)
+    ws = torch.full((need + 4096,), 171, dtype=torch.uint8, device="cuda")
+    B.cce_embedding_backward(torch.from_numpy(t).cuda(), bf16_dev(dy), V, IGN, scale=scale, d_weight=dw, accumulate_dw=accumulate,
+                             workspace=ws[:need])
+    assert bool((ws[need:] == 171).all())
     got = dw.cpu().numpy()
     want, size = E.backward(I.bf16_bits_to_f32(dy).astype(np.float64), t, V, IGN, float(np.float32(scale)), dw0 if accumulate else None)
     count = np.bincount(t[ok], minlength=V)
