@@ -88,7 +88,7 @@ constexpr int kOrderWaves = 16;
 constexpr int kOrderLoads = 8;                  // loads of tokens in flight, and as many ahead
 constexpr int kFound = 1024;                    // positions that a wavefront notes: 32 KB of LDS (two workgroups fit a CU)
 constexpr int kSmallTokens = 1024;              // one launch takes: a thread each
-constexpr int kSmallRows = 2048;                // and rows of strips, which one workgroup may have all of
+constexpr int kSmallRows = 2048, kSmallRowsAdd = 4096;    // and rows of strips, which one workgroup may have all of
 constexpr int kSmallShare = 16;                 // rows of a key that one wavefront adds up
 constexpr int kJoinShort = 16;                  // pieces of a group that one wavefront joins, and one more
 // Wavefronts that the sum is cut into, if there are rows for them.  Added to dW, the pieces take unequal times (rows of dW are read
@@ -478,8 +478,9 @@ __global__ __launch_bounds__(64 * WAVES) void embedding_join_kernel(const EmbedB
 // Few tokens: one launch.  A workgroup per slice finds its positions among all N <= kSmallTokens in order, then a wavefront
 // sums a key's rows (a strip of 512 columns of them) by itself, or all of them share the rows of a key that has many.
 // Bound by latency, launches above all.  Against the three launches: 257 x 64 into a new dW 13.1 -> 4.9 us; added to dW, 512 x 896
-// 15.9 -> 6.1, 1024 x 896 16.9 -> 7.5, 256 x 4096 17.1 -> 8.9.  kSmallRows bounds what one workgroup may have to sum if all tokens
-// are the same: 14.5 -> 24.4 us for 1024 x 896 then, 15.0 -> 46.9 for 1024 x 2048, which takes three launches.
+// 15.9 -> 6.1, 1024 x 896 16.9 -> 7.5, 1024 x 2048 17.6 -> 10.5, 512 x 3584 19.1 -> 9.8.  kSmallRows bounds what one workgroup may
+// have to sum if all tokens are the same: 14.5 -> 24.4 us for 1024 x 896 then, 15.0 -> 46.9 for 1024 x 2048.  A new dW has its
+// zeros written beside the rows' sums by the three launches: 1024 x 2048 into 32000 rows 61 us against 71 in one.
 // ------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(64 * kOrderWaves) void embedding_small_kernel(const EmbedBackward a) {
     __shared__ uint32_t mine[kSmallTokens];                  // this slice's positions, ascending, and their keys in the upper 16 bits
@@ -693,7 +694,7 @@ int cce_embedding_backward(const int32_t* tokens, const void* d_out, int64_t N, 
     a.partial = (float*)at;
     const int64_t pieces = (N + a.piece - 1) / a.piece;
     if ((size_t)(at - (char*)workspace) + (size_t)pieces * 2 * D * 4 > workspace_bytes) return CCE_ERR_INVALID;
-    if (N <= kSmallTokens && N * ((a.row_chunks + 63) / 64) <= kSmallRows) {
+    if (N <= kSmallTokens && N * ((a.row_chunks + 63) / 64) <= (a.accumulate ? kSmallRowsAdd : kSmallRows)) {
         a.strips = (a.row_chunks + 63) / 64;
         hipLaunchKernelGGL(embedding_small_kernel, dim3((unsigned)slices), dim3(64 * kOrderWaves), 0, stream, a);
         return hip_ok(hipGetLastError()) ? CCE_OK : CCE_ERR_HIP;
