@@ -142,7 +142,8 @@ __device__ __forceinline__ unsigned long long lanes_of_key(unsigned long long am
 // A workgroup per slice looks through all tokens (which stay in the L2s): its wavefronts, each with a range of positions,
 // count their keys in LDS and note what they found there; after a scan over keys and wavefronts they give the positions
 // of one key consecutive places.  64 tokens that none is in the slice of cost a handful of instructions, most of them
-// scalar: all slices together do that 256 N / 64 times, which is what bounds the kernel.
+// scalar: all slices together do that 256 N / 64 times, which is what bounds the kernel, and above 32768 tokens the slice of
+// the most frequent one: 7.7 us for 8192 tokens under Zipf's law, 16 for 32768, 25 for 65536 (16 if all are as frequent).
 __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const EmbedBackward a) {
     __shared__ uint32_t count[kOrderWaves * kSliceKeys];
     __shared__ uint16_t found[kOrderWaves][kFound];          // places in the wavefront's range
