@@ -21,6 +21,7 @@ typedef __attribute__((ext_vector_type(2))) float of32x2;
 constexpr int kStepValues = 1024;                      // values of a workgroup of a step: four a thread
 constexpr int kReadValues = 2048;                      // of a workgroup that reads 8-bit moments
 constexpr int64_t kMaxTensor = (int64_t)1 << 33;       // values of a tensor
+constexpr int64_t kMaxValues = (int64_t)1 << 40;       // of all tensors: 2^28 chunks of the norm and one a tensor, twice that in 32 bits
 constexpr int64_t kMaxGrid = (1 << 24) - 1;            // of 256 threads: a launch has fewer than 2^32 threads
 constexpr int kStepTensors = 64, kStepTensors8 = 52;   // tensors of a launch: kernel arguments hold 4 KB
 constexpr int kNormTensors = 160;
@@ -465,13 +466,12 @@ static bool misaligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to
 
 static int check_gradients(const cce_optim_tensor* tensors, int64_t count) {
     if (!tensors || count <= 0) return CCE_ERR_INVALID;
-    int64_t blocks = 0;
+    int64_t values = 0;
     for (int64_t i = 0; i < count; ++i) {
         const cce_optim_tensor& t = tensors[i];
         if (t.n < 0) return CCE_ERR_INVALID;
         if (t.n == 0) continue;
-        blocks += t.n / kStepValues + 1;
-        if (t.n > kMaxTensor || blocks > 0x3fffffff) return CCE_ERR_UNSUPPORTED;
+        if (t.n > kMaxTensor || (values += t.n) > kMaxValues) return CCE_ERR_UNSUPPORTED;
         if (!t.grad || misaligned(t.grad, 16) || (t.grad_bf16 != 0 && t.grad_bf16 != 1)) return CCE_ERR_INVALID;
     }
     return CCE_OK;

@@ -221,6 +221,18 @@ def test_sumsq_multi_refuses(L, entry, call, code):
     assert L.cce_grad_sumsq_multi(_entry(**entry), a["count"], a["sumsq"], 0, a["max_norm"], a["eps"], a["clip"], a["ws"], a["bytes"], None) == code
 
 
+@pytest.mark.parametrize("sizes,too_many", [([1 << 33], False), ([(1 << 33) + 1], True), ([1 << 33] * 128, False), ([1 << 33] * 128 + [1], True),
+                                            ([(1 << 33) - 1] * 128 + [128], False), ([1] * 5000 + [0], False)])
+def test_limits_of_a_list(L, sizes, too_many):
+    """A tensor of 2^33 values and 2^40 in all are the most that a list holds.  The calls are refused in either case: what is
+    within the limits for the argument that is missing."""
+    entries = (binding._OptimTensor * len(sizes))(*[binding._OptimTensor(param=P, grad=P, m=None, v=P, n=n, lr_scale=1.0) for n in sizes])
+    code = -2 if too_many else -1
+    need = L.cce_sumsq_multi_workspace_bytes(len(sizes))
+    assert L.cce_grad_sumsq_multi(entries, len(sizes), None, 0, 1.0, 1e-6, None, P, need, None) == code
+    assert L.cce_adamw_multi_step(entries, len(sizes), 1e-3, 0.9, 0.99, 1e-8, 1, None, 0, None) == code
+
+
 def test_state8_read_refuses(L):
     for codes, scales, n, second, out in ((None, P, 5, 0, P), (P, None, 5, 0, P), (P, P, 0, 0, P), (P, P, 5, 2, P), (P + 4, P, 5, 0, P), (P, P, 5, 0, P + 8)):
         assert L.cce_adamw_state8_read(codes, scales, n, second, out, None) == -1
