@@ -1105,6 +1105,9 @@ class OptimTensors:
     def __len__(self):
         return len(self._table)
 
+    def __reduce_ex__(self, protocol):
+        raise TypeError("OptimTensors holds the addresses of its tensors: it is not copied or pickled, make one from the other tensors")
+
     def _pointers(self, name, tensors, dtypes, sizes, wanted):
         device, pointers = self.device, []
         for i, (t, dtype, n, want) in enumerate(zip(tensors, dtypes, sizes, wanted)):

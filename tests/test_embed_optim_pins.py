@@ -1,6 +1,8 @@
 """Pins for the oracles of the embedding and of 8-bit moments (torch, closed forms, differences), and the refusals of
 the C entry points: none of these needs a GPU."""
+import copy
 import ctypes
+import pickle
 
 import numpy as np
 import pytest
@@ -248,3 +250,13 @@ def test_binding_refuses_host_tensors(L):
     with pytest.raises(ValueError):
         binding.cce_adamw_state8_read(torch.zeros(3, dtype=torch.uint8), torch.zeros(1, dtype=torch.uint8))
     assert ctypes.sizeof(binding._OptimTensor) == 80
+
+
+@pytest.mark.parametrize("how", [copy.copy, copy.deepcopy, pickle.dumps])
+def test_lists_are_not_copied(how):
+    """A copy would give the library the address of the original's table, which names the original's tensors and may be gone."""
+    tensors = object.__new__(binding.OptimTensors)
+    tensors._table = np.zeros(1, dtype=np.dtype(binding._OptimTensor))
+    tensors._address = tensors._table.ctypes.data
+    with pytest.raises(TypeError, match="OptimTensors"):
+        how(tensors)
