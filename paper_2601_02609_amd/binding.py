@@ -1052,6 +1052,8 @@ def cce_embedding_backward(tokens: torch.Tensor, d_out: torch.Tensor, V: int, ig
 class OptimTensors:
     """The tensors of an optimizer step, made once and given to every step.  It keeps the tensors alive and works on the memory
     that they have now: give it other gradients with set_grads, and make it anew for parameters or moments that move.
+    Tensors that a call on a given `stream` has read are recorded on that stream, so that they may be replaced or dropped at
+    once; for calls on the current stream torch's own rule holds.
 
     grads             fp32 or bf16, of any shape, contiguous; the other lists are parallel to it
     params, m, v      fp32 parameters and moments, of as many values; moments in 8 bits are uint8 and have a scale
@@ -1079,6 +1081,7 @@ class OptimTensors:
             if len(x) != count:
                 raise ValueError(f"{name}: expected {count} entries, got {len(x)}")
         self._keep = lists
+        self._streams = {}
         sizes = [g.numel() for g in grads]
         self._table["n"] = sizes
         if self.steps:
@@ -1087,8 +1090,8 @@ class OptimTensors:
                 if state not in (torch.float32, torch.uint8):
                     raise ValueError(f"m[{i}]: expected float32 or uint8, got {state}")
             eight = [state == torch.uint8 for state in states]
-            if not any(eight):
-                lists["m_scales"] = lists["v_scales"] = [None] * count
+            for name in ("m_scales", "v_scales"):
+                lists[name] = [x if e else None for x, e in zip(lists[name], eight)]
             blocks = [(n + STATE8_BLOCK - 1) // STATE8_BLOCK for n in sizes]
             all_of = [True] * count
             for field, name, dtypes, values, wanted in (
@@ -1100,6 +1103,8 @@ class OptimTensors:
             self._table["state8"] = eight
             self._table["lr_scale"] = lr_scale
             self._table["weight_decay"] = weight_decay
+        else:
+            lists.clear()
         self._take_grads(list(grads), sizes)
 
     def __len__(self):
@@ -1136,6 +1141,19 @@ class OptimTensors:
                 self._table[["grad", "grad_bf16"]] = before
                 raise
         self._keep["grads"] = grads
+        for stream in self._streams.values():
+            for g in grads:
+                g.record_stream(stream)
+
+    def _read_on(self, stream: Optional[torch.cuda.Stream]):
+        """A call on a stream of the caller's has been made."""
+        if stream is None or stream.cuda_stream in self._streams:
+            return
+        self._streams[stream.cuda_stream] = stream
+        for tensors in self._keep.values():
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
 
     def set_grads(self, grads):
         """Other gradients for the same parameters (a step whose gradients lie elsewhere)."""
@@ -1188,6 +1206,7 @@ def cce_grad_sumsq_multi(tensors: OptimTensors, sumsq: Optional[torch.Tensor] = 
     _call("cce_grad_sumsq_multi", lib().cce_grad_sumsq_multi, device, stream, tensors._address, len(tensors), sumsq.data_ptr(),
           1 if accumulate else 0, max_norm if max_norm is not None else 0.0, eps_norm,
           clip_coef.data_ptr() if clip_coef is not None else None, workspace.data_ptr(), workspace.numel())
+    tensors._read_on(stream)
     return sumsq, clip_coef
 
 
@@ -1201,6 +1220,7 @@ def cce_adamw_multi_step(tensors: OptimTensors, step: int, *, lr: float, beta1: 
         _check_on(tensors.device, clip_coef, torch.float32, (1,), "clip_coef")
     _call("cce_adamw_multi_step", lib().cce_adamw_multi_step, tensors.device, stream, tensors._address, len(tensors), lr, beta1, beta2,
           eps, step, clip_coef.data_ptr() if clip_coef is not None else None, seed & 0xFFFFFFFF)
+    tensors._read_on(stream)
 
 
 def cce_adamw_state8_read(codes: torch.Tensor, scales: torch.Tensor, *, second: bool = False,

@@ -260,3 +260,53 @@ def test_lists_are_not_copied(how):
     tensors._address = tensors._table.ctypes.data
     with pytest.raises(TypeError, match="OptimTensors"):
         how(tensors)
+
+
+class _Tensor:
+    """What a list asks of a tensor, without a device."""
+    address = 1 << 20
+
+    def __init__(self, dtype, n):
+        self.dtype, self.n, self.device, self.is_cuda, self.on = dtype, n, torch.device("cuda:0"), True, []
+        self.at, _Tensor.address = _Tensor.address, _Tensor.address + (4 * n + 255) // 256 * 256
+
+    numel = lambda self: self.n
+    is_contiguous = lambda self: True
+    data_ptr = lambda self: self.at
+    record_stream = lambda self, stream: self.on.append(stream.cuda_stream)
+
+
+class _Stream:
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+
+@pytest.mark.parametrize("state8", [False, True])
+def test_tensors_of_a_list_are_kept_for_the_stream_that_reads_them(monkeypatch, state8):
+    """A call on a stream of the caller's returns before its kernels have run: memory of the list, of gradients that
+    set_grads replaces above all, must not be handed out again until that stream has done with it."""
+    monkeypatch.setattr(binding, "_call", lambda *args: None)
+    monkeypatch.setattr(binding, "_new", lambda *args: torch.zeros(1))
+    f32, moment = torch.float32, torch.uint8 if state8 else torch.float32
+    new = lambda dtype, *sizes: [_Tensor(dtype, n) for n in sizes]
+    grads, copies = new(f32, 300, 0), [_Tensor(torch.bfloat16, 300), None]
+    rest = [new(f32, 300, 0), new(moment, 300, 0), new(moment, 300, 0)]
+    scales = [new(torch.uint8, 3, 0), new(torch.uint8, 3, 0)] if state8 else [None, None]
+    T = binding.OptimTensors(grads, *rest, params_bf16=copies, m_scales=scales[0], v_scales=scales[1])
+    a, b = _Stream(11), _Stream(12)
+    step = lambda stream: binding.cce_adamw_multi_step(T, 1, lr=1e-3, stream=stream)
+    norm = lambda stream: binding.cce_grad_sumsq_multi(T, stream=stream)
+    step(None)                                                              # the current stream: torch's own rule
+    assert all(t.on == [] for t in grads)
+    for _ in range(2):
+        step(a)
+    everything = [t for part in (grads, copies, *rest, *(x for x in scales if x)) for t in part if t is not None]
+    assert all(t.on == [11] for t in everything)
+    later = new(torch.bfloat16, 300, 0)
+    T.set_grads(later)
+    step(a)
+    assert all(t.on == [11] for t in later)
+    norm(b)
+    assert all(t.on == [11, 12] for t in later)
+    step(b)
+    assert all(t.on == [11, 12] for t in rest[0]) and all(t.on == [11] for t in grads)

@@ -315,3 +315,23 @@ def test_list_refuses(B):
         B.cce_adamw_multi_step(T, 0, lr=1e-3)
     with pytest.raises(B.CCEError):                                         # rows that do not start at 16 bytes
         B.cce_grad_sumsq_multi(B.OptimTensors([z(9)[1:]]))
+
+
+def test_replaced_gradients_stay_until_the_stream_has_read_them(B):
+    """Gradients replaced, and the memory asked for again, while a step on the caller's stream waits behind other work."""
+    n = 1 << 22
+    g = torch.randn(n, device="cuda")
+    state = lambda: [torch.zeros(n, device="cuda") for _ in range(3)]
+    want, got = state(), state()
+    B.cce_adamw_multi_step(B.OptimTensors([g], *([x] for x in want)), 1, lr=1e-3)
+    T = B.OptimTensors([g.clone()], *([x] for x in got))
+    big, s = torch.empty(1 << 28, device="cuda"), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        for _ in range(50):                                                 # 50 GB of writes in front of the step
+            big.fill_(1.0)
+    B.cce_adamw_multi_step(T, 1, lr=1e-3, stream=s)
+    T.set_grads([torch.zeros(n, device="cuda")])
+    junk = [torch.full((n,), 9.0, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(want, got)) and len(junk) == 4
