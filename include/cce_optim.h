@@ -70,8 +70,8 @@ int cce_grad_sumsq_multi(const cce_optim_tensor* tensors, int64_t count, double*
  * what the codes stand for, takes the update of param from them as they are, and rounds them to codes:
  * 2^(s - 127) is the smallest power of two, from 2^-100 to 2^120, with which the block's largest finite
  * |m| (sqrt(v)) is at most 448 (480), 1 for a block of zeros; a value between two codes goes up with the
- * probability of its place between them, in steps of 2^-17 (2^-16), and a sqrt(v) > 0 never to 0.  NaN and
- * infinite values get a NaN code.  sqrt(v / bias correction) + eps is at least 2^-126 in the update.
+ * probability of its place between them, in steps of 2^-17 (2^-16), and a sqrt(v) > 0 never to 0.  NaN,
+ * infinite values and those beyond 448 (480) times 2^120 get a NaN code.  sqrt(v / bias correction) + eps is at least 2^-126 in the update.
  * Rounded to nearest, v could not follow a beta2 near 1: 0.1 % of it a step is far below half the
  * distance of two codes.
  * The random numbers are a hash of `seed`, `step` and the value's place in its tensor: the same call gives

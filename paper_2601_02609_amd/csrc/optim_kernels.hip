@@ -276,10 +276,11 @@ __device__ __forceinline__ uint32_t half_max(uint32_t x) {
 
 // What four values of a block need to become codes: the high words of their magnitudes, and the block's exponent
 // e = ceil(log2(amax / top)), top = 1.75 * 2^8 or 1.875 * 2^8, of the largest finite magnitude.  High words decide it, but
-// where the largest one is top's own: then whether a low word is not 0.
+// where the largest one is top's own: then whether a low word is not 0.  fits: no value is NaN, infinite or beyond the largest
+// scale.
 constexpr uint32_t kNotFinite = 0x7ff00000u;
 template <int BITS>
-__device__ __forceinline__ int scale_exponent(const double (&x)[4], uint32_t (&word)[4], bool& finite) {
+__device__ __forceinline__ int scale_exponent(const double (&x)[4], uint32_t (&word)[4], bool& fits) {
     constexpr uint32_t border = BITS == 3 ? 0xc0000u : 0xe0000u;
     uint32_t top = 0u;
 #pragma unroll
@@ -287,8 +288,8 @@ __device__ __forceinline__ int scale_exponent(const double (&x)[4], uint32_t (&w
         word[i] = BITS == 3 ? high_word(x[i]) & 0x7fffffffu : high_word(x[i]);
         top = word[i] > top ? word[i] : top;
     }
-    finite = top < kNotFinite;
-    if (!finite) {
+    fits = top < kNotFinite;
+    if (!fits) {
         top = 0u;
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = word[i] < kNotFinite && word[i] > top ? word[i] : top;
@@ -302,12 +303,13 @@ __device__ __forceinline__ int scale_exponent(const double (&x)[4], uint32_t (&w
     top = half_max(top);
     if (top == 0u) return 0;
     const int e = (int)(top >> 20) - 1023 - 8 + ((top & 0xfffffu) > border ? 1 : 0);
+    fits = fits && e <= 120;
     return e < -100 ? -100 : (e > 120 ? 120 : e);
 }
 
 // The code of x 2^-e, rounded down after `dither` steps of 2^-(20 - BITS) of a code's step.  Scaled by 2^-1016 more, what the
 // formats' bias of 7 has as exponent field is fp64's own: its high word has the code's bits in front of those that the
-// dither meets, and subnormal codes are subnormal numbers.  `word`: of |x|, not NaN or infinite.
+// dither meets, and subnormal codes are subnormal numbers.  `word`: of |x|; nothing is said of an x that no scale fits.
 template <int BITS>
 __device__ __forceinline__ uint32_t encode8(double x, uint32_t word, int e, uint32_t dither) {
     const uint32_t y = high_word(ldexp(x, -1016 - e)) + dither;
@@ -368,8 +370,8 @@ __global__ __launch_bounds__(256) void adamw_multi8_kernel(const StepArgs8 a) {
         p[e] = fmaf(-rate * (float)m[e], __builtin_amdgcn_rcpf(under), p[e] * t.decay);
     }
     uint32_t mw[4], rw[4], cm[4], cr[4];
-    bool m_finite, r_finite;
-    const int em = scale_exponent<3>(m, mw, m_finite), er = scale_exponent<4>(r, rw, r_finite);
+    bool m_fits, r_fits;
+    const int em = scale_exponent<3>(m, mw, m_fits), er = scale_exponent<4>(r, rw, r_fits);
     const uint32_t key = (uint32_t)at + (uint32_t)((uint64_t)at >> 32) * 32310901u + a.key;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -377,11 +379,11 @@ __global__ __launch_bounds__(256) void adamw_multi8_kernel(const StepArgs8 a) {
         cm[e] = encode8<3>(m[e], mw[e], em, h >> 15);
         cr[e] = encode8<4>(r[e], rw[e], er, h & 0xffffu);
     }
-    if (!m_finite || !r_finite) {
+    if (!m_fits || !r_fits) {                                                            // fp32 has no value beyond 2^128 either
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            cm[e] = mw[e] >= kNotFinite ? 0x7fu : cm[e];
-            cr[e] = rw[e] >= kNotFinite ? 0xffu : cr[e];
+            cm[e] = fabs(m[e]) <= 0x1.cp128 ? cm[e] : 0x7fu;
+            cr[e] = r[e] <= 0x1.ep128 ? cr[e] : 0xffu;
         }
     }
     if (left <= 0) return;

@@ -335,3 +335,28 @@ def test_replaced_gradients_stay_until_the_stream_has_read_them(B):
     junk = [torch.full((n,), 9.0, device="cuda") for _ in range(4)]
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(want, got)) and len(junk) == 4
+
+
+@pytest.mark.parametrize("bf16", [0, 1])
+def test_state8_values_beyond_the_largest_scale(B, bf16):
+    """A coefficient above 1 and gradients near fp32's end: values that no scale holds get a NaN code and leave the others of
+    their block, the next ones' bytes above all, what they are."""
+    n = 700
+    T = _Tensors(B, [n], [1], [bf16], seed=19)
+    g = T.g[0].copy()
+    g[[5, 130, 131, 132, 133, 511]] = np.float32(2.0 ** 127) * np.float32(1.5)
+    g[600] = np.float32(-2.0 ** 127)
+    T.g[0] = g
+    T.gd[0].copy_(torch.from_numpy(g))
+    clip = 1000.0
+    before = T.host(0)
+    B.cce_adamw_multi_step(T.list, 1, lr=1e-3, clip_coef=torch.tensor([clip], device="cuda"), seed=5)
+    p1, m1, ms1, v1, vs1 = T.host(0)
+    _, state, _, _ = S.step(before[0], g, (before[1], before[2], before[3], before[4]), 1, 5, 1e-3, float(np.float32(0.9)),
+                            float(np.float32(0.999)), float(np.float32(1e-8)), 0.1, clip=clip)
+    big = np.abs(g) >= 2.0 ** 127
+    m, r = S.decode(m1, ms1, S.M), S.decode(v1, vs1, S.R)
+    assert np.array_equal(ms1, state[1]) and np.array_equal(vs1, state[3]) and (ms1[[0, 1, 3, 4]] == 247).all()
+    assert np.array_equal(np.isnan(m), big) and np.array_equal(np.isnan(r), big)
+    assert np.array_equal(m1[~big], state[0][~big]) and np.array_equal(v1[~big], state[2][~big])
+    assert np.isfinite(p1[~big]).all() and T.intact()
