@@ -81,7 +81,7 @@ int cce_adamw_multi_step(const cce_optim_tensor* tensors, int64_t count, float l
                          float eps, int64_t step, const float* clip_coef, uint32_t seed, void* stream);
 
 /*
- * What 8-bit moments stand for, in fp32 (a checkpoint, an inspection).
+ * What 8-bit moments stand for, in fp32 (a checkpoint, an inspection).  n >= 1.
  *   codes   in  uint8 [n]               8-byte aligned
  *   scales  in  uint8 [ceil(n / 128)]
  *   second  0: the first moment; 1: the second moment (the squares)

@@ -1235,6 +1235,8 @@ def cce_adamw_state8_read(codes: torch.Tensor, scales: torch.Tensor, *, second: 
         out = _new(codes.shape, torch.float32, device, stream)
     else:
         _check_on(device, out, torch.float32, codes.shape, "out")
+    if n == 0:
+        return out
     _call("cce_adamw_state8_read", lib().cce_adamw_state8_read, device, stream, codes.data_ptr(), scales.data_ptr(), n,
           1 if second else 0, out.data_ptr())
     return out

@@ -360,3 +360,16 @@ def test_state8_values_beyond_the_largest_scale(B, bf16):
     assert np.array_equal(np.isnan(m), big) and np.array_equal(np.isnan(r), big)
     assert np.array_equal(m1[~big], state[0][~big]) and np.array_equal(v1[~big], state[2][~big])
     assert np.isfinite(p1[~big]).all() and T.intact()
+
+
+def test_state8_read_of_an_empty_tensor(B):
+    """A list takes tensors without values: their moments are read back like the others'."""
+    z = lambda *shape, dtype=torch.uint8: torch.zeros(*shape, dtype=dtype, device="cuda")
+    for shape in ((0,), (3, 0)):
+        for second in (False, True):
+            out = B.cce_adamw_state8_read(z(*shape), z(0), second=second)
+            assert out.shape == shape and out.dtype == torch.float32 and out.is_cuda
+    given = z(0, dtype=torch.float32)
+    assert B.cce_adamw_state8_read(z(0), z(0), out=given) is given
+    with pytest.raises(ValueError):
+        B.cce_adamw_state8_read(z(0), z(1))
