@@ -373,3 +373,22 @@ def test_state8_read_of_an_empty_tensor(B):
     assert B.cce_adamw_state8_read(z(0), z(0), out=given) is given
     with pytest.raises(ValueError):
         B.cce_adamw_state8_read(z(0), z(1))
+
+
+@pytest.mark.parametrize("what", ["grads", "params", "m", "v", "params_bf16"])
+def test_a_tensor_that_is_not_aligned_is_named(B, what):
+    """A view into a bucket that does not begin at 16 bytes is refused when the list is used, by its name."""
+    f = lambda dtype=torch.float32: [torch.zeros(n, dtype=dtype, device="cuda") for n in (300, 9, 17)]
+    a = dict(grads=f(), params=f(), m=f(), v=f(), params_bf16=f(torch.bfloat16))
+    a[what][1] = a[what][1].new_zeros(24)[3:12]
+    T = B.OptimTensors(a["grads"], a["params"], a["m"], a["v"], params_bf16=a["params_bf16"])
+    with pytest.raises(B.CCEError, match=rf"{what}\[1\]") as refused:
+        B.cce_adamw_multi_step(T, 1, lr=1e-3)
+    assert refused.value.code == -1 and not any(bool(x.any()) for x in a["params"])
+    if what == "grads":
+        with pytest.raises(B.CCEError, match=r"grads\[1\]"):
+            B.cce_grad_sumsq_multi(T)
+    else:
+        assert float(B.cce_grad_sumsq_multi(T)[0]) == 0.0                   # which reads the gradients alone
+    with pytest.raises(B.CCEError, match="multi_step: "):                   # another reason: no tensor is named
+        B.cce_adamw_multi_step(B.OptimTensors(f(), f(), f(), f()), 0, lr=1e-3)
