@@ -241,3 +241,103 @@ def test_binding_refuses(B):
         B.cce_embedding_forward(t, torch.zeros(10, 12, dtype=torch.bfloat16, device="cuda"))
     with pytest.raises(B.CCEError):
         B.cce_embedding_backward(t[:0], dy[:0], 10)
+
+
+# ------------------------------------------------------------------ sizes from which other variants run
+def _whole_tokens(N, V, hot, seed, rows=None):
+    """Tokens of `rows` (all of them, if not given), both ends of the matrix among them; one of them has a share `hot` of the positions."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    rows = torch.arange(V, device="cuda", dtype=torch.int32) if rows is None else rows
+    t = rows[torch.randint(0, len(rows), (N,), device="cuda", generator=gen)]
+    t[torch.rand(N, device="cuda", generator=gen) < hot] = rows[len(rows) // 2]
+    t[torch.rand(N, device="cuda", generator=gen) < 0.1] = IGN
+    for i, at in enumerate((0, N // 2, N - 1)[:N]):
+        t[at] = (0, V - 1, 0)[i]
+    return t
+
+
+def _exact_gradient(B, N, D, V, accumulate, t, seed=0):
+    """Whole numbers, whose sums fp32 holds: the bits of the sum in 64 bits.  NaN in rows that take no part."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    dy = torch.randint(-4, 5, (N, D), device="cuda", generator=gen).bfloat16()
+    ok = t != IGN
+    assert int(torch.bincount(t[ok].long()).max()) * 4 < 2 ** 22
+    want = torch.zeros(V, D, dtype=torch.float64, device="cuda").index_add_(0, t[ok].long(), dy[ok].double())
+    want = (2.0 * want + (3.0 if accumulate else 0.0)).float()
+    dy[~ok] = float("nan")
+    dw, intact = _guarded((V, D), torch.float32)
+    dw.fill_(3.0 if accumulate else float("nan"))
+    print(f"[gradient] N={N} D={D} V={V} accumulate={accumulate}", flush=True)
+    need = B.embedding_workspace_bytes(N, D, V)
+    ws = torch.full((need + 4096,), 171, dtype=torch.uint8, device="cuda")
+    B.cce_embedding_backward(t, dy, V, IGN, scale=2.0, d_weight=dw, accumulate_dw=accumulate, workspace=ws[:need])
+    assert torch.equal(dw, want) and intact() and bool((ws[need:] == 171).all())
+
+
+@pytest.mark.parametrize("N,D,V", [(12287, 8192, 500), (12288, 8192, 500), (97601, 1032, 3000), (12_582_917, 8, 70)])
+def test_lookup_of_outputs_that_the_caches_do_not_hold(B, N, D, V):
+    """192 MiB of y and more, and one row less: the rounded products, bit for bit."""
+    assert (N * D * 2 >= 192 << 20) == (N != 12287)
+    t = _whole_tokens(N, V, 0.2, N)
+    w = (torch.randn(V, D, device="cuda") * 0.3).bfloat16()
+    out, intact = _guarded((N, D), torch.bfloat16)
+    print(f"[lookup] N={N} D={D} V={V}", flush=True)
+    B.cce_embedding_forward(t, w, IGN, scale=-1.7, out=out)
+    want = (w.float() * float(np.float32(-1.7))).bfloat16()[t.clamp(min=0).long()]
+    want[t == IGN] = 0
+    assert torch.equal(out.view(torch.int16), want.view(torch.int16)) and intact()
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("N,D,V", [(16400, 4104, 40), (16352, 4104, 40), (3000, 4104, 16400), (17000, 4096, 17000), (600_001, 120, 560_000)])
+def test_gradient_of_what_the_caches_do_not_hold(B, N, D, V, accumulate):
+    """128 MiB of dy (and a little less), 256 MiB of dW, both; a third of the rows get zeros."""
+    t = _whole_tokens(N, V, 0.3, N + D, torch.arange(V, device="cuda", dtype=torch.int32)[torch.arange(V, device="cuda") % 3 != 1])
+    _exact_gradient(B, N, D, V, accumulate, t)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("V", [1, 255, 256, 257, 163839, 163840, 163841, 327680, 327681])
+def test_gradient_at_the_borders_of_the_slices(B, V, accumulate):
+    """640 rows of the matrix are a slice's most: in one launch and in three, both ends of the matrix named."""
+    for N in (700, 2100, 9000):
+        _exact_gradient(B, N, 16, V, accumulate, _whole_tokens(N, V, 0.2, N + V))
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("N,D", [(1024, 64), (1025, 64), (1024, 1024), (682, 1032), (683, 1032), (1024, 2048), (1024, 2056), (16, 65536), (33, 65536)])
+def test_gradient_where_one_launch_ends(B, N, D, accumulate):
+    for hot in (0.0, 1.0):
+        _exact_gradient(B, N, D, 300, accumulate, _whole_tokens(N, 300, hot, N + D))
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_three_launches_beyond_32_bit_offsets_of_dw(B, accumulate):
+    """2.2 G values of dW with 3000 tokens: what is written, and that nothing else is."""
+    N, D, V = 3000, 8192, 270000
+    rows = torch.cat([torch.arange(600), torch.arange(V - 600, V), torch.arange(262100, 262200)]).cuda().int()
+    t = _whole_tokens(N, V, 0.1, 9, rows)
+    dy = torch.randint(-4, 5, (N, D), device="cuda").bfloat16()
+    ok, fill = t != IGN, 3.0 if accumulate else 0.0
+    named, at = torch.unique(t[ok].long(), return_inverse=True)
+    want = torch.zeros(len(named), D, dtype=torch.float64, device="cuda").index_add_(0, at, dy[ok].double()).float() + fill
+    dw = torch.full((V, D), 3.0, device="cuda")
+    B.cce_embedding_backward(t, dy, V, IGN, d_weight=dw, accumulate_dw=accumulate)
+    assert torch.equal(dw[named], want)
+    dw[named] = fill
+    assert bool((dw == fill).all())
+
+
+def test_rows_beyond_32_bit_offsets_of_y(B):
+    """2.2 G values of y and of dy: the lookup's rows, and their gradient, which is a row's count times itself."""
+    N, D, V = 270000, 8192, 50
+    t = _whole_tokens(N, V, 0.3, 10)
+    w = torch.randint(-3, 4, (V, D), device="cuda").bfloat16()
+    y = B.cce_embedding_forward(t, w, IGN)
+    for first in range(0, N, 30000):
+        part = slice(first, first + 30000)
+        want = w[t[part].clamp(min=0).long()]
+        want[t[part] == IGN] = 0
+        assert torch.equal(y[part], want), first
+    dw = B.cce_embedding_backward(t, y, V, IGN)
+    assert torch.equal(dw, torch.bincount(t[t != IGN].long(), minlength=V)[:, None] * w.float())

@@ -392,3 +392,63 @@ def test_a_tensor_that_is_not_aligned_is_named(B, what):
         assert float(B.cce_grad_sumsq_multi(T)[0]) == 0.0                   # which reads the gradients alone
     with pytest.raises(B.CCEError, match="multi_step: "):                   # another reason: no tensor is named
         B.cce_adamw_multi_step(B.OptimTensors(f(), f(), f(), f()), 0, lr=1e-3)
+
+
+@pytest.mark.parametrize("state8", [0, 1])
+@pytest.mark.parametrize("bf16", [0, 1])
+def test_step_with_copies_that_the_caches_do_not_hold(B, state8, bf16):
+    """192 MiB of bf16 copies and more: two steps, the second one from nonzero moments, checked at both ends of each tensor and
+    in the middle as the steps of small tensors are; the copies, and in the first step the parameters, everywhere."""
+    sizes = [100_650_003, 7001, 130, 8000]
+    assert 2 * sum(sizes) >= 192 << 20
+    hp, seed, clip = dict(lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8), 31, 0.37
+    gen = torch.Generator(device="cuda").manual_seed(20)
+    rand = lambda n, std: torch.randn(n, device="cuda", generator=gen).mul_(std)
+    kind = torch.uint8 if state8 else torch.float32
+    z = lambda of, dtype: [torch.zeros(of(n), dtype=dtype, device="cuda") for n in sizes]
+    same, blocks = (lambda n: n), (lambda n: (n + 127) // 128)
+    p, pb, m, v = [rand(n, 0.1) for n in sizes], z(same, torch.bfloat16), z(same, kind), z(same, kind)
+    ms, vs = (z(blocks, torch.uint8), z(blocks, torch.uint8)) if state8 else (None, None)
+    new_grads = lambda: [rand(n, 1e-3).to(torch.bfloat16 if bf16 else torch.float32) for n in sizes]
+    g = new_grads()
+    T = B.OptimTensors(g, p, m, v, params_bf16=pb, m_scales=ms, v_scales=vs, weight_decay=0.1)
+    f32 = lambda x: float(np.float32(x))
+    b1, b2, eps, lr, wd, clip = f32(hp["beta1"]), f32(hp["beta2"]), f32(hp["eps"]), f32(hp["lr"]), f32(0.1), f32(clip)
+    parts = []
+    for i, n in enumerate(sizes):
+        for first in {0, n // 2 // 128 * 128, max(0, n - 1500) // 128 * 128}:
+            parts.append((i, first, min(n, first + 2048)))                  # whole blocks, whose largest value fixes their scale
+    host = lambda x, a, b: x[a:b].float().cpu().numpy() if x.dtype == torch.bfloat16 else x[a:b].cpu().numpy()
+    cut = lambda i, a, b: ([host(x[i], a, b) for x in (p, m, v)], [host(x[i], a // 128, (b + 127) // 128) for x in (ms, vs)] if state8 else None)
+    for step in (1, 2):
+        before = [cut(*part) for part in parts]
+        whole0 = p[0].clone()
+        print(f"[adamw multi] state8={state8} bf16={bf16} step {step}", flush=True)
+        B.cce_adamw_multi_step(T, step, clip_coef=torch.tensor([clip], device="cuda"), seed=seed, **hp)
+        for (i, a, b), ((p0, m0, v0), scales0) in zip(parts, before):
+            (p1, m1, v1), scales1 = cut(i, a, b)
+            gp = host(g[i], a, b)
+            if state8:
+                want_p, _, want_m, want_v = S.step(p0, gp, (m0, scales0[0], v0, scales0[1]), step, seed, lr, b1, b2, eps, wd, clip=clip)
+                um, ur = S.dither(b - a, seed, step, first=a)
+                for got, got_s, want in ((m1, scales1[0], S.encode(want_m, um, S.M)), (v1, scales1[1], S.encode(np.sqrt(want_v), ur, S.R))):
+                    assert np.array_equal(got[:b - a], want[0]) and np.array_equal(got_s, want[1]), (i, a)
+                em = U * np.abs(want_m)
+            else:
+                want_p, want_m, want_v = A.adamw_step(p0, gp, m0, v0, step, lr, b1, b2, eps, wd, clip=clip)
+                em = 4 * U * (np.abs(b1 * m0) + np.abs((1 - b1) * clip * gp.astype(np.float64)))
+                assert np.all(np.abs(m1 - want_m) <= em + 1e-45) and np.all(np.abs(v1 - want_v) <= 6 * U * want_v + 1e-45), (i, a)
+            den = np.sqrt(want_v / (1 - b2 ** step)) + eps
+            update = lr * (want_m / (1 - b1 ** step)) / den
+            tol = 3 * U * (np.abs(p0) + np.abs(want_p)) + 12 * U * np.abs(update) + lr * em / (1 - b1 ** step) / den
+            assert np.all(np.abs(p1 - want_p) <= tol), (i, a)
+        assert all(torch.equal(x.view(torch.int16), y.bfloat16().view(torch.int16)) for x, y in zip(pb, p))
+        if step == 1:                                                       # from zero moments: the update is lr g / (|g| + eps)
+            gd = g[0].double() * clip
+            update = lr * gd / (gd.abs() + eps)
+            want = whole0.double() * (1.0 - lr * wd) - update
+            over = (p[0].double() - want).abs() - 3 * U * (whole0.double().abs() + want.abs()) - 16 * U * update.abs()
+            assert float(over.max()) <= 0.0
+            del gd, update, want, over
+        g = new_grads()
+        T.set_grads(g)
