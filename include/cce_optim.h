@@ -52,7 +52,8 @@ size_t cce_sumsq_multi_workspace_bytes(int64_t count);
  *              gradient is not; the coefficient of a NaN is 1, as cce_clip_coef's)
  *   clip_coef  out fp32 [1] device, may be NULL: min(1, max_norm / (sqrt(sumsq) + eps_norm)) of the new
  *              sumsq; max_norm > 0 and eps_norm >= 0 are looked at only then
- *   workspace  at least cce_sumsq_multi_workspace_bytes(count) bytes, 256-byte aligned
+ *   workspace  at least cce_sumsq_multi_workspace_bytes(count) bytes, 256-byte aligned; calls that may
+ *              run at the same time need one each
  * Squares and sums in fp64, in an order that the sizes alone decide.
  */
 int cce_grad_sumsq_multi(const cce_optim_tensor* tensors, int64_t count, double* sumsq, int accumulate,

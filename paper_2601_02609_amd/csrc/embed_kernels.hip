@@ -86,7 +86,7 @@ constexpr int kKeyBits = 10;
 static_assert(kSliceKeys <= 1 << kKeyBits, "bits of a key");
 constexpr int kOrderWaves = 16;
 constexpr int kOrderLoads = 8;                  // loads of tokens in flight, and as many ahead
-constexpr int kFound = 1024;                    // positions that a wavefront notes: 32 KB of LDS (two workgroups fit a CU)
+constexpr int kFound = 1024;                    // positions that a wavefront notes: 32 KB of LDS
 constexpr int kSmallTokens = 1024;              // one launch takes: a thread each
 constexpr int kSmallRows = 2048, kSmallRowsAdd = 4096;    // and rows of strips, which one workgroup may have all of
 constexpr int kSmallShare = 16;                 // rows of a key that one wavefront adds up
@@ -97,8 +97,9 @@ constexpr int kJoinShort = 16;                  // pieces of a group that one wa
 constexpr int64_t kSumWaves = 4096, kSumWavesAdd = 8192;
 constexpr int64_t kMaxPieces = 4096;            // more make the join of a frequent token's partial rows long
 constexpr int64_t kStreamBytes = (int64_t)128 << 20;      // half of the last-level cache
-// A dW of this size or more gets its zeros past the caches: 500 MiB with 16384 x 4096 rows 149 -> 133 us; smaller ones what reads
-// dW next finds there: the sum of squares of 219 MiB with the gradient in front of it 85 against 102 us.
+// A dW of this size or more gets its zeros past the caches in the three launches: 500 MiB with 16384 x 4096 rows 149 -> 133 us;
+// smaller ones what reads dW next finds there: the sum of squares of 219 MiB with the gradient in front of it 85 against 102 us.
+// The one launch for few tokens writes all zeros through the caches.
 constexpr int64_t kStreamZeros = (int64_t)256 << 20;
 
 // Slices of the vocabulary: token t is key t / slices of slice t % slices (a power of two).  The frequent tokens, which
@@ -142,8 +143,11 @@ __device__ __forceinline__ unsigned long long lanes_of_key(unsigned long long am
 // A workgroup per slice looks through all tokens (which stay in the L2s): its wavefronts, each with a range of positions,
 // count their keys in LDS and note what they found there; after a scan over keys and wavefronts they give the positions
 // of one key consecutive places.  64 tokens that none is in the slice of cost a handful of instructions, most of them
-// scalar: all slices together do that 256 N / 64 times, which is what bounds the kernel, and above 32768 tokens the slice of
+// scalar: all slices together do that slices * N / 64 times, which is what bounds the kernel, and above 32768 tokens the slice of
 // the most frequent one: 7.7 us for 8192 tokens under Zipf's law, 16 for 32768, 25 for 65536 (16 if all are as frequent).
+// That is for 256 slices, up to 163840 rows of the matrix.  A CU's registers (65 a thread here) hold one workgroup, so that 512
+// slices take two rounds: the whole call with rows of 256 values added to dW takes 19.2, 33.6 and 50.0 us for 8192, 32768 and
+// 65536 tokens of 163840 rows, and 22.5, 40.0 and 60.8 us of 163841 (262144: 23.4, 41.4, 61.5).
 __global__ __launch_bounds__(64 * kOrderWaves) void embedding_order_kernel(const EmbedBackward a) {
     __shared__ uint32_t count[kOrderWaves * kSliceKeys];
     __shared__ uint16_t found[kOrderWaves][kFound];          // places in the wavefront's range
@@ -292,6 +296,9 @@ __device__ __forceinline__ int of_lane(int x, int j) {
 // the rows of dW that they end at, are in flight.
 // STREAM: d_out of kStreamBytes or more, read past the caches, which keep more of dW then: 140 -> 123 us for 32768 x 3584 added to
 // dW, 93 -> 85 for 32768 x 2048 (128 MiB); below, rows that the launch before left there are worth more (16384 x 2048 45 -> 50).
+// Only where a wavefront has a row: narrower ones lose 1 to 4 % (262144 x 256 179 -> 185, 524288 x 128 318 -> 323, 1048576 x 64
+// 621 -> 630, into a new dW 603 -> 617).
+// 137 registers (147 with fewer lanes a row), three wavefronts a SIMD: what is in flight fills them.
 template <int LPR, bool STREAM>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbedBackward a, int sum_blocks) {
     const int slices = 1 << a.bits;
@@ -479,9 +486,13 @@ __global__ __launch_bounds__(64 * WAVES) void embedding_join_kernel(const EmbedB
 // Few tokens: one launch.  A workgroup per slice finds its positions among all N <= kSmallTokens in order, then a wavefront
 // sums a key's rows (a strip of 512 columns of them) by itself, or all of them share the rows of a key that has many.
 // Bound by latency, launches above all.  Against the three launches: 257 x 64 into a new dW 13.1 -> 4.9 us; added to dW, 512 x 896
-// 15.9 -> 6.1, 1024 x 896 16.9 -> 7.5, 1024 x 2048 17.6 -> 10.5, 512 x 3584 19.1 -> 9.8.  kSmallRows bounds what one workgroup may
-// have to sum if all tokens are the same: 14.5 -> 24.4 us for 1024 x 896 then, 15.0 -> 46.9 for 1024 x 2048.  A new dW has its
-// zeros written beside the rows' sums by the three launches: 1024 x 2048 into 32000 rows 61 us against 71 in one.
+// 15.9 -> 6.1, 1024 x 896 16.9 -> 7.5, 1024 x 2048 17.6 -> 10.5, 512 x 3584 19.1 -> 9.8.  kSmallRowsAdd bounds what one workgroup
+// may have to sum if all tokens are the same, which no rule on sizes can see and where the one launch loses: added to dW, 1024 x 896
+// 15.0 -> 25.2 us then, 1024 x 2048 15.2 -> 46.2, 512 x 3584 13.7 -> 40.2.
+// Into a new dW the launches saved count for as much with large matrices, whose zeros are the time: 512 x 2048 into 151936 rows
+// 238 -> 218 us, 1 x 896 into as many 108 -> 93, 256 x 4096 into 32000 105 -> 89, 1024 x 1024 into 32000 31 -> 21.  kSmallRows is where
+// a frequent token's workgroup begins to outlast the others' zeros: 1024 x 2048 into 32000 rows would take 53.2 us against 45.8
+// under Zipf's law (uniform tokens 38.3 against 44.5); if all tokens are the same, 1024 x 896 takes 37.8 against 27.0.
 // ------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(64 * kOrderWaves) void embedding_small_kernel(const EmbedBackward a) {
     __shared__ uint32_t mine[kSmallTokens];                  // this slice's positions, ascending, and their keys in the upper 16 bits

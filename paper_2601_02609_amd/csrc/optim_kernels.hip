@@ -100,7 +100,7 @@ __device__ __forceinline__ ou32x2 pack4(const af32x4& x) {
     return cv.u;
 }
 
-// Copies that the last-level cache cannot keep for the forward pass are written past it: AdamW of 411 M values 2188 -> 2083 us.
+// Copies that the last-level cache cannot keep for the forward pass are written past it: AdamW of 416 M values 2188 -> 2083 us.
 constexpr int64_t kStreamCopies = (int64_t)192 << 20;
 template <bool STREAM>
 __device__ __forceinline__ void store_copy(uint16_t* to, int q, const ou32x2& copy) {
@@ -110,7 +110,7 @@ __device__ __forceinline__ void store_copy(uint16_t* to, int q, const ou32x2& co
 // ------------------------------------------------------------------------------------------
 // Sum of squares of all gradients.  Squares of fp32 values are exact in fp64, whose sums leave nothing
 // to argue about.  Workgroups walk the chunks of all tensors with a grid stride, a chunk's loads in flight
-// together.  Bound by HBM reads: 411 M values, half of them bf16, in 232 us, 5.95 TB/s; chunks of 8192 values
+// together.  Bound by HBM reads: 416 M values, a third of them bf16, in 232 us, 5.95 TB/s; chunks of 8192 values
 // 282 us, of 2048 287; 1024 workgroups 265.
 // ------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void norm_partial_kernel(const NormArgs a) {
@@ -195,7 +195,7 @@ __device__ __forceinline__ void adamw_one(float& p, float g, float& m, float& v,
     p = p * decay - lr * ((m * a.inv_bc1) / (sqrtf(v * a.inv_bc2) + a.eps));
 }
 
-// Every value is touched once: streaming accesses of 16 bytes, one group of a tensor a thread.  Bound by HBM: 411 M values
+// Every value is touched once: streaming accesses of 16 bytes, one group of a tensor a thread.  Bound by HBM: 416 M values
 // (12.2 GB) in 2071 us, 5.88 TB/s where a copy of 1 GiB reaches 5.15.  Two groups a thread took 2.6 % longer, four 1.3 %; 32 bytes of a thread in a row 3.5 %.
 template <bool STREAM>
 __global__ __launch_bounds__(256) void adamw_multi_kernel(const StepArgs32 a) {
@@ -256,8 +256,8 @@ __device__ __forceinline__ double power_of_two(int e) { return __longlong_as_dou
 
 __device__ __forceinline__ uint32_t high_word(double x) { return (uint32_t)((uint64_t)__double_as_longlong(x) >> 32); }
 
-// sqrt of x >= 0 from the hardware's reciprocal root (2^-27 or so) and one correction of it: good to some 2^-52.
-// Infinite x gives NaN, as its code is.
+// sqrt of x >= 0 from the hardware's reciprocal root and one correction of it: a reciprocal root off by d leaves 1.5 d^2, always
+// downward; 2^-47.7 at worst over 65 M values (d some 2^-24).  Infinite x gives NaN, as its code is.
 __device__ __forceinline__ double root(double x) {
     const double y = __builtin_amdgcn_rsq(fmax(x, 1e-290)), s = x * y;
     return fma(0.5 * s, fma(-s, y, 1.0), s);
@@ -320,7 +320,7 @@ __device__ __forceinline__ uint32_t encode8(double x, uint32_t word, int e, uint
 
 // 32 lanes share a block of 128 values, four each.  The moments are formed in fp64, so that which way a value next to a
 // border goes does not depend on the order or the fusing of the operations.  The update takes sqrt(v / bc2) from the root
-// that is stored, and reciprocals to one unit in the last place.  Bound by HBM and by its arithmetic nearly as much: 411 M
+// that is stored, and reciprocals to one unit in the last place.  Bound by HBM and by its arithmetic nearly as much: 416 M
 // values (6.7 GB) in 1130 us, 5.9 TB/s.
 template <bool STREAM>
 __global__ __launch_bounds__(256) void adamw_multi8_kernel(const StepArgs8 a) {
@@ -410,7 +410,7 @@ __global__ __launch_bounds__(256) void adamw_multi8_kernel(const StepArgs8 a) {
     }
 }
 
-// Four values a thread, two groups of them 1024 values apart.  Bound by HBM, mostly writes: 411 M values (2.1 GB) in 330 us.
+// Four values a thread, two groups of them 1024 values apart.  Bound by HBM, mostly writes: 416 M values (2.1 GB) in 330 us.
 template <int BITS>
 __global__ __launch_bounds__(256) void state8_read_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                           int64_t n, float* __restrict__ out) {
