@@ -1145,9 +1145,9 @@ class OptimTensors:
             for g in grads:
                 g.record_stream(stream)
 
-    def _read_on(self, stream: Optional[torch.cuda.Stream]):
+    def _read_on(self, stream: torch.cuda.Stream):
         """A call on a stream of the caller's has been made."""
-        if stream is None or stream.cuda_stream in self._streams:
+        if stream.cuda_stream in self._streams:
             return
         self._streams[stream.cuda_stream] = stream
         for tensors in self._keep.values():
@@ -1161,13 +1161,13 @@ class OptimTensors:
             raise ValueError(f"grads: expected {len(self)} tensors, got {len(grads)}")
         self._take_grads(list(grads), self._table["n"].tolist())
 
-    def _misaligned(self, fields) -> str:
-        """The first tensor among these that the library refuses for where it begins, or nothing."""
+    def _refused(self, error: CCEError, where: str, fields) -> CCEError:
+        """The error of a call that reads these columns, with the first tensor's name that does not begin where the library wants it."""
         for field, name in fields.items():
             at = np.flatnonzero((self._table["n"] != 0) & (self._table[field] % 16 != 0))
-            if len(at):
-                return f", {name}[{at[0]}] does not begin at a multiple of 16 bytes"
-        return ""
+            if error.code == CCE_ERR_INVALID and len(at):
+                return CCEError(error.code, f"{where}, {name}[{at[0]}] does not begin at a multiple of 16 bytes")
+        return error
 
     def _check_overlap(self):
         t, n = self._table, self._table["n"]
@@ -1185,17 +1185,6 @@ class OptimTensors:
         if over.any():
             at = int(order[1 + int(np.argmax(over))])
             raise ValueError(f"{columns[at // len(n)][1]}[{at % len(n)}] overlaps another tensor of the list")
-
-
-def _list_call(where: str, fn, tensors: OptimTensors, fields, stream: Optional[torch.cuda.Stream], *args) -> None:
-    """_call with the list in front of the arguments; `fields`: the columns that it reads."""
-    try:
-        _call(where, fn, tensors.device, stream, tensors._address, len(tensors), *args)
-    except CCEError as refused:
-        if refused.code != CCE_ERR_INVALID:
-            raise
-        raise CCEError(refused.code, where + tensors._misaligned(fields)) from None
-    tensors._read_on(stream)
 
 
 def cce_grad_sumsq_multi(tensors: OptimTensors, sumsq: Optional[torch.Tensor] = None, accumulate: bool = False, *,
@@ -1222,9 +1211,14 @@ def cce_grad_sumsq_multi(tensors: OptimTensors, sumsq: Optional[torch.Tensor] = 
         workspace = _new((int(lib().cce_sumsq_multi_workspace_bytes(len(tensors))),), torch.uint8, device, stream)
     else:
         _check_on(device, workspace, torch.uint8, (workspace.numel(),), "workspace")
-    _list_call("cce_grad_sumsq_multi", lib().cce_grad_sumsq_multi, tensors, {"grad": "grads"}, stream, sumsq.data_ptr(),
-               1 if accumulate else 0, max_norm if max_norm is not None else 0.0, eps_norm,
-               clip_coef.data_ptr() if clip_coef is not None else None, workspace.data_ptr(), workspace.numel())
+    try:
+        _call("cce_grad_sumsq_multi", lib().cce_grad_sumsq_multi, device, stream, tensors._address, len(tensors), sumsq.data_ptr(),
+              1 if accumulate else 0, max_norm if max_norm is not None else 0.0, eps_norm,
+              clip_coef.data_ptr() if clip_coef is not None else None, workspace.data_ptr(), workspace.numel())
+    except CCEError as error:
+        raise tensors._refused(error, "cce_grad_sumsq_multi", {"grad": "grads"}) from None
+    if stream is not None:
+        tensors._read_on(stream)
     return sumsq, clip_coef
 
 
@@ -1236,9 +1230,14 @@ def cce_adamw_multi_step(tensors: OptimTensors, step: int, *, lr: float, beta1: 
         raise ValueError("tensors: the list has gradients alone")
     if clip_coef is not None:
         _check_on(tensors.device, clip_coef, torch.float32, (1,), "clip_coef")
-    _list_call("cce_adamw_multi_step", lib().cce_adamw_multi_step, tensors,
-               {"grad": "grads", "param": "params", "m": "m", "v": "v", "param_bf16": "params_bf16"}, stream, lr, beta1, beta2,
-               eps, step, clip_coef.data_ptr() if clip_coef is not None else None, seed & 0xFFFFFFFF)
+    try:
+        _call("cce_adamw_multi_step", lib().cce_adamw_multi_step, tensors.device, stream, tensors._address, len(tensors), lr, beta1, beta2,
+              eps, step, clip_coef.data_ptr() if clip_coef is not None else None, seed & 0xFFFFFFFF)
+    except CCEError as error:
+        raise tensors._refused(error, "cce_adamw_multi_step", {"grad": "grads", "param": "params", "m": "m", "v": "v",
+                                                               "param_bf16": "params_bf16"}) from None
+    if stream is not None:
+        tensors._read_on(stream)
 
 
 def cce_adamw_state8_read(codes: torch.Tensor, scales: torch.Tensor, *, second: bool = False,
