@@ -1,0 +1,82 @@
+/*
+ * libcce, optimizer entry points for matrices, for AMD MI355X (gfx950): updates orthogonalised by
+ * Newton-Schulz products (the Muon optimizer), for all matrices of a model in a few launches.  The tensors
+ * that are no matrices (embedding, head, norms) go through include/cce_optim.h.
+ *
+ *   G of m x n, r = min(m, n):   X = G / (|G|_F + eps), transposed where m > n
+ *   each step s:                 A = X X^T,   X = a_s X + (b_s A + c_s A A) X
+ *   result:                      X, transposed back: the singular values of G moved towards 1
+ *
+ * Products take operands of 16 bits (fp16, power-of-two scales) and add in fp32; the diagonals of A and of b A + c A A
+ * and what X loses by its rounding are held beside them, so that the result is within some 2^-9 of the
+ * formula's (2-norm of the difference over that of the result): less than bf16's own rounding adds.
+ *
+ * Conventions are those of cce.h: matrix pointers are DEVICE pointers owned by the caller, dense row-major, aligned
+ * to their elements; `stream` is a hipStream_t as void*; nothing is allocated, freed or synchronised: the
+ * calls consist of kernel launches only, and a stream under HIP graph capture may make them once each has been
+ * made once on the device outside a capture; CCE_OK or a negative CCE_ERR_* code is returned and nothing is
+ * enqueued on an error (CCE_ERR_HIP: as in cce.h).
+ *
+ * `matrices` is a HOST array, read before the call returns and not kept.  count >= 1.  A matrix with rows = 0 or
+ * cols = 0 takes no part and its pointers are not looked at.  CCE_ERR_UNSUPPORTED: rows * cols beyond 2^30, the smaller
+ * side beyond 16384.  The memory of no two entries may overlap, nor the workspace any of it.
+ */
+#ifndef CCE_MUON_H_
+#define CCE_MUON_H_
+
+#include <stddef.h>
+#include <stdint.h>
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+enum { CCE_NS_MAX_STEPS = 16 };
+
+typedef struct cce_matrix {
+    float* param;         /* i/o fp32 [rows, cols]  master parameters */
+    void* out_bf16;       /* out bf16 [rows, cols]  cce_orthogonalize_multi: the result; cce_muon_multi_step: the
+                             rounded copy of param, may be NULL */
+    const void* grad;     /* in  fp32 or bf16 [rows, cols] */
+    float* momentum;      /* i/o fp32 [rows, cols]  zeros before the first step */
+    int64_t rows, cols;
+    float lr_scale;       /* this matrix's learning rate is lr * lr_scale */
+    float weight_decay;
+    int32_t grad_bf16;    /* 0: grad is fp32, 1: bf16 */
+    int32_t reserved;     /* 0 */
+} cce_matrix;
+
+/* Bytes of device workspace both calls need for these matrices (rows and cols are read); at least 256; 0 where a call would
+ * refuse the sizes.  Host only.  A part of the list is worked on at a time: at most about 1 GB, or 1.1 times 8 bytes a value of the
+ * largest matrix. */
+size_t cce_muon_workspace_bytes(const cce_matrix* matrices, int64_t count);
+
+/*
+ * out_bf16 = the orthogonalised grad.  Of `matrices` it reads grad, rows, cols and grad_bf16.
+ *   coefficients  HOST fp32 [steps][3]: a, b, c of each step; 1 <= steps <= CCE_NS_MAX_STEPS.  CCE_ERR_UNSUPPORTED where they
+ *                 let a singular value grow beyond 2.5, or |b| x^2 + |c| x^4 beyond 60 for it: the 16-bit operands' range
+ *   eps           >= 0; with 0 a matrix of zeros gives NaN
+ *   workspace     at least cce_muon_workspace_bytes(matrices, count) bytes, 256-byte aligned; calls that may run at
+ *                 the same time need one each
+ * A matrix that holds a NaN or an infinity gives NaN in all of its values, and in no other matrix.
+ */
+int cce_orthogonalize_multi(const cce_matrix* matrices, int64_t count, const float* coefficients, int32_t steps, float eps,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * One step of momentum, orthogonalisation and update over all matrices:
+ *   g        = clip_coef * grad
+ *   momentum = mu momentum + (1 - mu) g
+ *   G        = mu momentum + (1 - mu) g (nesterov != 0) or momentum
+ *   param    = (1 - lr lr_scale weight_decay) param - lr lr_scale orthogonalised(G);   out_bf16 = its rounded copy
+ *   clip_coef  in fp32 [1] device, may be NULL (= 1);   0 <= mu < 1;   lr, lr_scale, weight_decay >= 0
+ * Everything beside the products in fp32; the orthogonalised G goes into param without being rounded to 16 bits.
+ */
+int cce_muon_multi_step(const cce_matrix* matrices, int64_t count, float lr, float mu, int32_t nesterov,
+                        const float* coefficients, int32_t steps, float eps, const float* clip_coef,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* CCE_MUON_H_ */

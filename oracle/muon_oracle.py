@@ -1,0 +1,64 @@
+"""fp64 CPU oracle for updates orthogonalised by Newton-Schulz products and for the Muon step around them.
+
+TEST INFRASTRUCTURE ONLY: the slow, plain definition the HIP kernels are checked against.  It shares no code with the
+GPU path, imports nothing from the package and is never called from the product path.
+
+    X = G / (|G|_F + eps), transposed where G is taller than wide
+    each step:  A = X X^T,  X = a X + (b A + c A A) X
+
+`orthogonalize` is that in 64 bits.  `orthogonalize_rounded` rounds to 16 bits where the kernels may -- the operands of the
+products, the diagonals of A and of b A + c A A apart, the linear part in two 16-bit values -- and is otherwise the same: how far
+it is from `orthogonalize` is how far the kernels may be, beside the order of their fp32 sums.
+"""
+from __future__ import annotations
+
+import numpy as np
+
+__all__ = ["orthogonalize", "orthogonalize_rounded", "muon_step"]
+
+
+def _steps(coefficients, steps):
+    c = np.asarray(coefficients, dtype=np.float32).astype(np.float64)
+    return np.broadcast_to(c, (steps, 3))
+
+
+def _start(g, eps):
+    g = np.asarray(g, dtype=np.float64)
+    x = g / (np.sqrt((g * g).sum()) + eps)
+    return (x.T, True) if g.shape[0] > g.shape[1] else (x, False)
+
+
+def orthogonalize(g, coefficients, steps, eps):
+    x, tall = _start(g, eps)
+    for a, b, c in _steps(coefficients, steps):
+        gram = x @ x.T
+        x = a * x + (b * gram + c * (gram @ gram)) @ x
+    return x.T if tall else x
+
+
+def _half(x, scale):
+    return (x * scale).astype(np.float16).astype(np.float64) / scale
+
+
+def orthogonalize_rounded(g, coefficients, steps, eps):
+    x, tall = _start(g, eps)
+    for a, b, c in _steps(coefficients, steps):
+        h = _half(x, 2.0 ** 13)
+        linear = h + _half(x - h, 2.0 ** 24)
+        gram = h @ h.T
+        diagonal = gram.diagonal().copy()
+        off = _half(gram - np.diag(diagonal), 2.0 ** 13)
+        square = off @ off
+        m = (b + c * (diagonal[:, None] + diagonal[None, :])) * off + c * square
+        dm = b * diagonal + c * (diagonal ** 2 + square.diagonal())
+        m = _half(m - np.diag(m.diagonal()), 2.0 ** 10)
+        x = (a + dm)[:, None] * linear + m @ h
+    return x.T if tall else x
+
+
+def muon_step(p, g, momentum, coefficients, steps, eps, lr, mu, nesterov, weight_decay, clip=1.0, orthogonal=orthogonalize):
+    """New (param, momentum) in 64 bits; lr is the matrix's own."""
+    g = np.asarray(g, dtype=np.float64) * clip
+    momentum = mu * np.asarray(momentum, dtype=np.float64) + (1.0 - mu) * g
+    u = mu * momentum + (1.0 - mu) * g if nesterov else momentum
+    return (1.0 - lr * weight_decay) * np.asarray(p, dtype=np.float64) - lr * orthogonal(u, coefficients, steps, eps), momentum

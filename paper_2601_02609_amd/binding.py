@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import numpy as np
 import torch
@@ -24,6 +24,10 @@ STATIC_SCRATCH_BYTES = 16 << 20
 CCE_STATUS_BAD_LABEL = 1
 CCE_STATUS_BAD_TOKEN = 4
 STATE8_BLOCK = 128
+NS_MAX_STEPS = 16
+NS_COEFFICIENTS = (3.4445, -4.7750, 2.0315)      # singular values from 1e-3 to 1 come near 1 in five steps
+ROUTER_MAX_EXPERTS = 1024
+ROUTER_MAX_TOP_K = 32
 
 EXPORTED_SYMBOLS = [
     "cce_version", "cce_strerror", "cce_last_hip_error", "cce_workspace_bytes",
@@ -49,6 +53,10 @@ EXPORTED_SYMBOLS = [
     "cce_embedding_forward", "cce_embedding_workspace_bytes", "cce_embedding_backward",
     # include/cce_optim.h
     "cce_sumsq_multi_workspace_bytes", "cce_grad_sumsq_multi", "cce_adamw_multi_step", "cce_adamw_state8_read",
+    # include/cce_muon.h
+    "cce_muon_workspace_bytes", "cce_orthogonalize_multi", "cce_muon_multi_step",
+    # include/cce_router.h
+    "cce_router_workspace_bytes", "cce_router_forward", "cce_router_backward",
 ]
 KERNEL_FAMILIES = ["lse_partial_kernel", "grad_tile_kernel", "grad_gemm_kernel"]
 
@@ -61,6 +69,13 @@ class _OptimTensor(ctypes.Structure):
                 ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
                 ("n", ctypes.c_int64), ("lr_scale", ctypes.c_float), ("weight_decay", ctypes.c_float),
                 ("grad_bf16", ctypes.c_int32), ("state8", ctypes.c_int32)]
+
+
+class _Matrix(ctypes.Structure):
+    """cce_matrix of include/cce_muon.h."""
+    _fields_ = [("param", ctypes.c_void_p), ("out_bf16", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("momentum", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("lr_scale", ctypes.c_float), ("weight_decay", ctypes.c_float),
+                ("grad_bf16", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class CCEError(RuntimeError):
@@ -193,6 +208,18 @@ def lib() -> ctypes.CDLL:
     L.cce_adamw_multi_step.argtypes = [vp, i64, f32, f32, f32, f32, i64, vp, ctypes.c_uint32, vp]
     L.cce_adamw_state8_read.restype = ctypes.c_int
     L.cce_adamw_state8_read.argtypes = [vp, vp, i64, ctypes.c_int, vp, vp]
+    L.cce_muon_workspace_bytes.restype = sz
+    L.cce_muon_workspace_bytes.argtypes = [vp, i64]
+    L.cce_orthogonalize_multi.restype = ctypes.c_int
+    L.cce_orthogonalize_multi.argtypes = [vp, i64, vp, i32, f32, vp, sz, vp]
+    L.cce_muon_multi_step.restype = ctypes.c_int
+    L.cce_muon_multi_step.argtypes = [vp, i64, f32, f32, i32, vp, i32, f32, vp, vp, sz, vp]
+    L.cce_router_workspace_bytes.restype = sz
+    L.cce_router_workspace_bytes.argtypes = [i64, i64]
+    L.cce_router_forward.restype = ctypes.c_int
+    L.cce_router_forward.argtypes = [vp, i32, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.cce_router_backward.restype = ctypes.c_int
+    L.cce_router_backward.argtypes = [vp, i32, vp, vp, vp, vp, vp, i64, i64, i32, i32, vp, vp]
     _lib = L
     return L
 
@@ -1063,6 +1090,8 @@ class OptimTensors:
     params, m and v may be left out for cce_grad_sumsq_multi alone.  Memory that a step writes may not overlap any
     other of the list."""
 
+    _entry = _OptimTensor
+
     def __init__(self, grads, params=None, m=None, v=None, *, params_bf16=None, m_scales=None, v_scales=None,
                  lr_scale=1.0, weight_decay=0.0):
         count = len(grads)
@@ -1174,17 +1203,28 @@ class OptimTensors:
         moment, blocks = n * np.where(t["state8"] != 0, 1, 4), (n + STATE8_BLOCK - 1) // STATE8_BLOCK
         columns = [("param", "params", n * 4), ("param_bf16", "params_bf16", n * 2), ("m", "m", moment), ("v", "v", moment),
                    ("m_scale", "m_scales", blocks), ("v_scale", "v_scales", blocks), ("grad", "grads", n * np.where(t["grad_bf16"] != 0, 2, 4))]
-        starts = np.concatenate([t[field].astype(np.int64) for field, _, _ in columns])
-        ends = starts + np.concatenate([size for _, _, size in columns])
-        writes = np.arange(len(starts)) < 6 * len(n)
-        order = np.argsort(starts, kind="stable")
-        order = order[(starts[order] != 0) & (ends[order] > starts[order])]
-        start, end, written = starts[order], np.maximum.accumulate(ends[order]), np.maximum.accumulate(np.where(writes[order], ends[order], 0))
-        # what is written begins behind the end of everything in front of it, a gradient behind that of what is written
-        over = start[1:] < np.where(writes[order][1:], end[:-1], written[:-1])
-        if over.any():
-            at = int(order[1 + int(np.argmax(over))])
-            raise ValueError(f"{columns[at // len(n)][1]}[{at % len(n)}] overlaps another tensor of the list")
+        _refuse_overlap(columns, t, 6)
+
+
+def _check_entries(tensors, entry):
+    if tensors._entry is not entry:
+        raise ValueError(f"tensors: expected {'MuonTensors' if entry is _Matrix else 'OptimTensors'}, got {type(tensors).__name__}")
+
+
+def _refuse_overlap(columns, table, written_columns: int):
+    """`columns`: (field of the table, its list's name, bytes of each entry), those that a call writes first."""
+    count = len(table)
+    starts = np.concatenate([table[field].astype(np.int64) for field, _, _ in columns])
+    ends = starts + np.concatenate([size for _, _, size in columns])
+    writes = np.arange(len(starts)) < written_columns * count
+    order = np.argsort(starts, kind="stable")
+    order = order[(starts[order] != 0) & (ends[order] > starts[order])]
+    start, end, written = starts[order], np.maximum.accumulate(ends[order]), np.maximum.accumulate(np.where(writes[order], ends[order], 0))
+    # what is written begins behind the end of everything in front of it, a gradient behind that of what is written
+    over = start[1:] < np.where(writes[order][1:], end[:-1], written[:-1])
+    if over.any():
+        at = int(order[1 + int(np.argmax(over))])
+        raise ValueError(f"{columns[at // count][1]}[{at % count}] overlaps another tensor of the list")
 
 
 def cce_grad_sumsq_multi(tensors: OptimTensors, sumsq: Optional[torch.Tensor] = None, accumulate: bool = False, *,
@@ -1193,6 +1233,7 @@ def cce_grad_sumsq_multi(tensors: OptimTensors, sumsq: Optional[torch.Tensor] = 
                          stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """(device fp64 [1]: sum of squares of all gradients, added to `sumsq` when accumulate; device fp32 [1]: the clipping
     coefficient for max_norm, or None without one)."""
+    _check_entries(tensors, _OptimTensor)
     device = tensors.device
     if sumsq is None:
         if accumulate:
@@ -1226,6 +1267,7 @@ def cce_adamw_multi_step(tensors: OptimTensors, step: int, *, lr: float, beta1: 
                          eps: float = 1e-8, clip_coef: Optional[torch.Tensor] = None, seed: int = 0,
                          stream: Optional[torch.cuda.Stream] = None) -> None:
     """In-place AdamW step on all tensors of the list; `seed` of the rounding of moments in 8 bits."""
+    _check_entries(tensors, _OptimTensor)
     if not tensors.steps:
         raise ValueError("tensors: the list has gradients alone")
     if clip_coef is not None:
@@ -1257,3 +1299,223 @@ def cce_adamw_state8_read(codes: torch.Tensor, scales: torch.Tensor, *, second: 
     _call("cce_adamw_state8_read", lib().cce_adamw_state8_read, device, stream, codes.data_ptr(), scales.data_ptr(), n,
           1 if second else 0, out.data_ptr())
     return out
+
+
+# ---------------------------------------------------------------- include/cce_muon.h
+
+class MuonTensors(OptimTensors):
+    """The matrices of a Muon step, made once and given to every step, as OptimTensors is for the other tensors of a model.
+
+    grads         fp32 or bf16, two-dimensional, contiguous; the other lists are parallel to it
+    params, momentum   fp32, of the same shapes (momentum: zeros before the first step)
+    params_bf16   None, or the bf16 copies to keep (None for a matrix without one)
+    lr_scale, weight_decay   a number, or one for each matrix; lr_scale 0.2 sqrt(max(rows, cols)) makes updates as large as AdamW's"""
+
+    _entry = _Matrix
+
+    def __init__(self, grads, params, momentum, *, params_bf16=None, lr_scale=1.0, weight_decay=0.0):
+        count = len(grads)
+        if count == 0:
+            raise ValueError("grads: expected at least one matrix")
+        self.steps = True
+        self.device = grads[0].device
+        self._table = np.zeros(count, dtype=np.dtype(_Matrix))
+        self._address = self._table.ctypes.data
+        self._streams = {}
+        lists = {"params": list(params), "momentum": list(momentum), "params_bf16": [None] * count if params_bf16 is None else list(params_bf16)}
+        rates = {"lr_scale": lr_scale, "weight_decay": weight_decay}
+        for name, x in [*lists.items(), *((name, x) for name, x in rates.items() if hasattr(x, "__len__"))]:
+            if len(x) != count:
+                raise ValueError(f"{name}: expected {count} entries, got {len(x)}")
+        for name in ("params", "momentum"):
+            for i, x in enumerate(lists[name]):
+                if x is None or x.dim() != 2:
+                    raise ValueError(f"{name}[{i}]: expected a matrix, got {'None' if x is None else tuple(x.shape)}")
+        self._keep = lists
+        self._shapes = [tuple(p.shape) for p in lists["params"]]
+        sizes = [p.numel() for p in lists["params"]]
+        self._table["rows"] = [m for m, _ in self._shapes]
+        self._table["cols"] = [n for _, n in self._shapes]
+        for field, name, dtype in (("param", "params", torch.float32), ("momentum", "momentum", torch.float32), ("out_bf16", "params_bf16", torch.bfloat16)):
+            wanted = [x is not None for x in lists[name]]
+            self._check_shapes(name, lists[name])
+            self._table[field] = self._pointers(name, lists[name], [dtype] * count, sizes, wanted)
+        self._table["lr_scale"] = lr_scale
+        self._table["weight_decay"] = weight_decay
+        self._take_grads(list(grads), sizes)
+
+    def _check_shapes(self, name, tensors):
+        for i, (t, shape) in enumerate(zip(tensors, self._shapes)):
+            if t is not None and tuple(t.shape) != shape:
+                raise ValueError(f"{name}[{i}]: expected a matrix of {shape}, got {tuple(t.shape)}")
+
+    def _take_grads(self, grads, sizes):
+        self._check_shapes("grads", grads)
+        super()._take_grads(grads, sizes)
+
+    def set_grads(self, grads):
+        """Other gradients for the same parameters (a step whose gradients lie elsewhere)."""
+        if len(grads) != len(self):
+            raise ValueError(f"grads: expected {len(self)} matrices, got {len(grads)}")
+        self._take_grads(list(grads), (self._table["rows"] * self._table["cols"]).tolist())
+
+    def _check_overlap(self):
+        t, n = self._table, self._table["rows"] * self._table["cols"]
+        _refuse_overlap([("param", "params", n * 4), ("momentum", "momentum", n * 4), ("out_bf16", "params_bf16", n * 2),
+                         ("grad", "grads", n * np.where(t["grad_bf16"] != 0, 2, 4))], t, 3)
+
+
+def _coefficients(coefficients, steps: int):
+    """fp32 [steps, 3] on the host: one (a, b, c) for all steps, or one for each."""
+    c = np.ascontiguousarray(coefficients, dtype=np.float32)
+    if c.shape == (3,):
+        c = np.ascontiguousarray(np.broadcast_to(c, (steps, 3)))
+    if c.shape != (steps, 3):
+        raise ValueError(f"coefficients: expected three numbers, or three for each of the {steps} steps, got {c.shape}")
+    return c
+
+
+def muon_workspace_bytes(tensors: MuonTensors) -> int:
+    _check_entries(tensors, _Matrix)
+    return int(lib().cce_muon_workspace_bytes(tensors._address, len(tensors)))
+
+
+def _muon_workspace(where: str, table, device, workspace, stream):
+    if workspace is not None:
+        _check_on(device, workspace, torch.uint8, (workspace.numel(),), "workspace")
+        return workspace
+    n = int(lib().cce_muon_workspace_bytes(table.ctypes.data, len(table)))
+    if n == 0:
+        raise CCEError(CCE_ERR_UNSUPPORTED, where)
+    return _new((n,), torch.uint8, device, stream)
+
+
+def cce_orthogonalize_multi(matrices, out=None, *, steps: int = 5, coefficients=NS_COEFFICIENTS, eps: float = 1e-7,
+                            workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """bf16 matrices: each of the list (fp32 or bf16, contiguous) orthogonalised by `steps` Newton-Schulz steps; written to `out`, a list of
+    as many bf16 matrices, if given.  `coefficients`: (a, b, c), or one such triple for each step."""
+    count = len(matrices)
+    if count == 0:
+        raise ValueError("matrices: expected at least one")
+    device = matrices[0].device
+    for i, t in enumerate(matrices):
+        if t.dtype not in (torch.float32, torch.bfloat16) or not t.is_cuda or t.device != device or t.dim() != 2 or not t.is_contiguous():
+            raise ValueError(f"matrices[{i}]: expected a contiguous cuda float32 or bfloat16 matrix on {device}, got {t.dtype} {tuple(t.shape)} "
+                             f"contiguous={t.is_contiguous()} on {t.device}")
+    if out is None:
+        out = [_new(t.shape, torch.bfloat16, device, stream) for t in matrices]
+    elif len(out) != count:
+        raise ValueError(f"out: expected {count} matrices, got {len(out)}")
+    else:
+        for i, (o, t) in enumerate(zip(out, matrices)):
+            _check_on(device, o, torch.bfloat16, t.shape, f"out[{i}]")
+    table = np.zeros(count, dtype=np.dtype(_Matrix))
+    table["grad"] = [t.data_ptr() for t in matrices]
+    table["out_bf16"] = [o.data_ptr() for o in out]
+    table["rows"] = [t.shape[0] for t in matrices]
+    table["cols"] = [t.shape[1] for t in matrices]
+    table["grad_bf16"] = [t.dtype == torch.bfloat16 for t in matrices]
+    n = table["rows"] * table["cols"]
+    _refuse_overlap([("out_bf16", "out", n * 2), ("grad", "matrices", n * np.where(table["grad_bf16"] != 0, 2, 4))], table, 1)
+    c = _coefficients(coefficients, steps)
+    workspace = _muon_workspace("cce_orthogonalize_multi", table, device, workspace, stream)
+    _call("cce_orthogonalize_multi", lib().cce_orthogonalize_multi, device, stream, table.ctypes.data, count, c.ctypes.data, steps, eps,
+          workspace.data_ptr(), workspace.numel())
+    return out
+
+
+def cce_muon_multi_step(tensors: MuonTensors, *, lr: float, momentum: float = 0.95, nesterov: bool = True, steps: int = 5,
+                        coefficients=NS_COEFFICIENTS, eps: float = 1e-7, clip_coef: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """In-place Muon step on all matrices of the list: momentum, orthogonalisation, decay and update."""
+    _check_entries(tensors, _Matrix)
+    if clip_coef is not None:
+        _check_on(tensors.device, clip_coef, torch.float32, (1,), "clip_coef")
+    c = _coefficients(coefficients, steps)
+    workspace = _muon_workspace("cce_muon_multi_step", tensors._table, tensors.device, workspace, stream)
+    _call("cce_muon_multi_step", lib().cce_muon_multi_step, tensors.device, stream, tensors._address, len(tensors), lr, momentum,
+          1 if nesterov else 0, c.ctypes.data, steps, eps, clip_coef.data_ptr() if clip_coef is not None else None,
+          workspace.data_ptr(), workspace.numel())
+    if stream is not None:
+        tensors._read_on(stream)
+
+
+# ---------------------------------------------------------------- include/cce_router.h
+
+class RouterOutput(NamedTuple):
+    """What cce_router_forward gives."""
+    indices: torch.Tensor     # int32 [N, k]: each row's experts, the likeliest first; -1 where there is none
+    weights: torch.Tensor     # fp32 [N, k]
+    lse: torch.Tensor         # fp32 [N]: log of the sum of the exponentials of the row's logits
+    counts: torch.Tensor      # int32 [E + 1]: rows that chose each expert; behind them, rows that take part
+    prob_sums: torch.Tensor   # fp32 [E]: each expert's probability, summed over the rows that take part
+    losses: torch.Tensor      # fp32 [2]: balance loss, z loss
+
+
+_ROUTER_DTYPES = (torch.float32, torch.bfloat16)
+
+
+def _router_logits(logits: torch.Tensor):
+    N, E = logits.shape
+    if logits.dtype not in _ROUTER_DTYPES:
+        raise ValueError(f"logits: expected float32 or bfloat16, got {logits.dtype}")
+    _check(logits, logits.dtype, (N, E), "logits")
+    return N, E
+
+
+def cce_router_forward(logits: torch.Tensor, top_k: int, labels: Optional[torch.Tensor] = None, ignore_index: int = -100, *,
+                       renormalize: bool = True, out: Optional[RouterOutput] = None, workspace: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> RouterOutput:
+    """The `top_k` experts of each row of `logits` (fp32 or bf16 [N, E]; -inf: not for this row), their softmax weights (of all experts'
+    softmax, or with renormalize of the chosen ones'), the experts' counts, the balance loss and the z loss.  Rows whose label is
+    `ignore_index` take no part."""
+    N, E = _router_logits(logits)
+    device = logits.device
+    if labels is not None:
+        _check_on(device, labels, torch.int32, (N,), "labels")
+    shapes = {"indices": ((N, top_k), torch.int32), "weights": ((N, top_k), torch.float32), "lse": ((N,), torch.float32),
+              "counts": ((E + 1,), torch.int32), "prob_sums": ((E,), torch.float32), "losses": ((2,), torch.float32)}
+    if out is None:
+        if not 1 <= top_k <= E:
+            raise CCEError(CCE_ERR_INVALID, "cce_router_forward, top_k")
+        out = RouterOutput(*(_new(shape, dtype, device, stream) for shape, dtype in shapes.values()))
+    else:
+        for name, (shape, dtype) in shapes.items():
+            _check_on(device, getattr(out, name), dtype, shape, name)
+    if workspace is None:
+        n = int(lib().cce_router_workspace_bytes(N, E))
+        if n == 0:
+            raise CCEError(CCE_ERR_UNSUPPORTED, "cce_router_workspace_bytes")
+        workspace = _new((n,), torch.uint8, device, stream)
+    else:
+        _check_on(device, workspace, torch.uint8, (workspace.numel(),), "workspace")
+    _call("cce_router_forward", lib().cce_router_forward, device, stream, logits.data_ptr(), 1 if logits.dtype == torch.bfloat16 else 0,
+          labels.data_ptr() if labels is not None else None, N, E, top_k, 1 if renormalize else 0, ignore_index,
+          out.indices.data_ptr(), out.weights.data_ptr(), out.lse.data_ptr(), out.counts.data_ptr(), out.prob_sums.data_ptr(),
+          out.losses.data_ptr(), workspace.data_ptr(), workspace.numel())
+    return out
+
+
+def cce_router_backward(logits: torch.Tensor, indices: torch.Tensor, lse: torch.Tensor, counts: torch.Tensor,
+                        d_weights: Optional[torch.Tensor], d_losses: Optional[torch.Tensor], *, renormalize: bool = True,
+                        d_logits: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Gradient of the logits, of their type, for the gradients of the weights (fp32 [N, k], or None) and of the two losses (fp32 [2], or
+    None).  counts may be summed over the ranks of a job: the losses are then those of all of their rows."""
+    N, E = _router_logits(logits)
+    device = logits.device
+    k = indices.shape[-1]
+    _check_on(device, indices, torch.int32, (N, k), "indices")
+    _check_on(device, lse, torch.float32, (N,), "lse")
+    _check_on(device, counts, torch.int32, (E + 1,), "counts")
+    if d_weights is not None:
+        _check_on(device, d_weights, torch.float32, (N, k), "d_weights")
+    if d_losses is not None:
+        _check_on(device, d_losses, torch.float32, (2,), "d_losses")
+    if d_logits is None:
+        d_logits = _new((N, E), logits.dtype, device, stream)
+    else:
+        _check_on(device, d_logits, logits.dtype, (N, E), "d_logits")
+    _call("cce_router_backward", lib().cce_router_backward, device, stream, logits.data_ptr(), 1 if logits.dtype == torch.bfloat16 else 0,
+          indices.data_ptr(), lse.data_ptr(), counts.data_ptr(), d_weights.data_ptr() if d_weights is not None else None,
+          d_losses.data_ptr() if d_losses is not None else None, N, E, k, 1 if renormalize else 0, d_logits.data_ptr())
+    return d_logits

@@ -10,7 +10,8 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libcce.so")
 SOURCES = [os.path.join(CSRC, "cce_kernels.hip"), os.path.join(CSRC, "aux_kernels.hip"),
-           os.path.join(CSRC, "embed_kernels.hip"), os.path.join(CSRC, "optim_kernels.hip")]
+           os.path.join(CSRC, "embed_kernels.hip"), os.path.join(CSRC, "optim_kernels.hip"),
+           os.path.join(CSRC, "muon_kernels.hip"), os.path.join(CSRC, "router_kernels.hip")]
 HEADERS = [os.path.join(CSRC, "gemm_core.h"), os.path.join(CSRC, "fused_backward.h"), os.path.join(CSRC, "host_util.h"), os.path.join(CSRC, "plan.h"), os.path.join(CSRC, "wg_map.h"),
            os.path.join(CSRC, "vec_util.h"),
            os.path.join(os.path.dirname(PKG_DIR), "include", "cce.h"),
@@ -19,7 +20,9 @@ HEADERS = [os.path.join(CSRC, "gemm_core.h"), os.path.join(CSRC, "fused_backward
            os.path.join(os.path.dirname(PKG_DIR), "include", "cce_fp8.h"),
            os.path.join(os.path.dirname(PKG_DIR), "include", "cce_compact.h"),
            os.path.join(os.path.dirname(PKG_DIR), "include", "cce_embed.h"),
-           os.path.join(os.path.dirname(PKG_DIR), "include", "cce_optim.h")]
+           os.path.join(os.path.dirname(PKG_DIR), "include", "cce_optim.h"),
+           os.path.join(os.path.dirname(PKG_DIR), "include", "cce_muon.h"),
+           os.path.join(os.path.dirname(PKG_DIR), "include", "cce_router.h")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

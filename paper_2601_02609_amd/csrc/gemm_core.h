@@ -39,6 +39,7 @@
 namespace cce {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((ext_vector_type(8))) short s16x8;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
@@ -324,6 +325,13 @@ struct FragAddr {
     }
 };
 
+// The 16 bits of an operand's values are bf16's or, with F16, fp16's: same layout, same rate.
+template <bool F16>
+__device__ __forceinline__ f32x16 mfma_32x32x16(const bf16x8 a, const bf16x8 b, const f32x16 c) {
+    if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
 // Scheduling hint: one MFMA, then PER LDS reads, repeated (compile-time recursion because
 // the builtin wants constant arguments).
 template <int I, int N_MFMA, int N_READS, int PER>
@@ -368,7 +376,7 @@ __device__ __forceinline__ void barrier_lds_only() {
 // visible to all and its first fragments can be read under those last MFMAs, and (b)
 // the current stage may be overwritten by the loads issued at the top of the next
 // iteration.
-template <class Cfg, bool A_KMAJOR, bool B_KMAJOR, bool PEEL = false, class OpA, class OpB>
+template <class Cfg, bool A_KMAJOR, bool B_KMAJOR, bool PEEL = false, bool F16 = false, class OpA, class OpB>
 __device__ __forceinline__ void gemm_mainloop(f32x16 (&acc)[Cfg::TM][Cfg::TN], const OpA& A, const OpB& B,
                                                int k_total, CCE_LDS char* smem) {
     constexpr int S = Cfg::STAGES, BK = Cfg::BK;
@@ -431,7 +439,7 @@ __device__ __forceinline__ void gemm_mainloop(f32x16 (&acc)[Cfg::TM][Cfg::TN], c
             for (int bm = 0; bm < Cfg::TM; ++bm)
 #pragma unroll
                 for (int bn = 0; bn < Cfg::TN; ++bn)
-                    acc[bm][bn] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[c][bm], bfr[c][bn], acc[bm][bn], 0, 0, 0);
+                    acc[bm][bn] = mfma_32x32x16<F16>(af[c][bm], bfr[c][bn], acc[bm][bn]);
             // issue order for the scheduler: the LDS reads of the next step are spread
             // one (or two) at a time behind the first MFMAs of this step
             constexpr int kReads = Cfg::TM * (A_KMAJOR ? 1 : 2) + Cfg::TN * (B_KMAJOR ? 1 : 2);

@@ -1,0 +1,577 @@
+// libcce, optimizer kernels for matrices: momentum, Newton-Schulz products, update.  C ABI declared in include/cce_muon.h.
+//
+// A matrix is worked on as X of r x c, r <= c (transposed on the way in and out where it is taller than wide), in the
+// workspace, rows and columns padded with zeros to multiples of 64.  Per step three launches over all matrices of a group:
+//
+//   gram    A = X X^T             half of the tiles, the other half mirrored
+//   poly    M = b A + c A A       the same
+//   apply   X = (a + M) X
+//
+// Rounding.  Products take fp16 operands (11 bits) and add in fp32.  Rounding all of X, A and M to them would leave an error of
+// 2 % (6e-3 of matrices with a few large directions), because the diagonals of A and M are much larger than what lies beside them, and the
+// linear part a X carries small directions next to large ones.  So the diagonals of A and M are kept in fp32 and taken out of the
+// 16-bit operands, and the linear part is taken from X as h + l, two 16-bit values: 0.5 to 1.4e-3 in all, half of bf16's own
+// rounding of the result.
+//
+// Scales, powers of two: X 2^13, A 2^13, M 2^10, the remainders l 2^24.  Singular values stay below 2.5 (checked for the coefficients),
+// values of X too; A's are below 6.25 and M's below 60: within fp16's 65504.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/cce.h"
+#include "../../include/cce_muon.h"
+#include "gemm_core.h"
+#include "host_util.h"
+#include "vec_util.h"
+#include "wg_map.h"
+
+namespace cce {
+
+typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
+
+constexpr int kGroup = 48;                             // matrices of a launch: kernel arguments hold 4 KB
+constexpr int64_t kGroupBytes = (int64_t)1 << 30;      // workspace of a group of more than one matrix
+constexpr int64_t kMaxMatrix = (int64_t)1 << 30;       // values of a matrix: byte offsets of 16-bit values stay below 2^32
+constexpr int64_t kMaxSide = 16384;                    // smaller side
+constexpr int kNormParts = 256;                        // partial sums of a matrix
+constexpr int kNormValues = 8192;                      // values of a part, more where that gives too many parts
+constexpr float kScaleX = 0x1p13f, kScaleA = 0x1p13f, kScaleM = 0x1p10f, kScaleL = 0x1p24f;
+constexpr double kMaxSigma = 2.5, kMaxM = 60.0;
+
+struct NsMatrix {
+    const void* grad;
+    float* momentum;
+    float* param;              // null: only out is written
+    uint16_t* out;
+    uint64_t base;             // byte offset in the workspace
+    int32_t rows, cols;        // of the caller's matrix
+    float lr, decay;           // decay: 1 - lr * weight_decay
+};
+
+struct NsArgs {
+    NsMatrix t[kGroup];
+    uint32_t first_norm[kGroup];      // a matrix's first workgroup; twice that, plus 1 if its gradient is bf16
+    uint32_t first_prep[kGroup], first_sym[kGroup], first_apply[kGroup];      // twice the first workgroup
+    char* ws;
+    const float* clip_coef;
+    float mu, a, b, c, eps;
+    int32_t nesterov;
+    uint32_t count, flip;             // flip: which of the two copies of h is read
+};
+static_assert(sizeof(NsArgs) <= 4096, "kernel arguments hold 4 KB");
+
+// Where a matrix's operands lie, in bytes behind its base.
+struct NsLayout {
+    int r, c, rp, cp;                 // sides and padded sides
+    uint64_t h[2], l, a, m, da, dm, partials, bytes;
+    __host__ __device__ __forceinline__ NsLayout(int rows, int cols) {
+        r = rows < cols ? rows : cols;
+        c = rows < cols ? cols : rows;
+        rp = (r + 63) & ~63;
+        cp = (c + 63) & ~63;
+        const uint64_t x = (uint64_t)rp * cp * 2, s = (uint64_t)rp * rp * 2, d = (uint64_t)rp * 4;
+        h[0] = 0;
+        h[1] = x;
+        l = 2 * x;
+        a = l + x;
+        m = a + s;
+        da = m + s;
+        dm = da + d;
+        partials = dm + d;
+        bytes = partials + kNormParts * 8;
+    }
+};
+
+// Which matrix workgroup w belongs to, b = 2 w + 1: the last one that begins at or before it.
+__device__ __forceinline__ int matrix_of(const uint32_t* first, int count, uint32_t b) {
+    const int i = (int)(threadIdx.x & 63);
+    return __builtin_amdgcn_readfirstlane((int)__popcll(__ballot(i < count && first[i] <= b)) - 1);
+}
+
+__device__ __forceinline__ float grad_value(const void* grad, bool bf16, int64_t i) {
+    return bf16 ? __uint_as_float((uint32_t)((const uint16_t*)grad)[i] << 16) : ((const float*)grad)[i];
+}
+__device__ __forceinline__ af32x4 grad_values(const void* grad, bool bf16, int64_t i) {
+    if (!bf16) return *(const af32x4*)((const float*)grad + i);
+    const u32x2 p = *(const u32x2*)((const uint16_t*)grad + i);
+    return af32x4{__uint_as_float(p[0] << 16), __uint_as_float(p[0] & 0xffff0000u), __uint_as_float(p[1] << 16), __uint_as_float(p[1] & 0xffff0000u)};
+}
+__device__ __forceinline__ bool aligned(const void* p, unsigned to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+// A pointer that is the same in every lane, in scalar registers: base of the loads into LDS.
+template <class T>
+__device__ __forceinline__ T* uniform(T* p) {
+    const uint64_t x = (uint64_t)(uintptr_t)p;
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(x >> 32));
+    return (T*)(uintptr_t)((uint64_t)hi << 32 | lo);
+}
+
+__device__ __forceinline__ float new_momentum(float m, float g, float mu) { return mu * m + (1.f - mu) * g; }
+__device__ __forceinline__ float direction(float m, float g, float mu, int nesterov) { return nesterov ? mu * m + (1.f - mu) * g : m; }
+
+// Sum of a double over a workgroup of four wavefronts, for all of its threads.
+__device__ __forceinline__ double group_sum(double x, double* red) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+__device__ __forceinline__ int norm_parts(int64_t n) {
+    const int64_t parts = (n + kNormValues - 1) / kNormValues;
+    return parts < kNormParts ? (int)parts : kNormParts;
+}
+
+// ------------------------------------------------------------------------------------------
+// Momentum, and partial sums of squares of what is orthogonalised, in fp64: 1e-20 and 1e20 have squares in no fp32.
+// ------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void ns_norm_kernel(const NsArgs a) {
+    __shared__ double red[4];
+    const int i = matrix_of(a.first_norm, (int)a.count, 2 * blockIdx.x + 1);
+    const NsMatrix& t = a.t[i];
+    const bool bf16 = (a.first_norm[i] & 1u) != 0u;
+    const int64_t n = (int64_t)t.rows * t.cols;
+    const int part = (int)(blockIdx.x - (a.first_norm[i] >> 1)), parts = norm_parts(n);
+    const float clip = a.clip_coef ? a.clip_coef[0] : 1.f;
+    const bool vec = aligned(t.grad, bf16 ? 8 : 16) && aligned(t.momentum, 16);
+    double sum = 0.0;
+    for (int64_t at = ((int64_t)part * 256 + threadIdx.x) * 4; at < n; at += (int64_t)parts * 1024) {
+        const int left = n - at < 4 ? (int)(n - at) : 4;
+        af32x4 u = {0.f, 0.f, 0.f, 0.f};
+        if (vec && left == 4) {
+            u = grad_values(t.grad, bf16, at);
+            if (t.momentum) {
+                af32x4 m = *(const af32x4*)(t.momentum + at);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float g = u[e] * clip;
+                    m[e] = new_momentum(m[e], g, a.mu);
+                    u[e] = direction(m[e], g, a.mu, a.nesterov);
+                }
+                *(af32x4*)(t.momentum + at) = m;
+            }
+        } else {
+            for (int e = 0; e < left; ++e) {
+                float g = grad_value(t.grad, bf16, at + e);
+                if (t.momentum) {
+                    g *= clip;
+                    const float m = new_momentum(t.momentum[at + e], g, a.mu);
+                    t.momentum[at + e] = m;
+                    g = direction(m, g, a.mu, a.nesterov);
+                }
+                u[e] = g;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum = fma((double)u[e], (double)u[e], sum);
+    }
+    sum = group_sum(sum, red);
+    if (threadIdx.x == 0) ((double*)(a.ws + t.base + NsLayout(t.rows, t.cols).partials))[part] = sum;
+}
+
+// x as h + l: h has x's first 11 bits, l the next ones.
+__device__ __forceinline__ void split4(const af32x4& x, f16x4& h, f16x4& l) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float s = x[e] * kScaleX;
+        h[e] = (_Float16)s;
+        l[e] = (_Float16)((s - (float)h[e]) * (kScaleL / kScaleX));
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// X = G / (|G| + eps), 64 x 64 values a workgroup, transposed through LDS where G is taller than wide.
+// ------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void ns_prep_kernel(const NsArgs a) {
+    __shared__ double red[4];
+    __shared__ float tile[64][65];
+    const int i = matrix_of(a.first_prep, (int)a.count, 2 * blockIdx.x + 1);
+    const NsMatrix& t = a.t[i];
+    const bool bf16 = (a.first_norm[i] & 1u) != 0u;
+    const NsLayout at(t.rows, t.cols);
+    char* const base = a.ws + t.base;
+    const int64_t n = (int64_t)t.rows * t.cols;
+    const int w = (int)(blockIdx.x - (a.first_prep[i] >> 1)), tiles = at.cp / 64;
+    const int row0 = w / tiles * 64, col0 = w % tiles * 64;
+    const double sum = group_sum((int)threadIdx.x < norm_parts(n) ? ((const double*)(base + at.partials))[threadIdx.x] : 0.0, red);
+    const double inv = sum <= 0x1.fffffffffffffp1023 ? 1.0 / (sqrt(sum) + (double)a.eps) : (double)NAN;
+    const float clip = a.clip_coef ? a.clip_coef[0] : 1.f;
+    const bool tall = t.rows > t.cols;
+    const bool vec = (t.cols & 3) == 0 && aligned(t.grad, bf16 ? 8 : 16) && aligned(t.momentum, 16);
+    const int r0 = tall ? col0 : row0, c0 = tall ? row0 : col0;                // in the caller's matrix
+    const int q = (threadIdx.x & 15) * 4;
+    _Float16* const H = (_Float16*)(base + at.h[0]);
+    _Float16* const L = (_Float16*)(base + at.l);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int y = (int)(threadIdx.x >> 4) + 16 * k, row = r0 + y, col = c0 + q;
+        const int left = row < t.rows ? t.cols - col : 0;
+        const int64_t j = (int64_t)row * t.cols + col;
+        af32x4 x = {0.f, 0.f, 0.f, 0.f};
+        if (vec && left >= 4) {
+            x = grad_values(t.grad, bf16, j);
+            if (t.momentum) {
+                const af32x4 m = *(const af32x4*)(t.momentum + j);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = direction(m[e], x[e] * clip, a.mu, a.nesterov);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = (float)((double)x[e] * inv);
+        } else {
+            for (int e = 0; e < 4; ++e) {
+                if (e >= left) continue;
+                float u = grad_value(t.grad, bf16, j + e);
+                if (t.momentum) u = direction(t.momentum[j + e], u * clip, a.mu, a.nesterov);
+                x[e] = (float)((double)u * inv);
+            }
+        }
+        if (tall) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) tile[y][q + e] = x[e];
+        } else {
+            f16x4 h, l;
+            split4(x, h, l);
+            const uint32_t to = (uint32_t)(row0 + y) * (uint32_t)at.cp + (uint32_t)(col0 + q);
+            *(f16x4*)(H + to) = h;
+            *(f16x4*)(L + to) = l;
+        }
+    }
+    if (!tall) return;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int y = (int)(threadIdx.x >> 4) + 16 * k;
+        f16x4 h, l;
+        split4(af32x4{tile[q][y], tile[q + 1][y], tile[q + 2][y], tile[q + 3][y]}, h, l);
+        const uint32_t to = (uint32_t)(row0 + y) * (uint32_t)at.cp + (uint32_t)(col0 + q);
+        *(f16x4*)(H + to) = h;
+        *(f16x4*)(L + to) = l;
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// The products.
+// ------------------------------------------------------------------------------------------
+typedef TileSmall NsTile;
+constexpr int kNsTile = NsTile::BM;
+static_assert(NsTile::BM == NsTile::BN, "square tiles: half of them mirrored");
+
+// Tile w of the lower triangle, by rows.
+__device__ __forceinline__ void triangle(int w, int& i, int& j) {
+    i = (int)((sqrtf(8.f * (float)w + 1.f) - 1.f) * 0.5f);
+    while ((i + 1) * (i + 2) / 2 <= w) ++i;
+    while (i * (i + 1) / 2 > w) --i;
+    j = w - i * (i + 1) / 2;
+}
+
+enum { kGram, kPoly, kApply, kLast };
+
+template <int OP>
+__global__ __launch_bounds__(512) void ns_product_kernel(const NsArgs a) {
+    extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
+    CCE_LDS char* const smem = (CCE_LDS char*)smem_generic;
+    const uint32_t* const first = OP <= kPoly ? a.first_sym : a.first_apply;
+    const uint32_t id = (uint32_t)xcd_linear_id((int)blockIdx.x, (int)gridDim.x);
+    const int i = matrix_of(first, (int)a.count, 2 * id + 1);
+    const NsMatrix& t = a.t[i];
+    const NsLayout at(t.rows, t.cols);
+    char* const base = a.ws + t.base;
+    const int w = (int)(id - (first[i] >> 1));
+    const _Float16* const H = uniform((const _Float16*)(base + at.h[a.flip]));
+    _Float16* const A = uniform((_Float16*)(base + at.a));
+    _Float16* const M = uniform((_Float16*)(base + at.m));
+    float* const da = (float*)(base + at.da);
+    float* const dm = (float*)(base + at.dm);
+    f32x16 acc[NsTile::TM][NsTile::TN];
+#pragma unroll
+    for (int bm = 0; bm < NsTile::TM; ++bm)
+#pragma unroll
+        for (int bn = 0; bn < NsTile::TN; ++bn) acc[bm][bn] = f32x16{};
+    int m0, n0;
+    if (OP <= kPoly) {
+        int ti, tj;
+        triangle(w, ti, tj);
+        m0 = ti * kNsTile;
+        n0 = tj * kNsTile;
+        OperandTile<true, NsTile::BM> x, y;
+        const void* from = OP == kGram ? (const void*)H : (const void*)A;
+        const int k = OP == kGram ? at.cp : at.rp;
+        x.init(from, k, m0, at.rp, k);
+        y.init(from, k, n0, at.rp, k);
+        gemm_mainloop<NsTile, true, true, false, true>(acc, x, y, k, smem);
+    } else {
+        const int tiles = (at.cp + kNsTile - 1) / kNsTile;
+        m0 = w % tiles * kNsTile;
+        n0 = w / tiles * kNsTile;
+        OperandTile<false, NsTile::BM> x;
+        OperandTile<true, NsTile::BN> y;
+        x.init(H, at.cp, m0, at.cp, at.rp);
+        y.init(M, at.rp, n0, at.rp, at.rp);
+        gemm_mainloop<NsTile, false, true, false, true>(acc, x, y, at.rp, smem);
+    }
+    const int lane = threadIdx.x & 63;
+    const bool tall = t.rows > t.cols;
+#pragma unroll
+    for (int bm = 0; bm < NsTile::TM; ++bm)
+#pragma unroll
+        for (int bn = 0; bn < NsTile::TN; ++bn)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                // four values in a row of the result: columns m .. m + 3 of row n
+                const int m = m0 + (wave_m<NsTile>() * NsTile::TM + bm) * 32 + 8 * g + 4 * (lane >> 5);
+                const int n = n0 + (wave_n<NsTile>() * NsTile::TN + bn) * 32 + (lane & 31);
+                const f32x16& s = acc[bm][bn];
+                if (OP <= kPoly) {
+                    if (m >= at.rp || n >= at.rp) continue;
+                    f16x4 v;
+                    if (OP == kGram) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float x = s[4 * g + e] * (1.f / (kScaleX * kScaleX));
+                            if (m + e == n) da[n] = x;
+                            v[e] = m + e == n ? (_Float16)0.f : (_Float16)(x * kScaleA);
+                        }
+                    } else {
+                        const f16x4 o = *(const f16x4*)(A + (uint32_t)n * (uint32_t)at.rp + m);
+                        const af32x4 dr = *(const af32x4*)(da + m);
+                        const float dn = da[n];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float p = s[4 * g + e] * (a.c / (kScaleA * kScaleA));
+                            const float x = (a.b + a.c * (dn + dr[e])) * ((float)o[e] * (1.f / kScaleA)) + p;
+                            if (m + e == n) dm[n] = a.b * dn + (a.c * dn * dn + p);
+                            v[e] = m + e == n ? (_Float16)0.f : (_Float16)(x * kScaleM);
+                        }
+                    }
+                    _Float16* const to = OP == kGram ? A : M;
+                    *(f16x4*)(to + (uint32_t)n * (uint32_t)at.rp + m) = v;
+                    if (m0 != n0)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) to[(uint32_t)(m + e) * (uint32_t)at.rp + n] = v[e];
+                } else {
+                    if (m >= at.cp || n >= at.rp) continue;
+                    const uint32_t j = (uint32_t)n * (uint32_t)at.cp + m;
+                    const f16x4 h = *(const f16x4*)(H + j);
+                    _Float16* const L = (_Float16*)(base + at.l);
+                    const f16x4 l = *(const f16x4*)(L + j);
+                    const float keep = a.a + dm[n];
+                    af32x4 x;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        x[e] = keep * ((float)h[e] * (1.f / kScaleX) + (float)l[e] * (1.f / kScaleL)) + s[4 * g + e] * (1.f / (kScaleX * kScaleM));
+                    if (OP == kApply) {
+                        f16x4 h1, l1;
+                        split4(x, h1, l1);
+                        *(f16x4*)((_Float16*)(base + at.h[a.flip ^ 1]) + j) = h1;
+                        *(f16x4*)(L + j) = l1;
+                    } else {
+                        if (n >= at.r) continue;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if (m + e >= at.c) continue;
+                            const int64_t to = tall ? (int64_t)(m + e) * t.cols + n : (int64_t)n * t.cols + (m + e);
+                            float y = x[e];
+                            if (t.param) {
+                                y = t.param[to] * t.decay - t.lr * y;
+                                t.param[to] = y;
+                            }
+                            if (t.out) {
+                                union { __bf16 h; uint16_t u; } cv;
+                                cv.h = (__bf16)y;
+                                t.out[to] = cv.u;
+                            }
+                        }
+                    }
+                }
+            }
+}
+
+// ------------------------------------------------------------------------------------------
+// Host side.
+// ------------------------------------------------------------------------------------------
+static bool misaligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
+
+static int check_sizes(const cce_matrix* matrices, int64_t count) {
+    if (!matrices || count <= 0) return CCE_ERR_INVALID;
+    for (int64_t i = 0; i < count; ++i) {
+        const cce_matrix& t = matrices[i];
+        if (t.rows < 0 || t.cols < 0) return CCE_ERR_INVALID;
+        if (t.rows == 0 || t.cols == 0) continue;
+        if (t.rows > kMaxMatrix || t.cols > kMaxMatrix || t.rows * t.cols > kMaxMatrix) return CCE_ERR_UNSUPPORTED;
+        if (t.rows > kMaxSide && t.cols > kMaxSide) return CCE_ERR_UNSUPPORTED;
+    }
+    return CCE_OK;
+}
+
+static int check_gradients(const cce_matrix* matrices, int64_t count) {
+    const int rc = check_sizes(matrices, count);
+    if (rc != CCE_OK) return rc;
+    for (int64_t i = 0; i < count; ++i) {
+        const cce_matrix& t = matrices[i];
+        if (t.rows == 0 || t.cols == 0) continue;
+        if (t.reserved != 0 || (t.grad_bf16 != 0 && t.grad_bf16 != 1)) return CCE_ERR_INVALID;
+        if (!t.grad || misaligned(t.grad, t.grad_bf16 ? 2 : 4)) return CCE_ERR_INVALID;
+    }
+    return CCE_OK;
+}
+
+// Whether the steps keep singular values that begin at 1 or below within what the scales hold.  A polynomial a x + b x^3 + c x^5 has its
+// largest value in [0, top] at an end or where its derivative a + 3 b y + 5 c y^2, y = x^2, is 0.
+static int check_coefficients(const float* coefficients, int steps) {
+    double top = 1.0;
+    for (int s = 0; s < steps; ++s) {
+        const double a = coefficients[3 * s], b = coefficients[3 * s + 1], c = coefficients[3 * s + 2];
+        if (!(isfinite(a) && isfinite(b) && isfinite(c))) return CCE_ERR_INVALID;
+        if (fabs(b) * top * top + fabs(c) * top * top * top * top > kMaxM) return CCE_ERR_UNSUPPORTED;
+        double at[3] = {top, 0.0, 0.0};
+        int n = 1;
+        const double root = 9.0 * b * b - 20.0 * a * c;
+        if (c != 0.0 && root >= 0.0) {
+            const double y0 = (-3.0 * b - sqrt(root)) / (10.0 * c), y1 = (-3.0 * b + sqrt(root)) / (10.0 * c);
+            if (y0 > 0.0 && y0 < top * top) at[n++] = sqrt(y0);
+            if (y1 > 0.0 && y1 < top * top) at[n++] = sqrt(y1);
+        } else if (c == 0.0 && b != 0.0) {
+            const double y = -a / (3.0 * b);
+            if (y > 0.0 && y < top * top) at[n++] = sqrt(y);
+        }
+        double next = 0.0;
+        for (int k = 0; k < n; ++k) {
+            const double x = at[k];
+            next = fmax(next, fabs(a * x + b * x * x * x + c * x * x * x * x * x));
+        }
+        if (next > kMaxSigma) return CCE_ERR_UNSUPPORTED;
+        top = fmax(next, 1e-6);
+    }
+    return CCE_OK;
+}
+
+static uint32_t sym_tiles(const NsLayout& at) {
+    const uint32_t n = (uint32_t)((at.rp + kNsTile - 1) / kNsTile);
+    return n * (n + 1) / 2;
+}
+static uint32_t apply_tiles(const NsLayout& at) {
+    return (uint32_t)((at.rp + kNsTile - 1) / kNsTile) * (uint32_t)((at.cp + kNsTile - 1) / kNsTile);
+}
+
+// The matrices from `i` on that share their launches; moves i behind them.  Returns their workspace.
+template <class Take>
+static int64_t next_group(const cce_matrix* matrices, int64_t count, int64_t& i, Take take) {
+    int64_t bytes = 0;
+    int n = 0;
+    for (; i < count && n < kGroup; ++i) {
+        const cce_matrix& t = matrices[i];
+        if (t.rows == 0 || t.cols == 0) continue;
+        const int64_t own = (int64_t)NsLayout((int)t.rows, (int)t.cols).bytes;
+        if (n != 0 && bytes + own > kGroupBytes) break;
+        take(n++, t, (uint64_t)bytes);
+        bytes += own;
+    }
+    return bytes;
+}
+
+static int run_groups(const cce_matrix* matrices, int64_t count, bool step, float lr, float mu, int nesterov, const float* coefficients,
+                      int steps, float eps, const float* clip_coef, void* workspace, hipStream_t stream) {
+    if (!hip_ok(hipFuncSetAttribute((const void*)ns_product_kernel<kGram>, hipFuncAttributeMaxDynamicSharedMemorySize, NsTile::kLdsBytes)) ||
+        !hip_ok(hipFuncSetAttribute((const void*)ns_product_kernel<kPoly>, hipFuncAttributeMaxDynamicSharedMemorySize, NsTile::kLdsBytes)) ||
+        !hip_ok(hipFuncSetAttribute((const void*)ns_product_kernel<kApply>, hipFuncAttributeMaxDynamicSharedMemorySize, NsTile::kLdsBytes)) ||
+        !hip_ok(hipFuncSetAttribute((const void*)ns_product_kernel<kLast>, hipFuncAttributeMaxDynamicSharedMemorySize, NsTile::kLdsBytes)))
+        return CCE_ERR_HIP;
+    NsArgs a;
+    a.ws = (char*)workspace;
+    a.clip_coef = clip_coef;
+    a.mu = mu;
+    a.nesterov = nesterov;
+    a.eps = eps;
+    for (int64_t i = 0; i < count;) {
+        uint32_t norm = 0, prep = 0, sym = 0, apply = 0;
+        a.count = 0;
+        next_group(matrices, count, i, [&](int n, const cce_matrix& t, uint64_t base) {
+            const NsLayout at((int)t.rows, (int)t.cols);
+            const float rate = lr * t.lr_scale;
+            a.t[n] = NsMatrix{t.grad, step ? t.momentum : nullptr, step ? t.param : nullptr, (uint16_t*)t.out_bf16, base,
+                              (int32_t)t.rows, (int32_t)t.cols, rate, 1.f - rate * t.weight_decay};
+            a.first_norm[n] = 2 * norm + (uint32_t)t.grad_bf16;
+            a.first_prep[n] = 2 * prep;
+            a.first_sym[n] = 2 * sym;
+            a.first_apply[n] = 2 * apply;
+            const int64_t parts = (t.rows * t.cols + kNormValues - 1) / kNormValues;
+            norm += (uint32_t)(parts < kNormParts ? parts : kNormParts);
+            prep += (uint32_t)(at.rp / 64) * (uint32_t)(at.cp / 64);
+            sym += sym_tiles(at);
+            apply += apply_tiles(at);
+            a.count = (uint32_t)n + 1;
+        });
+        if (a.count == 0) continue;
+        hipLaunchKernelGGL(ns_norm_kernel, dim3(norm), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL(ns_prep_kernel, dim3(prep), dim3(256), 0, stream, a);
+        for (int s = 0; s < steps; ++s) {
+            a.flip = (uint32_t)s & 1u;
+            a.a = coefficients[3 * s];
+            a.b = coefficients[3 * s + 1];
+            a.c = coefficients[3 * s + 2];
+            hipLaunchKernelGGL(ns_product_kernel<kGram>, dim3(sym), dim3(512), NsTile::kLdsBytes, stream, a);
+            hipLaunchKernelGGL(ns_product_kernel<kPoly>, dim3(sym), dim3(512), NsTile::kLdsBytes, stream, a);
+            if (s + 1 < steps) hipLaunchKernelGGL(ns_product_kernel<kApply>, dim3(apply), dim3(512), NsTile::kLdsBytes, stream, a);
+            else hipLaunchKernelGGL(ns_product_kernel<kLast>, dim3(apply), dim3(512), NsTile::kLdsBytes, stream, a);
+        }
+    }
+    return hip_ok(hipGetLastError()) ? CCE_OK : CCE_ERR_HIP;
+}
+
+static int check_steps(const cce_matrix* matrices, int64_t count, const float* coefficients, int32_t steps, float eps,
+                       const void* workspace, size_t workspace_bytes) {
+    if (!coefficients || steps < 1 || steps > CCE_NS_MAX_STEPS || !(eps >= 0.f)) return CCE_ERR_INVALID;
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < cce_muon_workspace_bytes(matrices, count)) return CCE_ERR_INVALID;
+    return check_coefficients(coefficients, steps);
+}
+
+}  // namespace cce
+
+using namespace cce;
+
+extern "C" {
+
+size_t cce_muon_workspace_bytes(const cce_matrix* matrices, int64_t count) {
+    if (check_sizes(matrices, count) != CCE_OK) return 0;
+    int64_t most = 256;
+    for (int64_t i = 0; i < count;) {
+        const int64_t bytes = next_group(matrices, count, i, [](int, const cce_matrix&, uint64_t) {});
+        most = bytes > most ? bytes : most;
+    }
+    return (size_t)most;
+}
+
+int cce_orthogonalize_multi(const cce_matrix* matrices, int64_t count, const float* coefficients, int32_t steps, float eps,
+                            void* workspace, size_t workspace_bytes, void* stream_) {
+    int rc = check_gradients(matrices, count);
+    if (rc == CCE_OK) rc = check_steps(matrices, count, coefficients, steps, eps, workspace, workspace_bytes);
+    if (rc != CCE_OK) return rc;
+    for (int64_t i = 0; i < count; ++i) {
+        const cce_matrix& t = matrices[i];
+        if (t.rows != 0 && t.cols != 0 && (!t.out_bf16 || misaligned(t.out_bf16, 2))) return CCE_ERR_INVALID;
+    }
+    (void)hipGetLastError();
+    return run_groups(matrices, count, false, 0.f, 0.f, 0, coefficients, steps, eps, nullptr, workspace, (hipStream_t)stream_);
+}
+
+int cce_muon_multi_step(const cce_matrix* matrices, int64_t count, float lr, float mu, int32_t nesterov,
+                        const float* coefficients, int32_t steps, float eps, const float* clip_coef,
+                        void* workspace, size_t workspace_bytes, void* stream_) {
+    int rc = check_gradients(matrices, count);
+    if (rc == CCE_OK) rc = check_steps(matrices, count, coefficients, steps, eps, workspace, workspace_bytes);
+    if (rc != CCE_OK) return rc;
+    if (!(lr >= 0.f && mu >= 0.f && mu < 1.f) || misaligned(clip_coef, 4)) return CCE_ERR_INVALID;
+    for (int64_t i = 0; i < count; ++i) {
+        const cce_matrix& t = matrices[i];
+        if (t.rows == 0 || t.cols == 0) continue;
+        if (!t.param || !t.momentum || misaligned(t.param, 4) || misaligned(t.momentum, 4) || misaligned(t.out_bf16, 2)) return CCE_ERR_INVALID;
+        if (!(t.lr_scale >= 0.f && t.weight_decay >= 0.f)) return CCE_ERR_INVALID;
+    }
+    (void)hipGetLastError();
+    return run_groups(matrices, count, true, lr, mu, nesterov != 0, coefficients, steps, eps, clip_coef, workspace, (hipStream_t)stream_);
+}
+
+}  // extern "C"
