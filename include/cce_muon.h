@@ -18,8 +18,8 @@
  * enqueued on an error (CCE_ERR_HIP: as in cce.h).
  *
  * `matrices` is a HOST array, read before the call returns and not kept.  count >= 1.  A matrix with rows = 0 or
- * cols = 0 takes no part and its pointers are not looked at.  CCE_ERR_UNSUPPORTED: rows * cols beyond 2^30, the smaller
- * side beyond 16384.  The memory of no two entries may overlap, nor the workspace any of it.
+ * cols = 0 takes no part and its pointers are not looked at.  CCE_ERR_UNSUPPORTED: rows * cols, both rounded up to multiples
+ * of 64, beyond 2^30, or the smaller side beyond 16384.  The memory of no two entries may overlap, nor the workspace any of it.
  */
 #ifndef CCE_MUON_H_
 #define CCE_MUON_H_

@@ -33,11 +33,11 @@ typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
 
 constexpr int kGroup = 48;                             // matrices of a launch: kernel arguments hold 4 KB
 constexpr int64_t kGroupBytes = (int64_t)1 << 30;      // workspace of a group of more than one matrix
-constexpr int64_t kMaxMatrix = (int64_t)1 << 30;       // values of a matrix: byte offsets of 16-bit values stay below 2^32
+constexpr int64_t kMaxMatrix = (int64_t)1 << 30;       // values of a padded matrix: byte offsets of 16-bit values stay below 2^32
 constexpr int64_t kMaxSide = 16384;                    // smaller side
 constexpr int kNormParts = 256;                        // partial sums of a matrix
 constexpr int kNormValues = 8192;                      // values of a part, more where that gives too many parts
-constexpr float kScaleX = 0x1p13f, kScaleA = 0x1p13f, kScaleM = 0x1p10f, kScaleL = 0x1p24f;
+constexpr float kScaleX = 0x1p13f, kScaleA = 0x1p13f, kScaleM = 0x1p10f, kScaleL = 0x1p18f;
 constexpr double kMaxSigma = 2.5, kMaxM = 60.0;
 
 struct NsMatrix {
@@ -71,16 +71,21 @@ struct NsLayout {
         c = rows < cols ? cols : rows;
         rp = (r + 63) & ~63;
         cp = (c + 63) & ~63;
-        const uint64_t x = (uint64_t)rp * cp * 2, s = (uint64_t)rp * rp * 2, d = (uint64_t)rp * 4;
+        const uint64_t x = (uint64_t)rp * cp * 2, s = (uint64_t)rp * rp * 2, p = (uint64_t)rp * panel_rows() * 2, d = (uint64_t)rp * 4;
         h[0] = 0;
         h[1] = x;
         l = 2 * x;
-        a = l + x;
+        a = l + x / 2;
         m = a + s;
-        da = m + s;
+        da = m + p;
         dm = da + d;
         partials = dm + d;
         bytes = partials + kNormParts * 8;
+    }
+    // M lies in panels of 32 columns, whose rows are padded to whole tiles
+    __host__ __device__ __forceinline__ int panel_rows() const { return (r + 127) & ~127; }
+    __device__ __forceinline__ uint32_t panel(int row, int col) const {
+        return (uint32_t)(col >> 5) * (uint32_t)panel_rows() * 32u + (uint32_t)row * 32u + (uint32_t)(col & 31);
     }
 };
 
@@ -172,14 +177,34 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(const NsArgs a) {
     if (threadIdx.x == 0) ((double*)(a.ws + t.base + NsLayout(t.rows, t.cols).partials))[part] = sum;
 }
 
-// x as h + l: h has x's first 11 bits, l the next ones.
-__device__ __forceinline__ void split4(const af32x4& x, f16x4& h, f16x4& l) {
+// x as h + l: h has x's first 11 bits, l, in E4M3, the next four.
+__device__ __forceinline__ float split1(float x, _Float16& h) {
+    const float s = x * kScaleX;
+    h = (_Float16)s;
+    return (s - (float)h) * (kScaleL / kScaleX);
+}
+__device__ __forceinline__ uint32_t pack_fp8(float a, float b, float c, float d) {
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+}
+__device__ __forceinline__ void split8(const float (&x)[8], f16x8& h, u32x2& l) {
+    float r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        _Float16 v;
+        r[e] = split1(x[e], v);
+        h[e] = v;
+    }
+    l = u32x2{pack_fp8(r[0], r[1], r[2], r[3]), pack_fp8(r[4], r[5], r[6], r[7])};
+}
+__device__ __forceinline__ void split4(const af32x4& x, f16x4& h, uint32_t& l) {
+    float r[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const float s = x[e] * kScaleX;
-        h[e] = (_Float16)s;
-        l[e] = (_Float16)((s - (float)h[e]) * (kScaleL / kScaleX));
+        _Float16 v;
+        r[e] = split1(x[e], v);
+        h[e] = v;
     }
+    l = pack_fp8(r[0], r[1], r[2], r[3]);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -204,7 +229,7 @@ __global__ __launch_bounds__(256) void ns_prep_kernel(const NsArgs a) {
     const int r0 = tall ? col0 : row0, c0 = tall ? row0 : col0;                // in the caller's matrix
     const int q = (threadIdx.x & 15) * 4;
     _Float16* const H = (_Float16*)(base + at.h[0]);
-    _Float16* const L = (_Float16*)(base + at.l);
+    uint8_t* const L = (uint8_t*)(base + at.l);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const int y = (int)(threadIdx.x >> 4) + 16 * k, row = r0 + y, col = c0 + q;
@@ -232,11 +257,12 @@ __global__ __launch_bounds__(256) void ns_prep_kernel(const NsArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) tile[y][q + e] = x[e];
         } else {
-            f16x4 h, l;
+            f16x4 h;
+            uint32_t l;
             split4(x, h, l);
             const uint32_t to = (uint32_t)(row0 + y) * (uint32_t)at.cp + (uint32_t)(col0 + q);
             *(f16x4*)(H + to) = h;
-            *(f16x4*)(L + to) = l;
+            *(uint32_t*)(L + to) = l;
         }
     }
     if (!tall) return;
@@ -244,20 +270,28 @@ __global__ __launch_bounds__(256) void ns_prep_kernel(const NsArgs a) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const int y = (int)(threadIdx.x >> 4) + 16 * k;
-        f16x4 h, l;
+        f16x4 h;
+        uint32_t l;
         split4(af32x4{tile[q][y], tile[q + 1][y], tile[q + 2][y], tile[q + 3][y]}, h, l);
         const uint32_t to = (uint32_t)(row0 + y) * (uint32_t)at.cp + (uint32_t)(col0 + q);
         *(f16x4*)(H + to) = h;
-        *(f16x4*)(L + to) = l;
+        *(uint32_t*)(L + to) = l;
     }
 }
 
 // ------------------------------------------------------------------------------------------
-// The products.
+// The products.  A wavefront's results go through LDS, 32 rows at a time, from the matrix instruction's layout (four rows of a
+// column a lane) to whole lines of rows: eight neighbouring values a lane.
 // ------------------------------------------------------------------------------------------
-typedef TileSmall NsTile;
-constexpr int kNsTile = NsTile::BM;
-static_assert(NsTile::BM == NsTile::BN, "square tiles: half of them mirrored");
+typedef TileCfg<2, 2, 2, 2, 2> SymTile;                // 128 x 128 by four wavefronts of 64 x 64, 2 x 32 KB stages: two workgroups a CU
+constexpr int kSymPitch = 64 + 4;                      // floats of a staged row
+constexpr int kSymMirror = 64 + 8;                     // 16-bit values of a staged row of the mirrored tile
+constexpr int kSymWave = 32 * kSymPitch * 4 + 64 * kSymMirror * 2;
+constexpr int kSymLds = 4 * kSymWave > SymTile::kLdsBytes ? 4 * kSymWave : SymTile::kLdsBytes;
+typedef TileDuo ApplyTile;                             // 256 columns of X x 128 rows
+constexpr int kApplyPitch = 128 + 4;
+constexpr int kApplyWave = 32 * kApplyPitch * 4;
+static_assert(4 * kApplyWave <= ApplyTile::kLdsBytes && 2 * kSymLds <= 160 * 1024 && 2 * ApplyTile::kLdsBytes <= 160 * 1024, "two workgroups a CU");
 
 // Tile w of the lower triangle, by rows.
 __device__ __forceinline__ void triangle(int w, int& i, int& j) {
@@ -267,126 +301,232 @@ __device__ __forceinline__ void triangle(int w, int& i, int& j) {
     j = w - i * (i + 1) / 2;
 }
 
-enum { kGram, kPoly, kApply, kLast };
+__device__ __forceinline__ void read8(const CCE_LDS float* p, float (&x)[8]) {
+    const f32x4 lo = *(const CCE_LDS f32x4*)p, hi = *(const CCE_LDS f32x4*)(p + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[e] = lo[e];
+        x[4 + e] = hi[e];
+    }
+}
 
-template <int OP>
-__global__ __launch_bounds__(512) void ns_product_kernel(const NsArgs a) {
+// A = X X^T (POLY = false) or M = b A + c A A, a tile and its mirror image.
+template <bool POLY>
+__global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(const NsArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
     CCE_LDS char* const smem = (CCE_LDS char*)smem_generic;
-    const uint32_t* const first = OP <= kPoly ? a.first_sym : a.first_apply;
     const uint32_t id = (uint32_t)xcd_linear_id((int)blockIdx.x, (int)gridDim.x);
-    const int i = matrix_of(first, (int)a.count, 2 * id + 1);
+    const int i = matrix_of(a.first_sym, (int)a.count, 2 * id + 1);
     const NsMatrix& t = a.t[i];
     const NsLayout at(t.rows, t.cols);
     char* const base = a.ws + t.base;
-    const int w = (int)(id - (first[i] >> 1));
-    const _Float16* const H = uniform((const _Float16*)(base + at.h[a.flip]));
     _Float16* const A = uniform((_Float16*)(base + at.a));
     _Float16* const M = uniform((_Float16*)(base + at.m));
     float* const da = (float*)(base + at.da);
     float* const dm = (float*)(base + at.dm);
-    f32x16 acc[NsTile::TM][NsTile::TN];
+    int ti, tj;
+    triangle((int)(id - (a.first_sym[i] >> 1)), ti, tj);
+    const int m0 = __builtin_amdgcn_readfirstlane(ti * SymTile::BM), n0 = __builtin_amdgcn_readfirstlane(tj * SymTile::BN);
+    f32x16 acc[SymTile::TM][SymTile::TN];
 #pragma unroll
-    for (int bm = 0; bm < NsTile::TM; ++bm)
+    for (int bm = 0; bm < SymTile::TM; ++bm)
 #pragma unroll
-        for (int bn = 0; bn < NsTile::TN; ++bn) acc[bm][bn] = f32x16{};
-    int m0, n0;
-    if (OP <= kPoly) {
-        int ti, tj;
-        triangle(w, ti, tj);
-        m0 = ti * kNsTile;
-        n0 = tj * kNsTile;
-        OperandTile<true, NsTile::BM> x, y;
-        const void* from = OP == kGram ? (const void*)H : (const void*)A;
-        const int k = OP == kGram ? at.cp : at.rp;
+        for (int bn = 0; bn < SymTile::TN; ++bn) acc[bm][bn] = f32x16{};
+    {
+        const _Float16* const from = POLY ? A : uniform((const _Float16*)(base + at.h[a.flip]));
+        const int k = POLY ? at.rp : at.cp;
+        OperandTile<true, SymTile::BM, 0, SymTile::NW, SymTile::BK> x, y;
         x.init(from, k, m0, at.rp, k);
         y.init(from, k, n0, at.rp, k);
-        gemm_mainloop<NsTile, true, true, false, true>(acc, x, y, k, smem);
-    } else {
-        const int tiles = (at.cp + kNsTile - 1) / kNsTile;
-        m0 = w % tiles * kNsTile;
-        n0 = w / tiles * kNsTile;
-        OperandTile<false, NsTile::BM> x;
-        OperandTile<true, NsTile::BN> y;
-        x.init(H, at.cp, m0, at.cp, at.rp);
-        y.init(M, at.rp, n0, at.rp, at.rp);
-        gemm_mainloop<NsTile, false, true, false, true>(acc, x, y, at.rp, smem);
+        gemm_mainloop<SymTile, true, true, true, true>(acc, x, y, k, smem);
     }
-    const int lane = threadIdx.x & 63;
-    const bool tall = t.rows > t.cols;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    CCE_LDS float* const rows = (CCE_LDS float*)(smem + wave * kSymWave);
+    CCE_LDS _Float16* const mirror = (CCE_LDS _Float16*)(smem + wave * kSymWave + 32 * kSymPitch * 4);
+    const int wm = m0 + wave_m<SymTile>() * 64, wn = n0 + wave_n<SymTile>() * 64;      // this wavefront's corner
+    const int q = (lane & 7) * 8;                                                      // this lane's columns
+    const int m = wm + q;
 #pragma unroll
-    for (int bm = 0; bm < NsTile::TM; ++bm)
+    for (int bn = 0; bn < SymTile::TN; ++bn) {
 #pragma unroll
-        for (int bn = 0; bn < NsTile::TN; ++bn)
+        for (int bm = 0; bm < SymTile::TM; ++bm)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                // four values in a row of the result: columns m .. m + 3 of row n
-                const int m = m0 + (wave_m<NsTile>() * NsTile::TM + bm) * 32 + 8 * g + 4 * (lane >> 5);
-                const int n = n0 + (wave_n<NsTile>() * NsTile::TN + bn) * 32 + (lane & 31);
-                const f32x16& s = acc[bm][bn];
-                if (OP <= kPoly) {
-                    if (m >= at.rp || n >= at.rp) continue;
-                    f16x4 v;
-                    if (OP == kGram) {
+            for (int g = 0; g < 4; ++g)
+                *(CCE_LDS f32x4*)(rows + (lane & 31) * kSymPitch + bm * 32 + 8 * g + 4 * (lane >> 5)) =
+                    f32x4{acc[bm][bn][4 * g], acc[bm][bn][4 * g + 1], acc[bm][bn][4 * g + 2], acc[bm][bn][4 * g + 3]};
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float x = s[4 * g + e] * (1.f / (kScaleX * kScaleX));
-                            if (m + e == n) da[n] = x;
-                            v[e] = m + e == n ? (_Float16)0.f : (_Float16)(x * kScaleA);
-                        }
-                    } else {
-                        const f16x4 o = *(const f16x4*)(A + (uint32_t)n * (uint32_t)at.rp + m);
-                        const af32x4 dr = *(const af32x4*)(da + m);
-                        const float dn = da[n];
+        for (int k = 0; k < 4; ++k) {
+            const int y = 8 * k + (lane >> 3), n = wn + bn * 32 + y;
+            const bool inside = n < at.rp && m < at.rp;
+            float x[8];
+            read8(rows + y * kSymPitch + q, x);
+            f16x8 v;
+            if (!POLY) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float p = s[4 * g + e] * (a.c / (kScaleA * kScaleA));
-                            const float x = (a.b + a.c * (dn + dr[e])) * ((float)o[e] * (1.f / kScaleA)) + p;
-                            if (m + e == n) dm[n] = a.b * dn + (a.c * dn * dn + p);
-                            v[e] = m + e == n ? (_Float16)0.f : (_Float16)(x * kScaleM);
-                        }
-                    }
-                    _Float16* const to = OP == kGram ? A : M;
-                    *(f16x4*)(to + (uint32_t)n * (uint32_t)at.rp + m) = v;
-                    if (m0 != n0)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) to[(uint32_t)(m + e) * (uint32_t)at.rp + n] = v[e];
-                } else {
-                    if (m >= at.cp || n >= at.rp) continue;
-                    const uint32_t j = (uint32_t)n * (uint32_t)at.cp + m;
-                    const f16x4 h = *(const f16x4*)(H + j);
-                    _Float16* const L = (_Float16*)(base + at.l);
-                    const f16x4 l = *(const f16x4*)(L + j);
-                    const float keep = a.a + dm[n];
-                    af32x4 x;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        x[e] = keep * ((float)h[e] * (1.f / kScaleX) + (float)l[e] * (1.f / kScaleL)) + s[4 * g + e] * (1.f / (kScaleX * kScaleM));
-                    if (OP == kApply) {
-                        f16x4 h1, l1;
-                        split4(x, h1, l1);
-                        *(f16x4*)((_Float16*)(base + at.h[a.flip ^ 1]) + j) = h1;
-                        *(f16x4*)(L + j) = l1;
-                    } else {
-                        if (n >= at.r) continue;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            if (m + e >= at.c) continue;
-                            const int64_t to = tall ? (int64_t)(m + e) * t.cols + n : (int64_t)n * t.cols + (m + e);
-                            float y = x[e];
-                            if (t.param) {
-                                y = t.param[to] * t.decay - t.lr * y;
-                                t.param[to] = y;
-                            }
-                            if (t.out) {
-                                union { __bf16 h; uint16_t u; } cv;
-                                cv.h = (__bf16)y;
-                                t.out[to] = cv.u;
-                            }
-                        }
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    const float s = x[e] * (1.f / (kScaleX * kScaleX));
+                    if (m + e == n && inside) da[n] = s;
+                    v[e] = m + e == n ? (_Float16)0.f : (_Float16)(s * kScaleA);
                 }
+                if (inside) *(f16x8*)(A + (uint32_t)n * (uint32_t)at.rp + m) = v;
+            } else if (inside) {
+                const f16x8 o = *(const f16x8*)(A + (uint32_t)n * (uint32_t)at.rp + m);
+                const float dn = da[n];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float p = x[e] * (a.c / (kScaleA * kScaleA));
+                    const float s = (a.b + a.c * (dn + da[m + e])) * ((float)o[e] * (1.f / kScaleA)) + p;
+                    if (m + e == n) dm[n] = a.b * dn + (a.c * dn * dn + p);
+                    v[e] = m + e == n ? (_Float16)0.f : (_Float16)(s * kScaleM);
+                }
+                *(f16x8*)(M + at.panel(n, m)) = v;
+            } else {
+                v = f16x8{};
             }
+            if (m0 != n0)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) mirror[(q + e) * kSymMirror + bn * 32 + y] = v[e];
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+    if (m0 == n0) return;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int y = 8 * k + (lane >> 3), row = wm + y, col = wn + q;                 // of the mirrored tile
+        const f16x8 v = *(const CCE_LDS f16x8*)(mirror + y * kSymMirror + q);
+        if (row < at.rp && col < at.rp) *(f16x8*)(POLY ? M + at.panel(row, col) : A + (uint32_t)row * (uint32_t)at.rp + col) = v;
+    }
+}
+
+__device__ __forceinline__ uint16_t bf16_bits(float x) {
+    union { __bf16 h; uint16_t u; } cv;
+    cv.h = (__bf16)x;
+    return cv.u;
+}
+
+// Four values of the result for the caller: into the parameters and their copy, or into the copy alone.  vec: all four are
+// there and lie where 16-byte (8-byte) accesses may be made.
+__device__ __forceinline__ void give4(const NsMatrix& t, int64_t to, af32x4 x, int count, bool vec) {
+    if (vec) {
+        if (t.param) {
+            const af32x4 p = *(const af32x4*)(t.param + to);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = p[e] * t.decay - t.lr * x[e];
+            *(af32x4*)(t.param + to) = x;
+        }
+        if (t.out) {
+            union { __bf16 h[4]; u32x2 u; } cv;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) cv.h[e] = (__bf16)x[e];
+            *(u32x2*)(t.out + to) = cv.u;
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (e >= count) continue;
+        float y = x[e];
+        if (t.param) {
+            y = t.param[to + e] * t.decay - t.lr * y;
+            t.param[to + e] = y;
+        }
+        if (t.out) t.out[to + e] = bf16_bits(y);
+    }
+}
+
+// X = (a + M) X; LAST: to the caller.
+template <bool LAST>
+__global__ __launch_bounds__(ApplyTile::kThreads, 2) void ns_apply_kernel(const NsArgs a) {
+    extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
+    CCE_LDS char* const smem = (CCE_LDS char*)smem_generic;
+    const uint32_t id = (uint32_t)xcd_linear_id((int)blockIdx.x, (int)gridDim.x);
+    const int i = matrix_of(a.first_apply, (int)a.count, 2 * id + 1);
+    const NsMatrix& t = a.t[i];
+    const NsLayout at(t.rows, t.cols);
+    char* const base = a.ws + t.base;
+    const int w = (int)(id - (a.first_apply[i] >> 1)), row_tiles = (at.rp + ApplyTile::BN - 1) / ApplyTile::BN;
+    const int m0 = __builtin_amdgcn_readfirstlane(w / row_tiles * ApplyTile::BM), n0 = __builtin_amdgcn_readfirstlane(w % row_tiles * ApplyTile::BN);
+    const _Float16* const H = uniform((const _Float16*)(base + at.h[a.flip]));
+    f32x16 acc[ApplyTile::TM][ApplyTile::TN];
+#pragma unroll
+    for (int bm = 0; bm < ApplyTile::TM; ++bm)
+#pragma unroll
+        for (int bn = 0; bn < ApplyTile::TN; ++bn) acc[bm][bn] = f32x16{};
+    {
+        OperandTile<false, ApplyTile::BM, 0, ApplyTile::NW, ApplyTile::BK> x;
+        PanelTile<true, ApplyTile::BN, ApplyTile::NW, ApplyTile::BK> y;
+        x.init(H, at.cp, m0, at.cp, at.rp);
+        y.init((const uint16_t*)uniform(base + at.m), (uint32_t)at.panel_rows() * 32u, n0, 0);
+        y.base = uniform(y.base);
+        gemm_mainloop<ApplyTile, false, true, true, true>(acc, x, y, at.rp, smem);
+    }
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    CCE_LDS float* const rows = (CCE_LDS float*)(smem + wave * kApplyWave);
+    const int wm = m0 + wave_m<ApplyTile>() * 128, wn = n0 + wave_n<ApplyTile>() * 64;
+    const int q = (lane & 15) * 8, m = wm + q;
+    const float* const dm = (const float*)(base + at.dm);
+    uint8_t* const L = (uint8_t*)(base + at.l);
+    _Float16* const H1 = (_Float16*)(base + at.h[a.flip ^ 1]);
+    const bool tall = t.rows > t.cols;
+    const bool vec = LAST && (t.cols & 3) == 0 && aligned(t.param, 16) && aligned(t.out, 8);
+#pragma unroll
+    for (int bn = 0; bn < ApplyTile::TN; ++bn) {
+#pragma unroll
+        for (int bm = 0; bm < ApplyTile::TM; ++bm)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *(CCE_LDS f32x4*)(rows + (lane & 31) * kApplyPitch + bm * 32 + 8 * g + 4 * (lane >> 5)) =
+                    f32x4{acc[bm][bn][4 * g], acc[bm][bn][4 * g + 1], acc[bm][bn][4 * g + 2], acc[bm][bn][4 * g + 3]};
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int y = 4 * k + (lane >> 4), n = wn + bn * 32 + y;
+            if (n >= at.rp || m >= at.cp) continue;
+            const uint32_t j = (uint32_t)n * (uint32_t)at.cp + m;
+            const f16x8 h = *(const f16x8*)(H + j);
+            const u32x2 l = *(const u32x2*)(L + j);
+            const float keep = a.a + dm[n];
+            float x[8];
+            read8(rows + y * kApplyPitch + q, x);
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const f32x2 r = e & 2 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)l[e >> 2], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)l[e >> 2], false);
+#pragma unroll
+                for (int f = 0; f < 2; ++f)
+                    x[e + f] = keep * ((float)h[e + f] * (1.f / kScaleX) + r[f] * (1.f / kScaleL)) + x[e + f] * (1.f / (kScaleX * kScaleM));
+            }
+            if (!LAST) {
+                f16x8 h1;
+                u32x2 l1;
+                split8(x, h1, l1);
+                *(f16x8*)(H1 + j) = h1;
+                *(u32x2*)(L + j) = l1;
+            } else if (tall) {
+                *(CCE_LDS f32x4*)(rows + y * kApplyPitch + q) = f32x4{x[0], x[1], x[2], x[3]};
+                *(CCE_LDS f32x4*)(rows + y * kApplyPitch + q + 4) = f32x4{x[4], x[5], x[6], x[7]};
+            } else if (n < at.r) {
+                const int64_t to = (int64_t)n * t.cols + m;
+#pragma unroll
+                for (int e = 0; e < 8; e += 4)
+                    if (m + e < at.c) give4(t, to + e, af32x4{x[e], x[e + 1], x[e + 2], x[e + 3]}, at.c - m - e, vec);
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (LAST && tall) {
+            const int z = (lane & 7) * 4, n = wn + bn * 32 + z;                       // four rows of X: neighbours of the caller's
+#pragma unroll 4
+            for (int k = 0; k < 16; ++k) {
+                const int y = 8 * k + (lane >> 3);
+                if (wm + y >= at.c || n >= at.r) continue;
+                af32x4 x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = rows[(z + e) * kApplyPitch + y];
+                give4(t, (int64_t)(wm + y) * t.cols + n, x, at.r - n, vec);
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
 }
 
 // ------------------------------------------------------------------------------------------
@@ -400,7 +540,7 @@ static int check_sizes(const cce_matrix* matrices, int64_t count) {
         const cce_matrix& t = matrices[i];
         if (t.rows < 0 || t.cols < 0) return CCE_ERR_INVALID;
         if (t.rows == 0 || t.cols == 0) continue;
-        if (t.rows > kMaxMatrix || t.cols > kMaxMatrix || t.rows * t.cols > kMaxMatrix) return CCE_ERR_UNSUPPORTED;
+        if (t.rows > kMaxMatrix || t.cols > kMaxMatrix || round_up(t.rows, 64) * round_up(t.cols, 64) > kMaxMatrix) return CCE_ERR_UNSUPPORTED;
         if (t.rows > kMaxSide && t.cols > kMaxSide) return CCE_ERR_UNSUPPORTED;
     }
     return CCE_OK;
@@ -449,12 +589,15 @@ static int check_coefficients(const float* coefficients, int steps) {
 }
 
 static uint32_t sym_tiles(const NsLayout& at) {
-    const uint32_t n = (uint32_t)((at.rp + kNsTile - 1) / kNsTile);
+    const uint32_t n = (uint32_t)((at.rp + SymTile::BM - 1) / SymTile::BM);
     return n * (n + 1) / 2;
 }
 static uint32_t apply_tiles(const NsLayout& at) {
-    return (uint32_t)((at.rp + kNsTile - 1) / kNsTile) * (uint32_t)((at.cp + kNsTile - 1) / kNsTile);
+    return (uint32_t)((at.rp + ApplyTile::BN - 1) / ApplyTile::BN) * (uint32_t)((at.cp + ApplyTile::BM - 1) / ApplyTile::BM);
 }
+
+template <class K>
+static bool allow_lds(K kernel, int bytes) { return hip_ok(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes)); }
 
 // The matrices from `i` on that share their launches; moves i behind them.  Returns their workspace.
 template <class Take>
@@ -474,10 +617,8 @@ static int64_t next_group(const cce_matrix* matrices, int64_t count, int64_t& i,
 
 static int run_groups(const cce_matrix* matrices, int64_t count, bool step, float lr, float mu, int nesterov, const float* coefficients,
                       int steps, float eps, const float* clip_coef, void* workspace, hipStream_t stream) {
-    if (!hip_ok(hipFuncSetAttribute((const void*)ns_product_kernel<kGram>, hipFuncAttributeMaxDynamicSharedMemorySize, NsTile::kLdsBytes)) ||
-        !hip_ok(hipFuncSetAttribute((const void*)ns_product_kernel<kPoly>, hipFuncAttributeMaxDynamicSharedMemorySize, NsTile::kLdsBytes)) ||
-        !hip_ok(hipFuncSetAttribute((const void*)ns_product_kernel<kApply>, hipFuncAttributeMaxDynamicSharedMemorySize, NsTile::kLdsBytes)) ||
-        !hip_ok(hipFuncSetAttribute((const void*)ns_product_kernel<kLast>, hipFuncAttributeMaxDynamicSharedMemorySize, NsTile::kLdsBytes)))
+    if (!allow_lds(ns_symmetric_kernel<false>, kSymLds) || !allow_lds(ns_symmetric_kernel<true>, kSymLds) ||
+        !allow_lds(ns_apply_kernel<false>, ApplyTile::kLdsBytes) || !allow_lds(ns_apply_kernel<true>, ApplyTile::kLdsBytes))
         return CCE_ERR_HIP;
     NsArgs a;
     a.ws = (char*)workspace;
@@ -512,10 +653,10 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
             a.a = coefficients[3 * s];
             a.b = coefficients[3 * s + 1];
             a.c = coefficients[3 * s + 2];
-            hipLaunchKernelGGL(ns_product_kernel<kGram>, dim3(sym), dim3(512), NsTile::kLdsBytes, stream, a);
-            hipLaunchKernelGGL(ns_product_kernel<kPoly>, dim3(sym), dim3(512), NsTile::kLdsBytes, stream, a);
-            if (s + 1 < steps) hipLaunchKernelGGL(ns_product_kernel<kApply>, dim3(apply), dim3(512), NsTile::kLdsBytes, stream, a);
-            else hipLaunchKernelGGL(ns_product_kernel<kLast>, dim3(apply), dim3(512), NsTile::kLdsBytes, stream, a);
+            hipLaunchKernelGGL(ns_symmetric_kernel<false>, dim3(sym), dim3(SymTile::kThreads), kSymLds, stream, a);
+            hipLaunchKernelGGL(ns_symmetric_kernel<true>, dim3(sym), dim3(SymTile::kThreads), kSymLds, stream, a);
+            if (s + 1 < steps) hipLaunchKernelGGL(ns_apply_kernel<false>, dim3(apply), dim3(ApplyTile::kThreads), ApplyTile::kLdsBytes, stream, a);
+            else hipLaunchKernelGGL(ns_apply_kernel<true>, dim3(apply), dim3(ApplyTile::kThreads), ApplyTile::kLdsBytes, stream, a);
         }
     }
     return hip_ok(hipGetLastError()) ? CCE_OK : CCE_ERR_HIP;
