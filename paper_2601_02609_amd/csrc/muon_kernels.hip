@@ -530,6 +530,292 @@ __global__ __launch_bounds__(ApplyTile::kThreads, 2) void ns_apply_kernel(const 
 }
 
 // ------------------------------------------------------------------------------------------
+// A matrix of few rows in one workgroup, all steps in one launch: X in fp32 in the accumulators (blocks of 16 x 16 by eight
+// wavefronts, block column j of wavefront w being 8 j + w), its h in LDS for the products.  The linear part a X needs no remainder here.
+//
+//   gram    wavefronts share the blocks of A, each over all columns of h
+//   poly    the same blocks; M takes A's place in LDS
+//   apply   each wavefront its own columns, which no other one reads: X stays in its registers
+//
+// The 17 launches of the tiled path take 115 us for 64 x 256 and 199 for 48 matrices of 16 x 896, mostly waiting for each other.
+// ------------------------------------------------------------------------------------------
+constexpr int kSmallThreads = 512;
+constexpr int kSmallMatrices = 48;
+
+struct NsSmallArgs {
+    NsMatrix t[kSmallMatrices];
+    uint64_t bf16;                                     // bit i: matrix i has a bf16 gradient
+    float coefficients[CCE_NS_MAX_STEPS][3];
+    const float* clip_coef;
+    float mu, eps;
+    int32_t nesterov, steps;
+};
+static_assert(sizeof(NsSmallArgs) <= 4096, "kernel arguments hold 4 KB");
+
+// RB blocks of 16 rows, up to NB block columns a wavefront.
+template <int RB_, int NB_>
+struct SmallShape {
+    static constexpr int RB = RB_, NB = NB_, kRows = 16 * RB_, kColumns = RB_ < 8 ? NB_ * 128 : 448;
+    static constexpr int kPitchA = kRows + 8;
+    static constexpr int pitch(int c) { return ((c + 63) & ~63) + 8; }
+    static constexpr int kStagePitch = 16 + 1, kStageBytes = kRows * kStagePitch * 4;      // a block column of a wavefront, on its way in or out
+    static constexpr int lds(int c) {
+        const int work = kRows * pitch(c) * 2 + kRows * kPitchA * 2 + kRows * 8, stages = 8 * kStageBytes;
+        return 64 + (work > stages ? work : stages);
+    }
+    static constexpr bool takes(int64_t r, int64_t c) { return r <= kRows && c <= kColumns; }
+};
+typedef SmallShape<2, 16> Small32;
+typedef SmallShape<4, 8> Small64;
+typedef SmallShape<8, 4> Small128;
+static_assert(Small32::lds(Small32::kColumns) <= 160 * 1024 && Small64::lds(Small64::kColumns) <= 160 * 1024 &&
+              Small128::lds(Small128::kColumns) <= 160 * 1024, "160 KB LDS");
+
+template <class S>
+__device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatrix& t, bool bf16, CCE_LDS char* smem) {
+    constexpr int RB = S::RB, NB = S::NB;
+    constexpr int kBlocks = RB * RB >= 8 ? RB * RB / 8 : 1;           // blocks of A a wavefront computes: of one row of blocks
+    const int r = t.rows < t.cols ? t.rows : t.cols, c = t.rows < t.cols ? t.cols : t.rows;
+    const bool tall = t.rows > t.cols;
+    const int columns = (c + 63) & ~63, block_columns = columns >> 4, pitch = columns + 8;
+    CCE_LDS double* const red = (CCE_LDS double*)smem;
+    CCE_LDS _Float16* const H = (CCE_LDS _Float16*)(smem + 64);
+    CCE_LDS _Float16* const A = H + S::kRows * pitch;
+    CCE_LDS float* const da = (CCE_LDS float*)(A + S::kRows * S::kPitchA);
+    CCE_LDS float* const dm = da + S::kRows;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int l16 = lane & 15, quad = lane >> 4;
+    const float clip = a.clip_coef ? a.clip_coef[0] : 1.f;
+    const bool vec_in = !tall && (t.cols & 3) == 0 && aligned(t.grad, bf16 ? 8 : 16) && aligned(t.momentum, 16);
+    const bool vec_out = !tall && (t.cols & 3) == 0 && aligned(t.param, 16) && aligned(t.out, 8);
+    // Where lines of the caller's memory and a lane's four columns do not meet, a block column goes through this wavefront's stage: element k
+    // of it is the k-th in the caller's order.
+    CCE_LDS float* const stage = (CCE_LDS float*)(smem + 64 + wave * S::kStageBytes);
+    auto staged = [&](int j, auto element) {
+#pragma nounroll
+        for (int k = lane; k < S::kRows * 16; k += 64) {
+            const int row = tall ? k & (S::kRows - 1) : k >> 4, in = tall ? k / S::kRows : k & 15, col = 16 * (8 * j + wave) + in;
+            if (row < r && col < c) element(tall ? (int64_t)col * t.cols + row : (int64_t)row * t.cols + col, stage[row * S::kStagePitch + in]);
+        }
+    };
+    // accumulator element e of block (rb, j): row 16 rb + l16, column 16 (8 j + wave) + 4 quad + e
+    f32x4 x[NB][RB];
+    double sum = 0.0;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) x[j][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (8 * j + wave >= block_columns) continue;
+        const int col = 16 * (8 * j + wave) + 4 * quad;
+        if (vec_in) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const int row = 16 * rb + l16;
+                if (row >= r || col >= c) continue;
+                const int at = row * t.cols + col;
+                f32x4 u = grad_values(t.grad, bf16, at);
+                if (t.momentum) {
+                    f32x4 m = *(const f32x4*)(t.momentum + at);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float g = u[e] * clip;
+                        m[e] = new_momentum(m[e], g, a.mu);
+                        u[e] = direction(m[e], g, a.mu, a.nesterov);
+                    }
+                    *(f32x4*)(t.momentum + at) = m;
+                }
+                x[j][rb] = u;
+            }
+        } else {
+            __builtin_amdgcn_wave_barrier();
+            staged(j, [&](int64_t at, CCE_LDS float& to) {
+                float g = grad_value(t.grad, bf16, at);
+                if (t.momentum) {
+                    g *= clip;
+                    const float m = new_momentum(t.momentum[at], g, a.mu);
+                    t.momentum[at] = m;
+                    g = direction(m, g, a.mu, a.nesterov);
+                }
+                to = g;
+            });
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const int row = 16 * rb + l16;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (row < r && col + e < c) x[j][rb][e] = stage[row * S::kStagePitch + 4 * quad + e];
+            }
+        }
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = fma((double)x[j][rb][e], (double)x[j][rb][e], sum);
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
+    if (lane == 0) red[wave] = sum;
+    __syncthreads();
+    sum = ((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]));
+    const double inv = sum <= 0x1.fffffffffffffp1023 ? 1.0 / (sqrt(sum) + (double)a.eps) : (double)NAN;
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const bool inside = 16 * rb + l16 < r;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)               // (zeros behind the edges also where inv is no number)
+                x[j][rb][e] = inside && 16 * (8 * j + wave) + 4 * quad + e < c ? (float)((double)x[j][rb][e] * inv) : 0.f;
+        }
+
+    const int bi = RB >= 4 ? wave * kBlocks / RB : wave / RB, bj = RB >= 4 ? wave * kBlocks % RB : wave % RB;      // this wavefront's blocks of A: (bi, bj ...)
+    const bool has_blocks = bi < RB;
+    const int frag = l16 * pitch + 8 * quad, frag_a = l16 * S::kPitchA + 8 * quad;
+    for (int s = 0; s < a.steps; ++s) {
+        const float ca = a.coefficients[s][0], cb = a.coefficients[s][1], cc = a.coefficients[s][2];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            if (8 * j + wave >= block_columns) continue;
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                f16x4 h;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[e] = (_Float16)(x[j][rb][e] * kScaleX);
+                *(CCE_LDS f16x4*)(H + (16 * rb + l16) * pitch + 16 * (8 * j + wave) + 4 * quad) = h;
+            }
+        }
+        __syncthreads();
+        f32x4 g[kBlocks], g1[kBlocks];
+        f16x4 o[kBlocks];
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) g[b] = g1[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (has_blocks) {
+            const CCE_LDS _Float16* const hm = H + 16 * bi * pitch + frag;
+            const CCE_LDS _Float16* const hn = H + 16 * bj * pitch + frag;
+            for (int k = 0; k < columns; k += 64) {
+                const f16x8 m = *(const CCE_LDS f16x8*)(hm + k), m1 = *(const CCE_LDS f16x8*)(hm + k + 32);
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) {
+                    g[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(m, *(const CCE_LDS f16x8*)(hn + 16 * b * pitch + k), g[b], 0, 0, 0);
+                    g1[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(m1, *(const CCE_LDS f16x8*)(hn + 16 * b * pitch + k + 32), g1[b], 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) g[b] += g1[b];
+            // element e of a block: column 16 bi + 4 quad + e of row 16 (bj + b) + l16
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float v = g[b][e] * (1.f / (kScaleX * kScaleX));
+                    const bool diagonal = 16 * bi + 4 * quad + e == 16 * (bj + b) + l16;
+                    if (diagonal) da[16 * bi + 4 * quad + e] = v;
+                    o[b][e] = diagonal ? (_Float16)0.f : (_Float16)(v * kScaleA);
+                }
+                *(CCE_LDS f16x4*)(A + (16 * (bj + b) + l16) * S::kPitchA + 16 * bi + 4 * quad) = o[b];
+            }
+        }
+        __syncthreads();
+        if (has_blocks) {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) g[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < S::kRows; k += 32) {
+                const f16x8 m = *(const CCE_LDS f16x8*)(A + 16 * bi * S::kPitchA + frag_a + k);
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+                    g[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(m, *(const CCE_LDS f16x8*)(A + 16 * (bj + b) * S::kPitchA + frag_a + k), g[b], 0, 0, 0);
+            }
+        }
+        __syncthreads();
+        if (has_blocks) {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+                const float dn = da[16 * (bj + b) + l16];
+                f16x4 m;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int col = 16 * bi + 4 * quad + e;
+                    const bool diagonal = col == 16 * (bj + b) + l16;
+                    const float p = g[b][e] * (cc / (kScaleA * kScaleA));
+                    const float v = (cb + cc * (dn + da[col])) * ((float)o[b][e] * (1.f / kScaleA)) + p;
+                    if (diagonal) dm[col] = cb * dn + (cc * dn * dn + p);
+                    m[e] = diagonal ? (_Float16)0.f : (_Float16)(v * kScaleM);
+                }
+                *(CCE_LDS f16x4*)(A + (16 * (bj + b) + l16) * S::kPitchA + 16 * bi + 4 * quad) = m;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const float keep = (ca + dm[16 * rb + l16]) * (kScaleX * kScaleM);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) x[j][rb] *= keep;
+        }
+#pragma unroll
+        for (int k = 0; k < S::kRows; k += 32) {
+            f16x8 m[RB];
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) m[rb] = *(const CCE_LDS f16x8*)(A + 16 * rb * S::kPitchA + frag_a + k);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                if (8 * j + wave >= block_columns) continue;
+                // transpose reads: 8 rows of a column a lane
+                const CCE_LDS _Float16* const p = H + (k + 8 * quad + (l16 >> 2)) * pitch + 16 * (8 * j + wave) + 4 * (l16 & 3);
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CCE_LDS s16x4*)p);
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CCE_LDS s16x4*)(p + 4 * pitch));
+                const f16x8 h = __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) x[j][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(h, m[rb], x[j][rb], 0, 0, 0);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) x[j][rb] *= 1.f / (kScaleX * kScaleM);
+    }
+    __syncthreads();                                   // the stages lie over other wavefronts' columns
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        if (8 * j + wave >= block_columns) continue;
+        const int col = 16 * (8 * j + wave) + 4 * quad;
+        if (vec_out) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const int row = 16 * rb + l16;
+                if (row < r && col < c) give4(t, row * t.cols + col, x[j][rb], 4, true);
+            }
+        } else {
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) stage[(16 * rb + l16) * S::kStagePitch + 4 * quad + e] = x[j][rb][e];
+            __builtin_amdgcn_wave_barrier();
+            staged(j, [&](int64_t at, CCE_LDS float& from) {
+                float y = from;
+                if (t.param) {
+                    y = t.param[at] * t.decay - t.lr * y;
+                    t.param[at] = y;
+                }
+                if (t.out) t.out[at] = bf16_bits(y);
+            });
+        }
+    }
+}
+
+__global__ __launch_bounds__(kSmallThreads, 2) void ns_small_kernel(const NsSmallArgs a) {
+    extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
+    CCE_LDS char* const smem = (CCE_LDS char*)smem_generic;
+    const NsMatrix& t = a.t[blockIdx.x];
+    const int r = t.rows < t.cols ? t.rows : t.cols, c = t.rows < t.cols ? t.cols : t.rows;
+    const bool bf16 = (a.bf16 >> blockIdx.x & 1u) != 0u;
+    if (Small32::takes(r, c)) small_matrix<Small32>(a, t, bf16, smem);
+    else if (Small64::takes(r, c)) small_matrix<Small64>(a, t, bf16, smem);
+    else small_matrix<Small128>(a, t, bf16, smem);
+}
+
+// ------------------------------------------------------------------------------------------
 // Host side.
 // ------------------------------------------------------------------------------------------
 static bool misaligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
@@ -599,6 +885,12 @@ static uint32_t apply_tiles(const NsLayout& at) {
 template <class K>
 static bool allow_lds(K kernel, int bytes) { return hip_ok(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes)); }
 
+// LDS of a matrix that a workgroup takes alone; 0 of one for the tiled launches.
+static int small_lds(const cce_matrix& t) {
+    const int64_t r = t.rows < t.cols ? t.rows : t.cols, c = t.rows < t.cols ? t.cols : t.rows;
+    return Small32::takes(r, c) ? Small32::lds((int)c) : Small64::takes(r, c) ? Small64::lds((int)c) : Small128::takes(r, c) ? Small128::lds((int)c) : 0;
+}
+
 // The matrices from `i` on that share their launches; moves i behind them.  Returns their workspace.
 template <class Take>
 static int64_t next_group(const cce_matrix* matrices, int64_t count, int64_t& i, Take take) {
@@ -606,7 +898,7 @@ static int64_t next_group(const cce_matrix* matrices, int64_t count, int64_t& i,
     int n = 0;
     for (; i < count && n < kGroup; ++i) {
         const cce_matrix& t = matrices[i];
-        if (t.rows == 0 || t.cols == 0) continue;
+        if (t.rows == 0 || t.cols == 0 || small_lds(t) != 0) continue;
         const int64_t own = (int64_t)NsLayout((int)t.rows, (int)t.cols).bytes;
         if (n != 0 && bytes + own > kGroupBytes) break;
         take(n++, t, (uint64_t)bytes);
@@ -615,11 +907,44 @@ static int64_t next_group(const cce_matrix* matrices, int64_t count, int64_t& i,
     return bytes;
 }
 
+static NsMatrix table_entry(const cce_matrix& t, bool step, float lr, uint64_t base) {
+    const float rate = lr * t.lr_scale;
+    return NsMatrix{t.grad, step ? t.momentum : nullptr, step ? t.param : nullptr, (uint16_t*)t.out_bf16, base,
+                    (int32_t)t.rows, (int32_t)t.cols, rate, 1.f - rate * t.weight_decay};
+}
+
+// The matrices that a workgroup takes alone.
+static bool run_small(const cce_matrix* matrices, int64_t count, bool step, float lr, float mu, int nesterov, const float* coefficients,
+                      int steps, float eps, const float* clip_coef, hipStream_t stream) {
+    NsSmallArgs a;
+    a.clip_coef = clip_coef;
+    a.mu = mu;
+    a.eps = eps;
+    a.nesterov = nesterov;
+    a.steps = steps;
+    for (int s = 0; s < 3 * steps; ++s) a.coefficients[s / 3][s % 3] = coefficients[s];
+    for (int64_t i = 0; i < count;) {
+        int n = 0, bytes = 0;
+        a.bf16 = 0;
+        for (; i < count && n < kSmallMatrices; ++i) {
+            const cce_matrix& t = matrices[i];
+            if (t.rows == 0 || t.cols == 0) continue;
+            const int own = small_lds(t);
+            if (own == 0) continue;
+            bytes = own > bytes ? own : bytes;
+            a.bf16 |= (uint64_t)t.grad_bf16 << n;
+            a.t[n++] = table_entry(t, step, lr, 0);
+        }
+        if (n == 0) continue;
+        if (!allow_lds(ns_small_kernel, 160 * 1024)) return false;
+        hipLaunchKernelGGL(ns_small_kernel, dim3((unsigned)n), dim3(kSmallThreads), bytes, stream, a);
+    }
+    return true;
+}
+
 static int run_groups(const cce_matrix* matrices, int64_t count, bool step, float lr, float mu, int nesterov, const float* coefficients,
                       int steps, float eps, const float* clip_coef, void* workspace, hipStream_t stream) {
-    if (!allow_lds(ns_symmetric_kernel<false>, kSymLds) || !allow_lds(ns_symmetric_kernel<true>, kSymLds) ||
-        !allow_lds(ns_apply_kernel<false>, ApplyTile::kLdsBytes) || !allow_lds(ns_apply_kernel<true>, ApplyTile::kLdsBytes))
-        return CCE_ERR_HIP;
+    if (!run_small(matrices, count, step, lr, mu, nesterov, coefficients, steps, eps, clip_coef, stream)) return CCE_ERR_HIP;
     NsArgs a;
     a.ws = (char*)workspace;
     a.clip_coef = clip_coef;
@@ -631,9 +956,7 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
         a.count = 0;
         next_group(matrices, count, i, [&](int n, const cce_matrix& t, uint64_t base) {
             const NsLayout at((int)t.rows, (int)t.cols);
-            const float rate = lr * t.lr_scale;
-            a.t[n] = NsMatrix{t.grad, step ? t.momentum : nullptr, step ? t.param : nullptr, (uint16_t*)t.out_bf16, base,
-                              (int32_t)t.rows, (int32_t)t.cols, rate, 1.f - rate * t.weight_decay};
+            a.t[n] = table_entry(t, step, lr, base);
             a.first_norm[n] = 2 * norm + (uint32_t)t.grad_bf16;
             a.first_prep[n] = 2 * prep;
             a.first_sym[n] = 2 * sym;
@@ -646,6 +969,9 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
             a.count = (uint32_t)n + 1;
         });
         if (a.count == 0) continue;
+        if (!allow_lds(ns_symmetric_kernel<false>, kSymLds) || !allow_lds(ns_symmetric_kernel<true>, kSymLds) ||
+            !allow_lds(ns_apply_kernel<false>, ApplyTile::kLdsBytes) || !allow_lds(ns_apply_kernel<true>, ApplyTile::kLdsBytes))
+            return CCE_ERR_HIP;
         hipLaunchKernelGGL(ns_norm_kernel, dim3(norm), dim3(256), 0, stream, a);
         hipLaunchKernelGGL(ns_prep_kernel, dim3(prep), dim3(256), 0, stream, a);
         for (int s = 0; s < steps; ++s) {

@@ -23,7 +23,8 @@ U = 2.0 ** -24
 ABC = (3.4445, -4.7750, 2.0315)
 EPS = 1e-7
 SHAPES = [(1, 1), (1, 7), (9, 1), (3, 5), (16, 16), (17, 129), (64, 64), (63, 65), (65, 63), (128, 300), (300, 128), (127, 511), (129, 257),
-          (192, 192), (256, 1024), (1024, 130), (16, 896), (896, 16), (33, 2049), (385, 641)]
+          (192, 192), (256, 1024), (1024, 130), (16, 896), (896, 16), (33, 2049), (385, 641), (32, 2048), (2000, 29), (31, 2052), (64, 1024), (1000, 50), (128, 448), (448, 100), (449, 128),
+          (97, 128), (65, 444), (2, 100)]
 
 
 @pytest.fixture(scope="module")
