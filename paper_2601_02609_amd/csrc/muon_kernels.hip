@@ -574,7 +574,8 @@ static_assert(Small32::lds(Small32::kColumns) <= 160 * 1024 && Small64::lds(Smal
 template <class S>
 __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatrix& t, bool bf16, CCE_LDS char* smem) {
     constexpr int RB = S::RB, NB = S::NB;
-    constexpr int kBlocks = RB * RB >= 8 ? RB * RB / 8 : 1;           // blocks of A a wavefront computes: of one row of blocks
+    constexpr int BI = RB == 8 ? 2 : 1, BJ = RB == 8 ? 4 : RB == 4 ? 2 : 1;        // blocks of A a wavefront computes
+    constexpr int kPerRow = RB / BJ;                                               // wavefronts beside each other
     const int r = t.rows < t.cols ? t.rows : t.cols, c = t.rows < t.cols ? t.cols : t.rows;
     const bool tall = t.rows > t.cols;
     const int columns = (c + 63) & ~63, block_columns = columns >> 4, pitch = columns + 8;
@@ -585,6 +586,8 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
     CCE_LDS float* const dm = da + S::kRows;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int l16 = lane & 15, quad = lane >> 4;
+    int mine = __builtin_amdgcn_readfirstlane((block_columns + 7 - wave) >> 3);       // this wavefront's block columns
+    const float coefficient = a.coefficients[0][lane < 3 * CCE_NS_MAX_STEPS ? lane : 0];
     const float clip = a.clip_coef ? a.clip_coef[0] : 1.f;
     const bool vec_in = !tall && (t.cols & 3) == 0 && aligned(t.grad, bf16 ? 8 : 16) && aligned(t.momentum, 16);
     const bool vec_out = !tall && (t.cols & 3) == 0 && aligned(t.param, 16) && aligned(t.out, 8);
@@ -605,7 +608,7 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
     for (int j = 0; j < NB; ++j) {
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) x[j][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (8 * j + wave >= block_columns) continue;
+        if (j >= mine) continue;
         const int col = 16 * (8 * j + wave) + 4 * quad;
         if (vec_in) {
 #pragma unroll
@@ -657,7 +660,8 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
     if (lane == 0) red[wave] = sum;
     __syncthreads();
     sum = ((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]));
-    const double inv = sum <= 0x1.fffffffffffffp1023 ? 1.0 / (sqrt(sum) + (double)a.eps) : (double)NAN;
+    // X scaled as its h is; M, whose rows are few, needs no scale
+    const double inv = sum <= 0x1.fffffffffffffp1023 ? (double)kScaleX / (sqrt(sum) + (double)a.eps) : (double)NAN;
 #pragma unroll
     for (int j = 0; j < NB; ++j)
 #pragma unroll
@@ -668,89 +672,124 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
                 x[j][rb][e] = inside && 16 * (8 * j + wave) + 4 * quad + e < c ? (float)((double)x[j][rb][e] * inv) : 0.f;
         }
 
-    const int bi = RB >= 4 ? wave * kBlocks / RB : wave / RB, bj = RB >= 4 ? wave * kBlocks % RB : wave % RB;      // this wavefront's blocks of A: (bi, bj ...)
+    const int bi = wave / kPerRow * BI, bj = wave % kPerRow * BJ;     // this wavefront's blocks of A: from (bi, bj) on
     const bool has_blocks = bi < RB;
     const int frag = l16 * pitch + 8 * quad, frag_a = l16 * S::kPitchA + 8 * quad;
+    // blocks (bi + y, bj + z) += P P^T over columns [0, n) of P, whose fragments lie at p
+    auto blocks_product = [&](f32x4 (&g)[BI][BJ], const CCE_LDS _Float16* p, int pitch_p, int k) {
+        f16x8 m[BI];
+#pragma unroll
+        for (int y = 0; y < BI; ++y) m[y] = *(const CCE_LDS f16x8*)(p + 16 * (bi + y) * pitch_p + k);
+#pragma unroll
+        for (int z = 0; z < BJ; ++z) {
+            const f16x8 n = *(const CCE_LDS f16x8*)(p + 16 * (bj + z) * pitch_p + k);
+#pragma unroll
+            for (int y = 0; y < BI; ++y) g[y][z] = __builtin_amdgcn_mfma_f32_16x16x32_f16(m[y], n, g[y][z], 0, 0, 0);
+        }
+    };
     for (int s = 0; s < a.steps; ++s) {
-        const float ca = a.coefficients[s][0], cb = a.coefficients[s][1], cc = a.coefficients[s][2];
+        auto of_lane = [&](int i) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(coefficient), i)); };
+        const float ca = of_lane(3 * s), cb = of_lane(3 * s + 1), cc = of_lane(3 * s + 2);
+        asm volatile("" : "+s"(mine));                // (comparisons with it are made where they are needed: kept over the loop they were spilled)
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            if (8 * j + wave >= block_columns) continue;
+            if (j >= mine) continue;
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
                 f16x4 h;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) h[e] = (_Float16)(x[j][rb][e] * kScaleX);
+                for (int e = 0; e < 4; ++e) h[e] = (_Float16)x[j][rb][e];
                 *(CCE_LDS f16x4*)(H + (16 * rb + l16) * pitch + 16 * (8 * j + wave) + 4 * quad) = h;
             }
         }
         __syncthreads();
-        f32x4 g[kBlocks], g1[kBlocks];
-        f16x4 o[kBlocks];
+        f32x4 g[BI][BJ];
+        f16x4 o[BI][BJ];
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) g[b] = g1[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int y = 0; y < BI; ++y)
+#pragma unroll
+            for (int z = 0; z < BJ; ++z) g[y][z] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (has_blocks) {
-            const CCE_LDS _Float16* const hm = H + 16 * bi * pitch + frag;
-            const CCE_LDS _Float16* const hn = H + 16 * bj * pitch + frag;
-            for (int k = 0; k < columns; k += 64) {
-                const f16x8 m = *(const CCE_LDS f16x8*)(hm + k), m1 = *(const CCE_LDS f16x8*)(hm + k + 32);
+            if constexpr (BI * BJ <= 2) {             // few products at a time: two sums of each
+                f32x4 g1[BI][BJ];
 #pragma unroll
-                for (int b = 0; b < kBlocks; ++b) {
-                    g[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(m, *(const CCE_LDS f16x8*)(hn + 16 * b * pitch + k), g[b], 0, 0, 0);
-                    g1[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(m1, *(const CCE_LDS f16x8*)(hn + 16 * b * pitch + k + 32), g1[b], 0, 0, 0);
+                for (int y = 0; y < BI; ++y)
+#pragma unroll
+                    for (int z = 0; z < BJ; ++z) g1[y][z] = f32x4{0.f, 0.f, 0.f, 0.f};
+                int k = 0;
+                for (; k + 64 < columns; k += 128) {
+                    blocks_product(g, H + frag, pitch, k);
+                    blocks_product(g1, H + frag, pitch, k + 32);
+                    blocks_product(g, H + frag, pitch, k + 64);
+                    blocks_product(g1, H + frag, pitch, k + 96);
+                }
+                if (k < columns) {
+                    blocks_product(g, H + frag, pitch, k);
+                    blocks_product(g1, H + frag, pitch, k + 32);
+                }
+#pragma unroll
+                for (int y = 0; y < BI; ++y)
+#pragma unroll
+                    for (int z = 0; z < BJ; ++z) g[y][z] += g1[y][z];
+            } else {
+                for (int k = 0; k < columns; k += 64) {
+                    blocks_product(g, H + frag, pitch, k);
+                    blocks_product(g, H + frag, pitch, k + 32);
                 }
             }
+            // element e of a block: column 16 (bi + y) + 4 quad + e of row 16 (bj + z) + l16
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) g[b] += g1[b];
-            // element e of a block: column 16 bi + 4 quad + e of row 16 (bj + b) + l16
+            for (int y = 0; y < BI; ++y)
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) {
+                for (int z = 0; z < BJ; ++z) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float v = g[b][e] * (1.f / (kScaleX * kScaleX));
-                    const bool diagonal = 16 * bi + 4 * quad + e == 16 * (bj + b) + l16;
-                    if (diagonal) da[16 * bi + 4 * quad + e] = v;
-                    o[b][e] = diagonal ? (_Float16)0.f : (_Float16)(v * kScaleA);
+                    for (int e = 0; e < 4; ++e) {
+                        const float v = g[y][z][e] * (1.f / (kScaleX * kScaleX));
+                        const bool diagonal = 16 * (bi + y) + 4 * quad + e == 16 * (bj + z) + l16;
+                        if (diagonal) da[16 * (bi + y) + 4 * quad + e] = v;
+                        o[y][z][e] = diagonal ? (_Float16)0.f : (_Float16)(v * kScaleA);
+                        g[y][z][e] = 0.f;
+                    }
+                    *(CCE_LDS f16x4*)(A + (16 * (bj + z) + l16) * S::kPitchA + 16 * (bi + y) + 4 * quad) = o[y][z];
                 }
-                *(CCE_LDS f16x4*)(A + (16 * (bj + b) + l16) * S::kPitchA + 16 * bi + 4 * quad) = o[b];
-            }
         }
         __syncthreads();
         if (has_blocks) {
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) g[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < S::kRows; k += 32) {
-                const f16x8 m = *(const CCE_LDS f16x8*)(A + 16 * bi * S::kPitchA + frag_a + k);
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b)
-                    g[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(m, *(const CCE_LDS f16x8*)(A + 16 * (bj + b) * S::kPitchA + frag_a + k), g[b], 0, 0, 0);
-            }
+            for (int k = 0; k < S::kRows; k += 32) blocks_product(g, A + frag_a, S::kPitchA, k);
         }
         __syncthreads();
         if (has_blocks) {
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) {
-                const float dn = da[16 * (bj + b) + l16];
-                f16x4 m;
+            for (int y = 0; y < BI; ++y) {
+                const f32x4 dc = *(const CCE_LDS f32x4*)(da + 16 * (bi + y) + 4 * quad);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int col = 16 * bi + 4 * quad + e;
-                    const bool diagonal = col == 16 * (bj + b) + l16;
-                    const float p = g[b][e] * (cc / (kScaleA * kScaleA));
-                    const float v = (cb + cc * (dn + da[col])) * ((float)o[b][e] * (1.f / kScaleA)) + p;
-                    if (diagonal) dm[col] = cb * dn + (cc * dn * dn + p);
-                    m[e] = diagonal ? (_Float16)0.f : (_Float16)(v * kScaleM);
+                for (int z = 0; z < BJ; ++z) {
+                    const float dn = da[16 * (bj + z) + l16];
+                    f16x4 m;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int col = 16 * (bi + y) + 4 * quad + e;
+                        const bool diagonal = col == 16 * (bj + z) + l16;
+                        const float p = g[y][z][e] * (cc / (kScaleA * kScaleA));
+                        const float v = (cb + cc * (dn + dc[e])) * ((float)o[y][z][e] * (1.f / kScaleA)) + p;
+                        if (diagonal) dm[col] = cb * dn + (cc * dn * dn + p);
+                        m[e] = diagonal ? (_Float16)0.f : (_Float16)v;
+                    }
+                    *(CCE_LDS f16x4*)(A + (16 * (bj + z) + l16) * S::kPitchA + 16 * (bi + y) + 4 * quad) = m;
                 }
-                *(CCE_LDS f16x4*)(A + (16 * (bj + b) + l16) * S::kPitchA + 16 * bi + 4 * quad) = m;
             }
         }
         __syncthreads();
+        asm volatile("" : "+s"(mine));
+        float keep[RB];
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            const float keep = (ca + dm[16 * rb + l16]) * (kScaleX * kScaleM);
+        for (int rb = 0; rb < RB; ++rb) keep[rb] = ca + dm[16 * rb + l16];
 #pragma unroll
-            for (int j = 0; j < NB; ++j) x[j][rb] *= keep;
+        for (int j = 0; j < NB; ++j) {
+            if (j >= mine) continue;
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) x[j][rb] *= keep[rb];
         }
 #pragma unroll
         for (int k = 0; k < S::kRows; k += 32) {
@@ -759,7 +798,7 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
             for (int rb = 0; rb < RB; ++rb) m[rb] = *(const CCE_LDS f16x8*)(A + 16 * rb * S::kPitchA + frag_a + k);
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
-                if (8 * j + wave >= block_columns) continue;
+                if (j >= mine) continue;
                 // transpose reads: 8 rows of a column a lane
                 const CCE_LDS _Float16* const p = H + (k + 8 * quad + (l16 >> 2)) * pitch + 16 * (8 * j + wave) + 4 * (l16 & 3);
                 const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CCE_LDS s16x4*)p);
@@ -769,16 +808,14 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
                 for (int rb = 0; rb < RB; ++rb) x[j][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(h, m[rb], x[j][rb], 0, 0, 0);
             }
         }
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) x[j][rb] *= 1.f / (kScaleX * kScaleM);
     }
     __syncthreads();                                   // the stages lie over other wavefronts' columns
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-        if (8 * j + wave >= block_columns) continue;
+        if (j >= mine) continue;
         const int col = 16 * (8 * j + wave) + 4 * quad;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) x[j][rb] *= 1.f / kScaleX;
         if (vec_out) {
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
