@@ -1,8 +1,8 @@
 // libcce, router of a mixture-of-experts layer: top-k experts, their weights and counts, balance and z loss, and the gradient of the
 // logits.  C ABI declared in include/cce_router.h.
 //
-// A row belongs to L lanes of a wavefront, each with VALUES neighbouring logits in registers; a wavefront takes 64 / L rows at a time
-// and walks the rows with a grid stride.
+// A row belongs to L lanes of a wavefront, each with VALUES logits in registers, 16 bytes of neighbours at a time (Columns); a wavefront
+// takes 64 / L rows at a time and walks the rows with a grid stride.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stddef.h>
@@ -16,10 +16,11 @@
 
 namespace cce {
 
-constexpr int kRouterThreads = 256;
-constexpr int kRouterWaves = kRouterThreads / 64;
-constexpr int kRouterBlocks = 512;                     // workgroups of the forward pass, each with one set of partial sums
-constexpr int kJoinExperts = 16;                       // experts of a workgroup that joins them
+constexpr int kRouterBlocks = 256;                     // workgroups of the forward pass, each with one set of partial sums: one a CU
+// Wavefronts of a workgroup: as many of 128 registers as a CU holds, half of them where the sums of each would fill the LDS.
+constexpr int router_waves(int lanes) { return lanes == 64 ? 8 : 16; }
+constexpr int kGradBlocks = 512;                       // workgroups of the backward pass: two a CU, several trips each
+constexpr int kJoinExperts = 8, kJoinParts = 256 / kJoinExperts;      // experts of a workgroup that joins them, threads of an expert
 
 struct RouterArgs {
     const void* logits;
@@ -76,41 +77,98 @@ __device__ __forceinline__ uint32_t lanes_min(uint32_t x) {
     return over_lanes<L>(x, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
 }
 template <int L>
+__device__ __forceinline__ float lanes_fmax(float x) {
+    return __uint_as_float(over_lanes<L>(__float_as_uint(x), [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
+}
+template <int L>
 __device__ __forceinline__ float lanes_sum(float x) {
     return __uint_as_float(over_lanes<L>(__float_as_uint(x), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
 }
 
-// VALUES logits from column `at` on of a row at `from`; -inf behind the row's end.  whole: the row's start and length allow
-// loads of as many bytes as a lane has.
-template <bool BF16, int VALUES>
-__device__ __forceinline__ void load_logits(const void* from, int64_t row, int E, int at, bool whole, float (&x)[VALUES]) {
-    constexpr int kBytes = VALUES * (BF16 ? 2 : 4);
-    if (kBytes >= 8 && whole && at < E) {
-        const char* p = (const char*)from + (row * E + at) * (BF16 ? 2 : 4);
-        if constexpr (BF16 && kBytes >= 8) {
+// The columns of a lane: value j of lane `sub` of a row.
+template <bool BF16, int L, int VALUES>
+struct Columns {
+    static constexpr int kVec = VALUES < (BF16 ? 8 : 4) ? VALUES : (BF16 ? 8 : 4), kGroups = VALUES / kVec;
+    static constexpr int of(int sub, int j) { return (j / kVec * L + sub) * kVec + j % kVec; }
+};
+
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+    union { __bf16 h[2]; uint32_t u; } cv;
+    cv.h[0] = (__bf16)lo;
+    cv.h[1] = (__bf16)hi;
+    return cv.u;
+}
+
+// A lane's logits of a row at `from` as they lie in memory, two bf16 values a word; -inf behind the row's end, and everywhere if not
+// read.  whole: the row's start and length allow 16-byte accesses.
+template <bool BF16, int L, int VALUES>
+struct RawLogits {
+    using C = Columns<BF16, L, VALUES>;
+    static constexpr int kWords = BF16 ? (VALUES + 1) / 2 : VALUES;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const void* from, int64_t row, int E, int sub, bool whole, bool read) {
 #pragma unroll
-            for (int j = 0; j < VALUES; j += 4) {
-                const uint2 v = *(const uint2*)(p + 2 * j);
-                x[j] = __uint_as_float(v.x << 16);
-                x[j + 1] = __uint_as_float(v.x & 0xffff0000u);
-                x[j + 2] = __uint_as_float(v.y << 16);
-                x[j + 3] = __uint_as_float(v.y & 0xffff0000u);
-            }
-        } else if constexpr (!BF16 && kBytes >= 8) {
+        for (int i = 0; i < kWords; ++i) w[i] = BF16 ? 0xff80ff80u : 0xff800000u;
+        if (!read) return;
+        if (C::kVec == (BF16 ? 8 : 4) && whole) {
+            const char* const p = (const char*)from + row * E * (BF16 ? 2 : 4);
 #pragma unroll
-            for (int j = 0; j < VALUES; j += 2) {
-                const float2 v = *(const float2*)(p + 4 * j);
-                x[j] = v.x;
-                x[j + 1] = v.y;
+            for (int g = 0; g < C::kGroups; ++g) {
+                const int at = C::of(sub, g * C::kVec);
+                if (at >= E) continue;
+                const au32x4 v = *(const au32x4*)(p + at * (BF16 ? 2 : 4));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[(4 * g + e) % kWords] = v[e];
             }
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < VALUES; ++j) {
+            const int at = C::of(sub, j);
+            if (at >= E) continue;
+            if (!BF16) w[j % kWords] = ((const uint32_t*)from)[row * E + at];
+            else {
+                const uint32_t u = ((const uint16_t*)from)[row * E + at];
+                w[j / 2] = j & 1 ? (w[j / 2] & 0xffffu) | u << 16 : (w[j / 2] & 0xffff0000u) | u;
+            }
+        }
+    }
+    __device__ __forceinline__ float value(int j) const {
+        if (!BF16) return __uint_as_float(w[j % kWords]);
+        return __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
+    }
+    // bf16: the values as 16-bit numbers around 2^15 in the same order, -0 as 0, two a word.
+    __device__ __forceinline__ uint32_t ordered(int i) const {
+        typedef __attribute__((ext_vector_type(2))) short s16x2;
+        const s16x2 u = __builtin_bit_cast(s16x2, w[i]), sign = u >> 15, m = u & (short)0x7fff;
+        return __builtin_bit_cast(uint32_t, (m ^ sign) - sign) ^ 0x80008000u;
+    }
+};
+
+template <bool BF16, int L, int VALUES>
+__device__ __forceinline__ void store_values(void* to, int64_t row, int E, int sub, bool whole, const float (&x)[VALUES]) {
+    using C = Columns<BF16, L, VALUES>;
+    if (C::kVec == (BF16 ? 8 : 4) && whole) {
+        char* const p = (char*)to + row * E * (BF16 ? 2 : 4);
+#pragma unroll
+        for (int g = 0; g < C::kGroups; ++g) {
+            const int at = C::of(sub, g * C::kVec);
+            if (at >= E) continue;
+            au32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = BF16 ? bf16_pair(x[(g * C::kVec + 2 * e) % VALUES], x[(g * C::kVec + 2 * e + 1) % VALUES])
+                            : __float_as_uint(x[(g * C::kVec + e) % VALUES]);
+            *(au32x4*)(p + at * (BF16 ? 2 : 4)) = v;
         }
         return;
     }
 #pragma unroll
     for (int j = 0; j < VALUES; ++j) {
-        if (at + j >= E) x[j] = -INFINITY;
-        else if (BF16) x[j] = __uint_as_float((uint32_t)((const uint16_t*)from)[row * E + at + j] << 16);
-        else x[j] = ((const float*)from)[row * E + at + j];
+        const int at = C::of(sub, j);
+        if (at >= E) continue;
+        if (BF16) ((uint16_t*)to)[row * E + at] = (uint16_t)bf16_pair(x[j], 0.f);
+        else ((float*)to)[row * E + at] = x[j];
     }
 }
 
@@ -137,82 +195,179 @@ __device__ __forceinline__ void write_losses(const RouterArgs& a, double balance
     a.losses[1] = (float)(z / rows);
 }
 
-template <bool BF16, int L, int VALUES>
-__global__ __launch_bounds__(kRouterThreads) void router_forward_kernel(const RouterArgs a) {
+// Sorting networks: x[0] the largest.  Of x whose first half falls and whose second half rises (or any rotation of that) the
+// last log2 N steps are enough.
+template <int N, bool MERGE>
+__device__ __forceinline__ void sort_falling(uint32_t* x) {
+#pragma unroll
+    for (int size = MERGE ? N : 2; size <= N; size *= 2)
+#pragma unroll
+        for (int step = size / 2; step >= 1; step /= 2)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int k = i ^ step;
+                if (k < i) continue;
+                const uint32_t a = x[i], b = x[k], most = a > b ? a : b, least = a > b ? b : a;
+                const bool falls = size == N || (i & size) == 0;
+                x[i] = falls ? most : least;
+                x[k] = falls ? least : most;
+            }
+}
+
+// The K largest of a row's keys, falling, in every lane of the row: each lane's own, then lists merged with other lanes'.  The
+// larger of a falling list and another one read backwards are the K largest of both.
+template <int K, int L, int STEP = 1>
+__device__ __forceinline__ void merge_lanes(uint32_t (&list)[K]) {
+    if constexpr (STEP < L) {
+        uint32_t other[K];
+#pragma unroll
+        for (int i = 0; i < K; ++i) other[i] = other_lane<STEP>(list[i]);
+#pragma unroll
+        for (int i = 0; i < K; ++i) list[i] = list[i] > other[K - 1 - i] ? list[i] : other[K - 1 - i];
+        sort_falling<K, true>(list);
+        merge_lanes<K, L, STEP * 2>(list);
+    }
+}
+template <int K, int VALUES>
+__device__ __forceinline__ void own_largest(const uint32_t (&key)[VALUES], uint32_t (&list)[K]) {
+#pragma unroll
+    for (int g = 0; g < VALUES; g += K) {
+        uint32_t part[K];
+#pragma unroll
+        for (int i = 0; i < K; ++i) part[i] = g + i < VALUES ? key[(g + i) % VALUES] : 0u;
+        sort_falling<K, false>(part);
+        if (g == 0) {
+#pragma unroll
+            for (int i = 0; i < K; ++i) list[i] = part[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < K; ++i) list[i] = list[i] > part[K - 1 - i] ? list[i] : part[K - 1 - i];
+            sort_falling<K, true>(list);
+        }
+    }
+}
+
+// TOP > 0 (bf16, k <= TOP): a logit and its column make one 32-bit key, and the TOP largest of a row come out of sorting networks;
+// 0, and rows that hold a NaN or +inf: k rounds of a maximum over the row.  65536 x 256 bf16, k = 8: rounds 53 us, networks see below.
+template <bool BF16, int L, int VALUES, int TOP>
+__global__ __launch_bounds__(64 * router_waves(L), 4) void router_forward_kernel(const RouterArgs a) {
+    using C = Columns<BF16, L, VALUES>;
     constexpr int kRows = 64 / L;                                     // of a wavefront
-    constexpr int kSlots = (CCE_ROUTER_MAX_TOP_K + L - 1) / L;        // chosen experts a lane keeps
+    constexpr int kRouterWaves = router_waves(L), kRouterThreads = 64 * kRouterWaves;
+    constexpr int kSlots = TOP ? 1 : (CCE_ROUTER_MAX_TOP_K + L - 1) / L;      // chosen experts a lane keeps
     constexpr int kColumns = L * VALUES;
+    static_assert(TOP <= L && (TOP == 0 || BF16), "a lane for each chosen expert");
     __shared__ int32_t count[kColumns];
     __shared__ float sums[kRouterWaves][kColumns];
     __shared__ double zs[kRouterWaves];
     __shared__ int32_t ns[kRouterWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane & (L - 1), at = sub * VALUES;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane & (L - 1);
     for (int e = threadIdx.x; e < kColumns; e += kRouterThreads) count[e] = 0;
     __syncthreads();
-    const bool whole = a.E % VALUES == 0 && ((uintptr_t)a.logits & 15) == 0;
+    const bool whole = a.E % C::kVec == 0 && ((uintptr_t)a.logits & 15) == 0;
     float total_p[VALUES];
 #pragma unroll
     for (int j = 0; j < VALUES; ++j) total_p[j] = 0.f;
     double z = 0.0;
     int rows = 0;
     const int64_t step = (int64_t)gridDim.x * kRouterWaves * kRows;
-    for (int64_t first = ((int64_t)blockIdx.x * kRouterWaves + wave) * kRows; first < a.N; first += step) {
+    // the labels two trips ahead, the logits one: nothing of a trip waits for memory
+    auto taken_row = [&](int64_t row) { return row < a.N && !(a.labels && a.labels[row] == a.ignore_index); };
+    const int64_t begin = ((int64_t)blockIdx.x * kRouterWaves + wave) * kRows;
+    RawLogits<BF16, L, VALUES> ahead;
+    ahead.load(a.logits, begin + lane / L, a.E, sub, whole, taken_row(begin + lane / L));
+    bool read_next = taken_row(begin + step + lane / L);
+    for (int64_t first = begin; first < a.N; first += step) {
         const int64_t row = first + lane / L;
-        const bool there = row < a.N, read = there && !(a.labels && a.labels[row] == a.ignore_index);
+        const bool there = row < a.N;
+        const RawLogits<BF16, L, VALUES> raw = ahead;
         float x[VALUES];
-        if (read) load_logits<BF16, VALUES>(a.logits, row, a.E, at, whole, x);
-        else {
 #pragma unroll
-            for (int j = 0; j < VALUES; ++j) x[j] = -INFINITY;
-        }
-        uint32_t rank[VALUES], best = 0u;
+        for (int j = 0; j < VALUES; ++j) x[j] = raw.value(j);
+        ahead.load(a.logits, row + step, a.E, sub, whole, read_next);
+        read_next = taken_row(row + 2 * step);
+        float most_x = x[0];
 #pragma unroll
-        for (int j = 0; j < VALUES; ++j) {
-            rank[j] = rank_of(x[j]);
-            best = rank[j] > best ? rank[j] : best;
-        }
-        uint32_t most = lanes_max<L>(best);
-        const bool live = most != 0u;
-        const float top = live ? value_of(most) : 0.f;
+        for (int j = 1; j < VALUES; ++j) most_x = fmaxf(most_x, x[j]);
+        most_x = lanes_fmax<L>(most_x);
+        bool live = most_x > -INFINITY;
+        float top = live ? most_x : 0.f;
         float p[VALUES], part = 0.f;
 #pragma unroll
         for (int j = 0; j < VALUES; ++j) {
             p[j] = __expf(x[j] - top);
             part += p[j];
         }
-        const float total = lanes_sum<L>(part), inv = live ? 1.f / total : 0.f;
-        const float lse = live ? top + __logf(total) : 0.f;
-#pragma unroll
-        for (int j = 0; j < VALUES; ++j) total_p[j] += live ? p[j] * inv : 0.f;
+        float total = lanes_sum<L>(part);
         int index[kSlots];
         float weight[kSlots], chosen = 0.f;
-#pragma unroll
-        for (int q = 0; q < kSlots; ++q) {
-            index[q] = -1;
-            weight[q] = 0.f;
-            for (int s = 0; s < L && q * L + s < a.k; ++s) {
-                // the largest rank left, its first column, and both out of the running
-                uint32_t mine = (uint32_t)kColumns;
-#pragma unroll
-                for (int j = VALUES - 1; j >= 0; --j) mine = rank[j] == most ? (uint32_t)(at + j) : mine;
-                const uint32_t column = lanes_min<L>(mine);
-                const bool taken = most != 0u;
-                const float w = taken ? __expf(value_of(most) - top) : 0.f;
-                chosen += w;
-                if (sub == s) {
-                    index[q] = taken ? (int)column : -1;
-                    weight[q] = w;
-                }
-                best = 0u;
+        bool rounds = TOP == 0;
+        if constexpr (TOP != 0) rounds = __ballot(total != total) != 0;          // a NaN, or +inf less itself, in one of the rows
+        if constexpr (TOP != 0) {
+            if (!rounds) {
+                uint32_t key[VALUES], list[TOP];
 #pragma unroll
                 for (int j = 0; j < VALUES; ++j) {
-                    rank[j] = column == (uint32_t)(at + j) ? 0u : rank[j];
-                    best = rank[j] > best ? rank[j] : best;
+                    const uint32_t pair = raw.ordered(j / 2);
+                    key[j] = (j & 1 ? pair & 0xffff0000u : pair << 16) | (uint32_t)(0xffff - C::of(sub, j));
                 }
-                most = lanes_max<L>(best);
+                own_largest<TOP, VALUES>(key, list);
+                merge_lanes<TOP, L>(list);
+                uint32_t mine = 0u;
+#pragma unroll
+                for (int i = 0; i < TOP; ++i) mine = sub == i ? list[i] : mine;
+                // 0x8000 - 0x7f80: -inf
+                const bool taken = sub < a.k && (mine >> 16) > 0x80u;
+                const int32_t v = (int32_t)(mine >> 16) - 0x8000, magnitude = v < 0 ? -v : v;
+                index[0] = taken ? (int)(0xffffu - (mine & 0xffffu)) : -1;
+                weight[0] = taken ? __expf(__uint_as_float((uint32_t)magnitude << 16 | (v < 0 ? 0x80000000u : 0u)) - top) : 0.f;
+                chosen = lanes_sum<L>(weight[0]);
             }
         }
-        const float norm = a.renormalize ? (live ? 1.f / chosen : 0.f) : inv;
+        if (rounds) {
+            uint32_t rank[VALUES], best = 0u;
+#pragma unroll
+            for (int j = 0; j < VALUES; ++j) {
+                rank[j] = rank_of(x[j]);
+                best = rank[j] > best ? rank[j] : best;
+            }
+            uint32_t most = lanes_max<L>(best);
+            live = most != 0u;                                        // (also of a row of NaN)
+            chosen = 0.f;
+            if (live) top = value_of(most);
+            if (total != total) total = __uint_as_float(0x7fc00000u);
+#pragma unroll
+            for (int q = 0; q < kSlots; ++q) {
+                index[q] = -1;
+                weight[q] = 0.f;
+                for (int s = 0; s < L && q * L + s < a.k; ++s) {
+                    // the largest rank left, its first column, and both out of the running
+                    uint32_t mine = (uint32_t)kColumns;
+#pragma unroll
+                    for (int j = VALUES - 1; j >= 0; --j) mine = rank[j] == most ? (uint32_t)C::of(sub, j) : mine;
+                    const uint32_t column = lanes_min<L>(mine);
+                    const bool taken = most != 0u;
+                    const float w = taken ? __expf(value_of(most) - top) : 0.f;
+                    chosen += w;
+                    if (sub == s) {
+                        index[q] = taken ? (int)column : -1;
+                        weight[q] = w;
+                    }
+                    best = 0u;
+#pragma unroll
+                    for (int j = 0; j < VALUES; ++j) {
+                        rank[j] = column == (uint32_t)C::of(sub, j) ? 0u : rank[j];
+                        best = rank[j] > best ? rank[j] : best;
+                    }
+                    most = lanes_max<L>(best);
+                }
+            }
+        }
+        const float inv = live ? __builtin_amdgcn_rcpf(total) : 0.f;              // (a row that takes no part: p is 0)
+        const float lse = live ? top + __logf(total) : 0.f;
+#pragma unroll
+        for (int j = 0; j < VALUES; ++j) total_p[j] = fmaf(p[j], inv, total_p[j]);
+        const float norm = a.renormalize ? (live ? __builtin_amdgcn_rcpf(chosen) : 0.f) : inv;
 #pragma unroll
         for (int q = 0; q < kSlots; ++q) {
             const int s = q * L + sub;
@@ -232,7 +387,7 @@ __global__ __launch_bounds__(kRouterThreads) void router_forward_kernel(const Ro
     for (int j = 0; j < VALUES; ++j) {
 #pragma unroll
         for (int o = L; o < 64; o *= 2) total_p[j] += __shfl_xor(total_p[j], o);
-        if (lane < L) sums[wave][at + j] = total_p[j];
+        if (lane < L) sums[wave][C::of(sub, j)] = total_p[j];
     }
 #pragma unroll
     for (int o = L; o < 64; o *= 2) {
@@ -280,35 +435,54 @@ __global__ __launch_bounds__(kRouterThreads) void router_forward_kernel(const Ro
     if (lane == 0) zs[wave] = balance;
     __syncthreads();
     if (threadIdx.x == 0) {
+        balance = 0.0;
+#pragma unroll
+        for (int w = 0; w < kRouterWaves; ++w) balance += zs[w];
         a.counts[a.E] = group_rows;
-        write_losses(a, (zs[0] + zs[1]) + (zs[2] + zs[3]), group_z, group_rows);
+        write_losses(a, balance, group_z, group_rows);
     }
 }
 
-// Joins the workgroups' sums: kJoinExperts experts a workgroup, 16 threads an expert; the last workgroup to end forms the losses.
+// Joins the workgroups' sums: kJoinExperts experts a workgroup, kJoinParts threads an expert, all loads in flight; the last
+// workgroup to end forms the losses.
 __global__ __launch_bounds__(256) void router_join_kernel(const RouterArgs a) {
     __shared__ double red[256];
     __shared__ int32_t redn[256];
     __shared__ int32_t last;
-    const int e = (int)blockIdx.x * kJoinExperts + (int)(threadIdx.x & 15), part = (int)(threadIdx.x >> 4);
+    const int of = (int)threadIdx.x % kJoinExperts, part = (int)threadIdx.x / kJoinExperts, e = (int)blockIdx.x * kJoinExperts + of;
+    constexpr int kLoads = kRouterBlocks / kJoinParts;
+    static_assert(kRouterBlocks == 256, "a thread for each workgroup's z");
+    float x[kLoads];
+    int n[kLoads];
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+        const int at = part + u * kJoinParts;
+        const bool there = at < a.blocks && e < a.E;
+        x[u] = there ? a.part_sums[(int64_t)at * a.E + e] : 0.f;
+        n[u] = there ? a.part_counts[(int64_t)at * a.E + e] : 0;
+    }
+    double z = (int)threadIdx.x < a.blocks ? a.part_z[threadIdx.x] : 0.0;
+    int rows = (int)threadIdx.x < a.blocks ? a.part_rows[threadIdx.x] : 0;
     double sum = 0.0;
     int count = 0;
-    if (e < a.E) {
-        for (int b = part; b < a.blocks; b += 16) {
-            sum += (double)a.part_sums[(int64_t)b * a.E + e];
-            count += a.part_counts[(int64_t)b * a.E + e];
-        }
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+        sum += (double)x[u];
+        count += n[u];
     }
     red[threadIdx.x] = sum;
     redn[threadIdx.x] = count;
     __syncthreads();
-    if (threadIdx.x < 16 && e < a.E) {
-        for (int p = 1; p < 16; ++p) {
-            sum += red[16 * p + threadIdx.x];
-            count += redn[16 * p + threadIdx.x];
+    for (int half = 128; half >= kJoinExperts; half >>= 1) {
+        if ((int)threadIdx.x < half) {
+            red[threadIdx.x] += red[threadIdx.x + half];
+            redn[threadIdx.x] += redn[threadIdx.x + half];
         }
-        __hip_atomic_store(a.prob_sums + e, (float)sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_store(a.counts + e, count, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+    }
+    if (threadIdx.x < kJoinExperts && e < a.E) {
+        __hip_atomic_store(a.prob_sums + e, (float)red[threadIdx.x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(a.counts + e, redn[threadIdx.x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __threadfence();
     __syncthreads();
@@ -316,15 +490,10 @@ __global__ __launch_bounds__(256) void router_join_kernel(const RouterArgs a) {
     __syncthreads();
     if (!last) return;
     __threadfence();
-    double balance = 0.0, z = 0.0;
-    int rows = 0;
+    double balance = 0.0;
     for (int i = threadIdx.x; i < a.E; i += 256)
         balance += (double)__hip_atomic_load(a.counts + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) *
                    (double)__hip_atomic_load(a.prob_sums + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    for (int b = threadIdx.x; b < a.blocks; b += 256) {
-        z += a.part_z[b];
-        rows += a.part_rows[b];
-    }
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) {
         balance += __shfl_xor(balance, o);
@@ -351,14 +520,15 @@ __global__ __launch_bounds__(256) void router_join_kernel(const RouterArgs a) {
 // row's chosen p and T that of p dw; the latter parts' share of sum p d is T, or 0 (T / S - S T / S^2).
 // ------------------------------------------------------------------------------------------
 template <bool BF16, int L, int VALUES>
-__global__ __launch_bounds__(kRouterThreads) void router_backward_kernel(const RouterGradArgs a) {
-    constexpr int kRows = 64 / L;
+__global__ __launch_bounds__(512, 4) void router_backward_kernel(const RouterGradArgs a) {
+    using C = Columns<BF16, L, VALUES>;
+    constexpr int kRows = 64 / L, kRouterWaves = 8;
     constexpr int kSlots = (CCE_ROUTER_MAX_TOP_K + L - 1) / L;
     constexpr int kColumns = L * VALUES;
-    __shared__ float chosen_d[kRouterWaves * kRows][kColumns];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane & (L - 1), at = sub * VALUES;
+    __shared__ float chosen_d[kRouterWaves * kRows][kColumns];      // 16 to 32 KB
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane & (L - 1);
     float* const mine = chosen_d[wave * kRows + lane / L];
-    const bool whole = a.E % VALUES == 0 && (((uintptr_t)a.logits | (uintptr_t)a.d_logits) & 15) == 0;
+    const bool whole = a.E % C::kVec == 0 && (((uintptr_t)a.logits | (uintptr_t)a.d_logits) & 15) == 0;
     float share[VALUES];                                              // beta c_e
     const int n = a.counts[a.E];
     const double rows = n > 0 ? (double)n : 1.0;
@@ -366,20 +536,21 @@ __global__ __launch_bounds__(kRouterThreads) void router_backward_kernel(const R
     const float gamma = a.d_losses ? (float)(2.0 * (double)a.d_losses[1] / rows) : 0.f;
 #pragma unroll
     for (int j = 0; j < VALUES; ++j) {
-        share[j] = at + j < a.E ? beta * (float)a.counts[at + j] : 0.f;
-        mine[at + j] = 0.f;
+        share[j] = C::of(sub, j) < a.E ? beta * (float)a.counts[C::of(sub, j)] : 0.f;
+        mine[C::of(sub, j)] = 0.f;
     }
     const int64_t step = (int64_t)gridDim.x * kRouterWaves * kRows;
-    for (int64_t first = ((int64_t)blockIdx.x * kRouterWaves + wave) * kRows; first < a.N; first += step) {
+    const int64_t begin = ((int64_t)blockIdx.x * kRouterWaves + wave) * kRows;
+    // a trip's first index, by which its loads go, one trip ahead
+    auto first_index = [&](int64_t row) { return row < a.N ? a.indices[row * a.k] : -1; };
+    int next = first_index(begin + lane / L);
+    for (int64_t first = begin; first < a.N; first += step) {
         const int64_t row = first + lane / L;
-        const bool there = row < a.N, live = there && a.indices[row * a.k] >= 0;
+        const bool there = row < a.N, live = next >= 0;
+        next = first_index(row + step);
         const float lse = live ? a.lse[row] : 0.f;
-        float x[VALUES];
-        if (live) load_logits<BF16, VALUES>(a.logits, row, a.E, at, whole, x);
-        else {
-#pragma unroll
-            for (int j = 0; j < VALUES; ++j) x[j] = -INFINITY;
-        }
+        RawLogits<BF16, L, VALUES> x;
+        x.load(a.logits, row, a.E, sub, whole, live);
         int index[kSlots];
         float ps[kSlots], dw[kSlots], S = 0.f, T = 0.f;
 #pragma unroll
@@ -402,7 +573,7 @@ __global__ __launch_bounds__(kRouterThreads) void router_backward_kernel(const R
         float p[VALUES], dot = 0.f;
 #pragma unroll
         for (int j = 0; j < VALUES; ++j) {
-            p[j] = __expf(x[j] - lse);
+            p[j] = __expf(x.value(j) - lse);
             dot += p[j] * share[j];
         }
         dot = lanes_sum<L>(dot) + (a.renormalize ? 0.f : T) - gamma * lse;
@@ -412,27 +583,13 @@ __global__ __launch_bounds__(kRouterThreads) void router_backward_kernel(const R
         __builtin_amdgcn_wave_barrier();                              // a row's lanes are of one wavefront, whose LDS accesses keep their order
         float d[VALUES];
 #pragma unroll
-        for (int j = 0; j < VALUES; ++j) d[j] = live ? p[j] * (share[j] + mine[at + j] - dot) : 0.f;
+        for (int j = 0; j < VALUES; ++j) d[j] = live ? p[j] * (share[j] + mine[C::of(sub, j)] - dot) : 0.f;
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int q = 0; q < kSlots; ++q)
             if (index[q] >= 0) mine[index[q]] = 0.f;
         __builtin_amdgcn_wave_barrier();
-        if (!there) continue;
-        if (BF16) {
-            uint16_t* const to = (uint16_t*)a.d_logits + row * a.E + at;
-#pragma unroll
-            for (int j = 0; j < VALUES; ++j) {
-                union { __bf16 h; uint16_t u; } cv;
-                cv.h = (__bf16)d[j];
-                if (at + j < a.E) to[j] = cv.u;
-            }
-        } else {
-            float* const to = (float*)a.d_logits + row * a.E + at;
-#pragma unroll
-            for (int j = 0; j < VALUES; ++j)
-                if (at + j < a.E) to[j] = d[j];
-        }
+        if (there) store_values<BF16, L, VALUES>(a.d_logits, row, a.E, sub, whole, d);
     }
 }
 
@@ -447,10 +604,12 @@ static int check_sizes(int64_t N, int64_t E) {
     return CCE_OK;
 }
 
-static int rows_of_group(int64_t E) { return kRouterWaves * (E <= 64 ? 8 : E <= 256 ? 4 : E <= 512 ? 2 : 1); }
+// Rows that a workgroup of so many wavefronts takes at a time.
+static int64_t rows_of_group(int64_t E, int waves) { return waves * (E <= 64 ? 8 : E <= 256 ? 4 : E <= 512 ? 2 : 1); }
+
 
 static int64_t forward_blocks(int64_t N, int64_t E) {
-    const int64_t rows = rows_of_group(E), want = (N + rows - 1) / rows;
+    const int64_t rows = rows_of_group(E, router_waves(E > 512 ? 64 : 8)), want = (N + rows - 1) / rows;
     return want < kRouterBlocks ? want : kRouterBlocks;
 }
 
@@ -508,8 +667,17 @@ int cce_router_forward(const void* logits, int32_t logits_bf16, const int32_t* l
     a.ticket = (int32_t*)p;
     a.N = N; a.E = (int32_t)E; a.k = top_k; a.renormalize = renormalize; a.ignore_index = ignore_index; a.blocks = (int32_t)blocks;
     with_shape(logits_bf16 != 0, E, [&](auto bf16, auto l, auto values) {
-        hipLaunchKernelGGL((router_forward_kernel<decltype(bf16)::value, decltype(l)::value, decltype(values)::value>),
-                           dim3((unsigned)blocks), dim3(kRouterThreads), 0, stream, a);
+        constexpr bool BF16 = decltype(bf16)::value;
+        constexpr int L = decltype(l)::value, VALUES = decltype(values)::value;
+        const dim3 grid((unsigned)blocks), threads(64 * router_waves(L));
+        if constexpr (BF16) {
+            if (top_k <= 2) hipLaunchKernelGGL((router_forward_kernel<BF16, L, VALUES, 2>), grid, threads, 0, stream, a);
+            else if (top_k <= 4) hipLaunchKernelGGL((router_forward_kernel<BF16, L, VALUES, 4>), grid, threads, 0, stream, a);
+            else if (top_k <= 8) hipLaunchKernelGGL((router_forward_kernel<BF16, L, VALUES, 8>), grid, threads, 0, stream, a);
+            else hipLaunchKernelGGL((router_forward_kernel<BF16, L, VALUES, 0>), grid, threads, 0, stream, a);
+        } else {
+            hipLaunchKernelGGL((router_forward_kernel<BF16, L, VALUES, 0>), grid, threads, 0, stream, a);
+        }
     });
     if (blocks > 1)
         hipLaunchKernelGGL(router_join_kernel, dim3((unsigned)((E + kJoinExperts - 1) / kJoinExperts)), dim3(256), 0, stream, a);
@@ -531,10 +699,10 @@ int cce_router_backward(const void* logits, int32_t logits_bf16, const int32_t* 
     RouterGradArgs a;
     a.logits = logits; a.indices = indices; a.lse = lse; a.counts = counts; a.d_weights = d_weights; a.d_losses = d_losses;
     a.d_logits = d_logits; a.N = N; a.E = (int32_t)E; a.k = top_k; a.renormalize = renormalize;
-    const int64_t rows = rows_of_group(E), want = (N + rows - 1) / rows, blocks = want < 2048 ? want : 2048;
+    const int64_t rows = rows_of_group(E, 8), want = (N + rows - 1) / rows, blocks = want < kGradBlocks ? want : kGradBlocks;
     with_shape(logits_bf16 != 0, E, [&](auto bf16, auto l, auto values) {
         hipLaunchKernelGGL((router_backward_kernel<decltype(bf16)::value, decltype(l)::value, decltype(values)::value>),
-                           dim3((unsigned)blocks), dim3(kRouterThreads), 0, stream, a);
+                           dim3((unsigned)blocks), dim3(512), 0, stream, a);
     });
     return hip_ok(hipGetLastError()) ? CCE_OK : CCE_ERR_HIP;
 }
