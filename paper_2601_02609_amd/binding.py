@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import NamedTuple, Optional, Tuple
 
 import numpy as np
@@ -1365,14 +1366,16 @@ class MuonTensors(OptimTensors):
                          ("grad", "grads", n * np.where(t["grad_bf16"] != 0, 2, 4))], t, 3)
 
 
-def _coefficients(coefficients, steps: int):
+def _coefficients(coefficients, steps: int) -> bytes:
     """fp32 [steps, 3] on the host: one (a, b, c) for all steps, or one for each."""
+    if type(coefficients) is tuple and len(coefficients) == 3 and all(type(x) is float for x in coefficients):
+        return struct.pack("3f", *coefficients) * steps
     c = np.ascontiguousarray(coefficients, dtype=np.float32)
     if c.shape == (3,):
-        c = np.ascontiguousarray(np.broadcast_to(c, (steps, 3)))
+        c = np.broadcast_to(c, (max(steps, 0), 3))
     if c.shape != (steps, 3):
         raise ValueError(f"coefficients: expected three numbers, or three for each of the {steps} steps, got {c.shape}")
-    return c
+    return c.tobytes()
 
 
 def muon_workspace_bytes(tensors: MuonTensors) -> int:
@@ -1380,14 +1383,18 @@ def muon_workspace_bytes(tensors: MuonTensors) -> int:
     return int(lib().cce_muon_workspace_bytes(tensors._address, len(tensors)))
 
 
-def _muon_workspace(where: str, table, device, workspace, stream):
+def _muon_workspace(where: str, table, count: int, device, workspace, stream):
     if workspace is not None:
         _check_on(device, workspace, torch.uint8, (workspace.numel(),), "workspace")
         return workspace
-    n = int(lib().cce_muon_workspace_bytes(table.ctypes.data, len(table)))
+    n = lib().cce_muon_workspace_bytes(table, count)
     if n == 0:
         raise CCEError(CCE_ERR_UNSUPPORTED, where)
     return _new((n,), torch.uint8, device, stream)
+
+
+_MATRIX = struct.Struct("4Q2q2f2i")                # cce_matrix
+assert _MATRIX.size == ctypes.sizeof(_Matrix)
 
 
 def cce_orthogonalize_multi(matrices, out=None, *, steps: int = 5, coefficients=NS_COEFFICIENTS, eps: float = 1e-7,
@@ -1398,30 +1405,38 @@ def cce_orthogonalize_multi(matrices, out=None, *, steps: int = 5, coefficients=
     if count == 0:
         raise ValueError("matrices: expected at least one")
     device = matrices[0].device
+    if out is not None and len(out) != count:
+        raise ValueError(f"out: expected {count} matrices, got {len(out)}")
+    entries, spans, outs = [], [], []
     for i, t in enumerate(matrices):
-        if t.dtype not in (torch.float32, torch.bfloat16) or not t.is_cuda or t.device != device or t.dim() != 2 or not t.is_contiguous():
+        bf16 = t.dtype == torch.bfloat16
+        if not (bf16 or t.dtype == torch.float32) or t.device != device or not t.is_cuda or t.dim() != 2 or not t.is_contiguous():
             raise ValueError(f"matrices[{i}]: expected a contiguous cuda float32 or bfloat16 matrix on {device}, got {t.dtype} {tuple(t.shape)} "
                              f"contiguous={t.is_contiguous()} on {t.device}")
-    if out is None:
-        out = [_new(t.shape, torch.bfloat16, device, stream) for t in matrices]
-    elif len(out) != count:
-        raise ValueError(f"out: expected {count} matrices, got {len(out)}")
-    else:
-        for i, (o, t) in enumerate(zip(out, matrices)):
-            _check_on(device, o, torch.bfloat16, t.shape, f"out[{i}]")
-    table = np.zeros(count, dtype=np.dtype(_Matrix))
-    table["grad"] = [t.data_ptr() for t in matrices]
-    table["out_bf16"] = [o.data_ptr() for o in out]
-    table["rows"] = [t.shape[0] for t in matrices]
-    table["cols"] = [t.shape[1] for t in matrices]
-    table["grad_bf16"] = [t.dtype == torch.bfloat16 for t in matrices]
-    n = table["rows"] * table["cols"]
-    _refuse_overlap([("out_bf16", "out", n * 2), ("grad", "matrices", n * np.where(table["grad_bf16"] != 0, 2, 4))], table, 1)
-    c = _coefficients(coefficients, steps)
-    workspace = _muon_workspace("cce_orthogonalize_multi", table, device, workspace, stream)
-    _call("cce_orthogonalize_multi", lib().cce_orthogonalize_multi, device, stream, table.ctypes.data, count, c.ctypes.data, steps, eps,
+        m, n = shape = t.shape
+        if out is None:
+            o = _new(shape, torch.bfloat16, device, stream)
+        else:
+            o = out[i]
+            _check_on(device, o, torch.bfloat16, shape, f"out[{i}]")
+        outs.append(o)
+        to, at, values = o.data_ptr(), t.data_ptr(), m * n
+        entries.append(_MATRIX.pack(0, to, at, 0, m, n, 0.0, 0.0, bf16, 0))
+        if values:
+            spans.append((to, to + 2 * values, True, i))
+            spans.append((at, at + (2 if bf16 else 4) * values, False, i))
+    spans.sort()
+    end = written = 0                              # of everything in front, of what is written in front
+    for start, stop, writes, i in spans:
+        if start < (end if writes else written):
+            raise ValueError(f"{'out' if writes else 'matrices'}[{i}] overlaps another tensor of the lists")
+        end = max(end, stop)
+        written = max(written, stop) if writes else written
+    table = b"".join(entries)
+    workspace = _muon_workspace("cce_orthogonalize_multi", table, count, device, workspace, stream)
+    _call("cce_orthogonalize_multi", lib().cce_orthogonalize_multi, device, stream, table, count, _coefficients(coefficients, steps), steps, eps,
           workspace.data_ptr(), workspace.numel())
-    return out
+    return out if out is not None else outs
 
 
 def cce_muon_multi_step(tensors: MuonTensors, *, lr: float, momentum: float = 0.95, nesterov: bool = True, steps: int = 5,
@@ -1431,10 +1446,9 @@ def cce_muon_multi_step(tensors: MuonTensors, *, lr: float, momentum: float = 0.
     _check_entries(tensors, _Matrix)
     if clip_coef is not None:
         _check_on(tensors.device, clip_coef, torch.float32, (1,), "clip_coef")
-    c = _coefficients(coefficients, steps)
-    workspace = _muon_workspace("cce_muon_multi_step", tensors._table, tensors.device, workspace, stream)
+    workspace = _muon_workspace("cce_muon_multi_step", tensors._address, len(tensors), tensors.device, workspace, stream)
     _call("cce_muon_multi_step", lib().cce_muon_multi_step, tensors.device, stream, tensors._address, len(tensors), lr, momentum,
-          1 if nesterov else 0, c.ctypes.data, steps, eps, clip_coef.data_ptr() if clip_coef is not None else None,
+          1 if nesterov else 0, _coefficients(coefficients, steps), steps, eps, clip_coef.data_ptr() if clip_coef is not None else None,
           workspace.data_ptr(), workspace.numel())
     if stream is not None:
         tensors._read_on(stream)
@@ -1473,26 +1487,39 @@ def cce_router_forward(logits: torch.Tensor, top_k: int, labels: Optional[torch.
     device = logits.device
     if labels is not None:
         _check_on(device, labels, torch.int32, (N,), "labels")
-    shapes = {"indices": ((N, top_k), torch.int32), "weights": ((N, top_k), torch.float32), "lse": ((N,), torch.float32),
-              "counts": ((E + 1,), torch.int32), "prob_sums": ((E,), torch.float32), "losses": ((2,), torch.float32)}
-    if out is None:
-        if not 1 <= top_k <= E:
-            raise CCEError(CCE_ERR_INVALID, "cce_router_forward, top_k")
-        out = RouterOutput(*(_new(shape, dtype, device, stream) for shape, dtype in shapes.values()))
-    else:
-        for name, (shape, dtype) in shapes.items():
-            _check_on(device, getattr(out, name), dtype, shape, name)
+    if not 1 <= top_k <= E:
+        raise CCEError(CCE_ERR_INVALID, "cce_router_forward, top_k")
+    need = 0
     if workspace is None:
-        n = int(lib().cce_router_workspace_bytes(N, E))
-        if n == 0:
+        need = lib().cce_router_workspace_bytes(N, E)
+        if need == 0:
             raise CCEError(CCE_ERR_UNSUPPORTED, "cce_router_workspace_bytes")
-        workspace = _new((n,), torch.uint8, device, stream)
     else:
         _check_on(device, workspace, torch.uint8, (workspace.numel(),), "workspace")
+    if out is None:
+        # two pieces of memory for all outputs, the fp32 ones behind a small workspace: a decode step is bound by the host
+        front = need // 4 if need <= 4096 else 0
+        ints = _new((N * top_k + E + 1,), torch.int32, device, stream)
+        floats = _new((front + N * top_k + N + E + 2,), torch.float32, device, stream)
+        lse = front + N * top_k
+        out = RouterOutput(ints.as_strided((N, top_k), (top_k, 1)), floats.as_strided((N, top_k), (top_k, 1), front),
+                           floats.as_strided((N,), (1,), lse), ints.as_strided((E + 1,), (1,), N * top_k),
+                           floats.as_strided((E,), (1,), lse + N), floats.as_strided((2,), (1,), lse + N + E))
+        workspace_at = floats.data_ptr() if front else None
+    else:
+        shapes = (((N, top_k), torch.int32), ((N, top_k), torch.float32), ((N,), torch.float32), ((E + 1,), torch.int32),
+                  ((E,), torch.float32), ((2,), torch.float32))
+        for name, t, (shape, dtype) in zip(RouterOutput._fields, out, shapes):
+            _check_on(device, t, dtype, shape, name)
+        workspace_at = None
+    if workspace_at is None:
+        if workspace is None:
+            workspace = _new((need,), torch.uint8, device, stream)
+        workspace_at, need = workspace.data_ptr(), workspace.numel()
     _call("cce_router_forward", lib().cce_router_forward, device, stream, logits.data_ptr(), 1 if logits.dtype == torch.bfloat16 else 0,
           labels.data_ptr() if labels is not None else None, N, E, top_k, 1 if renormalize else 0, ignore_index,
           out.indices.data_ptr(), out.weights.data_ptr(), out.lse.data_ptr(), out.counts.data_ptr(), out.prob_sums.data_ptr(),
-          out.losses.data_ptr(), workspace.data_ptr(), workspace.numel())
+          out.losses.data_ptr(), workspace_at, need)
     return out
 
 
