@@ -346,8 +346,26 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
     const int wm = m0 + wave_m<SymTile>() * 64, wn = n0 + wave_n<SymTile>() * 64;      // this wavefront's corner
     const int q = (lane & 7) * 8;                                                      // this lane's columns
     const int m = wm + q;
+    const bool inside_m = m < at.rp;
+    f32x4 dc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    if (POLY && inside_m) {
+        dc[0] = *(const f32x4*)(da + m);
+        dc[1] = *(const f32x4*)(da + m + 4);
+    }
 #pragma unroll
     for (int bn = 0; bn < SymTile::TN; ++bn) {
+        // all loads of 32 rows together, from rows that are there
+        f16x8 o[4];
+        float dn[4];
+        if (POLY) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int n = wn + bn * 32 + 8 * k + (lane >> 3);
+                const bool there = inside_m && n < at.rp;
+                o[k] = *(const f16x8*)(A + (there ? (uint32_t)n * (uint32_t)at.rp + m : 0u));
+                dn[k] = da[there ? n : 0];
+            }
+        }
 #pragma unroll
         for (int bm = 0; bm < SymTile::TM; ++bm)
 #pragma unroll
@@ -358,32 +376,26 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int y = 8 * k + (lane >> 3), n = wn + bn * 32 + y;
-            const bool inside = n < at.rp && m < at.rp;
+            const bool inside = inside_m && n < at.rp;
             float x[8];
             read8(rows + y * kSymPitch + q, x);
             f16x8 v;
-            if (!POLY) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float s = x[e] * (1.f / (kScaleX * kScaleX));
-                    if (m + e == n && inside) da[n] = s;
-                    v[e] = m + e == n ? (_Float16)0.f : (_Float16)(s * kScaleA);
+            for (int e = 0; e < 8; ++e) {
+                float diagonal, beside;
+                if (!POLY) {
+                    diagonal = x[e] * (1.f / (kScaleX * kScaleX));
+                    beside = diagonal * kScaleA;
+                } else {
+                    const float d = dn[k], p = x[e] * (a.c / (kScaleA * kScaleA));
+                    diagonal = a.b * d + (a.c * d * d + p);
+                    beside = ((a.b + a.c * (d + dc[e >> 2][e & 3])) * ((float)o[k][e] * (1.f / kScaleA)) + p) * kScaleM;
                 }
-                if (inside) *(f16x8*)(A + (uint32_t)n * (uint32_t)at.rp + m) = v;
-            } else if (inside) {
-                const f16x8 o = *(const f16x8*)(A + (uint32_t)n * (uint32_t)at.rp + m);
-                const float dn = da[n];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float p = x[e] * (a.c / (kScaleA * kScaleA));
-                    const float s = (a.b + a.c * (dn + da[m + e])) * ((float)o[e] * (1.f / kScaleA)) + p;
-                    if (m + e == n) dm[n] = a.b * dn + (a.c * dn * dn + p);
-                    v[e] = m + e == n ? (_Float16)0.f : (_Float16)(s * kScaleM);
-                }
-                *(f16x8*)(M + at.panel(n, m)) = v;
-            } else {
-                v = f16x8{};
+                const bool here = m + e == n;
+                if (here && inside) (POLY ? dm : da)[n] = diagonal;
+                v[e] = here ? (_Float16)0.f : (_Float16)beside;
             }
+            if (inside) *(f16x8*)(POLY ? M + at.panel(n, m) : A + (uint32_t)n * (uint32_t)at.rp + m) = v;
             if (m0 != n0)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) mirror[(q + e) * kSymMirror + bn * 32 + y] = v[e];
@@ -472,6 +484,19 @@ __global__ __launch_bounds__(ApplyTile::kThreads, 2) void ns_apply_kernel(const 
     const bool vec = LAST && (t.cols & 3) == 0 && aligned(t.param, 16) && aligned(t.out, 8);
 #pragma unroll
     for (int bn = 0; bn < ApplyTile::TN; ++bn) {
+        // all loads of 32 rows together, from rows that are there
+        f16x8 h[8];
+        u32x2 l[8];
+        float keep[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int n = wn + bn * 32 + 4 * k + (lane >> 4);
+            const bool there = n < at.rp && m < at.cp;
+            const uint32_t j = there ? (uint32_t)n * (uint32_t)at.cp + m : 0u;
+            h[k] = *(const f16x8*)(H + j);
+            l[k] = *(const u32x2*)(L + j);
+            keep[k] = dm[there ? n : 0];
+        }
 #pragma unroll
         for (int bm = 0; bm < ApplyTile::TM; ++bm)
 #pragma unroll
@@ -482,47 +507,81 @@ __global__ __launch_bounds__(ApplyTile::kThreads, 2) void ns_apply_kernel(const 
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const int y = 4 * k + (lane >> 4), n = wn + bn * 32 + y;
-            if (n >= at.rp || m >= at.cp) continue;
             const uint32_t j = (uint32_t)n * (uint32_t)at.cp + m;
-            const f16x8 h = *(const f16x8*)(H + j);
-            const u32x2 l = *(const u32x2*)(L + j);
-            const float keep = a.a + dm[n];
+            const float of_h = (a.a + keep[k]) * (1.f / kScaleX), of_l = (a.a + keep[k]) * (1.f / kScaleL);
             float x[8];
             read8(rows + y * kApplyPitch + q, x);
 #pragma unroll
             for (int e = 0; e < 8; e += 2) {
-                const f32x2 r = e & 2 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)l[e >> 2], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)l[e >> 2], false);
+                const f32x2 r = e & 2 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)l[k][e >> 2], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)l[k][e >> 2], false);
 #pragma unroll
                 for (int f = 0; f < 2; ++f)
-                    x[e + f] = keep * ((float)h[e + f] * (1.f / kScaleX) + r[f] * (1.f / kScaleL)) + x[e + f] * (1.f / (kScaleX * kScaleM));
+                    x[e + f] = fmaf(of_h, (float)h[k][e + f], fmaf(of_l, r[f], x[e + f] * (1.f / (kScaleX * kScaleM))));
             }
             if (!LAST) {
                 f16x8 h1;
                 u32x2 l1;
                 split8(x, h1, l1);
-                *(f16x8*)(H1 + j) = h1;
-                *(u32x2*)(L + j) = l1;
-            } else if (tall) {
+                if (n < at.rp && m < at.cp) {
+                    *(f16x8*)(H1 + j) = h1;
+                    *(u32x2*)(L + j) = l1;
+                }
+            } else {
                 *(CCE_LDS f32x4*)(rows + y * kApplyPitch + q) = f32x4{x[0], x[1], x[2], x[3]};
                 *(CCE_LDS f32x4*)(rows + y * kApplyPitch + q + 4) = f32x4{x[4], x[5], x[6], x[7]};
-            } else if (n < at.r) {
-                const int64_t to = (int64_t)n * t.cols + m;
-#pragma unroll
-                for (int e = 0; e < 8; e += 4)
-                    if (m + e < at.c) give4(t, to + e, af32x4{x[e], x[e + 1], x[e + 2], x[e + 3]}, at.c - m - e, vec);
             }
         }
         __builtin_amdgcn_wave_barrier();
-        if (LAST && tall) {
-            const int z = (lane & 7) * 4, n = wn + bn * 32 + z;                       // four rows of X: neighbours of the caller's
-#pragma unroll 4
-            for (int k = 0; k < 16; ++k) {
-                const int y = 8 * k + (lane >> 3);
-                if (wm + y >= at.c || n >= at.r) continue;
-                af32x4 x;
+        if (LAST) {
+            // to the caller, four values in a row of their matrix a lane: rows of X, or columns
+            const int n1 = wn + bn * 32, z = tall ? (lane & 7) * 4 : (lane & 31) * 4;
+            auto value = [&](int y, int e) { return tall ? rows[(z + e) * kApplyPitch + y] : rows[y * kApplyPitch + z + e]; };
+#pragma unroll 1
+            for (int k0 = 0; k0 < 16; k0 += 8) {
+                const int y0 = tall ? 8 * k0 + (lane >> 3) : 2 * k0 + (lane >> 5), step = tall ? 8 : 2;
+                const int line = (tall ? wm : n1) + y0, in_line = (tall ? n1 : wm) + z;
+                const int lines = tall ? at.c : at.r, length = tall ? at.r : at.c;
+                if (vec) {
+                    f32x4 p[8];
+                    if (t.param) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = rows[(z + e) * kApplyPitch + y];
-                give4(t, (int64_t)(wm + y) * t.cols + n, x, at.r - n, vec);
+                        for (int k = 0; k < 8; ++k)
+                            p[k] = *(const f32x4*)(t.param + (line + step * k < lines && in_line < length ? (int64_t)(line + step * k) * t.cols + in_line : 0));
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        f32x4 x;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            x[e] = value(y0 + step * k, e);
+                            if (t.param) x[e] = p[k][e] * t.decay - t.lr * x[e];
+                        }
+                        if (line + step * k < lines && in_line < length) {
+                            const int64_t to = (int64_t)(line + step * k) * t.cols + in_line;
+                            if (t.param) *(f32x4*)(t.param + to) = x;
+                            if (t.out) {
+                                union { __bf16 h[4]; u32x2 u; } cv;
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) cv.h[e] = (__bf16)x[e];
+                                *(u32x2*)(t.out + to) = cv.u;
+                            }
+                        }
+                    }
+                } else {
+#pragma unroll 1
+                    for (int k = 0; k < 8; ++k)
+#pragma unroll 1
+                        for (int e = 0; e < 4; ++e) {
+                            if (line + step * k >= lines || in_line + e >= length) continue;
+                            const int64_t to = (int64_t)(line + step * k) * t.cols + in_line + e;
+                            float y = value(y0 + step * k, e);
+                            if (t.param) {
+                                y = t.param[to] * t.decay - t.lr * y;
+                                t.param[to] = y;
+                            }
+                            if (t.out) t.out[to] = bf16_bits(y);
+                        }
+                }
             }
             __builtin_amdgcn_wave_barrier();
         }
