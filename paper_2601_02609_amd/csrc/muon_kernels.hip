@@ -19,6 +19,7 @@
 #include <math.h>
 #include <stddef.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "../../include/cce.h"
 #include "../../include/cce_muon.h"
@@ -31,8 +32,9 @@ namespace cce {
 
 typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
 
-constexpr int kGroup = 48;                             // matrices of a launch: kernel arguments hold 4 KB
-constexpr int64_t kGroupBytes = (int64_t)1 << 30;      // workspace of a group of more than one matrix
+constexpr int kGroup = 240;                            // matrices whose products share their launches
+constexpr int64_t kGroupBytes = (int64_t)3 << 30;      // workspace of a group of more than one matrix
+constexpr int kEnds = 56;                              // matrices of a launch that reads or writes the caller's: kernel arguments hold 4 KB
 constexpr int64_t kMaxMatrix = (int64_t)1 << 30;       // values of a padded matrix: byte offsets of 16-bit values stay below 2^32
 constexpr int64_t kMaxSide = 16384;                    // smaller side
 constexpr int kNormParts = 256;                        // partial sums of a matrix
@@ -51,16 +53,31 @@ struct NsMatrix {
 };
 
 struct NsArgs {
-    NsMatrix t[kGroup];
-    uint32_t first_norm[kGroup];      // a matrix's first workgroup; twice that, plus 1 if its gradient is bf16
-    uint32_t first_prep[kGroup], first_sym[kGroup], first_apply[kGroup];      // twice the first workgroup
+    NsMatrix t[kEnds];
+    uint32_t first[kEnds];     // twice a matrix's first workgroup, plus 1 if its gradient is bf16
     char* ws;
     const float* clip_coef;
     float mu, a, b, c, eps;
     int32_t nesterov;
-    uint32_t count, flip;             // flip: which of the two copies of h is read
+    uint32_t count, flip;      // flip: which of the two copies of h is read
 };
-static_assert(sizeof(NsArgs) <= 4096, "kernel arguments hold 4 KB");
+
+struct NsShape {
+    uint32_t base;             // in units of 256 bytes
+    int32_t rows, cols;
+};
+
+struct NsProductArgs {
+    NsShape t[kGroup];
+    uint32_t first[kGroup];    // twice a matrix's first workgroup
+    char* ws;
+    float a, b, c;
+    uint32_t count, flip;
+};
+static_assert(sizeof(NsArgs) <= 4096 && sizeof(NsProductArgs) <= 4096, "kernel arguments hold 4 KB");
+
+__device__ __forceinline__ char* workspace_of(const NsArgs& a, int i) { return a.ws + a.t[i].base; }
+__device__ __forceinline__ char* workspace_of(const NsProductArgs& a, int i) { return a.ws + (uint64_t)a.t[i].base * 256; }
 
 // Where a matrix's operands lie, in bytes behind its base.
 struct NsLayout {
@@ -91,8 +108,12 @@ struct NsLayout {
 
 // Which matrix workgroup w belongs to, b = 2 w + 1: the last one that begins at or before it.
 __device__ __forceinline__ int matrix_of(const uint32_t* first, int count, uint32_t b) {
-    const int i = (int)(threadIdx.x & 63);
-    return __builtin_amdgcn_readfirstlane((int)__popcll(__ballot(i < count && first[i] <= b)) - 1);
+    int n = 0;
+    for (int base = 0; base < count; base += 64) {
+        const int i = base + (int)(threadIdx.x & 63);
+        n += (int)__popcll(__ballot(i < count && first[i] <= b));
+    }
+    return __builtin_amdgcn_readfirstlane(n - 1);
 }
 
 __device__ __forceinline__ float grad_value(const void* grad, bool bf16, int64_t i) {
@@ -135,11 +156,11 @@ __device__ __forceinline__ int norm_parts(int64_t n) {
 // ------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void ns_norm_kernel(const NsArgs a) {
     __shared__ double red[4];
-    const int i = matrix_of(a.first_norm, (int)a.count, 2 * blockIdx.x + 1);
+    const int i = matrix_of(a.first, (int)a.count, 2 * blockIdx.x + 1);
     const NsMatrix& t = a.t[i];
-    const bool bf16 = (a.first_norm[i] & 1u) != 0u;
+    const bool bf16 = (a.first[i] & 1u) != 0u;
     const int64_t n = (int64_t)t.rows * t.cols;
-    const int part = (int)(blockIdx.x - (a.first_norm[i] >> 1)), parts = norm_parts(n);
+    const int part = (int)(blockIdx.x - (a.first[i] >> 1)), parts = norm_parts(n);
     const float clip = a.clip_coef ? a.clip_coef[0] : 1.f;
     const bool vec = aligned(t.grad, bf16 ? 8 : 16) && aligned(t.momentum, 16);
     double sum = 0.0;
@@ -213,13 +234,13 @@ __device__ __forceinline__ void split4(const af32x4& x, f16x4& h, uint32_t& l) {
 __global__ __launch_bounds__(256) void ns_prep_kernel(const NsArgs a) {
     __shared__ double red[4];
     __shared__ float tile[64][65];
-    const int i = matrix_of(a.first_prep, (int)a.count, 2 * blockIdx.x + 1);
+    const int i = matrix_of(a.first, (int)a.count, 2 * blockIdx.x + 1);
     const NsMatrix& t = a.t[i];
-    const bool bf16 = (a.first_norm[i] & 1u) != 0u;
+    const bool bf16 = (a.first[i] & 1u) != 0u;
     const NsLayout at(t.rows, t.cols);
     char* const base = a.ws + t.base;
     const int64_t n = (int64_t)t.rows * t.cols;
-    const int w = (int)(blockIdx.x - (a.first_prep[i] >> 1)), tiles = at.cp / 64;
+    const int w = (int)(blockIdx.x - (a.first[i] >> 1)), tiles = at.cp / 64;
     const int row0 = w / tiles * 64, col0 = w % tiles * 64;
     const double sum = group_sum((int)threadIdx.x < norm_parts(n) ? ((const double*)(base + at.partials))[threadIdx.x] : 0.0, red);
     const double inv = sum <= 0x1.fffffffffffffp1023 ? 1.0 / (sqrt(sum) + (double)a.eps) : (double)NAN;
@@ -291,6 +312,7 @@ constexpr int kSymLds = 4 * kSymWave > SymTile::kLdsBytes ? 4 * kSymWave : SymTi
 typedef TileDuo ApplyTile;                             // 256 columns of X x 128 rows
 constexpr int kApplyPitch = 128 + 4;
 constexpr int kApplyWave = 32 * kApplyPitch * 4;
+constexpr int kResident = 512;                         // workgroups on the card at a time
 static_assert(4 * kApplyWave <= ApplyTile::kLdsBytes && 2 * kSymLds <= 160 * 1024 && 2 * ApplyTile::kLdsBytes <= 160 * 1024, "two workgroups a CU");
 
 // Tile w of the lower triangle, by rows.
@@ -312,20 +334,19 @@ __device__ __forceinline__ void read8(const CCE_LDS float* p, float (&x)[8]) {
 
 // A = X X^T (POLY = false) or M = b A + c A A, a tile and its mirror image.
 template <bool POLY>
-__global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(const NsArgs a) {
+__global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(const NsProductArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
     CCE_LDS char* const smem = (CCE_LDS char*)smem_generic;
-    const uint32_t id = (uint32_t)xcd_linear_id((int)blockIdx.x, (int)gridDim.x);
-    const int i = matrix_of(a.first_sym, (int)a.count, 2 * id + 1);
-    const NsMatrix& t = a.t[i];
-    const NsLayout at(t.rows, t.cols);
-    char* const base = a.ws + t.base;
+    const uint32_t id = (uint32_t)xcd_round_id((int)blockIdx.x, (int)gridDim.x, kResident);
+    const int i = matrix_of(a.first, (int)a.count, 2 * id + 1);
+    const NsLayout at(a.t[i].rows, a.t[i].cols);
+    char* const base = workspace_of(a, i);
     _Float16* const A = uniform((_Float16*)(base + at.a));
     _Float16* const M = uniform((_Float16*)(base + at.m));
     float* const da = (float*)(base + at.da);
     float* const dm = (float*)(base + at.dm);
     int ti, tj;
-    triangle((int)(id - (a.first_sym[i] >> 1)), ti, tj);
+    triangle((int)(id - (a.first[i] >> 1)), ti, tj);
     const int m0 = __builtin_amdgcn_readfirstlane(ti * SymTile::BM), n0 = __builtin_amdgcn_readfirstlane(tj * SymTile::BN);
     f32x16 acc[SymTile::TM][SymTile::TN];
 #pragma unroll
@@ -449,15 +470,15 @@ __device__ __forceinline__ void give4(const NsMatrix& t, int64_t to, af32x4 x, i
 
 // X = (a + M) X; LAST: to the caller.
 template <bool LAST>
-__global__ __launch_bounds__(ApplyTile::kThreads, 2) void ns_apply_kernel(const NsArgs a) {
+__global__ __launch_bounds__(ApplyTile::kThreads, 2) void ns_apply_kernel(const std::conditional_t<LAST, NsArgs, NsProductArgs> a) {
     extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
     CCE_LDS char* const smem = (CCE_LDS char*)smem_generic;
-    const uint32_t id = (uint32_t)xcd_linear_id((int)blockIdx.x, (int)gridDim.x);
-    const int i = matrix_of(a.first_apply, (int)a.count, 2 * id + 1);
-    const NsMatrix& t = a.t[i];
+    const uint32_t id = (uint32_t)xcd_round_id((int)blockIdx.x, (int)gridDim.x, kResident);
+    const int i = matrix_of(a.first, (int)a.count, 2 * id + 1);
+    const auto& t = a.t[i];
     const NsLayout at(t.rows, t.cols);
-    char* const base = a.ws + t.base;
-    const int w = (int)(id - (a.first_apply[i] >> 1)), row_tiles = (at.rp + ApplyTile::BN - 1) / ApplyTile::BN;
+    char* const base = workspace_of(a, i);
+    const int w = (int)(id - (a.first[i] >> 1)), row_tiles = (at.rp + ApplyTile::BN - 1) / ApplyTile::BN;
     const int m0 = __builtin_amdgcn_readfirstlane(w / row_tiles * ApplyTile::BM), n0 = __builtin_amdgcn_readfirstlane(w % row_tiles * ApplyTile::BN);
     const _Float16* const H = uniform((const _Float16*)(base + at.h[a.flip]));
     f32x16 acc[ApplyTile::TM][ApplyTile::TN];
@@ -481,7 +502,6 @@ __global__ __launch_bounds__(ApplyTile::kThreads, 2) void ns_apply_kernel(const 
     uint8_t* const L = (uint8_t*)(base + at.l);
     _Float16* const H1 = (_Float16*)(base + at.h[a.flip ^ 1]);
     const bool tall = t.rows > t.cols;
-    const bool vec = LAST && (t.cols & 3) == 0 && aligned(t.param, 16) && aligned(t.out, 8);
 #pragma unroll
     for (int bn = 0; bn < ApplyTile::TN; ++bn) {
         // all loads of 32 rows together, from rows that are there
@@ -532,7 +552,8 @@ __global__ __launch_bounds__(ApplyTile::kThreads, 2) void ns_apply_kernel(const 
             }
         }
         __builtin_amdgcn_wave_barrier();
-        if (LAST) {
+        if constexpr (LAST) {
+            const bool vec = (t.cols & 3) == 0 && aligned(t.param, 16) && aligned(t.out, 8);
             // to the caller, four values in a row of their matrix a lane: rows of X, or columns
             const int n1 = wn + bn * 32, z = tall ? (lane & 7) * 4 : (lane & 31) * 4;
             auto value = [&](int y, int e) { return tall ? rows[(z + e) * kApplyPitch + y] : rows[y * kApplyPitch + z + e]; };
@@ -997,7 +1018,8 @@ static int64_t next_group(const cce_matrix* matrices, int64_t count, int64_t& i,
         if (t.rows == 0 || t.cols == 0 || small_lds(t) != 0) continue;
         const int64_t own = (int64_t)NsLayout((int)t.rows, (int)t.cols).bytes;
         if (n != 0 && bytes + own > kGroupBytes) break;
-        take(n++, t, (uint64_t)bytes);
+        take(t, (uint64_t)bytes);
+        ++n;
         bytes += own;
     }
     return bytes;
@@ -1042,44 +1064,84 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
                       int steps, float eps, const float* clip_coef, void* workspace, hipStream_t stream) {
     if (!run_small(matrices, count, step, lr, mu, nesterov, coefficients, steps, eps, clip_coef, stream)) return CCE_ERR_HIP;
     NsArgs a;
+    NsProductArgs products[3];                         // gram, poly, apply
     a.ws = (char*)workspace;
+    for (auto& p : products) p.ws = (char*)workspace;
     a.clip_coef = clip_coef;
     a.mu = mu;
     a.nesterov = nesterov;
     a.eps = eps;
     for (int64_t i = 0; i < count;) {
-        uint32_t norm = 0, prep = 0, sym = 0, apply = 0;
-        a.count = 0;
-        next_group(matrices, count, i, [&](int n, const cce_matrix& t, uint64_t base) {
-            const NsLayout at((int)t.rows, (int)t.cols);
-            a.t[n] = table_entry(t, step, lr, base);
-            a.first_norm[n] = 2 * norm + (uint32_t)t.grad_bf16;
-            a.first_prep[n] = 2 * prep;
-            a.first_sym[n] = 2 * sym;
-            a.first_apply[n] = 2 * apply;
-            const int64_t parts = (t.rows * t.cols + kNormValues - 1) / kNormValues;
-            norm += (uint32_t)(parts < kNormParts ? parts : kNormParts);
-            prep += (uint32_t)(at.rp / 64) * (uint32_t)(at.cp / 64);
-            sym += sym_tiles(at);
-            apply += apply_tiles(at);
-            a.count = (uint32_t)n + 1;
+        int64_t index[kGroup];
+        uint64_t base[kGroup];
+        int n = 0;
+        next_group(matrices, count, i, [&](const cce_matrix& t, uint64_t at) {
+            index[n] = &t - matrices;
+            base[n++] = at;
         });
-        if (a.count == 0) continue;
+        if (n == 0) continue;
         if (!allow_lds(ns_symmetric_kernel<false>, kSymLds) || !allow_lds(ns_symmetric_kernel<true>, kSymLds) ||
             !allow_lds(ns_apply_kernel<false>, ApplyTile::kLdsBytes) || !allow_lds(ns_apply_kernel<true>, ApplyTile::kLdsBytes))
             return CCE_ERR_HIP;
-        hipLaunchKernelGGL(ns_norm_kernel, dim3(norm), dim3(256), 0, stream, a);
-        hipLaunchKernelGGL(ns_prep_kernel, dim3(prep), dim3(256), 0, stream, a);
-        for (int s = 0; s < steps; ++s) {
-            a.flip = (uint32_t)s & 1u;
-            a.a = coefficients[3 * s];
-            a.b = coefficients[3 * s + 1];
-            a.c = coefficients[3 * s + 2];
-            hipLaunchKernelGGL(ns_symmetric_kernel<false>, dim3(sym), dim3(SymTile::kThreads), kSymLds, stream, a);
-            hipLaunchKernelGGL(ns_symmetric_kernel<true>, dim3(sym), dim3(SymTile::kThreads), kSymLds, stream, a);
-            if (s + 1 < steps) hipLaunchKernelGGL(ns_apply_kernel<false>, dim3(apply), dim3(ApplyTile::kThreads), ApplyTile::kLdsBytes, stream, a);
-            else hipLaunchKernelGGL(ns_apply_kernel<true>, dim3(apply), dim3(ApplyTile::kThreads), ApplyTile::kLdsBytes, stream, a);
+        auto layout = [&](int k) { return NsLayout((int)matrices[index[k]].rows, (int)matrices[index[k]].cols); };
+        // launches over as many matrices as their arguments hold
+        auto ends = [&](auto blocks_of, auto launch) {
+            for (int k = 0; k < n;) {
+                uint32_t blocks = 0;
+                for (a.count = 0; k < n && a.count < (uint32_t)kEnds; ++k, ++a.count) {
+                    const cce_matrix& t = matrices[index[k]];
+                    a.t[a.count] = table_entry(t, step, lr, base[k]);
+                    a.first[a.count] = 2 * blocks + (uint32_t)t.grad_bf16;
+                    blocks += blocks_of(t, layout(k));
+                }
+                launch(blocks);
+            }
+        };
+        // the matrices with the longest sums of a product first: the shorter ones fill what they leave
+        uint32_t grid[3];
+        for (int op = 0; op < 3; ++op) {
+            NsProductArgs& p = products[op];
+            int order[kGroup];
+            for (int k = 0; k < n; ++k) {
+                auto length = [&](int x) { return op == 0 ? layout(x).cp : layout(x).rp; };
+                int to = k;
+                for (; to > 0 && length(order[to - 1]) < length(k); --to) order[to] = order[to - 1];
+                order[to] = k;
+            }
+            grid[op] = 0;
+            p.count = (uint32_t)n;
+            for (int k = 0; k < n; ++k) {
+                const cce_matrix& t = matrices[index[order[k]]];
+                p.t[k] = NsShape{(uint32_t)(base[order[k]] / 256), (int32_t)t.rows, (int32_t)t.cols};
+                p.first[k] = 2 * grid[op];
+                grid[op] += op < 2 ? sym_tiles(layout(order[k])) : apply_tiles(layout(order[k]));
+            }
         }
+        ends([](const cce_matrix& t, const NsLayout&) {
+            const int64_t parts = (t.rows * t.cols + kNormValues - 1) / kNormValues;
+            return (uint32_t)(parts < kNormParts ? parts : kNormParts);
+        }, [&](uint32_t blocks) { hipLaunchKernelGGL(ns_norm_kernel, dim3(blocks), dim3(256), 0, stream, a); });
+        ends([](const cce_matrix&, const NsLayout& at) { return (uint32_t)(at.rp / 64) * (uint32_t)(at.cp / 64); },
+             [&](uint32_t blocks) { hipLaunchKernelGGL(ns_prep_kernel, dim3(blocks), dim3(256), 0, stream, a); });
+        for (int s = 0; s < steps; ++s) {
+            for (auto& p : products) {
+                p.flip = (uint32_t)s & 1u;
+                p.a = coefficients[3 * s];
+                p.b = coefficients[3 * s + 1];
+                p.c = coefficients[3 * s + 2];
+            }
+            hipLaunchKernelGGL(ns_symmetric_kernel<false>, dim3(grid[0]), dim3(SymTile::kThreads), kSymLds, stream, products[0]);
+            hipLaunchKernelGGL(ns_symmetric_kernel<true>, dim3(grid[1]), dim3(SymTile::kThreads), kSymLds, stream, products[1]);
+            if (s + 1 < steps)
+                hipLaunchKernelGGL(ns_apply_kernel<false>, dim3(grid[2]), dim3(ApplyTile::kThreads), ApplyTile::kLdsBytes, stream, products[2]);
+        }
+        a.flip = products[2].flip;
+        a.a = products[2].a;
+        a.b = products[2].b;
+        a.c = products[2].c;
+        ends([](const cce_matrix&, const NsLayout& at) { return apply_tiles(at); }, [&](uint32_t blocks) {
+            hipLaunchKernelGGL(ns_apply_kernel<true>, dim3(blocks), dim3(ApplyTile::kThreads), ApplyTile::kLdsBytes, stream, a);
+        });
     }
     return hip_ok(hipGetLastError()) ? CCE_OK : CCE_ERR_HIP;
 }
@@ -1101,7 +1163,7 @@ size_t cce_muon_workspace_bytes(const cce_matrix* matrices, int64_t count) {
     if (check_sizes(matrices, count) != CCE_OK) return 0;
     int64_t most = 256;
     for (int64_t i = 0; i < count;) {
-        const int64_t bytes = next_group(matrices, count, i, [](int, const cce_matrix&, uint64_t) {});
+        const int64_t bytes = next_group(matrices, count, i, [](const cce_matrix&, uint64_t) {});
         most = bytes > most ? bytes : most;
     }
     return (size_t)most;
