@@ -332,6 +332,12 @@ __device__ __forceinline__ f32x16 mfma_32x32x16(const bf16x8 a, const bf16x8 b, 
     else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
+template <bool F16>
+__device__ __forceinline__ f32x4 mfma_16x16x32(const bf16x8 a, const bf16x8 b, const f32x4 c) {
+    if constexpr (F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
 // Scheduling hint: one MFMA, then PER LDS reads, repeated (compile-time recursion because
 // the builtin wants constant arguments).
 template <int I, int N_MFMA, int N_READS, int PER>
@@ -646,7 +652,7 @@ typedef PingTile<4, 8> TileSquare;      // 256 x 256, wave tile 64 x 128: where 
 // wavefront, lane group g holding rows 8 g .. 8 g + 7 of them, four in each block: 16 bytes of bf16 results in a row.
 enum class ARows { kHalves, kPairs };
 
-template <class Cfg, ARows ROWS>
+template <class Cfg, ARows ROWS, bool F16 = false>
 struct PingPong {
     CCE_LDS char* smem;
     int group, wm, wn;           // wave-uniform
@@ -734,7 +740,7 @@ struct PingPong {
                 for (int jj = 0; jj < Cfg::NB; ++jj) {
                     const int j = i & 1 ? Cfg::NB - 1 - jj : jj;          // (back and forth: the B operand of the last product stays: 1 %)
                     f32x4& c = acc[p * Cfg::QA + i][j];
-                    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], c, 0, 0, 0);
+                    c = mfma_16x16x32<F16>(a[i], b[j], c);
                 }
             __builtin_amdgcn_sched_barrier(0);
         };
@@ -829,7 +835,7 @@ struct TurnTile {
 __device__ __forceinline__ int wave_lane() { return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)); }
 
 // MAP: the k-rows of X are reached through a table in LDS, as in OperandTile.
-template <bool G_KMAJOR, int MAP>
+template <bool G_KMAJOR, int MAP, bool F16 = false>
 struct TurnLoop {
     typedef TurnTile Cfg;
     CCE_LDS char* smem;
@@ -961,7 +967,7 @@ struct TurnLoop {
 #pragma unroll
             for (int m = 0; m < NM; ++m) {
                 const int j = m / Cfg::NA, i = j & 1 ? Cfg::NA - 1 - m % Cfg::NA : m % Cfg::NA;
-                if (ON) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
+                if (ON) acc[i][j] = mfma_16x16x32<F16>(a[i], b[j], acc[i][j]);
                 if (MORE && m % GAP == GAP - 1 && m / GAP < NL) {
                     __builtin_amdgcn_sched_barrier(0);
                     load(to, m / GAP);

@@ -34,6 +34,8 @@ typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
 
 constexpr int kGroup = 240;                            // matrices whose products share their launches
 constexpr int64_t kGroupBytes = (int64_t)3 << 30;      // workspace of a group of more than one matrix
+constexpr int64_t kPartialBytes = (int64_t)256 * 256 * 256 * 4;      // of a part of a tile's sum for each CU
+constexpr int64_t kLargeRows = 1024;                   // from so many (padded) rows on a group may have them
 constexpr int kEnds = 56;                              // matrices of a launch that reads or writes the caller's: kernel arguments hold 4 KB
 constexpr int64_t kMaxMatrix = (int64_t)1 << 30;       // values of a padded matrix: byte offsets of 16-bit values stay below 2^32
 constexpr int64_t kMaxSide = 16384;                    // smaller side
@@ -73,6 +75,8 @@ struct NsProductArgs {
     char* ws;
     float a, b, c;
     uint32_t count, flip;
+    uint32_t tiles, split_tiles, splits;      // tiles of 256 x 256: how many, the last of them in parts of their sums, parts each
+    uint32_t partials;         // the parts' place, in units of 256 bytes
 };
 static_assert(sizeof(NsArgs) <= 4096 && sizeof(NsProductArgs) <= 4096, "kernel arguments hold 4 KB");
 
@@ -82,15 +86,14 @@ __device__ __forceinline__ char* workspace_of(const NsProductArgs& a, int i) { r
 // Where a matrix's operands lie, in bytes behind its base.
 struct NsLayout {
     int r, c, rp, cp;                 // sides and padded sides
-    uint64_t h[2], l, a, m, da, dm, partials, bytes;
+    uint64_t h1, l, a, m, da, dm, partials, bytes;      // the first copy of h: 0
     __host__ __device__ __forceinline__ NsLayout(int rows, int cols) {
         r = rows < cols ? rows : cols;
         c = rows < cols ? cols : rows;
         rp = (r + 63) & ~63;
         cp = (c + 63) & ~63;
         const uint64_t x = (uint64_t)rp * cp * 2, s = (uint64_t)rp * rp * 2, p = (uint64_t)rp * panel_rows() * 2, d = (uint64_t)rp * 4;
-        h[0] = 0;
-        h[1] = x;
+        h1 = x;
         l = 2 * x;
         a = l + x / 2;
         m = a + s;
@@ -99,8 +102,9 @@ struct NsLayout {
         partials = dm + d;
         bytes = partials + kNormParts * 8;
     }
+    __device__ __forceinline__ uint64_t h(uint32_t flip) const { return flip ? h1 : 0; }
     // M lies in panels of 32 columns, whose rows are padded to whole tiles
-    __host__ __device__ __forceinline__ int panel_rows() const { return (r + 127) & ~127; }
+    __host__ __device__ __forceinline__ int panel_rows() const { return (r + 255) & ~255; }
     __device__ __forceinline__ uint32_t panel(int row, int col) const {
         return (uint32_t)(col >> 5) * (uint32_t)panel_rows() * 32u + (uint32_t)row * 32u + (uint32_t)(col & 31);
     }
@@ -249,7 +253,7 @@ __global__ __launch_bounds__(256) void ns_prep_kernel(const NsArgs a) {
     const bool vec = (t.cols & 3) == 0 && aligned(t.grad, bf16 ? 8 : 16) && aligned(t.momentum, 16);
     const int r0 = tall ? col0 : row0, c0 = tall ? row0 : col0;                // in the caller's matrix
     const int q = (threadIdx.x & 15) * 4;
-    _Float16* const H = (_Float16*)(base + at.h[0]);
+    _Float16* const H = (_Float16*)(base + at.h(0));
     uint8_t* const L = (uint8_t*)(base + at.l);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -332,6 +336,18 @@ __device__ __forceinline__ void read8(const CCE_LDS float* p, float (&x)[8]) {
     }
 }
 
+// A value of A or of M from the product's x: what lies beside the diagonal, scaled, and what the diagonal would be.
+template <bool POLY>
+__device__ __forceinline__ float symmetric_value(const NsProductArgs& a, float x, _Float16 o, float dn, float dm, float& diagonal) {
+    if (!POLY) {
+        diagonal = x * (1.f / (kScaleX * kScaleX));
+        return diagonal * kScaleA;
+    }
+    const float p = x * (a.c / (kScaleA * kScaleA));
+    diagonal = a.b * dn + (a.c * dn * dn + p);
+    return ((a.b + a.c * (dn + dm)) * ((float)o * (1.f / kScaleA)) + p) * kScaleM;
+}
+
 // A = X X^T (POLY = false) or M = b A + c A A, a tile and its mirror image.
 template <bool POLY>
 __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(const NsProductArgs a) {
@@ -354,7 +370,7 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
 #pragma unroll
         for (int bn = 0; bn < SymTile::TN; ++bn) acc[bm][bn] = f32x16{};
     {
-        const _Float16* const from = POLY ? A : uniform((const _Float16*)(base + at.h[a.flip]));
+        const _Float16* const from = POLY ? A : uniform((const _Float16*)(base + at.h(a.flip)));
         const int k = POLY ? at.rp : at.cp;
         OperandTile<true, SymTile::BM, 0, SymTile::NW, SymTile::BK> x, y;
         x.init(from, k, m0, at.rp, k);
@@ -403,15 +419,8 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
             f16x8 v;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                float diagonal, beside;
-                if (!POLY) {
-                    diagonal = x[e] * (1.f / (kScaleX * kScaleX));
-                    beside = diagonal * kScaleA;
-                } else {
-                    const float d = dn[k], p = x[e] * (a.c / (kScaleA * kScaleA));
-                    diagonal = a.b * d + (a.c * d * d + p);
-                    beside = ((a.b + a.c * (d + dc[e >> 2][e & 3])) * ((float)o[k][e] * (1.f / kScaleA)) + p) * kScaleM;
-                }
+                float diagonal;
+                const float beside = symmetric_value<POLY>(a, x[e], o[k][e], dn[k], dc[e >> 2][e & 3], diagonal);
                 const bool here = m + e == n;
                 if (here && inside) (POLY ? dm : da)[n] = diagonal;
                 v[e] = here ? (_Float16)0.f : (_Float16)beside;
@@ -430,6 +439,190 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
         const f16x8 v = *(const CCE_LDS f16x8*)(mirror + y * kSymMirror + q);
         if (row < at.rp && col < at.rp) *(f16x8*)(POLY ? M + at.panel(row, col) : A + (uint32_t)row * (uint32_t)at.rp + col) = v;
     }
+}
+
+// The same on 256 x 256 tiles of two groups of wavefronts that take turns (see PingTile), one workgroup a CU.
+typedef TileSquare SymPing;
+constexpr int kPingPitch = 32 + 4;                     // floats of a staged row: 32 columns of 64 rows
+constexpr int kPingMirror = 128 + 8;
+constexpr int kPingWave = 64 * kPingPitch * 4 + 32 * kPingMirror * 2;
+constexpr int kPingLds = 8 * kPingWave > SymPing::kLdsBytes ? 8 * kPingWave : SymPing::kLdsBytes;
+static_assert(kPingLds <= 160 * 1024, "160 KB LDS");
+
+// A wavefront's part of tile (ti, tj) and of its mirror image.
+template <bool POLY>
+__device__ __forceinline__ void symmetric_ping_rows(const NsProductArgs& a, const NsLayout& at, char* base, f32x4 (&acc)[SymPing::NA][SymPing::NB],
+                                                    int ti, int tj, int wave, CCE_LDS char* smem) {
+    const int lane = threadIdx.x & 63, wm = wave / SymPing::WN, wn = wave % SymPing::WN, m0 = ti * SymPing::BM, n0 = tj * SymPing::BN;
+    _Float16* const A = (_Float16*)(base + at.a);
+    _Float16* const M = (_Float16*)(base + at.m);
+    float* const da = (float*)(base + at.da);
+    float* const dm = (float*)(base + at.dm);
+    CCE_LDS float* const rows = (CCE_LDS float*)smem;
+    CCE_LDS _Float16* const mirror = (CCE_LDS _Float16*)(smem + 64 * kPingPitch * 4);
+    const int q = (lane & 3) * 8, nw = n0 + wn * SymPing::TNR;
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+        const int mw = m0 + part * (SymPing::BM / 2) + wm * 32, m = mw + q;            // 32 columns of the result
+        if (mw >= at.rp) continue;
+        f32x4 dc[2];
+        if (POLY) {
+            dc[0] = *(const f32x4*)(da + m);
+            dc[1] = *(const f32x4*)(da + m + 4);
+        }
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            f16x8 o[4];
+            float dn[4];
+            if (POLY) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int n = nw + 64 * side + 16 * k + (lane >> 2);
+                    o[k] = *(const f16x8*)(A + (n < at.rp ? (uint32_t)n * (uint32_t)at.rp + m : 0u));
+                    dn[k] = da[n < at.rp ? n : 0];
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int b = 0; b < SymPing::QA; ++b)
+                    *(CCE_LDS f32x4*)(rows + (16 * j + (lane & 15)) * kPingPitch + 16 * b + 4 * (lane >> 4)) = acc[part * SymPing::QA + b][4 * side + j];
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int y = 16 * k + (lane >> 2), n = nw + 64 * side + y;
+                float x[8];
+                read8(rows + y * kPingPitch + q, x);
+                f16x8 v;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float diagonal;
+                    const float beside = symmetric_value<POLY>(a, x[e], o[k][e], dn[k], dc[e >> 2][e & 3], diagonal);
+                    const bool here = m + e == n;
+                    if (here) (POLY ? dm : da)[n] = diagonal;
+                    v[e] = here ? (_Float16)0.f : (_Float16)beside;
+                }
+                if (n < at.rp) *(f16x8*)(POLY ? M + at.panel(n, m) : A + (uint32_t)n * (uint32_t)at.rp + m) = v;
+                if (ti != tj)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) mirror[(q + e) * kPingMirror + 64 * side + y] = v[e];
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+        if (ti != tj) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int y = 4 * k + (lane >> 4), row = mw + y, col = nw + (lane & 15) * 8;     // of the mirrored tile
+                const f16x8 v = *(const CCE_LDS f16x8*)(mirror + y * kPingMirror + (lane & 15) * 8);
+                *(f16x8*)(POLY ? M + at.panel(row, col) : A + (uint32_t)row * (uint32_t)at.rp + col) = v;
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+}
+
+// The last a.split_tiles tiles, where they would leave most CUs without one, are computed in a.splits parts of the sum each, which
+// ns_symmetric_join_kernel adds in their order.
+template <bool POLY>
+__global__ __launch_bounds__(SymPing::kThreads, 2) void ns_symmetric_ping_kernel(const NsProductArgs a) {
+    extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
+    CCE_LDS char* const smem = (CCE_LDS char*)smem_generic;
+    const uint32_t id = (uint32_t)xcd_round_id((int)blockIdx.x, (int)gridDim.x, kResident / 2), whole = gridDim.x - a.split_tiles * a.splits;
+    const bool part = id >= whole;
+    const uint32_t tile = part ? whole + (id - whole) / a.splits : id;
+    const int i = matrix_of(a.first, (int)a.count, 2 * tile + 1);
+    const NsLayout at(a.t[i].rows, a.t[i].cols);
+    char* const base = workspace_of(a, i);
+    int ti, tj;
+    triangle((int)(tile - (a.first[i] >> 1)), ti, tj);
+    ti = __builtin_amdgcn_readfirstlane(ti);
+    tj = __builtin_amdgcn_readfirstlane(tj);
+    const int m0 = ti * SymPing::BM, n0 = tj * SymPing::BN;
+    const int m_rows = at.rp - m0 < SymPing::BM ? at.rp - m0 : SymPing::BM, parts = m_rows > SymPing::BM / 2 ? 2 : 1;
+    f32x4 acc[SymPing::NA][SymPing::NB];
+#pragma unroll
+    for (int x = 0; x < SymPing::NA; ++x)
+#pragma unroll
+        for (int y = 0; y < SymPing::NB; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+    {
+        const uint32_t ld = (uint32_t)(POLY ? at.rp : at.cp) * 2u;
+        const int slices = (POLY ? at.rp : at.cp) / SymPing::BK;
+        int first = 0, KT = slices;
+        if (part) {
+            const int split = (int)((id - whole) % a.splits), splits = (int)a.splits;
+            first = slices * split / splits;
+            KT = slices * (split + 1) / splits - first;
+        }
+        const char* const from = uniform(base + (POLY ? at.a : at.h(a.flip)) + (size_t)first * (2 * SymPing::BK));
+        PingPong<SymPing, ARows::kHalves, true> turns;
+        PingLoads<SymPing, ARows::kHalves> loads;
+        turns.init(smem);
+        loads.init(smem, ld);
+#pragma unroll
+        for (int x = 0; x < SymPing::kBLoads; ++x) {
+            const int row = n0 + loads.row(x);
+            loads.set_b_row(x, row < at.rp ? row : at.rp - 1, ld);
+        }
+        loads.on = true;
+        loads.tile(uniform(from + (size_t)m0 * ld), m_rows, from, ld);
+        __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): what the compiler has loaded so far, which cannot see the loads of the slices
+        loads.issue(0, 0);
+        loads.issue(0, 1);
+        turns.start();
+        auto request = [&](int stage, int half) {
+            if (loads.on) loads.issue(stage, half);
+        };
+#pragma nounroll
+        for (int kt = 0;;) {
+            if (kt + 1 < KT) {
+                loads.a += 2 * SymPing::BK;
+                loads.b += 2 * SymPing::BK;
+            } else {
+                loads.on = false;
+            }
+            turns.slice(acc, parts, request);
+            if (++kt == KT) break;
+            turns.barrier();
+        }
+        turns.tile_done();                             // every wavefront has its last fragments
+    }
+    const int wave = threadIdx.x >> 6;
+    if (part) {
+        f32x4* const to = (f32x4*)(a.ws + (uint64_t)a.partials * 256) + ((size_t)(id - whole) * 8 + wave) * (SymPing::NA * SymPing::NB * 64) + (threadIdx.x & 63);
+#pragma unroll
+        for (int x = 0; x < SymPing::NA; ++x)
+#pragma unroll
+            for (int y = 0; y < SymPing::NB; ++y) to[(x * SymPing::NB + y) * 64] = acc[x][y];
+        return;
+    }
+    symmetric_ping_rows<POLY>(a, at, base, acc, ti, tj, wave, smem + wave * kPingWave);
+}
+
+// A wavefront of a split tile a workgroup.
+template <bool POLY>
+__global__ __launch_bounds__(64) void ns_symmetric_join_kernel(const NsProductArgs a) {
+    __shared__ __attribute__((aligned(1024))) char smem_generic[kPingWave];
+    const uint32_t split = blockIdx.x >> 3, tile = a.tiles - a.split_tiles + split;
+    const int wave = (int)(blockIdx.x & 7u);
+    const int i = matrix_of(a.first, (int)a.count, 2 * tile + 1);
+    const NsLayout at(a.t[i].rows, a.t[i].cols);
+    char* const base = workspace_of(a, i);
+    int ti, tj;
+    triangle((int)(tile - (a.first[i] >> 1)), ti, tj);
+    const f32x4* from = (const f32x4*)(a.ws + (uint64_t)a.partials * 256) + ((size_t)split * a.splits * 8 + wave) * (SymPing::NA * SymPing::NB * 64) + threadIdx.x;
+    f32x4 acc[SymPing::NA][SymPing::NB];
+#pragma unroll
+    for (int x = 0; x < SymPing::NA; ++x)
+#pragma unroll
+        for (int y = 0; y < SymPing::NB; ++y) acc[x][y] = from[(x * SymPing::NB + y) * 64];
+    for (uint32_t k = 1; k < a.splits; ++k) {
+        from += 8 * SymPing::NA * SymPing::NB * 64;
+#pragma unroll
+        for (int x = 0; x < SymPing::NA; ++x)
+#pragma unroll
+            for (int y = 0; y < SymPing::NB; ++y) acc[x][y] += from[(x * SymPing::NB + y) * 64];
+    }
+    symmetric_ping_rows<POLY>(a, at, base, acc, ti, tj, wave, (CCE_LDS char*)smem_generic);
 }
 
 __device__ __forceinline__ uint16_t bf16_bits(float x) {
@@ -468,65 +661,37 @@ __device__ __forceinline__ void give4(const NsMatrix& t, int64_t to, af32x4 x, i
     }
 }
 
-// X = (a + M) X; LAST: to the caller.
-template <bool LAST>
-__global__ __launch_bounds__(ApplyTile::kThreads, 2) void ns_apply_kernel(const std::conditional_t<LAST, NsArgs, NsProductArgs> a) {
-    extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
-    CCE_LDS char* const smem = (CCE_LDS char*)smem_generic;
-    const uint32_t id = (uint32_t)xcd_round_id((int)blockIdx.x, (int)gridDim.x, kResident);
-    const int i = matrix_of(a.first, (int)a.count, 2 * id + 1);
-    const auto& t = a.t[i];
-    const NsLayout at(t.rows, t.cols);
-    char* const base = workspace_of(a, i);
-    const int w = (int)(id - (a.first[i] >> 1)), row_tiles = (at.rp + ApplyTile::BN - 1) / ApplyTile::BN;
-    const int m0 = __builtin_amdgcn_readfirstlane(w / row_tiles * ApplyTile::BM), n0 = __builtin_amdgcn_readfirstlane(w % row_tiles * ApplyTile::BN);
-    const _Float16* const H = uniform((const _Float16*)(base + at.h[a.flip]));
-    f32x16 acc[ApplyTile::TM][ApplyTile::TN];
-#pragma unroll
-    for (int bm = 0; bm < ApplyTile::TM; ++bm)
-#pragma unroll
-        for (int bn = 0; bn < ApplyTile::TN; ++bn) acc[bm][bn] = f32x16{};
-    {
-        OperandTile<false, ApplyTile::BM, 0, ApplyTile::NW, ApplyTile::BK> x;
-        PanelTile<true, ApplyTile::BN, ApplyTile::NW, ApplyTile::BK> y;
-        x.init(H, at.cp, m0, at.cp, at.rp);
-        y.init((const uint16_t*)uniform(base + at.m), (uint32_t)at.panel_rows() * 32u, n0, 0);
-        y.base = uniform(y.base);
-        gemm_mainloop<ApplyTile, false, true, true, true>(acc, x, y, at.rp, smem);
-    }
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    CCE_LDS float* const rows = (CCE_LDS float*)(smem + wave * kApplyWave);
-    const int wm = m0 + wave_m<ApplyTile>() * 128, wn = n0 + wave_n<ApplyTile>() * 64;
-    const int q = (lane & 15) * 8, m = wm + q;
-    const float* const dm = (const float*)(base + at.dm);
-    uint8_t* const L = (uint8_t*)(base + at.l);
-    _Float16* const H1 = (_Float16*)(base + at.h[a.flip ^ 1]);
-    const bool tall = t.rows > t.cols;
-#pragma unroll
-    for (int bn = 0; bn < ApplyTile::TN; ++bn) {
-        // all loads of 32 rows together, from rows that are there
-        f16x8 h[8];
-        u32x2 l[8];
-        float keep[8];
+// X = (a + M) X of 32 rows and 128 columns of X a wavefront, from (n0, m0) on: what is loaded, in front of the products' way through
+// LDS, and what is made of them.
+struct ApplyRows {
+    f16x8 h[8];
+    u32x2 l[8];
+    float keep[8];
+    __device__ __forceinline__ void load(const NsLayout& at, const char* base, int flip, int n0, int m0) {
+        const _Float16* const H = (const _Float16*)(base + at.h((uint32_t)flip));
+        const uint8_t* const L = (const uint8_t*)(base + at.l);
+        const float* const dm = (const float*)(base + at.dm);
+        const int lane = threadIdx.x & 63, m = m0 + (lane & 15) * 8;
+        // all loads together, from rows that are there
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const int n = wn + bn * 32 + 4 * k + (lane >> 4);
+            const int n = n0 + 4 * k + (lane >> 4);
             const bool there = n < at.rp && m < at.cp;
             const uint32_t j = there ? (uint32_t)n * (uint32_t)at.cp + m : 0u;
             h[k] = *(const f16x8*)(H + j);
             l[k] = *(const u32x2*)(L + j);
             keep[k] = dm[there ? n : 0];
         }
-#pragma unroll
-        for (int bm = 0; bm < ApplyTile::TM; ++bm)
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-                *(CCE_LDS f32x4*)(rows + (lane & 31) * kApplyPitch + bm * 32 + 8 * g + 4 * (lane >> 5)) =
-                    f32x4{acc[bm][bn][4 * g], acc[bm][bn][4 * g + 1], acc[bm][bn][4 * g + 2], acc[bm][bn][4 * g + 3]};
-        __builtin_amdgcn_wave_barrier();
+    }
+    // rows: 32 rows of 128 products in LDS, kApplyPitch apart
+    template <bool LAST, class Args, class Matrix>
+    __device__ __forceinline__ void finish(const Args& a, const Matrix& t, const NsLayout& at, char* base, int n0, int m0, CCE_LDS float* rows) const {
+        _Float16* const H1 = (_Float16*)(base + at.h(a.flip ^ 1));
+        uint8_t* const L = (uint8_t*)(base + at.l);
+        const int lane = threadIdx.x & 63, q = (lane & 15) * 8, m = m0 + q;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const int y = 4 * k + (lane >> 4), n = wn + bn * 32 + y;
+            const int y = 4 * k + (lane >> 4), n = n0 + y;
             const uint32_t j = (uint32_t)n * (uint32_t)at.cp + m;
             const float of_h = (a.a + keep[k]) * (1.f / kScaleX), of_l = (a.a + keep[k]) * (1.f / kScaleL);
             float x[8];
@@ -553,14 +718,14 @@ __global__ __launch_bounds__(ApplyTile::kThreads, 2) void ns_apply_kernel(const 
         }
         __builtin_amdgcn_wave_barrier();
         if constexpr (LAST) {
-            const bool vec = (t.cols & 3) == 0 && aligned(t.param, 16) && aligned(t.out, 8);
             // to the caller, four values in a row of their matrix a lane: rows of X, or columns
-            const int n1 = wn + bn * 32, z = tall ? (lane & 7) * 4 : (lane & 31) * 4;
+            const bool tall = t.rows > t.cols, vec = (t.cols & 3) == 0 && aligned(t.param, 16) && aligned(t.out, 8);
+            const int z = tall ? (lane & 7) * 4 : (lane & 31) * 4;
             auto value = [&](int y, int e) { return tall ? rows[(z + e) * kApplyPitch + y] : rows[y * kApplyPitch + z + e]; };
 #pragma unroll 1
             for (int k0 = 0; k0 < 16; k0 += 8) {
                 const int y0 = tall ? 8 * k0 + (lane >> 3) : 2 * k0 + (lane >> 5), step = tall ? 8 : 2;
-                const int line = (tall ? wm : n1) + y0, in_line = (tall ? n1 : wm) + z;
+                const int line = (tall ? m0 : n0) + y0, in_line = (tall ? n0 : m0) + z;
                 const int lines = tall ? at.c : at.r, length = tall ? at.r : at.c;
                 if (vec) {
                     f32x4 p[8];
@@ -606,6 +771,101 @@ __global__ __launch_bounds__(ApplyTile::kThreads, 2) void ns_apply_kernel(const 
             }
             __builtin_amdgcn_wave_barrier();
         }
+    }
+};
+
+template <bool LAST> using ApplyArgs = std::conditional_t<LAST, NsArgs, NsProductArgs>;
+
+// X = (a + M) X; LAST: to the caller.  256 columns x 128 rows, two workgroups a CU.
+template <bool LAST>
+__global__ __launch_bounds__(ApplyTile::kThreads, 2) void ns_apply_kernel(const ApplyArgs<LAST> a) {
+    extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
+    CCE_LDS char* const smem = (CCE_LDS char*)smem_generic;
+    const uint32_t id = (uint32_t)xcd_round_id((int)blockIdx.x, (int)gridDim.x, kResident);
+    const int i = matrix_of(a.first, (int)a.count, 2 * id + 1);
+    const auto& t = a.t[i];
+    const NsLayout at(t.rows, t.cols);
+    char* const base = workspace_of(a, i);
+    const int w = (int)(id - (a.first[i] >> 1)), row_tiles = (at.rp + ApplyTile::BN - 1) / ApplyTile::BN;
+    const int m0 = __builtin_amdgcn_readfirstlane(w / row_tiles * ApplyTile::BM), n0 = __builtin_amdgcn_readfirstlane(w % row_tiles * ApplyTile::BN);
+    f32x16 acc[ApplyTile::TM][ApplyTile::TN];
+#pragma unroll
+    for (int bm = 0; bm < ApplyTile::TM; ++bm)
+#pragma unroll
+        for (int bn = 0; bn < ApplyTile::TN; ++bn) acc[bm][bn] = f32x16{};
+    {
+        OperandTile<false, ApplyTile::BM, 0, ApplyTile::NW, ApplyTile::BK> x;
+        PanelTile<true, ApplyTile::BN, ApplyTile::NW, ApplyTile::BK> y;
+        x.init(uniform((const _Float16*)(base + at.h(a.flip))), at.cp, m0, at.cp, at.rp);
+        y.init((const uint16_t*)uniform(base + at.m), (uint32_t)at.panel_rows() * 32u, n0, 0);
+        y.base = uniform(y.base);
+        gemm_mainloop<ApplyTile, false, true, true, true>(acc, x, y, at.rp, smem);
+    }
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    CCE_LDS float* const rows = (CCE_LDS float*)(smem + wave * kApplyWave);
+    const int wm = m0 + wave_m<ApplyTile>() * 128, wn = n0 + wave_n<ApplyTile>() * 64;
+#pragma unroll
+    for (int bn = 0; bn < ApplyTile::TN; ++bn) {
+        ApplyRows of;
+        of.load(at, base, (int)a.flip, wn + bn * 32, wm);
+#pragma unroll
+        for (int bm = 0; bm < ApplyTile::TM; ++bm)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *(CCE_LDS f32x4*)(rows + (lane & 31) * kApplyPitch + bm * 32 + 8 * g + 4 * (lane >> 5)) =
+                    f32x4{acc[bm][bn][4 * g], acc[bm][bn][4 * g + 1], acc[bm][bn][4 * g + 2], acc[bm][bn][4 * g + 3]};
+        __builtin_amdgcn_wave_barrier();
+        of.finish<LAST>(a, t, at, base, wn + bn * 32, wm, rows);
+    }
+}
+
+// The same on 256 x 256 tiles of two groups of wavefronts that take turns (see TurnTile), one workgroup a CU.
+constexpr int kTurnLds = 8 * kApplyWave > TurnTile::kLdsBytes ? 8 * kApplyWave : TurnTile::kLdsBytes;
+static_assert(kTurnLds <= 160 * 1024, "160 KB LDS");
+constexpr int kTurnRows = 128;                         // fewest (padded) rows: its loop has four slices at least
+
+template <bool LAST>
+__global__ __launch_bounds__(TurnTile::kThreads, 2) void ns_apply_turn_kernel(const ApplyArgs<LAST> a) {
+    extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
+    CCE_LDS char* const smem = (CCE_LDS char*)smem_generic;
+    const uint32_t id = (uint32_t)xcd_round_id((int)blockIdx.x, (int)gridDim.x, kResident / 2);
+    const int i = matrix_of(a.first, (int)a.count, 2 * id + 1);
+    const auto& t = a.t[i];
+    const NsLayout at(t.rows, t.cols);
+    char* const base = workspace_of(a, i);
+    const int w = (int)(id - (a.first[i] >> 1)), row_tiles = (at.rp + TurnTile::BN - 1) / TurnTile::BN;
+    const int m0 = __builtin_amdgcn_readfirstlane(w / row_tiles * TurnTile::BM), n0 = __builtin_amdgcn_readfirstlane(w % row_tiles * TurnTile::BN);
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    TurnLoop<true, 0, true> loop;
+    loop.init(smem, wave, uniform(base + at.h(a.flip)), (uint32_t)at.cp * 2u, m0, at.cp, at.rp,
+              (const uint16_t*)uniform(base + at.m), (uint32_t)at.panel_rows() * 32u, n0, 0);
+    __builtin_amdgcn_s_waitcnt(0x0f70);                // vmcnt(0): what the compiler has loaded so far, which cannot see the loads of the slices
+    const int KT = loop.slices(at.rp);
+    const int wm = m0 + 128 * loop.group, wn = n0 + (wave & 3) * 64;
+    if (wm >= at.cp) {                                 // (its columns lie behind the matrix: loads and barriers only)
+        loop.idle(KT);
+        return;
+    }
+    f32x4 acc[TurnTile::NA][TurnTile::NB];
+#pragma unroll
+    for (int x = 0; x < TurnTile::NA; ++x)
+#pragma unroll
+        for (int y = 0; y < TurnTile::NB; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+    loop.run(acc, KT);
+    const int lane = threadIdx.x & 63;
+    CCE_LDS float* const rows = (CCE_LDS float*)(smem + wave * kApplyWave);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        if (wn + half * 32 >= at.rp) continue;
+        ApplyRows of;
+        of.load(at, base, (int)a.flip, wn + half * 32, wm);
+#pragma unroll
+        for (int x = 0; x < TurnTile::NA; ++x)
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+                *(CCE_LDS f32x4*)(rows + (16 * y + (lane & 15)) * kApplyPitch + 16 * x + 4 * (lane >> 4)) = acc[x][2 * half + y];
+        __builtin_amdgcn_wave_barrier();
+        of.finish<LAST>(a, t, at, base, wn + half * 32, wm, rows);
     }
 }
 
@@ -991,13 +1251,16 @@ static int check_coefficients(const float* coefficients, int steps) {
     return CCE_OK;
 }
 
-static uint32_t sym_tiles(const NsLayout& at) {
-    const uint32_t n = (uint32_t)((at.rp + SymTile::BM - 1) / SymTile::BM);
+static uint32_t sym_tiles(const NsLayout& at, bool large) {
+    const int side = large ? SymPing::BM : SymTile::BM;
+    const uint32_t n = (uint32_t)((at.rp + side - 1) / side);
     return n * (n + 1) / 2;
 }
-static uint32_t apply_tiles(const NsLayout& at) {
-    return (uint32_t)((at.rp + ApplyTile::BN - 1) / ApplyTile::BN) * (uint32_t)((at.cp + ApplyTile::BM - 1) / ApplyTile::BM);
+static uint32_t apply_tiles(const NsLayout& at, bool large) {
+    const int rows = large ? TurnTile::BN : ApplyTile::BN;
+    return (uint32_t)((at.rp + rows - 1) / rows) * (uint32_t)((at.cp + ApplyTile::BM - 1) / ApplyTile::BM);
 }
+static_assert(ApplyTile::BM == TurnTile::BM, "either form of a launch covers as many columns");
 
 template <class K>
 static bool allow_lds(K kernel, int bytes) { return hip_ok(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes)); }
@@ -1013,16 +1276,18 @@ template <class Take>
 static int64_t next_group(const cce_matrix* matrices, int64_t count, int64_t& i, Take take) {
     int64_t bytes = 0;
     int n = 0;
+    bool large = false;
     for (; i < count && n < kGroup; ++i) {
         const cce_matrix& t = matrices[i];
         if (t.rows == 0 || t.cols == 0 || small_lds(t) != 0) continue;
-        const int64_t own = (int64_t)NsLayout((int)t.rows, (int)t.cols).bytes;
-        if (n != 0 && bytes + own > kGroupBytes) break;
+        const NsLayout at((int)t.rows, (int)t.cols);
+        if (n != 0 && bytes + (int64_t)at.bytes > kGroupBytes - kPartialBytes) break;
         take(t, (uint64_t)bytes);
         ++n;
-        bytes += own;
+        bytes += (int64_t)at.bytes;
+        large = large || at.rp >= kLargeRows;
     }
-    return bytes;
+    return bytes + (large ? kPartialBytes : 0);
 }
 
 static NsMatrix table_entry(const cce_matrix& t, bool step, float lr, uint64_t base) {
@@ -1060,6 +1325,49 @@ static bool run_small(const cce_matrix* matrices, int64_t count, bool step, floa
     return true;
 }
 
+// Whether a launch takes tiles of 256 x 256, one workgroup a CU, or the smaller ones, two a CU: by the rounds of slices that either takes.
+// A round of either does as many products a slice; smaller tiles that have a CU each take 0.6 of one.
+// A and M: the last tiles of a round of 256 x 256 that is less than half full are split (p.splits), which costs a launch as long as 20 slices.
+// X: an epilogue is as long as 12 slices, which only the smaller tiles put beside products; 256 x 256 from 2048 rows on.
+// Smaller tiles / 256 x 256 in all launches of a kind, whole calls, us: gram of 4 x 4096 x 4096 6240 / 5930, of 3584 x 14336 3460 / 3350, of
+// 1024 x 4096 470 / 423, of 2048 x 2048 498 / 558, of 64 x 640 x 640 923 / 931; apply of 4 x 4096 x 4096 5690 / 5280, of
+// 12 x 2048 x 2048 2460 / 2310, of 2048 x 2048 498 / 542, of 6 x 1536 x 6144 1926 / 1948, of a 24-layer model's matrices 7520 / 7750.
+template <class Length, class Tiles, class Layout>
+static bool large_tiles(int op, int n, Length length, Tiles tiles, Layout layout, NsProductArgs& p) {
+    constexpr uint32_t kCus = kResident / 2;
+    double work[2] = {0.0, 0.0};
+    uint32_t count[2] = {0, 0};
+    int shortest = 1 << 30;
+    bool any = false;
+    p.split_tiles = 0;
+    p.splits = 1;
+    for (int k = 0; k < n; ++k) {
+        if (op == 2 && layout(k).rp < kTurnRows) return false;
+        any = any || layout(k).rp >= kLargeRows;
+        shortest = length(k) < shortest ? length(k) : shortest;
+        for (int of_256 = 0; of_256 < 2; ++of_256) {
+            const uint32_t t = tiles(k, of_256 != 0);
+            work[of_256] += (double)t * length(k);
+            count[of_256] += t;
+        }
+    }
+    p.tiles = count[1];
+    if (!any) return false;
+    const double mean[2] = {work[0] / count[0], work[1] / count[1]};
+    const double small_rounds = count[0] <= kCus ? 0.6 : ceil((double)count[0] / kResident);
+    if (op == 2) return mean[1] >= 2048.0 && ceil((double)count[1] / kCus) <= small_rounds;
+    const uint32_t left = count[1] % kCus, most = left ? kCus / left : 1, longest = (uint32_t)(shortest / SymPing::BK);
+    uint32_t splits = most < longest ? most : longest;
+    splits = splits < 8 ? splits : 8;
+    const double rounds = (double)(count[1] / kCus) + (left == 0 ? 0.0 : 1.0 / splits);
+    if (rounds * mean[1] + (splits > 1 ? 20.0 * SymPing::BK : 0.0) >= small_rounds * mean[0]) return false;
+    if (splits > 1) {
+        p.split_tiles = left;
+        p.splits = splits;
+    }
+    return true;
+}
+
 static int run_groups(const cce_matrix* matrices, int64_t count, bool step, float lr, float mu, int nesterov, const float* coefficients,
                       int steps, float eps, const float* clip_coef, void* workspace, hipStream_t stream) {
     if (!run_small(matrices, count, step, lr, mu, nesterov, coefficients, steps, eps, clip_coef, stream)) return CCE_ERR_HIP;
@@ -1075,13 +1383,17 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
         int64_t index[kGroup];
         uint64_t base[kGroup];
         int n = 0;
+        int64_t partials = 0;                          // behind the matrices
         next_group(matrices, count, i, [&](const cce_matrix& t, uint64_t at) {
             index[n] = &t - matrices;
             base[n++] = at;
+            partials = (int64_t)at + (int64_t)NsLayout((int)t.rows, (int)t.cols).bytes;
         });
         if (n == 0) continue;
         if (!allow_lds(ns_symmetric_kernel<false>, kSymLds) || !allow_lds(ns_symmetric_kernel<true>, kSymLds) ||
-            !allow_lds(ns_apply_kernel<false>, ApplyTile::kLdsBytes) || !allow_lds(ns_apply_kernel<true>, ApplyTile::kLdsBytes))
+            !allow_lds(ns_symmetric_ping_kernel<false>, kPingLds) || !allow_lds(ns_symmetric_ping_kernel<true>, kPingLds) ||
+            !allow_lds(ns_apply_kernel<false>, ApplyTile::kLdsBytes) || !allow_lds(ns_apply_kernel<true>, ApplyTile::kLdsBytes) ||
+            !allow_lds(ns_apply_turn_kernel<false>, kTurnLds) || !allow_lds(ns_apply_turn_kernel<true>, kTurnLds))
             return CCE_ERR_HIP;
         auto layout = [&](int k) { return NsLayout((int)matrices[index[k]].rows, (int)matrices[index[k]].cols); };
         // launches over as many matrices as their arguments hold
@@ -1099,23 +1411,28 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
         };
         // the matrices with the longest sums of a product first: the shorter ones fill what they leave
         uint32_t grid[3];
+        bool large[3];
         for (int op = 0; op < 3; ++op) {
             NsProductArgs& p = products[op];
             int order[kGroup];
+            auto length = [&](int x) { return op == 0 ? layout(x).cp : layout(x).rp; };
+            auto tiles = [&](int x, bool of_256) { return op < 2 ? sym_tiles(layout(x), of_256) : apply_tiles(layout(x), of_256); };
             for (int k = 0; k < n; ++k) {
-                auto length = [&](int x) { return op == 0 ? layout(x).cp : layout(x).rp; };
                 int to = k;
                 for (; to > 0 && length(order[to - 1]) < length(k); --to) order[to] = order[to - 1];
                 order[to] = k;
             }
+            large[op] = large_tiles(op, n, length, tiles, layout, p);
             grid[op] = 0;
             p.count = (uint32_t)n;
             for (int k = 0; k < n; ++k) {
                 const cce_matrix& t = matrices[index[order[k]]];
                 p.t[k] = NsShape{(uint32_t)(base[order[k]] / 256), (int32_t)t.rows, (int32_t)t.cols};
                 p.first[k] = 2 * grid[op];
-                grid[op] += op < 2 ? sym_tiles(layout(order[k])) : apply_tiles(layout(order[k]));
+                grid[op] += tiles(order[k], large[op]);
             }
+            if (large[op]) grid[op] += p.split_tiles * (p.splits - 1);
+            p.partials = (uint32_t)(partials / 256);
         }
         ends([](const cce_matrix& t, const NsLayout&) {
             const int64_t parts = (t.rows * t.cols + kNormValues - 1) / kNormValues;
@@ -1130,17 +1447,23 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
                 p.b = coefficients[3 * s + 1];
                 p.c = coefficients[3 * s + 2];
             }
-            hipLaunchKernelGGL(ns_symmetric_kernel<false>, dim3(grid[0]), dim3(SymTile::kThreads), kSymLds, stream, products[0]);
-            hipLaunchKernelGGL(ns_symmetric_kernel<true>, dim3(grid[1]), dim3(SymTile::kThreads), kSymLds, stream, products[1]);
-            if (s + 1 < steps)
-                hipLaunchKernelGGL(ns_apply_kernel<false>, dim3(grid[2]), dim3(ApplyTile::kThreads), ApplyTile::kLdsBytes, stream, products[2]);
+            if (large[0]) hipLaunchKernelGGL(ns_symmetric_ping_kernel<false>, dim3(grid[0]), dim3(SymPing::kThreads), kPingLds, stream, products[0]);
+            else hipLaunchKernelGGL(ns_symmetric_kernel<false>, dim3(grid[0]), dim3(SymTile::kThreads), kSymLds, stream, products[0]);
+            if (large[0] && products[0].split_tiles) hipLaunchKernelGGL(ns_symmetric_join_kernel<false>, dim3(8 * products[0].split_tiles), dim3(64), 0, stream, products[0]);
+            if (large[1]) hipLaunchKernelGGL(ns_symmetric_ping_kernel<true>, dim3(grid[1]), dim3(SymPing::kThreads), kPingLds, stream, products[1]);
+            else hipLaunchKernelGGL(ns_symmetric_kernel<true>, dim3(grid[1]), dim3(SymTile::kThreads), kSymLds, stream, products[1]);
+            if (large[1] && products[1].split_tiles) hipLaunchKernelGGL(ns_symmetric_join_kernel<true>, dim3(8 * products[1].split_tiles), dim3(64), 0, stream, products[1]);
+            if (s + 1 == steps) break;
+            if (large[2]) hipLaunchKernelGGL(ns_apply_turn_kernel<false>, dim3(grid[2]), dim3(TurnTile::kThreads), kTurnLds, stream, products[2]);
+            else hipLaunchKernelGGL(ns_apply_kernel<false>, dim3(grid[2]), dim3(ApplyTile::kThreads), ApplyTile::kLdsBytes, stream, products[2]);
         }
         a.flip = products[2].flip;
         a.a = products[2].a;
         a.b = products[2].b;
         a.c = products[2].c;
-        ends([](const cce_matrix&, const NsLayout& at) { return apply_tiles(at); }, [&](uint32_t blocks) {
-            hipLaunchKernelGGL(ns_apply_kernel<true>, dim3(blocks), dim3(ApplyTile::kThreads), ApplyTile::kLdsBytes, stream, a);
+        ends([&](const cce_matrix&, const NsLayout& at) { return apply_tiles(at, large[2]); }, [&](uint32_t blocks) {
+            if (large[2]) hipLaunchKernelGGL(ns_apply_turn_kernel<true>, dim3(blocks), dim3(TurnTile::kThreads), kTurnLds, stream, a);
+            else hipLaunchKernelGGL(ns_apply_kernel<true>, dim3(blocks), dim3(ApplyTile::kThreads), ApplyTile::kLdsBytes, stream, a);
         });
     }
     return hip_ok(hipGetLastError()) ? CCE_OK : CCE_ERR_HIP;

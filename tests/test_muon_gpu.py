@@ -262,6 +262,30 @@ def test_groups_share_a_workspace(B):
         assert float(torch.linalg.norm(o.double() - y) / torch.linalg.norm(y)) <= 2.0 ** -9 + 2.0 ** -8
 
 
+@pytest.mark.parametrize("shape,count", [((1024, 4096), 1), ((5001, 1030), 1), ((1090, 1100), 30), ((2048, 2048), 13), ((3583, 2100), 6), ((3590, 3600), 1), ((4096, 4096), 2)],
+                         ids=lambda s: "x".join(map(str, s)) if isinstance(s, tuple) else str(s))
+def test_large_matrices(B, shape, count):
+    """Tiles of 256 x 256, split ones among them.  Values of one size: every 64 x 64 block is off by no more than the whole may be, twice."""
+    gen = torch.Generator(device="cuda").manual_seed(shape[0] + count)
+    x = [torch.randn(shape, device="cuda", generator=gen) for _ in range(count)]
+    out = B.cce_orthogonalize_multi(x)
+    for i in {0, count // 2, count - 1}:
+        y = x[i].double() / (torch.linalg.norm(x[i].double()) + EPS)
+        y = y if shape[0] <= shape[1] else y.T.contiguous()
+        for _ in range(5):
+            gram = y @ y.T
+            y = ABC[0] * y + (ABC[1] * gram + ABC[2] * (gram @ gram)) @ y
+        y = y if shape[0] <= shape[1] else y.T.contiguous()
+        off = out[i].double() - y
+        allowed = 2.0 ** -9 + 2.0 ** -8                                           # of the operands' rounding and of bf16's
+        assert float(torch.linalg.norm(off)) <= allowed * float(torch.linalg.norm(y))
+        pad = (0, -shape[1] % 64, 0, -shape[0] % 64)
+        blocks = [torch.nn.functional.pad(t.square(), pad).unflatten(0, (-1, 64)).unflatten(2, (-1, 64)).sum((1, 3)) for t in (off, y)]
+        assert bool((blocks[0].sqrt() <= 2 * allowed * blocks[1].sqrt()).all())
+    if count > 1:
+        assert torch.equal(out[1], B.cce_orthogonalize_multi(x)[1])
+
+
 def test_refusals(B):
     x = torch.randn(4, 6, device="cuda")
     for bad in ([], [x.half()], [x.t()], [x[0]], [x.cpu()]):
