@@ -873,8 +873,8 @@ __global__ __launch_bounds__(TurnTile::kThreads, 2) void ns_apply_turn_kernel(co
 // A matrix of few rows in one workgroup, all steps in one launch: X in fp32 in the accumulators (blocks of 16 x 16 by eight
 // wavefronts, block column j of wavefront w being 8 j + w), its h in LDS for the products.  The linear part a X needs no remainder here.
 //
-//   gram    wavefronts share the blocks of A, each over all columns of h
-//   poly    the same blocks; M takes A's place in LDS
+//   gram    up to 64 rows each wavefront sums over its own columns; of more rows wavefronts share the blocks of A, each over all columns of h
+//   poly    wavefronts share the blocks
 //   apply   each wavefront its own columns, which no other one reads: X stays in its registers
 //
 // The 17 launches of the tiled path take 115 us for 64 x 256 and 199 for 48 matrices of 16 x 896, mostly waiting for each other.
@@ -897,11 +897,19 @@ template <int RB_, int NB_>
 struct SmallShape {
     static constexpr int RB = RB_, NB = NB_, kRows = 16 * RB_, kColumns = RB_ < 8 ? NB_ * 128 : 448;
     static constexpr int kPitchA = kRows + 8;
-    static constexpr int pitch(int c) { return ((c + 63) & ~63) + 8; }
+    static constexpr bool kOwnSums = RB_ <= 4;           // A from each wavefront's own columns
+    static constexpr int kPairs = RB_ * (RB_ + 1) / 2;   // blocks of A, of each two that mirror each other one
+    static constexpr int kSumBytes = kOwnSums ? 8 * kPairs * 1024 : 0, kMBytes = kOwnSums ? kRows * kPitchA * 2 : 0;
     static constexpr int kStagePitch = 16 + 1, kStageBytes = kRows * kStagePitch * 4;      // a block column of a wavefront, on its way in or out
+    static constexpr int pitch(int c) { return ((c + 63) & ~63) + 8; }
+    static constexpr int h_bytes(int c) { return kRows * pitch(c) * 2; }
+    static constexpr int kRest = 64 + kRows * kPitchA * 2 + kMBytes + kRows * 8;
+    // whether the wavefronts' sums have room of their own; else they lie over h, of which none is needed then
+    static constexpr bool apart(int c) { return kRest + h_bytes(c) + kSumBytes <= 160 * 1024; }
+    static constexpr int h_room(int c) { return apart(c) || h_bytes(c) > kSumBytes ? h_bytes(c) : kSumBytes; }
     static constexpr int lds(int c) {
-        const int work = kRows * pitch(c) * 2 + kRows * kPitchA * 2 + kRows * 8, stages = 8 * kStageBytes;
-        return 64 + (work > stages ? work : stages);
+        const int work = kRest + h_room(c) + (apart(c) ? kSumBytes : 0), stages = 64 + 8 * kStageBytes;
+        return work > stages ? work : stages;
     }
     static constexpr bool takes(int64_t r, int64_t c) { return r <= kRows && c <= kColumns; }
 };
@@ -910,6 +918,14 @@ typedef SmallShape<4, 8> Small64;
 typedef SmallShape<8, 4> Small128;
 static_assert(Small32::lds(Small32::kColumns) <= 160 * 1024 && Small64::lds(Small64::kColumns) <= 160 * 1024 &&
               Small128::lds(Small128::kColumns) <= 160 * 1024, "160 KB LDS");
+static_assert(Small32::apart(Small32::kColumns) && Small64::apart(448) && !Small64::apart(449), "either form is tested");
+
+__device__ __forceinline__ f16x4 half4(const f32x4& x) {
+    f16x4 h;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = (_Float16)x[e];
+    return h;
+}
 
 template <class S>
 __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatrix& t, bool bf16, CCE_LDS char* smem) {
@@ -921,9 +937,12 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
     const int columns = (c + 63) & ~63, block_columns = columns >> 4, pitch = columns + 8;
     CCE_LDS double* const red = (CCE_LDS double*)smem;
     CCE_LDS _Float16* const H = (CCE_LDS _Float16*)(smem + 64);
-    CCE_LDS _Float16* const A = H + S::kRows * pitch;
-    CCE_LDS float* const da = (CCE_LDS float*)(A + S::kRows * S::kPitchA);
+    CCE_LDS _Float16* const A = (CCE_LDS _Float16*)(smem + 64 + S::h_room(c));
+    CCE_LDS _Float16* const M = A + (S::kOwnSums ? S::kRows * S::kPitchA : 0);        // (in A's place where it has no other)
+    CCE_LDS float* const da = (CCE_LDS float*)(M + S::kRows * S::kPitchA);
     CCE_LDS float* const dm = da + S::kRows;
+    const bool apart = S::apart(c);
+    CCE_LDS float* const sums = apart ? dm + S::kRows : (CCE_LDS float*)H;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int l16 = lane & 15, quad = lane >> 4;
     int mine = __builtin_amdgcn_readfirstlane((block_columns + 7 - wave) >> 3);       // this wavefront's block columns
@@ -1031,51 +1050,79 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
         auto of_lane = [&](int i) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(coefficient), i)); };
         const float ca = of_lane(3 * s), cb = of_lane(3 * s + 1), cc = of_lane(3 * s + 2);
         asm volatile("" : "+s"(mine));                // (comparisons with it are made where they are needed: kept over the loop they were spilled)
+        auto write_h = [&]() {
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            if (j >= mine) continue;
+            for (int j = 0; j < NB; ++j) {
+                if (j >= mine) continue;
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                f16x4 h;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) h[e] = (_Float16)x[j][rb][e];
-                *(CCE_LDS f16x4*)(H + (16 * rb + l16) * pitch + 16 * (8 * j + wave) + 4 * quad) = h;
+                for (int rb = 0; rb < RB; ++rb)
+                    *(CCE_LDS f16x4*)(H + (16 * rb + l16) * pitch + 16 * (8 * j + wave) + 4 * quad) = half4(x[j][rb]);
             }
-        }
-        __syncthreads();
+        };
         f32x4 g[BI][BJ];
         f16x4 o[BI][BJ];
 #pragma unroll
         for (int y = 0; y < BI; ++y)
 #pragma unroll
             for (int z = 0; z < BJ; ++z) g[y][z] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (has_blocks) {
-            if constexpr (BI * BJ <= 2) {             // few products at a time: two sums of each
-                f32x4 g1[BI][BJ];
+        if constexpr (S::kOwnSums) {
+            // Two block columns of a wavefront are a fragment as they lie in its registers (which of its k an element is does not matter, it is
+            // the same one in both operands): sums over its own columns of the blocks on and below the diagonal, without LDS.  Then the
+            // eight sums of each block through LDS: 64 x 256 in 23 us, 48 matrices of 16 x 896 in 29 when every wavefront read all of h.
+            f32x4 part[S::kPairs];
 #pragma unroll
-                for (int y = 0; y < BI; ++y)
+            for (int p = 0; p < S::kPairs; ++p) part[p] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int z = 0; z < BJ; ++z) g1[y][z] = f32x4{0.f, 0.f, 0.f, 0.f};
-                int k = 0;
-                for (; k + 64 < columns; k += 128) {
-                    blocks_product(g, H + frag, pitch, k);
-                    blocks_product(g1, H + frag, pitch, k + 32);
-                    blocks_product(g, H + frag, pitch, k + 64);
-                    blocks_product(g1, H + frag, pitch, k + 96);
-                }
-                if (k < columns) {
-                    blocks_product(g, H + frag, pitch, k);
-                    blocks_product(g1, H + frag, pitch, k + 32);
+            for (int j = 0; j < NB; j += 2) {
+                if (j >= mine) continue;
+                f16x8 h[RB];
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                    const f16x4 lo = half4(x[j][rb]), hi = half4(x[j + 1][rb]);
+                    h[rb] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
                 }
 #pragma unroll
-                for (int y = 0; y < BI; ++y)
+                for (int y = 0; y < RB; ++y)
 #pragma unroll
-                    for (int z = 0; z < BJ; ++z) g[y][z] += g1[y][z];
-            } else {
-                for (int k = 0; k < columns; k += 64) {
-                    blocks_product(g, H + frag, pitch, k);
-                    blocks_product(g, H + frag, pitch, k + 32);
+                    for (int z = 0; z <= y; ++z)
+                        part[y * (y + 1) / 2 + z] = __builtin_amdgcn_mfma_f32_16x16x32_f16(h[y], h[z], part[y * (y + 1) / 2 + z], 0, 0, 0);
+            }
+            if (!apart) __syncthreads();               // h is not needed any more
+#pragma unroll
+            for (int p = 0; p < S::kPairs; ++p) *(CCE_LDS f32x4*)(sums + (wave * S::kPairs + p) * 256 + 4 * lane) = part[p];
+            __syncthreads();
+        } else {
+            write_h();
+            __syncthreads();
+        }
+        if constexpr (S::kOwnSums) {
+#pragma unroll
+            for (int p0 = 0; p0 < S::kPairs; p0 += 8) {
+                const int p = p0 + wave;
+                if (p >= S::kPairs) continue;
+                const int y = p >= 6 ? 3 : p >= 3 ? 2 : p >= 1 ? 1 : 0, z = p - y * (y + 1) / 2;
+                f32x4 v[8];
+#pragma unroll
+                for (int w = 0; w < 8; ++w) v[w] = *(const CCE_LDS f32x4*)(sums + (w * S::kPairs + p) * 256 + 4 * lane);
+                const f32x4 sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+                // element e: column 16 y + 4 quad + e of row 16 z + l16
+                f16x4 of_a;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float value = sum[e] * (1.f / (kScaleX * kScaleX));
+                    const bool diagonal = y == z && 4 * quad + e == l16;
+                    if (diagonal) da[16 * y + l16] = value;
+                    of_a[e] = diagonal ? (_Float16)0.f : (_Float16)(value * kScaleA);
                 }
+                *(CCE_LDS f16x4*)(A + (16 * z + l16) * S::kPitchA + 16 * y + 4 * quad) = of_a;
+                if (y != z)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) A[(16 * y + 4 * quad + e) * S::kPitchA + 16 * z + l16] = of_a[e];
+            }
+        } else if (has_blocks) {
+            for (int k = 0; k < columns; k += 64) {
+                blocks_product(g, H + frag, pitch, k);
+                blocks_product(g, H + frag, pitch, k + 32);
             }
             // element e of a block: column 16 (bi + y) + 4 quad + e of row 16 (bj + z) + l16
 #pragma unroll
@@ -1098,8 +1145,13 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
 #pragma unroll
             for (int k = 0; k < S::kRows; k += 32) blocks_product(g, A + frag_a, S::kPitchA, k);
         }
-        __syncthreads();
+        if constexpr (S::kOwnSums) write_h();
+        else __syncthreads();                          // M takes A's place
         if (has_blocks) {
+            if constexpr (S::kOwnSums) {
+#pragma unroll
+                for (int z = 0; z < BJ; ++z) o[0][z] = *(const CCE_LDS f16x4*)(A + (16 * (bj + z) + l16) * S::kPitchA + 16 * bi + 4 * quad);
+            }
 #pragma unroll
             for (int y = 0; y < BI; ++y) {
                 const f32x4 dc = *(const CCE_LDS f32x4*)(da + 16 * (bi + y) + 4 * quad);
@@ -1116,7 +1168,7 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
                         if (diagonal) dm[col] = cb * dn + (cc * dn * dn + p);
                         m[e] = diagonal ? (_Float16)0.f : (_Float16)v;
                     }
-                    *(CCE_LDS f16x4*)(A + (16 * (bj + z) + l16) * S::kPitchA + 16 * (bi + y) + 4 * quad) = m;
+                    *(CCE_LDS f16x4*)(M + (16 * (bj + z) + l16) * S::kPitchA + 16 * (bi + y) + 4 * quad) = m;
                 }
             }
         }
@@ -1135,7 +1187,7 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
         for (int k = 0; k < S::kRows; k += 32) {
             f16x8 m[RB];
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) m[rb] = *(const CCE_LDS f16x8*)(A + 16 * rb * S::kPitchA + frag_a + k);
+            for (int rb = 0; rb < RB; ++rb) m[rb] = *(const CCE_LDS f16x8*)(M + 16 * rb * S::kPitchA + frag_a + k);
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
                 if (j >= mine) continue;
