@@ -1,7 +1,7 @@
 // libcce, optimizer kernels for matrices: momentum, Newton-Schulz products, update.  C ABI declared in include/cce_muon.h.
 //
-// A matrix is worked on as X of r x c, r <= c (transposed on the way in and out where it is taller than wide), in the
-// workspace, rows and columns padded with zeros to multiples of 64.  Per step three launches over all matrices of a group:
+// A matrix is worked on as X of r x c, r <= c (transposed on the way in and out where it is taller than wide).  Small ones are
+// taken by a workgroup each in one launch, thin ones in three (see both below), all others in the workspace, rows and columns padded with zeros to multiples of 64.  Per step three launches over all matrices of a group:
 //
 //   gram    A = X X^T             half of the tiles, the other half mirrored
 //   poly    M = b A + c A A       the same
@@ -1245,6 +1245,332 @@ __global__ __launch_bounds__(kSmallThreads, 2) void ns_small_kernel(const NsSmal
 }
 
 // ------------------------------------------------------------------------------------------
+// Up to 64 rows, more columns than a workgroup takes.  Every step's polynomial is one of the first A = X X^T: with S = a + b A + c A A the
+// next A is S A S, and the result Q X, where Q is the product of all S.  So X is read twice and written once, in three launches:
+//
+//   gram    momentum, and the sums of G G^T over a part of the columns each workgroup
+//   steps   a workgroup a matrix: joins the sums, |G| from their diagonal, the steps on r x r matrices
+//   apply   Q X, to the caller
+//
+// A direction that a step moves has its share of A amplified by up to the steps' square (2e5 for 3.4445^5), an error of A with
+// it: 1e-7 of fp32 would show where |G|'s largest directions are 500 times the others'.  The r x r matrices are held and multiplied in 64
+// bits, X and Q in 32.
+// 16 x 4096 takes 23 us, 48 matrices of 16 x 14336 (66 MB in and out) 50 us on the GPU (17 + 11 + 22), 8 of 64 x 4096 76 (13 + 44 + 17: the steps
+// are bound by the latency and rate of 64-bit products on a CU).  The tiled path, whose first product has one workgroup a matrix here, took
+// 300, 1108 and 268 (of 48 rows) us.
+// ------------------------------------------------------------------------------------------
+typedef __attribute__((ext_vector_type(4))) double f64x4;
+constexpr int64_t kThinRows = 64;
+constexpr int kThinThreads = 256, kThinStepThreads = 512;
+constexpr int kThinParts = 64;                         // workgroups that sum a matrix, at most
+constexpr int kThinColumns = 256;                      // columns of one, more where that gives too many
+
+struct NsThinArgs {
+    NsArgs a;
+    float coefficients[CCE_NS_MAX_STEPS][3];
+    int32_t steps;
+};
+static_assert(sizeof(NsThinArgs) <= 4096, "kernel arguments hold 4 KB");
+
+// Where a matrix's sums and Q lie, in bytes behind its base.
+struct ThinLayout {
+    int r, c, blocks, parts, columns;                  // blocks of 16 rows; columns of a part
+    uint64_t q, inv, bytes;
+    __host__ __device__ __forceinline__ ThinLayout(int rows, int cols) {
+        r = rows < cols ? rows : cols;
+        c = rows < cols ? cols : rows;
+        blocks = r <= 16 ? 1 : r <= 32 ? 2 : 4;
+        parts = c / kThinColumns < kThinParts ? (c + kThinColumns - 1) / kThinColumns : kThinParts;
+        columns = ((c + parts - 1) / parts + 63) & ~63;
+        parts = (c + columns - 1) / columns;
+        q = (uint64_t)parts * (uint64_t)(blocks * (blocks + 1) / 2) * 2048;
+        inv = q + (uint64_t)(blocks * blocks) * 1024;
+        bytes = inv + 256;
+    }
+};
+
+// Row of element e of a 64-bit matrix instruction's result.
+__device__ __forceinline__ int f64_row(int quad, int e) { return 4 * e + quad; }
+
+template <int RB>
+__device__ __forceinline__ void thin_gram(const NsArgs& a, const NsMatrix& t, bool bf16, const ThinLayout& at, int part, CCE_LDS double* red) {
+    constexpr int kPairs = RB * (RB + 1) / 2;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, quad = lane >> 4;
+    const bool tall = t.rows > t.cols, vec = !tall && (t.cols & 3) == 0 && aligned(t.grad, bf16 ? 8 : 16) && aligned(t.momentum, 16);
+    const float clip = a.clip_coef ? a.clip_coef[0] : 1.f;
+    const int end = (part + 1) * at.columns < at.c ? (part + 1) * at.columns : at.c;
+    f64x4 sum[kPairs];
+#pragma unroll
+    for (int p = 0; p < kPairs; ++p) sum[p] = f64x4{0.0, 0.0, 0.0, 0.0};
+    for (int col0 = part * at.columns + 16 * wave; col0 < end; col0 += 64) {
+        const int col = col0 + 4 * quad;
+        f32x4 x[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const int row = 16 * rb + l16;
+            x[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (row >= at.r || col >= at.c) continue;
+            if (vec) {
+                const int64_t i = (int64_t)row * t.cols + col;
+                x[rb] = grad_values(t.grad, bf16, i);
+                if (t.momentum) {
+                    f32x4 m = *(const f32x4*)(t.momentum + i);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float g = x[rb][e] * clip;
+                        m[e] = new_momentum(m[e], g, a.mu);
+                        x[rb][e] = direction(m[e], g, a.mu, a.nesterov);
+                    }
+                    *(f32x4*)(t.momentum + i) = m;
+                }
+                continue;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (col + e >= at.c) continue;
+                const int64_t i = tall ? (int64_t)(col + e) * t.cols + row : (int64_t)row * t.cols + col + e;
+                float g = grad_value(t.grad, bf16, i);
+                if (t.momentum) {
+                    g *= clip;
+                    const float m = new_momentum(t.momentum[i], g, a.mu);
+                    t.momentum[i] = m;
+                    g = direction(m, g, a.mu, a.nesterov);
+                }
+                x[rb][e] = g;
+            }
+        }
+        // which column an instruction's k is does not matter, it is the same one in both operands
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            double v[RB];
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) v[rb] = (double)x[rb][e];
+#pragma unroll
+            for (int y = 0; y < RB; ++y)
+#pragma unroll
+                for (int z = 0; z <= y; ++z)
+                    sum[y * (y + 1) / 2 + z] = __builtin_amdgcn_mfma_f64_16x16x4f64(v[y], v[z], sum[y * (y + 1) / 2 + z], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < kPairs; ++p)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) red[(wave * kPairs + p) * 256 + 64 * e + lane] = sum[p][e];
+    __syncthreads();
+    double* const to = (double*)(a.ws + t.base) + (size_t)part * (kPairs * 256);
+    for (int i = threadIdx.x; i < kPairs * 256; i += kThinThreads)
+        to[i] = (red[i] + red[kPairs * 256 + i]) + (red[2 * kPairs * 256 + i] + red[3 * kPairs * 256 + i]);
+}
+constexpr int kThinGramLds = 4 * 10 * 256 * 8;
+
+__global__ __launch_bounds__(kThinThreads, 2) void ns_thin_gram_kernel(const NsArgs a) {
+    extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
+    CCE_LDS double* const red = (CCE_LDS double*)smem_generic;
+    const int i = matrix_of(a.first, (int)a.count, 2 * blockIdx.x + 1);
+    const NsMatrix& t = a.t[i];
+    const bool bf16 = (a.first[i] & 1u) != 0u;
+    const ThinLayout at(t.rows, t.cols);
+    const int part = (int)(blockIdx.x - (a.first[i] >> 1));
+    if (at.blocks == 1) thin_gram<1>(a, t, bf16, at, part, red);
+    else if (at.blocks == 2) thin_gram<2>(a, t, bf16, at, part, red);
+    else thin_gram<4>(a, t, bf16, at, part, red);
+}
+
+// The r x r matrices lie in LDS, symmetric up to their rounding, so that either operand's fragments are read along rows.
+template <int RB>
+__device__ __forceinline__ void thin_steps(const NsThinArgs& args, const NsMatrix& t, const ThinLayout& at, CCE_LDS double* lds) {
+    constexpr int R = 16 * RB, P = R + 8, kPairs = RB * (RB + 1) / 2, BZ = RB == 4 ? 2 : 1;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    CCE_LDS double* const A = lds;
+    CCE_LDS double* const S = A + R * P;
+    CCE_LDS double* const U = S + R * P;
+    CCE_LDS double* const Q = U + R * P;
+    CCE_LDS double* const trace = Q + R * P;
+    char* const base = args.a.ws + t.base;
+    for (int i = threadIdx.x; i < kPairs * 256; i += kThinStepThreads) {
+        const double* from = (const double*)base + i;
+        double sum = 0.0;
+        for (int k0 = 0; k0 < at.parts; k0 += 8) {
+            double v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = k0 + k < at.parts ? from[(size_t)(k0 + k) * (kPairs * 256)] : 0.0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += v[k];
+        }
+        const int p = i >> 8, y = p >= 6 ? 3 : p >= 3 ? 2 : p >= 1 ? 1 : 0, z = p - y * (y + 1) / 2;
+        const int row = 16 * y + f64_row((i & 63) >> 4, (i & 255) >> 6), col = 16 * z + (i & 15);
+        A[row * P + col] = sum;
+        if (y != z) A[col * P + row] = sum;
+    }
+    __syncthreads();
+    if (wave == 0) {
+        double d = lane < R ? A[lane * P + lane] : 0.0;
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) d += __shfl_xor(d, o);
+        if (lane == 0) trace[0] = d;
+    }
+    __syncthreads();
+    const double sum = trace[0];
+    const double inv = sum <= 0x1.fffffffffffffp1023 ? 1.0 / (sqrt(sum) + (double)args.a.eps) : (double)NAN;
+    for (int i = threadIdx.x; i < R * R; i += kThinStepThreads) A[i / R * P + i % R] *= inv * inv;
+    __syncthreads();
+    const int by = wave * BZ / RB, bz = wave * BZ % RB;               // this wavefront's blocks: (by, bz), and the next
+    const bool has = by < RB;
+    auto product = [&](const CCE_LDS double* x, const CCE_LDS double* y, f64x4 (&g)[BZ]) {
+#pragma unroll
+        for (int b = 0; b < BZ; ++b) g[b] = f64x4{0.0, 0.0, 0.0, 0.0};
+        if (!has) return;
+#pragma unroll
+        for (int k0 = 0; k0 < R; k0 += 4) {
+            const int k = k0 + quad;
+            const double v = x[k * P + 16 * by + l16];
+#pragma unroll
+            for (int b = 0; b < BZ; ++b) g[b] = __builtin_amdgcn_mfma_f64_16x16x4f64(v, y[k * P + 16 * (bz + b) + l16], g[b], 0, 0, 0);
+        }
+    };
+    auto place = [&](int b, int e) { return (16 * by + f64_row(quad, e)) * P + 16 * (bz + b) + l16; };
+    auto write = [&](CCE_LDS double* to, const f64x4 (&g)[BZ]) {
+        if (!has) return;
+#pragma unroll
+        for (int b = 0; b < BZ; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) to[place(b, e)] = g[b][e];
+    };
+    f64x4 q[BZ];
+    for (int s = 0; s < args.steps; ++s) {
+        const double ca = args.coefficients[s][0], cb = args.coefficients[s][1], cc = args.coefficients[s][2];
+        f64x4 g[BZ];
+        product(A, A, g);
+        if (has) {
+#pragma unroll
+            for (int b = 0; b < BZ; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    g[b][e] = fma(cc, g[b][e], cb * A[place(b, e)]) + (by == bz + b && f64_row(quad, e) == l16 ? ca : 0.0);
+        }
+        write(S, g);
+        __syncthreads();
+        if (s == 0) {
+#pragma unroll
+            for (int b = 0; b < BZ; ++b) q[b] = g[b];
+        } else {
+            product(S, Q, q);
+        }
+        if (s + 1 == args.steps) break;
+        product(S, A, g);
+        write(U, g);
+        __syncthreads();
+        write(Q, q);
+        product(S, U, g);
+        write(A, g);
+        __syncthreads();
+    }
+    float* const out = (float*)(base + at.q);
+    if (has) {
+#pragma unroll
+        for (int b = 0; b < BZ; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[(16 * by + f64_row(quad, e)) * R + 16 * (bz + b) + l16] = (float)q[b][e];
+    }
+    if (threadIdx.x == 0) *(double*)(base + at.inv) = inv;
+}
+constexpr int thin_step_lds(int blocks) { return (4 * 16 * blocks * (16 * blocks + 8) + 1) * 8; }
+static_assert(thin_step_lds(4) <= 160 * 1024, "160 KB LDS");
+
+__global__ __launch_bounds__(kThinStepThreads, 2) void ns_thin_steps_kernel(const NsThinArgs a) {
+    extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
+    CCE_LDS double* const lds = (CCE_LDS double*)smem_generic;
+    const NsMatrix& t = a.a.t[blockIdx.x];
+    const ThinLayout at(t.rows, t.cols);
+    if (at.blocks == 1) thin_steps<1>(a, t, at, lds);
+    else if (at.blocks == 2) thin_steps<2>(a, t, at, lds);
+    else thin_steps<4>(a, t, at, lds);
+}
+
+// 64 columns a wavefront, as four sets of 16: of a wide matrix set s is every fourth column from the s-th on, so that a lane has four
+// neighbours of a row in memory; of a tall one 16 neighbouring columns, of which a lane has four neighbouring rows.
+template <int RB>
+__device__ __forceinline__ void thin_apply(const NsArgs& a, const NsMatrix& t, bool bf16, const ThinLayout& at, int c0) {
+    constexpr int R = 16 * RB;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+    const bool tall = t.rows > t.cols, vec_in = (t.cols & 3) == 0 && aligned(t.grad, bf16 ? 8 : 16) && aligned(t.momentum, 16);
+    const bool vec_out = (t.cols & 3) == 0 && aligned(t.param, 16) && aligned(t.out, 8);
+    const float clip = a.clip_coef ? a.clip_coef[0] : 1.f;
+    const char* const base = a.ws + t.base;
+    const double inv = *(const double*)(base + at.inv);
+    // four neighbours in memory: of line `line` of the caller's matrix from `in` on, `left` of them there
+    auto four = [&](int line, int in, int left) {
+        const int64_t i = (int64_t)line * t.cols + in;
+        f32x4 u = {0.f, 0.f, 0.f, 0.f};
+        if (vec_in && left >= 4) {
+            u = grad_values(t.grad, bf16, i);
+            if (t.momentum) {
+                const f32x4 m = *(const f32x4*)(t.momentum + i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) u[e] = direction(m[e], u[e] * clip, a.mu, a.nesterov);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (e >= left) continue;
+                u[e] = grad_value(t.grad, bf16, i + e);
+                if (t.momentum) u[e] = direction(t.momentum[i + e], u[e] * clip, a.mu, a.nesterov);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] = e < left ? (float)((double)u[e] * inv) : 0.f;
+        return u;
+    };
+    f32x4 x[RB][4];                                    // [t][e][s] wide, [t][s][e] tall: row 16 t + 4 quad + e, set s
+#pragma unroll
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int row = 16 * b + 4 * quad + (tall ? 0 : k), col = c0 + (tall ? 16 * k + l16 : 4 * l16);
+            const int left = row < at.r && col < at.c ? (tall ? at.r - row : at.c - col) : 0;
+            x[b][k] = tall ? four(col, row, left) : four(row, col, left);
+        }
+    f32x4 q[RB];
+    const float* const Q = (const float*)(base + at.q);
+#pragma unroll
+    for (int ro = 0; ro < RB; ++ro) {
+#pragma unroll
+        for (int b = 0; b < RB; ++b) q[b] = *(const f32x4*)(Q + (16 * ro + l16) * R + 16 * b + 4 * quad);
+        f32x4 y[4];                                    // of each set: rows 16 ro + 4 quad + g of column l16
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            y[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    y[s] = __builtin_amdgcn_mfma_f32_16x16x4f32(q[b][e], tall ? x[b][s][e] : x[b][e][s], y[s], 0, 0, 0);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int row = 16 * ro + 4 * quad + (tall ? 0 : k), col = c0 + (tall ? 16 * k + l16 : 4 * l16);
+            if (row >= at.r || col >= at.c) continue;
+            const int left = tall ? at.r - row : at.c - col;
+            const f32x4 v = tall ? y[k] : f32x4{y[0][k], y[1][k], y[2][k], y[3][k]};
+            give4(t, tall ? (int64_t)col * t.cols + row : (int64_t)row * t.cols + col, v, left, vec_out && left >= 4);
+        }
+    }
+}
+
+__global__ __launch_bounds__(kThinThreads, 2) void ns_thin_apply_kernel(const NsArgs a) {
+    const int i = matrix_of(a.first, (int)a.count, 2 * blockIdx.x + 1);
+    const NsMatrix& t = a.t[i];
+    const bool bf16 = (a.first[i] & 1u) != 0u;
+    const ThinLayout at(t.rows, t.cols);
+    const int c0 = ((int)(blockIdx.x - (a.first[i] >> 1)) * (kThinThreads / 64) + (int)(threadIdx.x >> 6)) * 64;
+    if (c0 >= at.c) return;
+    if (at.blocks == 1) thin_apply<1>(a, t, bf16, at, c0);
+    else if (at.blocks == 2) thin_apply<2>(a, t, bf16, at, c0);
+    else thin_apply<4>(a, t, bf16, at, c0);
+}
+
+// ------------------------------------------------------------------------------------------
 // Host side.
 // ------------------------------------------------------------------------------------------
 static bool misaligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
@@ -1323,6 +1649,23 @@ static int small_lds(const cce_matrix& t) {
     return Small32::takes(r, c) ? Small32::lds((int)c) : Small64::takes(r, c) ? Small64::lds((int)c) : Small128::takes(r, c) ? Small128::lds((int)c) : 0;
 }
 
+static bool is_thin(const cce_matrix& t) { return (t.rows <= kThinRows || t.cols <= kThinRows) && small_lds(t) == 0; }
+
+// The thin matrices from `i` on that share their launches; moves i behind them.  Returns their workspace.
+template <class Take>
+static int64_t next_thin_group(const cce_matrix* matrices, int64_t count, int64_t& i, Take take) {
+    int64_t bytes = 0;
+    int n = 0;
+    for (; i < count && n < kEnds; ++i) {
+        const cce_matrix& t = matrices[i];
+        if (t.rows == 0 || t.cols == 0 || !is_thin(t)) continue;
+        take(t, (uint64_t)bytes);
+        ++n;
+        bytes += (int64_t)ThinLayout((int)t.rows, (int)t.cols).bytes;
+    }
+    return bytes;
+}
+
 // The matrices from `i` on that share their launches; moves i behind them.  Returns their workspace.
 template <class Take>
 static int64_t next_group(const cce_matrix* matrices, int64_t count, int64_t& i, Take take) {
@@ -1331,7 +1674,7 @@ static int64_t next_group(const cce_matrix* matrices, int64_t count, int64_t& i,
     bool large = false;
     for (; i < count && n < kGroup; ++i) {
         const cce_matrix& t = matrices[i];
-        if (t.rows == 0 || t.cols == 0 || small_lds(t) != 0) continue;
+        if (t.rows == 0 || t.cols == 0 || small_lds(t) != 0 || is_thin(t)) continue;
         const NsLayout at((int)t.rows, (int)t.cols);
         if (n != 0 && bytes + (int64_t)at.bytes > kGroupBytes - kPartialBytes) break;
         take(t, (uint64_t)bytes);
@@ -1373,6 +1716,47 @@ static bool run_small(const cce_matrix* matrices, int64_t count, bool step, floa
         if (n == 0) continue;
         if (!allow_lds(ns_small_kernel, 160 * 1024)) return false;
         hipLaunchKernelGGL(ns_small_kernel, dim3((unsigned)n), dim3(kSmallThreads), bytes, stream, a);
+    }
+    return true;
+}
+
+static bool run_thin(const cce_matrix* matrices, int64_t count, bool step, float lr, float mu, int nesterov, const float* coefficients,
+                     int steps, float eps, const float* clip_coef, void* workspace, hipStream_t stream) {
+    NsThinArgs args;
+    NsArgs& a = args.a;
+    a.ws = (char*)workspace;
+    a.clip_coef = clip_coef;
+    a.mu = mu;
+    a.nesterov = nesterov;
+    a.eps = eps;
+    args.steps = steps;
+    for (int s = 0; s < 3 * steps; ++s) args.coefficients[s / 3][s % 3] = coefficients[s];
+    for (int64_t i = 0; i < count;) {
+        a.count = 0;
+        uint32_t blocks = 0, parts[kEnds], columns[kEnds], grads[kEnds];
+        int most = 1;
+        next_thin_group(matrices, count, i, [&](const cce_matrix& t, uint64_t base) {
+            const ThinLayout at((int)t.rows, (int)t.cols);
+            most = at.blocks > most ? at.blocks : most;
+            a.t[a.count] = table_entry(t, step, lr, base);
+            parts[a.count] = (uint32_t)at.parts;
+            columns[a.count] = (uint32_t)(at.c + kThinThreads - 1) / kThinThreads;
+            grads[a.count++] = (uint32_t)t.grad_bf16;
+        });
+        if (a.count == 0) continue;
+        if (!allow_lds(ns_thin_gram_kernel, kThinGramLds) || !allow_lds(ns_thin_steps_kernel, thin_step_lds(4))) return false;
+        auto place = [&](const uint32_t* per) {
+            blocks = 0;
+            for (uint32_t k = 0; k < a.count; ++k) {
+                a.first[k] = 2 * blocks + grads[k];
+                blocks += per[k];
+            }
+        };
+        place(parts);
+        hipLaunchKernelGGL(ns_thin_gram_kernel, dim3(blocks), dim3(kThinThreads), 4 * (most * (most + 1) / 2) * 2048, stream, a);
+        hipLaunchKernelGGL(ns_thin_steps_kernel, dim3(a.count), dim3(kThinStepThreads), thin_step_lds(most), stream, args);
+        place(columns);
+        hipLaunchKernelGGL(ns_thin_apply_kernel, dim3(blocks), dim3(kThinThreads), 0, stream, a);
     }
     return true;
 }
@@ -1423,6 +1807,7 @@ static bool large_tiles(int op, int n, Length length, Tiles tiles, Layout layout
 static int run_groups(const cce_matrix* matrices, int64_t count, bool step, float lr, float mu, int nesterov, const float* coefficients,
                       int steps, float eps, const float* clip_coef, void* workspace, hipStream_t stream) {
     if (!run_small(matrices, count, step, lr, mu, nesterov, coefficients, steps, eps, clip_coef, stream)) return CCE_ERR_HIP;
+    if (!run_thin(matrices, count, step, lr, mu, nesterov, coefficients, steps, eps, clip_coef, workspace, stream)) return CCE_ERR_HIP;
     NsArgs a;
     NsProductArgs products[3];                         // gram, poly, apply
     a.ws = (char*)workspace;
@@ -1539,6 +1924,10 @@ size_t cce_muon_workspace_bytes(const cce_matrix* matrices, int64_t count) {
     int64_t most = 256;
     for (int64_t i = 0; i < count;) {
         const int64_t bytes = next_group(matrices, count, i, [](const cce_matrix&, uint64_t) {});
+        most = bytes > most ? bytes : most;
+    }
+    for (int64_t i = 0; i < count;) {
+        const int64_t bytes = next_thin_group(matrices, count, i, [](const cce_matrix&, uint64_t) {});
         most = bytes > most ? bytes : most;
     }
     return (size_t)most;

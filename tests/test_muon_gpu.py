@@ -24,7 +24,7 @@ ABC = (3.4445, -4.7750, 2.0315)
 EPS = 1e-7
 SHAPES = [(1, 1), (1, 7), (9, 1), (3, 5), (16, 16), (17, 129), (64, 64), (63, 65), (65, 63), (128, 300), (300, 128), (127, 511), (129, 257),
           (192, 192), (256, 1024), (1024, 130), (16, 896), (896, 16), (33, 2049), (385, 641), (32, 2048), (2000, 29), (31, 2052), (64, 1024), (1000, 50), (128, 448), (448, 100), (449, 128),
-          (97, 128), (65, 444), (2, 100)]
+          (97, 128), (65, 444), (2, 100), (16, 4096), (5000, 13), (17, 2305), (50, 1030), (2051, 33), (64, 16500)]
 
 
 @pytest.fixture(scope="module")
@@ -105,14 +105,14 @@ def test_many_matrices_and_nothing_beside_them(B, offset):
 
 @pytest.mark.parametrize("scale", [1e-38, 1e-20, 1e18, 1e36])
 def test_scales_that_have_no_square_in_fp32(B, scale):
-    for shape in ((40, 100), (200, 150)):
+    for shape in ((40, 100), (200, 150), (24, 3000)):
         g = _matrix(*shape, 3, scale=scale)
         out, = B.cce_orthogonalize_multi([torch.from_numpy(g).cuda()], eps=0.0)
         _check(out.float().cpu().numpy().astype(np.float64), g, eps=0.0)
 
 
 def test_zeros_and_values_that_are_not_finite(B):
-    for shape in ((20, 30), (200, 130)):
+    for shape in ((20, 30), (200, 130), (20, 2500)):
         x = [torch.from_numpy(_matrix(*shape, i)).cuda() for i in range(4)]
         x[0].zero_()
         x[1][3, 5] = math.inf
@@ -128,7 +128,7 @@ def test_steps_and_coefficients(B, steps):
     rng = np.random.default_rng(steps)
     per = np.stack([rng.uniform(1.2, 3.5, steps), rng.uniform(-3.0, -0.5, steps), rng.uniform(0.1, 0.6, steps)], 1).astype(np.float32)
     per[:, 2] = np.minimum(per[:, 2], 1.0)
-    for shape in ((30, 50), (150, 260)):
+    for shape in ((30, 50), (150, 260), (2100, 20)):
         g = _matrix(*shape, 4)
         try:
             out, = B.cce_orthogonalize_multi([torch.from_numpy(g).cuda()], steps=steps, coefficients=per)
@@ -191,10 +191,10 @@ def test_muon_step(B, nesterov, copies):
 
 
 def test_a_step_repeated_gives_the_same_bits(B):
-    shapes = [(256, 700), (40, 60), (513, 129)]
+    shapes = [(256, 700), (40, 60), (513, 129), (40, 3000)]
     runs = []
     for _ in range(2):
-        _, _, _, gd, pd, md, cd = _step_state(shapes, [False, True, False])
+        _, _, _, gd, pd, md, cd = _step_state(shapes, [False, True, False, True])
         handle = B.MuonTensors(gd, pd, md, params_bf16=cd)
         for _ in range(3):
             B.cce_muon_multi_step(handle, lr=0.01)
@@ -203,8 +203,8 @@ def test_a_step_repeated_gives_the_same_bits(B):
 
 
 def test_captured_step_replayed(B):
-    shapes = [(256, 700), (40, 60), (700, 129), (16, 500)]
-    _, _, _, gd, pd, md, cd = _step_state(shapes, [False, True, False, True])
+    shapes = [(256, 700), (40, 60), (700, 129), (16, 500), (2200, 16)]
+    _, _, _, gd, pd, md, cd = _step_state(shapes, [False, True, False, True, True])
     start = [x.clone() for x in pd + md]
     handle = B.MuonTensors(gd, pd, md, params_bf16=cd)
     ws = torch.empty(B.muon_workspace_bytes(handle), dtype=torch.uint8, device="cuda")
@@ -240,6 +240,15 @@ def test_on_a_stream_of_the_callers(B):
     torch.cuda.current_stream().wait_stream(side)
     _check(out.float().cpu().numpy().astype(np.float64), g)
     _check_step(state, (pd, md, cd), 0.01, 0.95, True, [1.0, 1.0], [0.0, 0.0], 1.0)
+
+
+def test_thin_matrices_of_several_launches(B):
+    """More than share their launches; each as alone, also with more columns than 64 workgroups sum in 256 each."""
+    x = [torch.from_numpy(_matrix(16 + i % 5, 2100 + 10 * i, i)).cuda() for i in range(58)] + [torch.from_numpy(_matrix(40000, 9, 1)).cuda()]
+    out = B.cce_orthogonalize_multi(x)
+    for i in (0, 4, 55, 56, 57, 58):
+        assert torch.equal(out[i], B.cce_orthogonalize_multi([x[i]])[0])
+        _check(out[i].float().cpu().numpy().astype(np.float64), x[i].cpu().numpy())
 
 
 def test_groups_share_a_workspace(B):
