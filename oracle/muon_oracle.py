@@ -40,19 +40,38 @@ def _half(x, scale):
     return (x * scale).astype(np.float16).astype(np.float64) / scale
 
 
-def orthogonalize_rounded(g, coefficients, steps, eps):
+def _apart(x, scale):
+    """A symmetric matrix as its diagonal and the rest, rounded."""
+    diagonal = x.diagonal().copy()
+    return diagonal, _half(x - np.diag(diagonal), scale)
+
+
+def _product(x, y):
+    """Of two symmetric matrices held apart."""
+    (dx, ox), (dy, oy) = x, y
+    return np.diag(dx * dy) + dx[:, None] * oy + ox * dy[None, :] + ox @ oy
+
+
+def _polynomial(gram, a, b, c):
+    d, off = gram
+    square = _product(gram, gram)
+    return a * np.eye(len(d)) + b * (np.diag(d) + off) + c * square
+
+
+def orthogonalize_rounded(g, coefficients, steps, eps, pair=False):
+    """pair: the first two steps are taken as one, with the next A from the first one's polynomial S as S (S A)."""
     x, tall = _start(g, eps)
-    for a, b, c in _steps(coefficients, steps):
+    steps_left = list(_steps(coefficients, steps))
+    while steps_left:
         h = _half(x, 2.0 ** 13)
         linear = h + _half(x - h, 2.0 ** 24)
-        gram = h @ h.T
-        diagonal = gram.diagonal().copy()
-        off = _half(gram - np.diag(diagonal), 2.0 ** 13)
-        square = off @ off
-        m = (b + c * (diagonal[:, None] + diagonal[None, :])) * off + c * square
-        dm = b * diagonal + c * (diagonal ** 2 + square.diagonal())
-        m = _half(m - np.diag(m.diagonal()), 2.0 ** 10)
-        x = (a + dm)[:, None] * linear + m @ h
+        gram = _apart(h @ h.T, 2.0 ** 13)
+        keep, m = _apart(_polynomial(gram, *steps_left.pop(0)), 2.0 ** 10)
+        if pair:
+            pair = False
+            gram = _apart(_product((keep, m), _apart(_product((keep, m), gram), 2.0 ** 13)), 2.0 ** 13)
+            keep, m = _apart(_product(_apart(_polynomial(gram, *steps_left.pop(0)), 2.0 ** 10), (keep, m)), 2.0 ** 10)
+        x = keep[:, None] * linear + m @ h
     return x.T if tall else x
 
 

@@ -1,7 +1,9 @@
 // libcce, optimizer kernels for matrices: momentum, Newton-Schulz products, update.  C ABI declared in include/cce_muon.h.
 //
 // A matrix is worked on as X of r x c, r <= c (transposed on the way in and out where it is taller than wide).  Small ones are
-// taken by a workgroup each in one launch, thin ones in three (see both below), all others in the workspace, rows and columns padded with zeros to multiples of 64.  Per step three launches over all matrices of a group:
+// taken by a workgroup each in one launch, thin ones in three (see both below), all others in the workspace, rows and columns padded with zeros
+// to multiples of 64.  Per step three launches over all matrices of a group (the first two steps of matrices much wider than high are taken as one,
+// see pairs_steps):
 //
 //   gram    A = X X^T             half of the tiles, the other half mirrored
 //   poly    M = b A + c A A       the same
@@ -36,6 +38,7 @@ constexpr int kGroup = 240;                            // matrices whose product
 constexpr int64_t kGroupBytes = (int64_t)3 << 30;      // workspace of a group of more than one matrix
 constexpr int64_t kPartialBytes = (int64_t)256 * 256 * 256 * 4;      // of a part of a tile's sum for each CU
 constexpr int64_t kLargeRows = 1024;                   // from so many (padded) rows on a group may have them
+constexpr int kPairRows = 512;                         // from so many (padded) rows on two steps may be taken as one
 constexpr int kEnds = 56;                              // matrices of a launch that reads or writes the caller's: kernel arguments hold 4 KB
 constexpr int64_t kMaxMatrix = (int64_t)1 << 30;       // values of a padded matrix: byte offsets of 16-bit values stay below 2^32
 constexpr int64_t kMaxSide = 16384;                    // smaller side
@@ -77,6 +80,7 @@ struct NsProductArgs {
     uint32_t count, flip;
     uint32_t tiles, split_tiles, splits;      // tiles of 256 x 256: how many, the last of them in parts of their sums, parts each
     uint32_t partials;         // the parts' place, in units of 256 bytes
+    uint32_t kind;             // of a symmetric product
 };
 static_assert(sizeof(NsArgs) <= 4096 && sizeof(NsProductArgs) <= 4096, "kernel arguments hold 4 KB");
 
@@ -87,16 +91,21 @@ __device__ __forceinline__ char* workspace_of(const NsProductArgs& a, int i) { r
 struct NsLayout {
     int r, c, rp, cp;                 // sides and padded sides
     uint64_t h1, l, a, m, da, dm, partials, bytes;      // the first copy of h: 0
+    uint64_t s, t, ds, dt;            // of two steps taken as one, in the copy of h that is not read then
     __host__ __device__ __forceinline__ NsLayout(int rows, int cols) {
         r = rows < cols ? rows : cols;
         c = rows < cols ? cols : rows;
         rp = (r + 63) & ~63;
         cp = (c + 63) & ~63;
-        const uint64_t x = (uint64_t)rp * cp * 2, s = (uint64_t)rp * rp * 2, p = (uint64_t)rp * panel_rows() * 2, d = (uint64_t)rp * 4;
+        const uint64_t x = (uint64_t)rp * cp * 2, square = (uint64_t)rp * rp * 2, p = (uint64_t)rp * panel_rows() * 2, d = (uint64_t)rp * 4;
         h1 = x;
+        s = h1;
+        t = s + square;
+        ds = t + square;
+        dt = ds + d;
         l = 2 * x;
         a = l + x / 2;
-        m = a + s;
+        m = a + square;
         da = m + p;
         dm = da + d;
         partials = dm + d;
@@ -336,20 +345,84 @@ __device__ __forceinline__ void read8(const CCE_LDS float* p, float (&x)[8]) {
     }
 }
 
-// A value of A or of M from the product's x: what lies beside the diagonal, scaled, and what the diagonal would be.
-template <bool POLY>
-__device__ __forceinline__ float symmetric_value(const NsProductArgs& a, float x, _Float16 o, float dn, float dm, float& diagonal) {
-    if (!POLY) {
-        diagonal = x * (1.f / (kScaleX * kScaleX));
+// The symmetric products.  All matrices but X are polynomials of one A: they are symmetric, and any two of them commute.
+enum : int { kGram, kPoly, kProduct };
+enum SymKind : uint32_t {
+    kOfX,                      // A = X X^T
+    kOfA,                      // M = b A + c A A
+    // of two steps taken as one
+    kFirst,                    // S = a + b A + c A A
+    kBetween,                  // T = S A
+    kNextA,                    // A = S T
+    kSecond,                   // T = a + b A + c A A
+    kBoth                      // a + M = T S
+};
+
+// Operands X, Y and the result with the diagonals that are held beside them.
+struct SymBuffers {
+    const _Float16* x;
+    const _Float16* y;
+    const float* dx;
+    const float* dy;
+    _Float16* out;
+    float* dout;
+    float of_x;                // 1 / scale of x; y's is M's in a product
+    float add, scale;          // what the result's diagonal has more, and the result's scale
+    bool panel;                // the result lies in panels, as M does
+    template <int MODE>
+    __device__ __forceinline__ void init(const NsProductArgs& a, const NsLayout& at, char* base) {
+        if (MODE == kGram) {
+            x = y = (const _Float16*)(base + at.h(a.flip));
+            dx = dy = nullptr;
+            out = (_Float16*)(base + at.a);
+            dout = (float*)(base + at.da);
+            panel = false;
+            return;
+        }
+        const bool last = a.kind == kOfA || a.kind == kBoth, to_t = a.kind == kBetween || a.kind == kSecond;
+        if (MODE == kPoly) {
+            x = y = (const _Float16*)(base + at.a);
+            dx = dy = (const float*)(base + at.da);
+            out = (_Float16*)(base + (last ? at.m : to_t ? at.t : at.s));
+            dout = (float*)(base + (last ? at.dm : to_t ? at.dt : at.ds));
+            add = last ? 0.f : a.a;
+        } else {
+            x = (const _Float16*)(base + (to_t ? at.a : at.t));
+            y = (const _Float16*)(base + at.s);
+            dx = (const float*)(base + (to_t ? at.da : at.dt));
+            dy = (const float*)(base + at.ds);
+            out = (_Float16*)(base + (last ? at.m : to_t ? at.t : at.a));
+            dout = (float*)(base + (last ? at.dm : to_t ? at.dt : at.da));
+            of_x = last ? 1.f / kScaleM : 1.f / kScaleA;
+            add = last ? -a.a : 0.f;
+            scale = last ? kScaleM : kScaleA;
+        }
+        panel = last;
+    }
+    __device__ __forceinline__ _Float16* at_place(const NsLayout& at, int row, int col) const {
+        return out + (panel ? at.panel(row, col) : (uint32_t)row * (uint32_t)at.rp + col);
+    }
+};
+
+// A value of a result (row n, column m) from the product's p: what lies beside the diagonal, scaled, and what the diagonal would be.
+template <int MODE>
+__device__ __forceinline__ float symmetric_value(const NsProductArgs& a, const SymBuffers& of, float p, _Float16 x, _Float16 y, float dn, float dm, float& diagonal) {
+    if (MODE == kGram) {
+        diagonal = p * (1.f / (kScaleX * kScaleX));
         return diagonal * kScaleA;
     }
-    const float p = x * (a.c / (kScaleA * kScaleA));
-    diagonal = a.b * dn + (a.c * dn * dn + p);
-    return ((a.b + a.c * (dn + dm)) * ((float)o * (1.f / kScaleA)) + p) * kScaleM;
+    if (MODE == kPoly) {
+        p *= a.c / (kScaleA * kScaleA);
+        diagonal = a.b * dn + (a.c * dn * dn + p) + of.add;
+        return ((a.b + a.c * (dn + dm)) * ((float)x * (1.f / kScaleA)) + p) * kScaleM;
+    }
+    p *= of.of_x * (1.f / kScaleM);
+    diagonal = dn * dm + p + of.add;
+    return (dn * ((float)x * of.of_x) + (dm * ((float)y * (1.f / kScaleM)) + p)) * of.scale;
 }
 
-// A = X X^T (POLY = false) or M = b A + c A A, a tile and its mirror image.
-template <bool POLY>
+// A tile and its mirror image.
+template <int MODE>
 __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(const NsProductArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
     CCE_LDS char* const smem = (CCE_LDS char*)smem_generic;
@@ -357,10 +430,8 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
     const int i = matrix_of(a.first, (int)a.count, 2 * id + 1);
     const NsLayout at(a.t[i].rows, a.t[i].cols);
     char* const base = workspace_of(a, i);
-    _Float16* const A = uniform((_Float16*)(base + at.a));
-    _Float16* const M = uniform((_Float16*)(base + at.m));
-    float* const da = (float*)(base + at.da);
-    float* const dm = (float*)(base + at.dm);
+    SymBuffers of;
+    of.init<MODE>(a, at, base);
     int ti, tj;
     triangle((int)(id - (a.first[i] >> 1)), ti, tj);
     const int m0 = __builtin_amdgcn_readfirstlane(ti * SymTile::BM), n0 = __builtin_amdgcn_readfirstlane(tj * SymTile::BN);
@@ -370,11 +441,10 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
 #pragma unroll
         for (int bn = 0; bn < SymTile::TN; ++bn) acc[bm][bn] = f32x16{};
     {
-        const _Float16* const from = POLY ? A : uniform((const _Float16*)(base + at.h(a.flip)));
-        const int k = POLY ? at.rp : at.cp;
+        const int k = MODE == kGram ? at.cp : at.rp;
         OperandTile<true, SymTile::BM, 0, SymTile::NW, SymTile::BK> x, y;
-        x.init(from, k, m0, at.rp, k);
-        y.init(from, k, n0, at.rp, k);
+        x.init(uniform(of.x), k, m0, at.rp, k);
+        y.init(uniform(of.y), k, n0, at.rp, k);
         gemm_mainloop<SymTile, true, true, true, true>(acc, x, y, k, smem);
     }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -385,22 +455,24 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
     const int m = wm + q;
     const bool inside_m = m < at.rp;
     f32x4 dc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-    if (POLY && inside_m) {
-        dc[0] = *(const f32x4*)(da + m);
-        dc[1] = *(const f32x4*)(da + m + 4);
+    if (MODE != kGram && inside_m) {
+        dc[0] = *(const f32x4*)(of.dx + m);
+        dc[1] = *(const f32x4*)(of.dx + m + 4);
     }
 #pragma unroll
     for (int bn = 0; bn < SymTile::TN; ++bn) {
         // all loads of 32 rows together, from rows that are there
-        f16x8 o[4];
+        f16x8 ox[4], oy[4];
         float dn[4];
-        if (POLY) {
+        if (MODE != kGram) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int n = wn + bn * 32 + 8 * k + (lane >> 3);
                 const bool there = inside_m && n < at.rp;
-                o[k] = *(const f16x8*)(A + (there ? (uint32_t)n * (uint32_t)at.rp + m : 0u));
-                dn[k] = da[there ? n : 0];
+                const uint32_t place = there ? (uint32_t)n * (uint32_t)at.rp + m : 0u;
+                ox[k] = *(const f16x8*)(of.x + place);
+                if (MODE == kProduct) oy[k] = *(const f16x8*)(of.y + place);
+                dn[k] = of.dy[there ? n : 0];
             }
         }
 #pragma unroll
@@ -420,12 +492,12 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 float diagonal;
-                const float beside = symmetric_value<POLY>(a, x[e], o[k][e], dn[k], dc[e >> 2][e & 3], diagonal);
+                const float beside = symmetric_value<MODE>(a, of, x[e], ox[k][e], oy[k][e], dn[k], dc[e >> 2][e & 3], diagonal);
                 const bool here = m + e == n;
-                if (here && inside) (POLY ? dm : da)[n] = diagonal;
+                if (here && inside) of.dout[n] = diagonal;
                 v[e] = here ? (_Float16)0.f : (_Float16)beside;
             }
-            if (inside) *(f16x8*)(POLY ? M + at.panel(n, m) : A + (uint32_t)n * (uint32_t)at.rp + m) = v;
+            if (inside) *(f16x8*)of.at_place(at, n, m) = v;
             if (m0 != n0)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) mirror[(q + e) * kSymMirror + bn * 32 + y] = v[e];
@@ -437,7 +509,7 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
     for (int k = 0; k < 8; ++k) {
         const int y = 8 * k + (lane >> 3), row = wm + y, col = wn + q;                 // of the mirrored tile
         const f16x8 v = *(const CCE_LDS f16x8*)(mirror + y * kSymMirror + q);
-        if (row < at.rp && col < at.rp) *(f16x8*)(POLY ? M + at.panel(row, col) : A + (uint32_t)row * (uint32_t)at.rp + col) = v;
+        if (row < at.rp && col < at.rp) *(f16x8*)of.at_place(at, row, col) = v;
     }
 }
 
@@ -450,14 +522,10 @@ constexpr int kPingLds = 8 * kPingWave > SymPing::kLdsBytes ? 8 * kPingWave : Sy
 static_assert(kPingLds <= 160 * 1024, "160 KB LDS");
 
 // A wavefront's part of tile (ti, tj) and of its mirror image.
-template <bool POLY>
-__device__ __forceinline__ void symmetric_ping_rows(const NsProductArgs& a, const NsLayout& at, char* base, f32x4 (&acc)[SymPing::NA][SymPing::NB],
+template <int MODE>
+__device__ __forceinline__ void symmetric_ping_rows(const NsProductArgs& a, const NsLayout& at, const SymBuffers& of, f32x4 (&acc)[SymPing::NA][SymPing::NB],
                                                     int ti, int tj, int wave, CCE_LDS char* smem) {
     const int lane = threadIdx.x & 63, wm = wave / SymPing::WN, wn = wave % SymPing::WN, m0 = ti * SymPing::BM, n0 = tj * SymPing::BN;
-    _Float16* const A = (_Float16*)(base + at.a);
-    _Float16* const M = (_Float16*)(base + at.m);
-    float* const da = (float*)(base + at.da);
-    float* const dm = (float*)(base + at.dm);
     CCE_LDS float* const rows = (CCE_LDS float*)smem;
     CCE_LDS _Float16* const mirror = (CCE_LDS _Float16*)(smem + 64 * kPingPitch * 4);
     const int q = (lane & 3) * 8, nw = n0 + wn * SymPing::TNR;
@@ -466,20 +534,22 @@ __device__ __forceinline__ void symmetric_ping_rows(const NsProductArgs& a, cons
         const int mw = m0 + part * (SymPing::BM / 2) + wm * 32, m = mw + q;            // 32 columns of the result
         if (mw >= at.rp) continue;
         f32x4 dc[2];
-        if (POLY) {
-            dc[0] = *(const f32x4*)(da + m);
-            dc[1] = *(const f32x4*)(da + m + 4);
+        if (MODE != kGram) {
+            dc[0] = *(const f32x4*)(of.dx + m);
+            dc[1] = *(const f32x4*)(of.dx + m + 4);
         }
 #pragma unroll
         for (int side = 0; side < 2; ++side) {
-            f16x8 o[4];
+            f16x8 ox[4], oy[4];
             float dn[4];
-            if (POLY) {
+            if (MODE != kGram) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int n = nw + 64 * side + 16 * k + (lane >> 2);
-                    o[k] = *(const f16x8*)(A + (n < at.rp ? (uint32_t)n * (uint32_t)at.rp + m : 0u));
-                    dn[k] = da[n < at.rp ? n : 0];
+                    const uint32_t place = n < at.rp ? (uint32_t)n * (uint32_t)at.rp + m : 0u;
+                    ox[k] = *(const f16x8*)(of.x + place);
+                    if (MODE == kProduct) oy[k] = *(const f16x8*)(of.y + place);
+                    dn[k] = of.dy[n < at.rp ? n : 0];
                 }
             }
 #pragma unroll
@@ -497,12 +567,12 @@ __device__ __forceinline__ void symmetric_ping_rows(const NsProductArgs& a, cons
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     float diagonal;
-                    const float beside = symmetric_value<POLY>(a, x[e], o[k][e], dn[k], dc[e >> 2][e & 3], diagonal);
+                    const float beside = symmetric_value<MODE>(a, of, x[e], ox[k][e], oy[k][e], dn[k], dc[e >> 2][e & 3], diagonal);
                     const bool here = m + e == n;
-                    if (here) (POLY ? dm : da)[n] = diagonal;
+                    if (here) of.dout[n] = diagonal;
                     v[e] = here ? (_Float16)0.f : (_Float16)beside;
                 }
-                if (n < at.rp) *(f16x8*)(POLY ? M + at.panel(n, m) : A + (uint32_t)n * (uint32_t)at.rp + m) = v;
+                if (n < at.rp) *(f16x8*)of.at_place(at, n, m) = v;
                 if (ti != tj)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) mirror[(q + e) * kPingMirror + 64 * side + y] = v[e];
@@ -514,7 +584,7 @@ __device__ __forceinline__ void symmetric_ping_rows(const NsProductArgs& a, cons
             for (int k = 0; k < 8; ++k) {
                 const int y = 4 * k + (lane >> 4), row = mw + y, col = nw + (lane & 15) * 8;     // of the mirrored tile
                 const f16x8 v = *(const CCE_LDS f16x8*)(mirror + y * kPingMirror + (lane & 15) * 8);
-                *(f16x8*)(POLY ? M + at.panel(row, col) : A + (uint32_t)row * (uint32_t)at.rp + col) = v;
+                *(f16x8*)of.at_place(at, row, col) = v;
             }
             __builtin_amdgcn_wave_barrier();
         }
@@ -523,7 +593,7 @@ __device__ __forceinline__ void symmetric_ping_rows(const NsProductArgs& a, cons
 
 // The last a.split_tiles tiles, where they would leave most CUs without one, are computed in a.splits parts of the sum each, which
 // ns_symmetric_join_kernel adds in their order.
-template <bool POLY>
+template <int MODE>
 __global__ __launch_bounds__(SymPing::kThreads, 2) void ns_symmetric_ping_kernel(const NsProductArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
     CCE_LDS char* const smem = (CCE_LDS char*)smem_generic;
@@ -532,7 +602,8 @@ __global__ __launch_bounds__(SymPing::kThreads, 2) void ns_symmetric_ping_kernel
     const uint32_t tile = part ? whole + (id - whole) / a.splits : id;
     const int i = matrix_of(a.first, (int)a.count, 2 * tile + 1);
     const NsLayout at(a.t[i].rows, a.t[i].cols);
-    char* const base = workspace_of(a, i);
+    SymBuffers of;
+    of.init<MODE>(a, at, workspace_of(a, i));
     int ti, tj;
     triangle((int)(tile - (a.first[i] >> 1)), ti, tj);
     ti = __builtin_amdgcn_readfirstlane(ti);
@@ -545,15 +616,16 @@ __global__ __launch_bounds__(SymPing::kThreads, 2) void ns_symmetric_ping_kernel
 #pragma unroll
         for (int y = 0; y < SymPing::NB; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
     {
-        const uint32_t ld = (uint32_t)(POLY ? at.rp : at.cp) * 2u;
-        const int slices = (POLY ? at.rp : at.cp) / SymPing::BK;
+        const uint32_t ld = (uint32_t)(MODE == kGram ? at.cp : at.rp) * 2u;
+        const int slices = (MODE == kGram ? at.cp : at.rp) / SymPing::BK;
         int first = 0, KT = slices;
         if (part) {
             const int split = (int)((id - whole) % a.splits), splits = (int)a.splits;
             first = slices * split / splits;
             KT = slices * (split + 1) / splits - first;
         }
-        const char* const from = uniform(base + (POLY ? at.a : at.h(a.flip)) + (size_t)first * (2 * SymPing::BK));
+        const char* const from_x = uniform((const char*)of.x + (size_t)first * (2 * SymPing::BK));
+        const char* const from_y = uniform((const char*)of.y + (size_t)first * (2 * SymPing::BK));
         PingPong<SymPing, ARows::kHalves, true> turns;
         PingLoads<SymPing, ARows::kHalves> loads;
         turns.init(smem);
@@ -564,7 +636,7 @@ __global__ __launch_bounds__(SymPing::kThreads, 2) void ns_symmetric_ping_kernel
             loads.set_b_row(x, row < at.rp ? row : at.rp - 1, ld);
         }
         loads.on = true;
-        loads.tile(uniform(from + (size_t)m0 * ld), m_rows, from, ld);
+        loads.tile(uniform(from_x + (size_t)m0 * ld), m_rows, from_y, ld);
         __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): what the compiler has loaded so far, which cannot see the loads of the slices
         loads.issue(0, 0);
         loads.issue(0, 1);
@@ -595,18 +667,19 @@ __global__ __launch_bounds__(SymPing::kThreads, 2) void ns_symmetric_ping_kernel
             for (int y = 0; y < SymPing::NB; ++y) to[(x * SymPing::NB + y) * 64] = acc[x][y];
         return;
     }
-    symmetric_ping_rows<POLY>(a, at, base, acc, ti, tj, wave, smem + wave * kPingWave);
+    symmetric_ping_rows<MODE>(a, at, of, acc, ti, tj, wave, smem + wave * kPingWave);
 }
 
 // A wavefront of a split tile a workgroup.
-template <bool POLY>
+template <int MODE>
 __global__ __launch_bounds__(64) void ns_symmetric_join_kernel(const NsProductArgs a) {
     __shared__ __attribute__((aligned(1024))) char smem_generic[kPingWave];
     const uint32_t split = blockIdx.x >> 3, tile = a.tiles - a.split_tiles + split;
     const int wave = (int)(blockIdx.x & 7u);
     const int i = matrix_of(a.first, (int)a.count, 2 * tile + 1);
     const NsLayout at(a.t[i].rows, a.t[i].cols);
-    char* const base = workspace_of(a, i);
+    SymBuffers of;
+    of.init<MODE>(a, at, workspace_of(a, i));
     int ti, tj;
     triangle((int)(tile - (a.first[i] >> 1)), ti, tj);
     const f32x4* from = (const f32x4*)(a.ws + (uint64_t)a.partials * 256) + ((size_t)split * a.splits * 8 + wave) * (SymPing::NA * SymPing::NB * 64) + threadIdx.x;
@@ -622,7 +695,7 @@ __global__ __launch_bounds__(64) void ns_symmetric_join_kernel(const NsProductAr
 #pragma unroll
             for (int y = 0; y < SymPing::NB; ++y) acc[x][y] += from[(x * SymPing::NB + y) * 64];
     }
-    symmetric_ping_rows<POLY>(a, at, base, acc, ti, tj, wave, (CCE_LDS char*)smem_generic);
+    symmetric_ping_rows<MODE>(a, at, of, acc, ti, tj, wave, (CCE_LDS char*)smem_generic);
 }
 
 __device__ __forceinline__ uint16_t bf16_bits(float x) {
@@ -1599,34 +1672,55 @@ static int check_gradients(const cce_matrix* matrices, int64_t count) {
     return CCE_OK;
 }
 
-// Whether the steps keep singular values that begin at 1 or below within what the scales hold.  A polynomial a x + b x^3 + c x^5 has its
-// largest value in [0, top] at an end or where its derivative a + 3 b y + 5 c y^2, y = x^2, is 0.
+// The largest |a x + b x^3 + c x^5| in [0, top]: at its end or where the derivative a + 3 b y + 5 c y^2, y = x^2, is 0.
+static double largest_value(double a, double b, double c, double top) {
+    double at[3] = {top, 0.0, 0.0};
+    int n = 1;
+    const double root = 9.0 * b * b - 20.0 * a * c;
+    if (c != 0.0 && root >= 0.0) {
+        const double y0 = (-3.0 * b - sqrt(root)) / (10.0 * c), y1 = (-3.0 * b + sqrt(root)) / (10.0 * c);
+        if (y0 > 0.0 && y0 < top * top) at[n++] = sqrt(y0);
+        if (y1 > 0.0 && y1 < top * top) at[n++] = sqrt(y1);
+    } else if (c == 0.0 && b != 0.0) {
+        const double y = -a / (3.0 * b);
+        if (y > 0.0 && y < top * top) at[n++] = sqrt(y);
+    }
+    double next = 0.0;
+    for (int k = 0; k < n; ++k) {
+        const double x = at[k];
+        next = fmax(next, fabs(a * x + b * x * x * x + c * x * x * x * x * x));
+    }
+    return next;
+}
+
+// Whether the steps keep singular values that begin at 1 or below within what the scales hold.
 static int check_coefficients(const float* coefficients, int steps) {
     double top = 1.0;
     for (int s = 0; s < steps; ++s) {
         const double a = coefficients[3 * s], b = coefficients[3 * s + 1], c = coefficients[3 * s + 2];
         if (!(isfinite(a) && isfinite(b) && isfinite(c))) return CCE_ERR_INVALID;
         if (fabs(b) * top * top + fabs(c) * top * top * top * top > kMaxM) return CCE_ERR_UNSUPPORTED;
-        double at[3] = {top, 0.0, 0.0};
-        int n = 1;
-        const double root = 9.0 * b * b - 20.0 * a * c;
-        if (c != 0.0 && root >= 0.0) {
-            const double y0 = (-3.0 * b - sqrt(root)) / (10.0 * c), y1 = (-3.0 * b + sqrt(root)) / (10.0 * c);
-            if (y0 > 0.0 && y0 < top * top) at[n++] = sqrt(y0);
-            if (y1 > 0.0 && y1 < top * top) at[n++] = sqrt(y1);
-        } else if (c == 0.0 && b != 0.0) {
-            const double y = -a / (3.0 * b);
-            if (y > 0.0 && y < top * top) at[n++] = sqrt(y);
-        }
-        double next = 0.0;
-        for (int k = 0; k < n; ++k) {
-            const double x = at[k];
-            next = fmax(next, fabs(a * x + b * x * x * x + c * x * x * x * x * x));
-        }
+        const double next = largest_value(a, b, c, top);
         if (next > kMaxSigma) return CCE_ERR_UNSUPPORTED;
         top = fmax(next, 1e-6);
     }
     return CCE_OK;
+}
+
+// Whether S of the first two steps, and their product, stay within M's scale: singular values begin at 1 or below.
+static bool may_pair(const float* coefficients, int steps) {
+    if (steps < 2) return false;
+    double top = 1.0, both = 1.0;
+    for (int s = 0; s < 2; ++s) {
+        const double a = coefficients[3 * s], b = coefficients[3 * s + 1], c = coefficients[3 * s + 2];
+        const double vertex = c != 0.0 ? -b / (2.0 * c) : -1.0;
+        double largest = fmax(fabs(a), fabs(a + b * top * top + c * top * top * top * top));
+        if (vertex > 0.0 && vertex < top * top) largest = fmax(largest, fabs(a + b * vertex + c * vertex * vertex));
+        both *= largest;
+        if (largest > kMaxM || both > kMaxM) return false;
+        top = largest_value(a, b, c, top);
+    }
+    return true;
 }
 
 static uint32_t sym_tiles(const NsLayout& at, bool large) {
@@ -1666,15 +1760,25 @@ static int64_t next_thin_group(const cce_matrix* matrices, int64_t count, int64_
     return bytes;
 }
 
+// Whether the first two steps of a matrix are taken as one, X = (S2 S1) X with A = S1 X X^T S1: a product of r c and one of 2 r c are
+// saved for three of r r.  Not in later steps: the first A, whose trace is 1, takes its operands' rounding better than they do (2-norm of the
+// error for 256 x 1024: of a matrix of noise 5.1e-4, 5.1 with the first two, 6.7 with the second and third; with a spectrum down to 1e-3 8.9,
+// 9.1 and 12.5).  us without / with: 32 x 512 x 2048 650 / 620, 8 x 896 x 3584 707 / 653, 16 x 1024 x 4096 1738 / 1580, 4 x 1500 x 4096 955 / 905,
+// 3584 x 14336 3290 / 2960, a 24-layer model 7520 / 7130; 512 x 1088 254 / 260, 1024 x 2176 375 / 379: nothing gained below 2.5 columns a row.
+static bool pairs_steps(const cce_matrix& t) {
+    const NsLayout at((int)t.rows, (int)t.cols);
+    return at.rp >= kPairRows && 2 * at.cp >= 5 * at.rp;               // (S and T, and their diagonals, lie in a copy of h)
+}
+
 // The matrices from `i` on that share their launches; moves i behind them.  Returns their workspace.
 template <class Take>
-static int64_t next_group(const cce_matrix* matrices, int64_t count, int64_t& i, Take take) {
+static int64_t next_group(const cce_matrix* matrices, int64_t count, bool pairs, int64_t& i, Take take) {
     int64_t bytes = 0;
     int n = 0;
     bool large = false;
     for (; i < count && n < kGroup; ++i) {
         const cce_matrix& t = matrices[i];
-        if (t.rows == 0 || t.cols == 0 || small_lds(t) != 0 || is_thin(t)) continue;
+        if (t.rows == 0 || t.cols == 0 || small_lds(t) != 0 || is_thin(t) || pairs_steps(t) != pairs) continue;
         const NsLayout at((int)t.rows, (int)t.cols);
         if (n != 0 && bytes + (int64_t)at.bytes > kGroupBytes - kPartialBytes) break;
         take(t, (uint64_t)bytes);
@@ -1816,19 +1920,21 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
     a.mu = mu;
     a.nesterov = nesterov;
     a.eps = eps;
+    for (const bool pairs : {false, true})
     for (int64_t i = 0; i < count;) {
         int64_t index[kGroup];
         uint64_t base[kGroup];
         int n = 0;
         int64_t partials = 0;                          // behind the matrices
-        next_group(matrices, count, i, [&](const cce_matrix& t, uint64_t at) {
+        next_group(matrices, count, pairs, i, [&](const cce_matrix& t, uint64_t at) {
             index[n] = &t - matrices;
             base[n++] = at;
             partials = (int64_t)at + (int64_t)NsLayout((int)t.rows, (int)t.cols).bytes;
         });
         if (n == 0) continue;
-        if (!allow_lds(ns_symmetric_kernel<false>, kSymLds) || !allow_lds(ns_symmetric_kernel<true>, kSymLds) ||
-            !allow_lds(ns_symmetric_ping_kernel<false>, kPingLds) || !allow_lds(ns_symmetric_ping_kernel<true>, kPingLds) ||
+        if (!allow_lds(ns_symmetric_kernel<kGram>, kSymLds) || !allow_lds(ns_symmetric_kernel<kPoly>, kSymLds) ||
+            !allow_lds(ns_symmetric_kernel<kProduct>, kSymLds) || !allow_lds(ns_symmetric_ping_kernel<kGram>, kPingLds) ||
+            !allow_lds(ns_symmetric_ping_kernel<kPoly>, kPingLds) || !allow_lds(ns_symmetric_ping_kernel<kProduct>, kPingLds) ||
             !allow_lds(ns_apply_kernel<false>, ApplyTile::kLdsBytes) || !allow_lds(ns_apply_kernel<true>, ApplyTile::kLdsBytes) ||
             !allow_lds(ns_apply_turn_kernel<false>, kTurnLds) || !allow_lds(ns_apply_turn_kernel<true>, kTurnLds))
             return CCE_ERR_HIP;
@@ -1877,22 +1983,44 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
         }, [&](uint32_t blocks) { hipLaunchKernelGGL(ns_norm_kernel, dim3(blocks), dim3(256), 0, stream, a); });
         ends([](const cce_matrix&, const NsLayout& at) { return (uint32_t)(at.rp / 64) * (uint32_t)(at.cp / 64); },
              [&](uint32_t blocks) { hipLaunchKernelGGL(ns_prep_kernel, dim3(blocks), dim3(256), 0, stream, a); });
-        for (int s = 0; s < steps; ++s) {
+        auto coefficients_of = [&](int s) {
             for (auto& p : products) {
-                p.flip = (uint32_t)s & 1u;
                 p.a = coefficients[3 * s];
                 p.b = coefficients[3 * s + 1];
                 p.c = coefficients[3 * s + 2];
             }
-            if (large[0]) hipLaunchKernelGGL(ns_symmetric_ping_kernel<false>, dim3(grid[0]), dim3(SymPing::kThreads), kPingLds, stream, products[0]);
-            else hipLaunchKernelGGL(ns_symmetric_kernel<false>, dim3(grid[0]), dim3(SymTile::kThreads), kSymLds, stream, products[0]);
-            if (large[0] && products[0].split_tiles) hipLaunchKernelGGL(ns_symmetric_join_kernel<false>, dim3(8 * products[0].split_tiles), dim3(64), 0, stream, products[0]);
-            if (large[1]) hipLaunchKernelGGL(ns_symmetric_ping_kernel<true>, dim3(grid[1]), dim3(SymPing::kThreads), kPingLds, stream, products[1]);
-            else hipLaunchKernelGGL(ns_symmetric_kernel<true>, dim3(grid[1]), dim3(SymTile::kThreads), kSymLds, stream, products[1]);
-            if (large[1] && products[1].split_tiles) hipLaunchKernelGGL(ns_symmetric_join_kernel<true>, dim3(8 * products[1].split_tiles), dim3(64), 0, stream, products[1]);
+        };
+        auto symmetric = [&](auto mode, uint32_t kind) {
+            constexpr int MODE = decltype(mode)::value;
+            const int op = MODE == kGram ? 0 : 1;
+            NsProductArgs& p = products[op];
+            p.kind = kind;
+            if (large[op]) hipLaunchKernelGGL(ns_symmetric_ping_kernel<MODE>, dim3(grid[op]), dim3(SymPing::kThreads), kPingLds, stream, p);
+            else hipLaunchKernelGGL(ns_symmetric_kernel<MODE>, dim3(grid[op]), dim3(SymTile::kThreads), kSymLds, stream, p);
+            if (large[op] && p.split_tiles) hipLaunchKernelGGL(ns_symmetric_join_kernel<MODE>, dim3(8 * p.split_tiles), dim3(64), 0, stream, p);
+        };
+        constexpr std::integral_constant<int, kGram> gram{};
+        constexpr std::integral_constant<int, kPoly> poly{};
+        constexpr std::integral_constant<int, kProduct> product{};
+        uint32_t flip = 0;
+        for (int s = 0; s < steps; ++s) {
+            for (auto& p : products) p.flip = flip;
+            coefficients_of(s);
+            symmetric(gram, kOfX);
+            if (s == 0 && pairs && may_pair(coefficients, steps)) {
+                symmetric(poly, kFirst);
+                symmetric(product, kBetween);
+                symmetric(product, kNextA);
+                coefficients_of(++s);
+                symmetric(poly, kSecond);
+                symmetric(product, kBoth);
+            } else {
+                symmetric(poly, kOfA);
+            }
             if (s + 1 == steps) break;
             if (large[2]) hipLaunchKernelGGL(ns_apply_turn_kernel<false>, dim3(grid[2]), dim3(TurnTile::kThreads), kTurnLds, stream, products[2]);
             else hipLaunchKernelGGL(ns_apply_kernel<false>, dim3(grid[2]), dim3(ApplyTile::kThreads), ApplyTile::kLdsBytes, stream, products[2]);
+            flip ^= 1;
         }
         a.flip = products[2].flip;
         a.a = products[2].a;
@@ -1922,10 +2050,11 @@ extern "C" {
 size_t cce_muon_workspace_bytes(const cce_matrix* matrices, int64_t count) {
     if (check_sizes(matrices, count) != CCE_OK) return 0;
     int64_t most = 256;
-    for (int64_t i = 0; i < count;) {
-        const int64_t bytes = next_group(matrices, count, i, [](const cce_matrix&, uint64_t) {});
-        most = bytes > most ? bytes : most;
-    }
+    for (const bool pairs : {false, true})
+        for (int64_t i = 0; i < count;) {
+            const int64_t bytes = next_group(matrices, count, pairs, i, [](const cce_matrix&, uint64_t) {});
+            most = bytes > most ? bytes : most;
+        }
     for (int64_t i = 0; i < count;) {
         const int64_t bytes = next_thin_group(matrices, count, i, [](const cce_matrix&, uint64_t) {});
         most = bytes > most ? bytes : most;

@@ -49,10 +49,10 @@ def _rounded(x, bf16):
     return (t.bfloat16().float() if bf16 else t).numpy()
 
 
-def _check(got, g, steps=5, coefficients=ABC, eps=EPS, rate=1.0, bf16=True, extra=0.0):
+def _check(got, g, steps=5, coefficients=ABC, eps=EPS, rate=1.0, bf16=True, extra=0.0, pair=False):
     """got: rate * orthogonalised g, or what is left of it after `extra` (absolute, by value)."""
     want = M.orthogonalize(g, coefficients, steps, eps)
-    r = M.orthogonalize_rounded(g, coefficients, steps, eps) - want
+    r = M.orthogonalize_rounded(g, coefficients, steps, eps, pair) - want
     chance = 2.0 ** -10 / math.sqrt(min(g.shape))
     off = 1.5 * np.linalg.norm(r) + chance * np.linalg.norm(want)
     most = 2.0 * np.abs(r).max() + chance * np.abs(want).max()
@@ -153,7 +153,7 @@ def _step_state(shapes, bf16, copies=True, seed=0):
         [torch.empty(s, dtype=torch.bfloat16, device="cuda") if copies else None for s in shapes]
 
 
-def _check_step(state, after, lr, mu, nesterov, lr_scale, wd, clip):
+def _check_step(state, after, lr, mu, nesterov, lr_scale, wd, clip, pair=False):
     g, p, mom, *_ = state
     pd, md, cd = after
     lr, mu, clip = (float(np.float32(x)) for x in (lr, mu, clip))
@@ -167,7 +167,7 @@ def _check_step(state, after, lr, mu, nesterov, lr_scale, wd, clip):
         kept = (1.0 - rate * float(np.float32(wd[i]))) * p[i].astype(np.float64)
         got_p = pd[i].cpu().numpy().astype(np.float64)
         extra = 4 * U * (np.abs(kept) + rate * np.abs(M.orthogonalize(u, ABC, 5, EPS)))
-        _check(kept - got_p, u, rate=rate, bf16=False, extra=extra)
+        _check(kept - got_p, u, rate=rate, bf16=False, extra=extra, pair=pair)
         if cd[i] is not None:
             assert torch.equal(cd[i], pd[i].bfloat16())
         assert np.isfinite(want_p).all()
@@ -191,10 +191,10 @@ def test_muon_step(B, nesterov, copies):
 
 
 def test_a_step_repeated_gives_the_same_bits(B):
-    shapes = [(256, 700), (40, 60), (513, 129), (40, 3000)]
+    shapes = [(256, 700), (40, 60), (513, 129), (40, 3000), (600, 1800)]
     runs = []
     for _ in range(2):
-        _, _, _, gd, pd, md, cd = _step_state(shapes, [False, True, False, True])
+        _, _, _, gd, pd, md, cd = _step_state(shapes, [False, True, False, True, False])
         handle = B.MuonTensors(gd, pd, md, params_bf16=cd)
         for _ in range(3):
             B.cce_muon_multi_step(handle, lr=0.01)
@@ -203,8 +203,8 @@ def test_a_step_repeated_gives_the_same_bits(B):
 
 
 def test_captured_step_replayed(B):
-    shapes = [(256, 700), (40, 60), (700, 129), (16, 500), (2200, 16)]
-    _, _, _, gd, pd, md, cd = _step_state(shapes, [False, True, False, True, True])
+    shapes = [(256, 700), (40, 60), (700, 129), (16, 500), (2200, 16), (512, 1300)]
+    _, _, _, gd, pd, md, cd = _step_state(shapes, [False, True, False, True, True, False])
     start = [x.clone() for x in pd + md]
     handle = B.MuonTensors(gd, pd, md, params_bf16=cd)
     ws = torch.empty(B.muon_workspace_bytes(handle), dtype=torch.uint8, device="cuda")
@@ -240,6 +240,38 @@ def test_on_a_stream_of_the_callers(B):
     torch.cuda.current_stream().wait_stream(side)
     _check(out.float().cpu().numpy().astype(np.float64), g)
     _check_step(state, (pd, md, cd), 0.01, 0.95, True, [1.0, 1.0], [0.0, 0.0], 1.0)
+
+
+PAIRED = [(512, 1280), (1400, 500), (513, 2000)]         # the first two steps are taken as one
+
+
+@pytest.mark.parametrize("kind", ["noise", "directions", "rows"])
+@pytest.mark.parametrize("shape", PAIRED, ids=lambda s: f"{s[0]}x{s[1]}")
+def test_two_steps_taken_as_one(B, shape, kind):
+    g = _matrix(*shape, 11, kind)
+    x = torch.from_numpy(g).cuda()
+    # S of the last two has values up to 8 and 7.8: their product is beyond the operands' range, so that these are taken one by one
+    wide = np.array([[8.0, -32.0, 25.6], [7.78, -12.16, 3.8]], dtype=np.float32)
+    for steps, coefficients, pair in ((5, ABC, True), (2, ABC, True), (3, np.array([ABC, (2.0, -1.5, 0.5), (1.875, -1.25, 0.375)]), True), (2, wide, False), (1, ABC, False)):
+        out, = B.cce_orthogonalize_multi([x], steps=steps, coefficients=coefficients)
+        _check(out.float().cpu().numpy().astype(np.float64), g, steps=steps, coefficients=coefficients, pair=pair)
+
+
+def test_muon_step_of_two_steps_taken_as_one(B):
+    state = _step_state(PAIRED, [True, False, True])
+    _, _, _, gd, pd, md, cd = state
+    handle = B.MuonTensors(gd, pd, md, params_bf16=cd, weight_decay=0.1)
+    B.cce_muon_multi_step(handle, lr=0.02, momentum=0.9)
+    _check_step(state, (pd, md, cd), 0.02, 0.9, True, [1.0] * 3, [0.1] * 3, 1.0, pair=True)
+
+
+def test_matrices_of_every_form_in_a_list(B):
+    """Small, thin, tiled, of two steps taken as one, and empty ones in turn: each as alone."""
+    shapes = [(40, 60), (16, 3000), (300, 400), (512, 1400), (0, 5), (2500, 600), (70, 900), (33, 2200), (1, 1)]
+    x = [torch.from_numpy(_matrix(m, n, 3)).cuda() for m, n in shapes]
+    for o, v in zip(B.cce_orthogonalize_multi(x), x):
+        if v.numel():
+            assert torch.equal(o, B.cce_orthogonalize_multi([v])[0])
 
 
 def test_thin_matrices_of_several_launches(B):

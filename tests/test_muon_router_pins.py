@@ -38,6 +38,14 @@ def test_rounded_form_is_near(m, n):
     assert np.linalg.norm(got - want) <= 2.0 ** -9 * np.linalg.norm(want)
 
 
+@pytest.mark.parametrize("m,n", [(16, 60), (200, 64), (130, 400)])
+def test_rounded_form_of_two_steps_taken_as_one_is_near(m, n):
+    g = np.random.default_rng(m + n).standard_normal((m, n))
+    for steps in (2, 5):
+        want = M.orthogonalize(g, ABC, steps, 1e-7)
+        assert np.linalg.norm(M.orthogonalize_rounded(g, ABC, steps, 1e-7, True) - want) <= 2.0 ** -9 * np.linalg.norm(want)
+
+
 def test_muon_step_of_a_single_value():
     p, m = M.muon_step([[2.0]], [[-0.5]], [[0.0]], ABC, 5, 0.0, 0.1, 0.9, True, 0.01)
     np.testing.assert_allclose(m, [[-0.05]])
