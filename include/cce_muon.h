@@ -49,7 +49,7 @@ typedef struct cce_matrix {
 
 /* Bytes of device workspace both calls need for these matrices (rows and cols are read); at least 256; 0 where a call would
  * refuse the sizes.  Host only.  A part of the list is worked on at a time, in at most 3 GB, or what the largest matrix needs: 5
- * bytes a value and 4 for each of the square of its smaller side. */
+ * bytes a value and 4 for each of the square of its smaller side; 64 MB of it for parts of long sums. */
 size_t cce_muon_workspace_bytes(const cce_matrix* matrices, int64_t count);
 
 /*

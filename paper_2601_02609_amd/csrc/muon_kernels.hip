@@ -37,7 +37,8 @@ typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
 constexpr int kGroup = 240;                            // matrices whose products share their launches
 constexpr int64_t kGroupBytes = (int64_t)3 << 30;      // workspace of a group of more than one matrix
 constexpr int64_t kPartialBytes = (int64_t)256 * 256 * 256 * 4;      // of a part of a tile's sum for each CU
-constexpr int64_t kLargeRows = 1024;                   // from so many (padded) rows on a group may have them
+constexpr int64_t kLargeRows = 1024, kLongColumns = 2048;      // from so many (padded) rows or columns on a group may have them
+constexpr uint32_t kMaxSplits = 8;                     // parts of a sum: 16 cost the join more than they save (14336 x 100 347 us / 357, 4 x 4096 x 256 331 / 383)
 constexpr int kPairRows = 512;                         // from so many (padded) rows on two steps may be taken as one
 constexpr int kEnds = 56;                              // matrices of a launch that reads or writes the caller's: kernel arguments hold 4 KB
 constexpr int64_t kMaxMatrix = (int64_t)1 << 30;       // values of a padded matrix: byte offsets of 16-bit values stay below 2^32
@@ -1784,7 +1785,7 @@ static int64_t next_group(const cce_matrix* matrices, int64_t count, bool pairs,
         take(t, (uint64_t)bytes);
         ++n;
         bytes += (int64_t)at.bytes;
-        large = large || at.rp >= kLargeRows;
+        large = large || at.rp >= kLargeRows || at.cp >= kLongColumns;
     }
     return bytes + (large ? kPartialBytes : 0);
 }
@@ -1869,6 +1870,7 @@ static bool run_thin(const cce_matrix* matrices, int64_t count, bool step, float
 // A round of either does as many products a slice; smaller tiles that have a CU each take 0.6 of one.
 // A and M: the last tiles of a round of 256 x 256 that is less than half full are split (p.splits), which costs a launch as long as 20 slices.
 // X: an epilogue is as long as 12 slices, which only the smaller tiles put beside products; 256 x 256 from 2048 rows on.
+// Few rows and many columns: the one or few tiles of gram split, 100 x 4096 319 -> 257 us, 100 x 14336 824 -> 347, 512 x 14336 841 -> 445.
 // Smaller tiles / 256 x 256 in all launches of a kind, whole calls, us: gram of 4 x 4096 x 4096 6240 / 5930, of 3584 x 14336 3460 / 3350, of
 // 1024 x 4096 470 / 423, of 2048 x 2048 498 / 558, of 64 x 640 x 640 923 / 931; apply of 4 x 4096 x 4096 5690 / 5280, of
 // 12 x 2048 x 2048 2460 / 2310, of 2048 x 2048 498 / 542, of 6 x 1536 x 6144 1926 / 1948, of a 24-layer model's matrices 7520 / 7750.
@@ -1883,7 +1885,7 @@ static bool large_tiles(int op, int n, Length length, Tiles tiles, Layout layout
     p.splits = 1;
     for (int k = 0; k < n; ++k) {
         if (op == 2 && layout(k).rp < kTurnRows) return false;
-        any = any || layout(k).rp >= kLargeRows;
+        any = any || layout(k).rp >= kLargeRows || (op == 0 && layout(k).cp >= kLongColumns);
         shortest = length(k) < shortest ? length(k) : shortest;
         for (int of_256 = 0; of_256 < 2; ++of_256) {
             const uint32_t t = tiles(k, of_256 != 0);
@@ -1898,7 +1900,7 @@ static bool large_tiles(int op, int n, Length length, Tiles tiles, Layout layout
     if (op == 2) return mean[1] >= 2048.0 && ceil((double)count[1] / kCus) <= small_rounds;
     const uint32_t left = count[1] % kCus, most = left ? kCus / left : 1, longest = (uint32_t)(shortest / SymPing::BK);
     uint32_t splits = most < longest ? most : longest;
-    splits = splits < 8 ? splits : 8;
+    splits = splits < kMaxSplits ? splits : kMaxSplits;
     const double rounds = (double)(count[1] / kCus) + (left == 0 ? 0.0 : 1.0 / splits);
     if (rounds * mean[1] + (splits > 1 ? 20.0 * SymPing::BK : 0.0) >= small_rounds * mean[0]) return false;
     if (splits > 1) {

@@ -303,7 +303,7 @@ def test_groups_share_a_workspace(B):
         assert float(torch.linalg.norm(o.double() - y) / torch.linalg.norm(y)) <= 2.0 ** -9 + 2.0 ** -8
 
 
-@pytest.mark.parametrize("shape,count", [((1024, 4096), 1), ((5001, 1030), 1), ((1090, 1100), 30), ((2048, 2048), 13), ((3583, 2100), 6), ((3590, 3600), 1), ((4096, 4096), 2)],
+@pytest.mark.parametrize("shape,count", [((100, 4096), 3), ((6000, 300), 1), ((1024, 4096), 1), ((5001, 1030), 1), ((1090, 1100), 30), ((2048, 2048), 13), ((3583, 2100), 6), ((3590, 3600), 1), ((4096, 4096), 2)],
                          ids=lambda s: "x".join(map(str, s)) if isinstance(s, tuple) else str(s))
 def test_large_matrices(B, shape, count):
     """Tiles of 256 x 256, split ones among them.  Values of one size: every 64 x 64 block is off by no more than the whole may be, twice."""
