@@ -17,8 +17,10 @@
 namespace cce {
 
 constexpr int kRouterBlocks = 256;                     // workgroups of the forward pass, each with one set of partial sums: one a CU
-// Wavefronts of a workgroup: as many of 128 registers as a CU holds, half of them where the sums of each would fill the LDS.
-constexpr int router_waves(int lanes) { return lanes == 64 ? 8 : 16; }
+// Wavefronts of a workgroup: as many of 128 registers as a CU holds, half of them where the sums of each would fill the LDS or where lanes
+// have more values (with_wide_shape).
+constexpr bool wide_lanes(int lanes, int values) { return values >= 2 * lanes; }
+constexpr int router_waves(int lanes, int values) { return lanes == 64 || wide_lanes(lanes, values) ? 8 : 16; }
 constexpr int kGradBlocks = 512;                       // workgroups of the backward pass: two a CU, several trips each
 constexpr int kJoinExperts = 8, kJoinParts = 256 / kJoinExperts;      // experts of a workgroup that joins them, threads of an expert
 
@@ -250,10 +252,10 @@ __device__ __forceinline__ void own_largest(const uint32_t (&key)[VALUES], uint3
 // TOP > 0 (bf16, k <= TOP): a logit and its column make one 32-bit key, and the TOP largest of a row come out of sorting networks;
 // 0, and rows that hold a NaN or +inf: k rounds of a maximum over the row.  65536 x 256 bf16, k = 8: rounds 53 us, networks see below.
 template <bool BF16, int L, int VALUES, int TOP>
-__global__ __launch_bounds__(64 * router_waves(L), 4) void router_forward_kernel(const RouterArgs a) {
+__global__ __launch_bounds__(64 * router_waves(L, VALUES), wide_lanes(L, VALUES) ? 2 : 4) void router_forward_kernel(const RouterArgs a) {
     using C = Columns<BF16, L, VALUES>;
     constexpr int kRows = 64 / L;                                     // of a wavefront
-    constexpr int kRouterWaves = router_waves(L), kRouterThreads = 64 * kRouterWaves;
+    constexpr int kRouterWaves = router_waves(L, VALUES), kRouterThreads = 64 * kRouterWaves;
     constexpr int kSlots = TOP ? 1 : (CCE_ROUTER_MAX_TOP_K + L - 1) / L;      // chosen experts a lane keeps
     constexpr int kColumns = L * VALUES;
     static_assert(TOP <= L && (TOP == 0 || BF16), "a lane for each chosen expert");
@@ -607,9 +609,8 @@ static int check_sizes(int64_t N, int64_t E) {
 // Rows that a workgroup of so many wavefronts takes at a time.
 static int64_t rows_of_group(int64_t E, int waves) { return waves * (E <= 64 ? 8 : E <= 256 ? 4 : E <= 512 ? 2 : 1); }
 
-
 static int64_t forward_blocks(int64_t N, int64_t E) {
-    const int64_t rows = rows_of_group(E, router_waves(E > 512 ? 64 : 8)), want = (N + rows - 1) / rows;
+    const int64_t rows = rows_of_group(E, router_waves(E > 512 ? 64 : 8, 1)), want = (N + rows - 1) / rows;
     return want < kRouterBlocks ? want : kRouterBlocks;
 }
 
@@ -628,6 +629,17 @@ static void with_shape(bool bf16, int64_t E, Launch launch) {
     else if (E <= 512) CCE_ROUTER_SHAPE(32, 16);
     else CCE_ROUTER_SHAPE(64, 16);
 #undef CCE_ROUTER_SHAPE
+}
+
+// Half as many lanes a row, each with twice the values: fewer operations, most of them saved in merging the lanes' lists, but fewer
+// wavefronts and longer gathers.  For lists of 8 and whole 16-byte loads; narrow / wide, us: 65536 x 256, k = 8: 34.3 / 31.4, 65536 x 128, k = 8:
+// 23.7 / 22.0, 32768 x 512, k = 8: 35.5 / 32.0; 65536 x 160, k = 4: 25.6 / 26.2, 32768 x 511, k = 8: 45.4 / 56.8.
+static bool takes_wide(const RouterArgs& a) { return a.k > 4 && a.E > 64 && a.E <= 512 && a.E % 8 == 0 && ((uintptr_t)a.logits & 15) == 0; }
+template <class Launch>
+static void with_wide_shape(int64_t E, Launch launch) {
+    if (E <= 128) launch(std::integral_constant<int, 8>{}, std::integral_constant<int, 16>{});
+    else if (E <= 256) launch(std::integral_constant<int, 8>{}, std::integral_constant<int, 32>{});
+    else launch(std::integral_constant<int, 16>{}, std::integral_constant<int, 32>{});
 }
 
 }  // namespace cce
@@ -666,19 +678,23 @@ int cce_router_forward(const void* logits, int32_t logits_bf16, const int32_t* l
     a.part_rows = (int32_t*)p; p += blocks * 4;
     a.ticket = (int32_t*)p;
     a.N = N; a.E = (int32_t)E; a.k = top_k; a.renormalize = renormalize; a.ignore_index = ignore_index; a.blocks = (int32_t)blocks;
-    with_shape(logits_bf16 != 0, E, [&](auto bf16, auto l, auto values) {
-        constexpr bool BF16 = decltype(bf16)::value;
+    auto run = [&](auto bf16, auto l, auto values, auto top) {
         constexpr int L = decltype(l)::value, VALUES = decltype(values)::value;
-        const dim3 grid((unsigned)blocks), threads(64 * router_waves(L));
-        if constexpr (BF16) {
-            if (top_k <= 2) hipLaunchKernelGGL((router_forward_kernel<BF16, L, VALUES, 2>), grid, threads, 0, stream, a);
-            else if (top_k <= 4) hipLaunchKernelGGL((router_forward_kernel<BF16, L, VALUES, 4>), grid, threads, 0, stream, a);
-            else if (top_k <= 8) hipLaunchKernelGGL((router_forward_kernel<BF16, L, VALUES, 8>), grid, threads, 0, stream, a);
-            else hipLaunchKernelGGL((router_forward_kernel<BF16, L, VALUES, 0>), grid, threads, 0, stream, a);
-        } else {
-            hipLaunchKernelGGL((router_forward_kernel<BF16, L, VALUES, 0>), grid, threads, 0, stream, a);
-        }
-    });
+        hipLaunchKernelGGL((router_forward_kernel<decltype(bf16)::value, L, VALUES, decltype(top)::value>), dim3((unsigned)blocks),
+                           dim3(64 * router_waves(L, VALUES)), 0, stream, a);
+    };
+    if (logits_bf16 != 0 && top_k <= 8 && takes_wide(a)) {
+        with_wide_shape(E, [&](auto l, auto values) { run(std::true_type{}, l, values, std::integral_constant<int, 8>{}); });
+    } else {
+        with_shape(logits_bf16 != 0, E, [&](auto bf16, auto l, auto values) {
+            if constexpr (decltype(bf16)::value) {
+                if (top_k <= 2) return run(bf16, l, values, std::integral_constant<int, 2>{});
+                if (top_k <= 4) return run(bf16, l, values, std::integral_constant<int, 4>{});
+                if (top_k <= 8) return run(bf16, l, values, std::integral_constant<int, 8>{});
+            }
+            run(bf16, l, values, std::integral_constant<int, 0>{});
+        });
+    }
     if (blocks > 1)
         hipLaunchKernelGGL(router_join_kernel, dim3((unsigned)((E + kJoinExperts - 1) / kJoinExperts)), dim3(256), 0, stream, a);
     return hip_ok(hipGetLastError()) ? CCE_OK : CCE_ERR_HIP;

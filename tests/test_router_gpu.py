@@ -21,7 +21,7 @@ U = 2.0 ** -24
 IGN = -100
 # N, E, k
 SIZES = [(1, 1, 1), (1, 8, 2), (3, 2, 1), (5, 7, 7), (4, 64, 4), (33, 8, 2), (100, 16, 3), (65, 17, 5), (257, 60, 4), (130, 61, 6), (70, 128, 8), (33, 129, 9),
-         (41, 256, 8), (19, 255, 32), (9, 300, 12), (7, 512, 8), (6, 513, 32), (5, 1023, 5), (5, 1024, 32), (6, 33, 32), (2100, 8, 1)]
+         (41, 256, 8), (19, 255, 32), (9, 300, 12), (7, 512, 8), (6, 513, 32), (5, 1023, 5), (5, 1024, 32), (6, 33, 32), (2100, 8, 1), (200, 96, 6), (150, 200, 8), (90, 264, 5), (400, 512, 7)]
 
 
 @pytest.fixture(scope="module")
@@ -132,22 +132,23 @@ def test_ties_and_signed_zeros_go_to_the_lowest_index(B):
             _check_forward(B.cce_router_forward(x.cuda(), k), x, None, k)
 
 
-def test_values_that_are_no_numbers(B):
-    x = torch.randn(40, 60)
+@pytest.mark.parametrize("E,k,bf16", [(60, 3, False), (64, 4, True), (256, 8, True), (512, 6, True)])
+def test_values_that_are_no_numbers(B, E, k, bf16):
+    x = torch.randn(40, E)
     x[3, 7] = math.nan
     x[4, 9], x[4, 2] = math.inf, math.nan
     x[5, 11] = -math.nan
-    got = B.cce_router_forward(x.cuda(), 3)
+    got = B.cce_router_forward(x.bfloat16().cuda() if bf16 else x.cuda(), k)
     idx = got.indices.cpu()
     assert idx[3, 0] == 7 and idx[4, 0] == 2 and idx[4, 1] == 9 and idx[5, 0] == 11
     bad = torch.zeros(40, dtype=torch.bool)
     bad[3:6] = True
     w = got.weights.cpu()
     assert bool(w[bad].isnan().all()) and bool(w[~bad].isfinite().all()) and bool(got.lse.cpu()[bad].isnan().all())
-    assert bool(got.losses.isnan().all()) and int(got.counts[-1]) == 40 and int(got.counts[:-1].sum()) == 120
+    assert bool(got.losses.isnan().all()) and int(got.counts[-1]) == 40 and int(got.counts[:-1].sum()) == 40 * k
 
 
-@pytest.mark.parametrize("E,k", [(8, 2), (61, 6), (256, 8)])
+@pytest.mark.parametrize("E,k", [(8, 2), (61, 6), (128, 6), (256, 8), (512, 8)])
 def test_large_logits_and_many_rows(B, E, k):
     """Far more rows than the workgroups take at a time; logits whose exponentials fp32 does not hold."""
     N = 20011
