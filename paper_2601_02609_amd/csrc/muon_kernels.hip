@@ -706,15 +706,24 @@ __device__ __forceinline__ uint16_t bf16_bits(float x) {
 }
 
 // Four values of the result for the caller: into the parameters and their copy, or into the copy alone.  vec: all four are
-// there and lie where 16-byte (8-byte) accesses may be made.
-__device__ __forceinline__ void give4(const NsMatrix& t, int64_t to, af32x4 x, int count, bool vec) {
-    if (vec) {
-        if (t.param) {
-            const af32x4 p = *(const af32x4*)(t.param + to);
+// there and lie where 16-byte (8-byte) accesses may be made.  The parameters are loaded in front, those of several calls together: the
+// compiler moves no load before a store that might write the same memory.
+__device__ __forceinline__ f32x4 param4(const NsMatrix& t, int64_t at, int count, bool vec) {
+    f32x4 p = {0.f, 0.f, 0.f, 0.f};
+    if (!t.param) return p;
+    if (vec) return *(const f32x4*)(t.param + at);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = p[e] * t.decay - t.lr * x[e];
-            *(af32x4*)(t.param + to) = x;
-        }
+    for (int e = 0; e < 4; ++e)
+        if (e < count) p[e] = t.param[at + e];
+    return p;
+}
+__device__ __forceinline__ void give4(const NsMatrix& t, int64_t to, const f32x4& p, f32x4 x, int count, bool vec) {
+    if (t.param) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = p[e] * t.decay - t.lr * x[e];
+    }
+    if (vec) {
+        if (t.param) *(f32x4*)(t.param + to) = x;
         if (t.out) {
             union { __bf16 h[4]; u32x2 u; } cv;
 #pragma unroll
@@ -726,12 +735,8 @@ __device__ __forceinline__ void give4(const NsMatrix& t, int64_t to, af32x4 x, i
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         if (e >= count) continue;
-        float y = x[e];
-        if (t.param) {
-            y = t.param[to + e] * t.decay - t.lr * y;
-            t.param[to + e] = y;
-        }
-        if (t.out) t.out[to + e] = bf16_bits(y);
+        if (t.param) t.param[to + e] = x[e];
+        if (t.out) t.out[to + e] = bf16_bits(x[e]);
     }
 }
 
@@ -985,14 +990,19 @@ struct SmallShape {
         const int work = kRest + h_room(c) + (apart(c) ? kSumBytes : 0), stages = 64 + 8 * kStageBytes;
         return work > stages ? work : stages;
     }
-    static constexpr bool takes(int64_t r, int64_t c) { return r <= kRows && c <= kColumns; }
 };
-typedef SmallShape<2, 16> Small32;
+typedef SmallShape<2, 6> Small32;
 typedef SmallShape<4, 8> Small64;
 typedef SmallShape<8, 4> Small128;
 static_assert(Small32::lds(Small32::kColumns) <= 160 * 1024 && Small64::lds(Small64::kColumns) <= 160 * 1024 &&
               Small128::lds(Small128::kColumns) <= 160 * 1024, "160 KB LDS");
 static_assert(Small32::apart(Small32::kColumns) && Small64::apart(448) && !Small64::apart(449), "either form is tested");
+// Columns of the matrices that are taken so; from there on thin ones take three launches, us of a step on 48 matrices in one workgroup each /
+// in three launches: 16 x 512 20 / 22, 16 x 896 27 / 23, 16 x 2048 46 / 26, 32 x 512 25 / 32, 32 x 896 35 / 34, 32 x 2048 67 / 42,
+// 64 x 512 43 / 78, 64 x 1024 71 / 89.
+__host__ __device__ constexpr int small_columns(int64_t rows) {
+    return rows <= 16 ? 512 : rows <= 32 ? Small32::kColumns : rows <= 64 ? Small64::kColumns : rows <= 128 ? Small128::kColumns : 0;
+}
 
 __device__ __forceinline__ f16x4 half4(const f32x4& x) {
     f16x4 h;
@@ -1285,8 +1295,8 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
         if (vec_out) {
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
-                const int row = 16 * rb + l16;
-                if (row < r && col < c) give4(t, row * t.cols + col, x[j][rb], 4, true);
+                const int at = (16 * rb + l16) * t.cols + col;
+                if (16 * rb + l16 < r && col < c) give4(t, at, param4(t, at, 4, true), x[j][rb], 4, true);
             }
         } else {
             __builtin_amdgcn_wave_barrier();
@@ -1313,9 +1323,17 @@ __global__ __launch_bounds__(kSmallThreads, 2) void ns_small_kernel(const NsSmal
     const NsMatrix& t = a.t[blockIdx.x];
     const int r = t.rows < t.cols ? t.rows : t.cols, c = t.rows < t.cols ? t.cols : t.rows;
     const bool bf16 = (a.bf16 >> blockIdx.x & 1u) != 0u;
-    if (Small32::takes(r, c)) small_matrix<Small32>(a, t, bf16, smem);
-    else if (Small64::takes(r, c)) small_matrix<Small64>(a, t, bf16, smem);
-    else small_matrix<Small128>(a, t, bf16, smem);
+    if (r <= 32) {
+        if (c <= 256) small_matrix<SmallShape<2, 2>>(a, t, bf16, smem);
+        else small_matrix<Small32>(a, t, bf16, smem);
+    } else if (r <= 64) {
+        if (c <= 256) small_matrix<SmallShape<4, 2>>(a, t, bf16, smem);
+        else if (c <= 512) small_matrix<SmallShape<4, 4>>(a, t, bf16, smem);
+        else small_matrix<Small64>(a, t, bf16, smem);
+    } else {
+        if (c <= 256) small_matrix<SmallShape<8, 2>>(a, t, bf16, smem);
+        else small_matrix<Small128>(a, t, bf16, smem);
+    }
 }
 
 // ------------------------------------------------------------------------------------------
@@ -1376,43 +1394,56 @@ __device__ __forceinline__ void thin_gram(const NsArgs& a, const NsMatrix& t, bo
     f64x4 sum[kPairs];
 #pragma unroll
     for (int p = 0; p < kPairs; ++p) sum[p] = f64x4{0.0, 0.0, 0.0, 0.0};
+    // a trip's loads are in flight during the products of the trip before
+    f32x4 g[RB], m[RB];
+    auto place = [&](int row, int col) { return tall ? (int64_t)col * t.cols + row : (int64_t)row * t.cols + col; };
+    auto load = [&](int col0) {
+        const int col = col0 + 4 * quad;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const int row = 16 * rb + l16;
+            g[rb] = m[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (row >= at.r || col >= end) continue;
+            if (vec) {
+                g[rb] = grad_values(t.grad, bf16, place(row, col));
+                if (t.momentum) m[rb] = *(const f32x4*)(t.momentum + place(row, col));
+                continue;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t i = place(row, col + e < end ? col + e : col);
+                g[rb][e] = grad_value(t.grad, bf16, i);
+                if (t.momentum) m[rb][e] = t.momentum[i];
+            }
+        }
+    };
+    load(part * at.columns + 16 * wave);
     for (int col0 = part * at.columns + 16 * wave; col0 < end; col0 += 64) {
         const int col = col0 + 4 * quad;
         f32x4 x[RB];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             const int row = 16 * rb + l16;
-            x[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (row >= at.r || col >= at.c) continue;
-            if (vec) {
-                const int64_t i = (int64_t)row * t.cols + col;
-                x[rb] = grad_values(t.grad, bf16, i);
-                if (t.momentum) {
-                    f32x4 m = *(const f32x4*)(t.momentum + i);
+            x[rb] = g[rb];
+            if (t.momentum) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float g = x[rb][e] * clip;
-                        m[e] = new_momentum(m[e], g, a.mu);
-                        x[rb][e] = direction(m[e], g, a.mu, a.nesterov);
-                    }
-                    *(f32x4*)(t.momentum + i) = m;
+                for (int e = 0; e < 4; ++e) {
+                    const float clipped = g[rb][e] * clip;
+                    m[rb][e] = new_momentum(m[rb][e], clipped, a.mu);
+                    x[rb][e] = direction(m[rb][e], clipped, a.mu, a.nesterov);
                 }
-                continue;
+                if (row < at.r && col < end) {
+                    if (vec) *(f32x4*)(t.momentum + place(row, col)) = m[rb];
+                    else
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (col + e < end) t.momentum[place(row, col + e)] = m[rb][e];
+                }
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (col + e >= at.c) continue;
-                const int64_t i = tall ? (int64_t)(col + e) * t.cols + row : (int64_t)row * t.cols + col + e;
-                float g = grad_value(t.grad, bf16, i);
-                if (t.momentum) {
-                    g *= clip;
-                    const float m = new_momentum(t.momentum[i], g, a.mu);
-                    t.momentum[i] = m;
-                    g = direction(m, g, a.mu, a.nesterov);
-                }
-                x[rb][e] = g;
-            }
+            for (int e = 0; e < 4; ++e) x[rb][e] = row < at.r && col + e < end ? x[rb][e] : 0.f;
         }
+        load(col0 + 64);
         // which column an instruction's k is does not matter, it is the same one in both operands
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -1611,6 +1642,17 @@ __device__ __forceinline__ void thin_apply(const NsArgs& a, const NsMatrix& t, b
     for (int ro = 0; ro < RB; ++ro) {
 #pragma unroll
         for (int b = 0; b < RB; ++b) q[b] = *(const f32x4*)(Q + (16 * ro + l16) * R + 16 * b + 4 * quad);
+        f32x4 p[4];
+        int left[4];
+        int64_t to[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int row = 16 * ro + 4 * quad + (tall ? 0 : k), col = c0 + (tall ? 16 * k + l16 : 4 * l16);
+            const bool there = row < at.r && col < at.c;
+            left[k] = there ? (tall ? at.r - row : at.c - col) : 0;
+            to[k] = !there ? 0 : tall ? (int64_t)col * t.cols + row : (int64_t)row * t.cols + col;
+            p[k] = param4(t, to[k], left[k], vec_out);
+        }
         f32x4 y[4];                                    // of each set: rows 16 ro + 4 quad + g of column l16
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
@@ -1623,11 +1665,8 @@ __device__ __forceinline__ void thin_apply(const NsArgs& a, const NsMatrix& t, b
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int row = 16 * ro + 4 * quad + (tall ? 0 : k), col = c0 + (tall ? 16 * k + l16 : 4 * l16);
-            if (row >= at.r || col >= at.c) continue;
-            const int left = tall ? at.r - row : at.c - col;
-            const f32x4 v = tall ? y[k] : f32x4{y[0][k], y[1][k], y[2][k], y[3][k]};
-            give4(t, tall ? (int64_t)col * t.cols + row : (int64_t)row * t.cols + col, v, left, vec_out && left >= 4);
+            if (left[k] == 0) continue;
+            give4(t, to[k], p[k], tall ? y[k] : f32x4{y[0][k], y[1][k], y[2][k], y[3][k]}, left[k], vec_out);
         }
     }
 }
@@ -1741,7 +1780,8 @@ static bool allow_lds(K kernel, int bytes) { return hip_ok(hipFuncSetAttribute((
 // LDS of a matrix that a workgroup takes alone; 0 of one for the tiled launches.
 static int small_lds(const cce_matrix& t) {
     const int64_t r = t.rows < t.cols ? t.rows : t.cols, c = t.rows < t.cols ? t.cols : t.rows;
-    return Small32::takes(r, c) ? Small32::lds((int)c) : Small64::takes(r, c) ? Small64::lds((int)c) : Small128::takes(r, c) ? Small128::lds((int)c) : 0;
+    if (c > small_columns(r)) return 0;
+    return r <= 32 ? Small32::lds((int)c) : r <= 64 ? Small64::lds((int)c) : Small128::lds((int)c);
 }
 
 static bool is_thin(const cce_matrix& t) { return (t.rows <= kThinRows || t.cols <= kThinRows) && small_lds(t) == 0; }
