@@ -1011,13 +1011,19 @@ __device__ __forceinline__ f16x4 half4(const f32x4& x) {
     return h;
 }
 
-template <class S>
+// How a wavefront's block columns go in and out.
+enum : int {
+    kVectors,                  // wide, four columns of a lane by one access
+    kStaged,                   // wide, where lines of the caller's memory and a lane's four columns do not meet
+    kColumns                   // tall: neighbouring lanes have neighbours in memory
+};
+
+template <class S, int WAY>
 __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatrix& t, bool bf16, CCE_LDS char* smem) {
     constexpr int RB = S::RB, NB = S::NB;
     constexpr int BI = RB == 8 ? 2 : 1, BJ = RB == 8 ? 4 : RB == 4 ? 2 : 1;        // blocks of A a wavefront computes
     constexpr int kPerRow = RB / BJ;                                               // wavefronts beside each other
     const int r = t.rows < t.cols ? t.rows : t.cols, c = t.rows < t.cols ? t.cols : t.rows;
-    const bool tall = t.rows > t.cols;
     const int columns = (c + 63) & ~63, block_columns = columns >> 4, pitch = columns + 8;
     CCE_LDS double* const red = (CCE_LDS double*)smem;
     CCE_LDS _Float16* const H = (CCE_LDS _Float16*)(smem + 64);
@@ -1032,17 +1038,24 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
     int mine = __builtin_amdgcn_readfirstlane((block_columns + 7 - wave) >> 3);       // this wavefront's block columns
     const float coefficient = a.coefficients[0][lane < 3 * CCE_NS_MAX_STEPS ? lane : 0];
     const float clip = a.clip_coef ? a.clip_coef[0] : 1.f;
-    const bool vec_in = !tall && (t.cols & 3) == 0 && aligned(t.grad, bf16 ? 8 : 16) && aligned(t.momentum, 16);
-    const bool vec_out = !tall && (t.cols & 3) == 0 && aligned(t.param, 16) && aligned(t.out, 8);
-    // Where lines of the caller's memory and a lane's four columns do not meet, a block column goes through this wavefront's stage: element k
-    // of it is the k-th in the caller's order.
+    // kStaged: a block column goes through this wavefront's stage, element k of it is the k-th in the caller's order
     CCE_LDS float* const stage = (CCE_LDS float*)(smem + 64 + wave * S::kStageBytes);
     auto staged = [&](int j, auto element) {
 #pragma nounroll
         for (int k = lane; k < S::kRows * 16; k += 64) {
-            const int row = tall ? k & (S::kRows - 1) : k >> 4, in = tall ? k / S::kRows : k & 15, col = 16 * (8 * j + wave) + in;
-            if (row < r && col < c) element(tall ? (int64_t)col * t.cols + row : (int64_t)row * t.cols + col, stage[row * S::kStagePitch + in]);
+            const int row = k >> 4, in = k & 15, col = 16 * (8 * j + wave) + in;
+            if (row < r && col < c) element(row * t.cols + col, stage[row * S::kStagePitch + in]);
         }
+    };
+    // kColumns: element by element
+    auto each = [&](auto element, int j) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int row = 16 * rb + l16, col = 16 * (8 * j + wave) + 4 * quad + e;
+                if (row < r && col < c) element(rb, e, col * t.cols + row);
+            }
     };
     // accumulator element e of block (rb, j): row 16 rb + l16, column 16 (8 j + wave) + 4 quad + e
     f32x4 x[NB][RB];
@@ -1053,7 +1066,7 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
         for (int rb = 0; rb < RB; ++rb) x[j][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (j >= mine) continue;
         const int col = 16 * (8 * j + wave) + 4 * quad;
-        if (vec_in) {
+        if constexpr (WAY == kVectors) {
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
                 const int row = 16 * rb + l16;
@@ -1072,9 +1085,25 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
                 }
                 x[j][rb] = u;
             }
+        } else if constexpr (WAY == kColumns) {
+            f32x4 grads[RB], moments[RB];
+            each([&](int rb, int e, int at) {
+                grads[rb][e] = grad_value(t.grad, bf16, at);
+                moments[rb][e] = t.momentum ? t.momentum[at] : 0.f;
+            }, j);
+            each([&](int rb, int e, int at) {
+                float g = grads[rb][e];
+                if (t.momentum) {
+                    g *= clip;
+                    const float m = new_momentum(moments[rb][e], g, a.mu);
+                    t.momentum[at] = m;
+                    g = direction(m, g, a.mu, a.nesterov);
+                }
+                x[j][rb][e] = g;
+            }, j);
         } else {
             __builtin_amdgcn_wave_barrier();
-            staged(j, [&](int64_t at, CCE_LDS float& to) {
+            staged(j, [&](int at, CCE_LDS float& to) {
                 float g = grad_value(t.grad, bf16, at);
                 if (t.momentum) {
                     g *= clip;
@@ -1285,19 +1314,30 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
             }
         }
     }
-    __syncthreads();                                   // the stages lie over other wavefronts' columns
+    if constexpr (WAY == kStaged) __syncthreads();     // the stages lie over other wavefronts' columns
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
         if (j >= mine) continue;
         const int col = 16 * (8 * j + wave) + 4 * quad;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) x[j][rb] *= 1.f / kScaleX;
-        if (vec_out) {
+        if constexpr (WAY == kVectors) {
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
                 const int at = (16 * rb + l16) * t.cols + col;
                 if (16 * rb + l16 < r && col < c) give4(t, at, param4(t, at, 4, true), x[j][rb], 4, true);
             }
+        } else if constexpr (WAY == kColumns) {
+            f32x4 p[RB];
+            if (t.param) each([&](int rb, int e, int at) { p[rb][e] = t.param[at]; }, j);
+            each([&](int rb, int e, int at) {
+                float y = x[j][rb][e];
+                if (t.param) {
+                    y = p[rb][e] * t.decay - t.lr * y;
+                    t.param[at] = y;
+                }
+                if (t.out) t.out[at] = bf16_bits(y);
+            }, j);
         } else {
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -1305,7 +1345,7 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
 #pragma unroll
                 for (int e = 0; e < 4; ++e) stage[(16 * rb + l16) * S::kStagePitch + 4 * quad + e] = x[j][rb][e];
             __builtin_amdgcn_wave_barrier();
-            staged(j, [&](int64_t at, CCE_LDS float& from) {
+            staged(j, [&](int at, CCE_LDS float& from) {
                 float y = from;
                 if (t.param) {
                     y = t.param[at] * t.decay - t.lr * y;
@@ -1317,23 +1357,32 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
     }
 }
 
+// Code for the matrix's columns and its way in and out: as one piece of code for all it takes 3 us longer, a half of it 1 us.
+template <int WAY>
+__device__ __forceinline__ void small_matrix_of(const NsSmallArgs& a, const NsMatrix& t, bool bf16, CCE_LDS char* smem) {
+    const int r = t.rows < t.cols ? t.rows : t.cols, c = t.rows < t.cols ? t.cols : t.rows;
+    if (r <= 32) {
+        if (c <= 256) small_matrix<SmallShape<2, 2>, WAY>(a, t, bf16, smem);
+        else small_matrix<Small32, WAY>(a, t, bf16, smem);
+    } else if (r <= 64) {
+        if (c <= 256) small_matrix<SmallShape<4, 2>, WAY>(a, t, bf16, smem);
+        else if (c <= 512) small_matrix<SmallShape<4, 4>, WAY>(a, t, bf16, smem);
+        else small_matrix<Small64, WAY>(a, t, bf16, smem);
+    } else {
+        if (c <= 256) small_matrix<SmallShape<8, 2>, WAY>(a, t, bf16, smem);
+        else small_matrix<Small128, WAY>(a, t, bf16, smem);
+    }
+}
+
 __global__ __launch_bounds__(kSmallThreads, 2) void ns_small_kernel(const NsSmallArgs a) {
     extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
     CCE_LDS char* const smem = (CCE_LDS char*)smem_generic;
     const NsMatrix& t = a.t[blockIdx.x];
-    const int r = t.rows < t.cols ? t.rows : t.cols, c = t.rows < t.cols ? t.cols : t.rows;
     const bool bf16 = (a.bf16 >> blockIdx.x & 1u) != 0u;
-    if (r <= 32) {
-        if (c <= 256) small_matrix<SmallShape<2, 2>>(a, t, bf16, smem);
-        else small_matrix<Small32>(a, t, bf16, smem);
-    } else if (r <= 64) {
-        if (c <= 256) small_matrix<SmallShape<4, 2>>(a, t, bf16, smem);
-        else if (c <= 512) small_matrix<SmallShape<4, 4>>(a, t, bf16, smem);
-        else small_matrix<Small64>(a, t, bf16, smem);
-    } else {
-        if (c <= 256) small_matrix<SmallShape<8, 2>>(a, t, bf16, smem);
-        else small_matrix<Small128>(a, t, bf16, smem);
-    }
+    if (t.rows > t.cols) small_matrix_of<kColumns>(a, t, bf16, smem);
+    else if ((t.cols & 3) == 0 && aligned(t.grad, bf16 ? 8 : 16) && aligned(t.momentum, 16) && aligned(t.param, 16) && aligned(t.out, 8))
+        small_matrix_of<kVectors>(a, t, bf16, smem);
+    else small_matrix_of<kStaged>(a, t, bf16, smem);
 }
 
 // ------------------------------------------------------------------------------------------
