@@ -1357,34 +1357,6 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
     }
 }
 
-// Code for the matrix's columns and its way in and out: as one piece of code for all it takes 3 us longer, a half of it 1 us.
-template <int WAY>
-__device__ __forceinline__ void small_matrix_of(const NsSmallArgs& a, const NsMatrix& t, bool bf16, CCE_LDS char* smem) {
-    const int r = t.rows < t.cols ? t.rows : t.cols, c = t.rows < t.cols ? t.cols : t.rows;
-    if (r <= 32) {
-        if (c <= 256) small_matrix<SmallShape<2, 2>, WAY>(a, t, bf16, smem);
-        else small_matrix<Small32, WAY>(a, t, bf16, smem);
-    } else if (r <= 64) {
-        if (c <= 256) small_matrix<SmallShape<4, 2>, WAY>(a, t, bf16, smem);
-        else if (c <= 512) small_matrix<SmallShape<4, 4>, WAY>(a, t, bf16, smem);
-        else small_matrix<Small64, WAY>(a, t, bf16, smem);
-    } else {
-        if (c <= 256) small_matrix<SmallShape<8, 2>, WAY>(a, t, bf16, smem);
-        else small_matrix<Small128, WAY>(a, t, bf16, smem);
-    }
-}
-
-__global__ __launch_bounds__(kSmallThreads, 2) void ns_small_kernel(const NsSmallArgs a) {
-    extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
-    CCE_LDS char* const smem = (CCE_LDS char*)smem_generic;
-    const NsMatrix& t = a.t[blockIdx.x];
-    const bool bf16 = (a.bf16 >> blockIdx.x & 1u) != 0u;
-    if (t.rows > t.cols) small_matrix_of<kColumns>(a, t, bf16, smem);
-    else if ((t.cols & 3) == 0 && aligned(t.grad, bf16 ? 8 : 16) && aligned(t.momentum, 16) && aligned(t.param, 16) && aligned(t.out, 8))
-        small_matrix_of<kVectors>(a, t, bf16, smem);
-    else small_matrix_of<kStaged>(a, t, bf16, smem);
-}
-
 // ------------------------------------------------------------------------------------------
 // Up to 64 rows, more columns than a workgroup takes.  Every step's polynomial is one of the first A = X X^T: with S = a + b A + c A A the
 // next A is S A S, and the result Q X, where Q is the product of all S.  So X is read twice and written once, in three launches:
@@ -1433,16 +1405,14 @@ struct ThinLayout {
 // Row of element e of a 64-bit matrix instruction's result.
 __device__ __forceinline__ int f64_row(int quad, int e) { return 4 * e + quad; }
 
-template <int RB>
-__device__ __forceinline__ void thin_gram(const NsArgs& a, const NsMatrix& t, bool bf16, const ThinLayout& at, int part, CCE_LDS double* red) {
-    constexpr int kPairs = RB * (RB + 1) / 2;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, quad = lane >> 4;
+// Momentum, and the sums of G G^T over the columns of a wavefront: 16 from `begin` on, and every `step` columns, up to `end`.
+template <int RB, class Args>
+__device__ __forceinline__ void thin_sums(const Args& a, const NsMatrix& t, bool bf16, int begin, int step, int end, f64x4 (&sum)[RB * (RB + 1) / 2]) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4, r = t.rows < t.cols ? t.rows : t.cols;
     const bool tall = t.rows > t.cols, vec = !tall && (t.cols & 3) == 0 && aligned(t.grad, bf16 ? 8 : 16) && aligned(t.momentum, 16);
     const float clip = a.clip_coef ? a.clip_coef[0] : 1.f;
-    const int end = (part + 1) * at.columns < at.c ? (part + 1) * at.columns : at.c;
-    f64x4 sum[kPairs];
 #pragma unroll
-    for (int p = 0; p < kPairs; ++p) sum[p] = f64x4{0.0, 0.0, 0.0, 0.0};
+    for (int p = 0; p < RB * (RB + 1) / 2; ++p) sum[p] = f64x4{0.0, 0.0, 0.0, 0.0};
     // a trip's loads are in flight during the products of the trip before
     f32x4 g[RB], m[RB];
     auto place = [&](int row, int col) { return tall ? (int64_t)col * t.cols + row : (int64_t)row * t.cols + col; };
@@ -1452,7 +1422,7 @@ __device__ __forceinline__ void thin_gram(const NsArgs& a, const NsMatrix& t, bo
         for (int rb = 0; rb < RB; ++rb) {
             const int row = 16 * rb + l16;
             g[rb] = m[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (row >= at.r || col >= end) continue;
+            if (row >= r || col >= end) continue;
             if (vec) {
                 g[rb] = grad_values(t.grad, bf16, place(row, col));
                 if (t.momentum) m[rb] = *(const f32x4*)(t.momentum + place(row, col));
@@ -1466,8 +1436,8 @@ __device__ __forceinline__ void thin_gram(const NsArgs& a, const NsMatrix& t, bo
             }
         }
     };
-    load(part * at.columns + 16 * wave);
-    for (int col0 = part * at.columns + 16 * wave; col0 < end; col0 += 64) {
+    load(begin);
+    for (int col0 = begin; col0 < end; col0 += step) {
         const int col = col0 + 4 * quad;
         f32x4 x[RB];
 #pragma unroll
@@ -1481,7 +1451,7 @@ __device__ __forceinline__ void thin_gram(const NsArgs& a, const NsMatrix& t, bo
                     m[rb][e] = new_momentum(m[rb][e], clipped, a.mu);
                     x[rb][e] = direction(m[rb][e], clipped, a.mu, a.nesterov);
                 }
-                if (row < at.r && col < end) {
+                if (row < r && col < end) {
                     if (vec) *(f32x4*)(t.momentum + place(row, col)) = m[rb];
                     else
 #pragma unroll
@@ -1490,9 +1460,9 @@ __device__ __forceinline__ void thin_gram(const NsArgs& a, const NsMatrix& t, bo
                 }
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[rb][e] = row < at.r && col + e < end ? x[rb][e] : 0.f;
+            for (int e = 0; e < 4; ++e) x[rb][e] = row < r && col + e < end ? x[rb][e] : 0.f;
         }
-        load(col0 + 64);
+        load(col0 + step);
         // which column an instruction's k is does not matter, it is the same one in both operands
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -1506,6 +1476,14 @@ __device__ __forceinline__ void thin_gram(const NsArgs& a, const NsMatrix& t, bo
                     sum[y * (y + 1) / 2 + z] = __builtin_amdgcn_mfma_f64_16x16x4f64(v[y], v[z], sum[y * (y + 1) / 2 + z], 0, 0, 0);
         }
     }
+}
+
+template <int RB>
+__device__ __forceinline__ void thin_gram(const NsArgs& a, const NsMatrix& t, bool bf16, const ThinLayout& at, int part, CCE_LDS double* red) {
+    constexpr int kPairs = RB * (RB + 1) / 2;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    f64x4 sum[kPairs];
+    thin_sums<RB>(a, t, bf16, part * at.columns + 16 * wave, 64, (part + 1) * at.columns < at.c ? (part + 1) * at.columns : at.c, sum);
 #pragma unroll
     for (int p = 0; p < kPairs; ++p)
 #pragma unroll
@@ -1530,10 +1508,14 @@ __global__ __launch_bounds__(kThinThreads, 2) void ns_thin_gram_kernel(const NsA
     else thin_gram<4>(a, t, bf16, at, part, red);
 }
 
-// The r x r matrices lie in LDS, symmetric up to their rounding, so that either operand's fragments are read along rows.
+// Q from G G^T in A, and what scales G to X.  The r x r matrices lie in LDS, symmetric up to their rounding, so that either operand's fragments are
+// read along rows.  Of Q each wavefront has its blocks (thin_block), in registers.
+template <int RB> constexpr int kThinPitch = 16 * RB + 8;
+template <int RB> constexpr int kThinBlocks = RB == 4 ? 2 : 1;           // of a wavefront, beside each other
 template <int RB>
-__device__ __forceinline__ void thin_steps(const NsThinArgs& args, const NsMatrix& t, const ThinLayout& at, CCE_LDS double* lds) {
-    constexpr int R = 16 * RB, P = R + 8, kPairs = RB * (RB + 1) / 2, BZ = RB == 4 ? 2 : 1;
+__device__ __forceinline__ void thin_polynomial(const float (&coefficients)[CCE_NS_MAX_STEPS][3], int steps, float eps, int threads, CCE_LDS double* lds,
+                                                f64x4 (&q)[kThinBlocks<RB>], double& inv) {
+    constexpr int R = 16 * RB, P = kThinPitch<RB>, BZ = kThinBlocks<RB>;
     const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     CCE_LDS double* const A = lds;
@@ -1541,22 +1523,6 @@ __device__ __forceinline__ void thin_steps(const NsThinArgs& args, const NsMatri
     CCE_LDS double* const U = S + R * P;
     CCE_LDS double* const Q = U + R * P;
     CCE_LDS double* const trace = Q + R * P;
-    char* const base = args.a.ws + t.base;
-    for (int i = threadIdx.x; i < kPairs * 256; i += kThinStepThreads) {
-        const double* from = (const double*)base + i;
-        double sum = 0.0;
-        for (int k0 = 0; k0 < at.parts; k0 += 8) {
-            double v[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = k0 + k < at.parts ? from[(size_t)(k0 + k) * (kPairs * 256)] : 0.0;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sum += v[k];
-        }
-        const int p = i >> 8, y = p >= 6 ? 3 : p >= 3 ? 2 : p >= 1 ? 1 : 0, z = p - y * (y + 1) / 2;
-        const int row = 16 * y + f64_row((i & 63) >> 4, (i & 255) >> 6), col = 16 * z + (i & 15);
-        A[row * P + col] = sum;
-        if (y != z) A[col * P + row] = sum;
-    }
     __syncthreads();
     if (wave == 0) {
         double d = lane < R ? A[lane * P + lane] : 0.0;
@@ -1566,8 +1532,8 @@ __device__ __forceinline__ void thin_steps(const NsThinArgs& args, const NsMatri
     }
     __syncthreads();
     const double sum = trace[0];
-    const double inv = sum <= 0x1.fffffffffffffp1023 ? 1.0 / (sqrt(sum) + (double)args.a.eps) : (double)NAN;
-    for (int i = threadIdx.x; i < R * R; i += kThinStepThreads) A[i / R * P + i % R] *= inv * inv;
+    inv = sum <= 0x1.fffffffffffffp1023 ? 1.0 / (sqrt(sum) + (double)eps) : (double)NAN;
+    for (int i = threadIdx.x; i < R * R; i += threads) A[i / R * P + i % R] *= inv * inv;
     __syncthreads();
     const int by = wave * BZ / RB, bz = wave * BZ % RB;               // this wavefront's blocks: (by, bz), and the next
     const bool has = by < RB;
@@ -1591,9 +1557,8 @@ __device__ __forceinline__ void thin_steps(const NsThinArgs& args, const NsMatri
 #pragma unroll
             for (int e = 0; e < 4; ++e) to[place(b, e)] = g[b][e];
     };
-    f64x4 q[BZ];
-    for (int s = 0; s < args.steps; ++s) {
-        const double ca = args.coefficients[s][0], cb = args.coefficients[s][1], cc = args.coefficients[s][2];
+    for (int s = 0; s < steps; ++s) {
+        const double ca = coefficients[s][0], cb = coefficients[s][1], cc = coefficients[s][2];
         f64x4 g[BZ];
         product(A, A, g);
         if (has) {
@@ -1611,7 +1576,7 @@ __device__ __forceinline__ void thin_steps(const NsThinArgs& args, const NsMatri
         } else {
             product(S, Q, q);
         }
-        if (s + 1 == args.steps) break;
+        if (s + 1 == steps) break;
         product(S, A, g);
         write(U, g);
         __syncthreads();
@@ -1620,13 +1585,44 @@ __device__ __forceinline__ void thin_steps(const NsThinArgs& args, const NsMatri
         write(A, g);
         __syncthreads();
     }
-    float* const out = (float*)(base + at.q);
-    if (has) {
+}
+
+// q(row, column) of this wavefront's blocks
+template <int RB, class Element>
+__device__ __forceinline__ void thin_block(const f64x4 (&q)[kThinBlocks<RB>], Element element) {
+    constexpr int BZ = kThinBlocks<RB>;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (wave * BZ / RB >= RB) return;
 #pragma unroll
-        for (int b = 0; b < BZ; ++b)
+    for (int b = 0; b < BZ; ++b)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) out[(16 * by + f64_row(quad, e)) * R + 16 * (bz + b) + l16] = (float)q[b][e];
+        for (int e = 0; e < 4; ++e) element(16 * (wave * BZ / RB) + f64_row(lane >> 4, e), 16 * (wave * BZ % RB + b) + (lane & 15), (float)q[b][e]);
+}
+
+template <int RB>
+__device__ __forceinline__ void thin_steps(const NsThinArgs& args, const NsMatrix& t, const ThinLayout& at, CCE_LDS double* A) {
+    constexpr int R = 16 * RB, P = kThinPitch<RB>, kPairs = RB * (RB + 1) / 2;
+    char* const base = args.a.ws + t.base;
+    for (int i = threadIdx.x; i < kPairs * 256; i += kThinStepThreads) {
+        const double* from = (const double*)base + i;
+        double sum = 0.0;
+        for (int k0 = 0; k0 < at.parts; k0 += 8) {
+            double v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = k0 + k < at.parts ? from[(size_t)(k0 + k) * (kPairs * 256)] : 0.0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += v[k];
+        }
+        const int p = i >> 8, y = p >= 6 ? 3 : p >= 3 ? 2 : p >= 1 ? 1 : 0, z = p - y * (y + 1) / 2;
+        const int row = 16 * y + f64_row((i & 63) >> 4, (i & 255) >> 6), col = 16 * z + (i & 15);
+        A[row * P + col] = sum;
+        if (y != z) A[col * P + row] = sum;
     }
+    f64x4 q[kThinBlocks<RB>];
+    double inv;
+    thin_polynomial<RB>(args.coefficients, args.steps, args.a.eps, kThinStepThreads, A, q, inv);
+    float* const out = (float*)(base + at.q);
+    thin_block<RB>(q, [&](int row, int col, float x) { out[row * R + col] = x; });
     if (threadIdx.x == 0) *(double*)(base + at.inv) = inv;
 }
 constexpr int thin_step_lds(int blocks) { return (4 * 16 * blocks * (16 * blocks + 8) + 1) * 8; }
@@ -1644,15 +1640,13 @@ __global__ __launch_bounds__(kThinStepThreads, 2) void ns_thin_steps_kernel(cons
 
 // 64 columns a wavefront, as four sets of 16: of a wide matrix set s is every fourth column from the s-th on, so that a lane has four
 // neighbours of a row in memory; of a tall one 16 neighbouring columns, of which a lane has four neighbouring rows.
-template <int RB>
-__device__ __forceinline__ void thin_apply(const NsArgs& a, const NsMatrix& t, bool bf16, const ThinLayout& at, int c0) {
-    constexpr int R = 16 * RB;
+template <int RB, class Args, class Row>
+__device__ __forceinline__ void thin_columns(const Args& a, const NsMatrix& t, bool bf16, double inv, Row q_of, int c0) {
+    const int r = t.rows < t.cols ? t.rows : t.cols, c = t.rows < t.cols ? t.cols : t.rows;
     const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
     const bool tall = t.rows > t.cols, vec_in = (t.cols & 3) == 0 && aligned(t.grad, bf16 ? 8 : 16) && aligned(t.momentum, 16);
     const bool vec_out = (t.cols & 3) == 0 && aligned(t.param, 16) && aligned(t.out, 8);
     const float clip = a.clip_coef ? a.clip_coef[0] : 1.f;
-    const char* const base = a.ws + t.base;
-    const double inv = *(const double*)(base + at.inv);
     // four neighbours in memory: of line `line` of the caller's matrix from `in` on, `left` of them there
     auto four = [&](int line, int in, int left) {
         const int64_t i = (int64_t)line * t.cols + in;
@@ -1682,23 +1676,22 @@ __device__ __forceinline__ void thin_apply(const NsArgs& a, const NsMatrix& t, b
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int row = 16 * b + 4 * quad + (tall ? 0 : k), col = c0 + (tall ? 16 * k + l16 : 4 * l16);
-            const int left = row < at.r && col < at.c ? (tall ? at.r - row : at.c - col) : 0;
+            const int left = row < r && col < c ? (tall ? r - row : c - col) : 0;
             x[b][k] = tall ? four(col, row, left) : four(row, col, left);
         }
     f32x4 q[RB];
-    const float* const Q = (const float*)(base + at.q);
 #pragma unroll
     for (int ro = 0; ro < RB; ++ro) {
 #pragma unroll
-        for (int b = 0; b < RB; ++b) q[b] = *(const f32x4*)(Q + (16 * ro + l16) * R + 16 * b + 4 * quad);
+        for (int b = 0; b < RB; ++b) q[b] = q_of(16 * ro + l16, 16 * b + 4 * quad);
         f32x4 p[4];
         int left[4];
         int64_t to[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int row = 16 * ro + 4 * quad + (tall ? 0 : k), col = c0 + (tall ? 16 * k + l16 : 4 * l16);
-            const bool there = row < at.r && col < at.c;
-            left[k] = there ? (tall ? at.r - row : at.c - col) : 0;
+            const bool there = row < r && col < c;
+            left[k] = there ? (tall ? r - row : c - col) : 0;
             to[k] = !there ? 0 : tall ? (int64_t)col * t.cols + row : (int64_t)row * t.cols + col;
             p[k] = param4(t, to[k], left[k], vec_out);
         }
@@ -1720,6 +1713,13 @@ __device__ __forceinline__ void thin_apply(const NsArgs& a, const NsMatrix& t, b
     }
 }
 
+template <int RB>
+__device__ __forceinline__ void thin_apply(const NsArgs& a, const NsMatrix& t, bool bf16, const ThinLayout& at, int c0) {
+    const char* const base = a.ws + t.base;
+    const float* const Q = (const float*)(base + at.q);
+    thin_columns<RB>(a, t, bf16, *(const double*)(base + at.inv), [&](int row, int col) { return *(const f32x4*)(Q + row * (16 * RB) + col); }, c0);
+}
+
 __global__ __launch_bounds__(kThinThreads, 2) void ns_thin_apply_kernel(const NsArgs a) {
     const int i = matrix_of(a.first, (int)a.count, 2 * blockIdx.x + 1);
     const NsMatrix& t = a.t[i];
@@ -1730,6 +1730,62 @@ __global__ __launch_bounds__(kThinThreads, 2) void ns_thin_apply_kernel(const Ns
     if (at.blocks == 1) thin_apply<1>(a, t, bf16, at, c0);
     else if (at.blocks == 2) thin_apply<2>(a, t, bf16, at, c0);
     else thin_apply<4>(a, t, bf16, at, c0);
+}
+
+// Code for the matrix's columns and its way in and out: as one piece of code for all it takes 3 us longer, a half of it 1 us.
+template <int WAY>
+__device__ __forceinline__ void small_matrix_of(const NsSmallArgs& a, const NsMatrix& t, bool bf16, CCE_LDS char* smem) {
+    const int r = t.rows < t.cols ? t.rows : t.cols, c = t.rows < t.cols ? t.cols : t.rows;
+    if (r <= 32) {
+        if (c <= 256) small_matrix<SmallShape<2, 2>, WAY>(a, t, bf16, smem);
+        else small_matrix<Small32, WAY>(a, t, bf16, smem);
+    } else if (r <= 64) {
+        if (c <= 256) small_matrix<SmallShape<4, 2>, WAY>(a, t, bf16, smem);
+        else if (c <= 512) small_matrix<SmallShape<4, 4>, WAY>(a, t, bf16, smem);
+        else small_matrix<Small64, WAY>(a, t, bf16, smem);
+    } else {
+        if (c <= 256) small_matrix<SmallShape<8, 2>, WAY>(a, t, bf16, smem);
+        else small_matrix<Small128, WAY>(a, t, bf16, smem);
+    }
+}
+
+// Up to 16 rows: as thin matrices are, in one launch.  With few values to a matrix the roundings of 16-bit operands need not even out: they left
+// up to 3e-3 of a matrix of 5 x 7.  16 x 16 10 us with them, 11 here, 16 x 512 16 and 14.
+__device__ __forceinline__ void tiny_matrix(const NsSmallArgs& a, const NsMatrix& t, bool bf16, CCE_LDS char* smem) {
+    CCE_LDS double* const red = (CCE_LDS double*)smem;
+    CCE_LDS double* const A = red + kSmallThreads / 64 * 256;
+    CCE_LDS float* const Q = (CCE_LDS float*)red;
+    const int c = t.rows < t.cols ? t.cols : t.rows, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    f64x4 sum[1], q[1];
+    thin_sums<1>(a, t, bf16, 16 * wave, kSmallThreads / 4, c, sum);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) red[wave * 256 + 64 * e + lane] = sum[0][e];
+    __syncthreads();
+    if (threadIdx.x < 256) {
+        double x = red[threadIdx.x];
+#pragma unroll
+        for (int w = 1; w < kSmallThreads / 64; ++w) x += red[w * 256 + threadIdx.x];
+        A[f64_row((int)(threadIdx.x & 63) >> 4, (int)threadIdx.x >> 6) * kThinPitch<1> + (int)(threadIdx.x & 15)] = x;
+    }
+    double inv;
+    thin_polynomial<1>(a.coefficients, a.steps, a.eps, kSmallThreads, A, q, inv);
+    thin_block<1>(q, [&](int row, int col, float x) { Q[row * 16 + col] = x; });
+    __syncthreads();
+    for (int c0 = 64 * wave; c0 < c; c0 += kSmallThreads)
+        thin_columns<1>(a, t, bf16, inv, [&](int row, int col) { return *(const CCE_LDS f32x4*)(Q + row * 16 + col); }, c0);
+}
+constexpr int kTinyLds = (kSmallThreads / 64 * 256 + 4 * 16 * kThinPitch<1> + 1) * 8;
+
+__global__ __launch_bounds__(kSmallThreads, 2) void ns_small_kernel(const NsSmallArgs a) {
+    extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
+    CCE_LDS char* const smem = (CCE_LDS char*)smem_generic;
+    const NsMatrix& t = a.t[blockIdx.x];
+    const bool bf16 = (a.bf16 >> blockIdx.x & 1u) != 0u;
+    if (t.rows <= 16 || t.cols <= 16) tiny_matrix(a, t, bf16, smem);
+    else if (t.rows > t.cols) small_matrix_of<kColumns>(a, t, bf16, smem);
+    else if ((t.cols & 3) == 0 && aligned(t.grad, bf16 ? 8 : 16) && aligned(t.momentum, 16) && aligned(t.param, 16) && aligned(t.out, 8))
+        small_matrix_of<kVectors>(a, t, bf16, smem);
+    else small_matrix_of<kStaged>(a, t, bf16, smem);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -1830,7 +1886,7 @@ static bool allow_lds(K kernel, int bytes) { return hip_ok(hipFuncSetAttribute((
 static int small_lds(const cce_matrix& t) {
     const int64_t r = t.rows < t.cols ? t.rows : t.cols, c = t.rows < t.cols ? t.cols : t.rows;
     if (c > small_columns(r)) return 0;
-    return r <= 32 ? Small32::lds((int)c) : r <= 64 ? Small64::lds((int)c) : Small128::lds((int)c);
+    return r <= 16 ? kTinyLds : r <= 32 ? Small32::lds((int)c) : r <= 64 ? Small64::lds((int)c) : Small128::lds((int)c);
 }
 
 static bool is_thin(const cce_matrix& t) { return (t.rows <= kThinRows || t.cols <= kThinRows) && small_lds(t) == 0; }

@@ -242,6 +242,21 @@ def test_on_a_stream_of_the_callers(B):
     _check_step(state, (pd, md, cd), 0.01, 0.95, True, [1.0, 1.0], [0.0, 0.0], 1.0)
 
 
+@pytest.mark.parametrize("shape", [(1, 1), (5, 7), (16, 16), (300, 13), (16, 512), (513, 3), (32, 769), (3000, 20), (60, 1100), (64, 5000)],
+                         ids=lambda s: f"{s[0]}x{s[1]}")
+def test_few_rows_are_off_by_their_last_rounding(B, shape):
+    """X = Q G with Q from 64 bits, its 2-norm at most 3.4445^5 < 486: a result is off by bf16's half step and by the rounding to fp32 of Q, of G's
+    scaled value, of r products and of r sums, (r + 3) 2^-24 of |row of Q| |column of X| <= 486 |column of X|."""
+    for kind in ("noise", "directions", "rows"):
+        g = _matrix(*shape, 13, kind)
+        out, = B.cce_orthogonalize_multi([torch.from_numpy(g).cuda()])
+        want = M.orthogonalize(g, ABC, 5, EPS)
+        x = g.astype(np.float64) / (np.linalg.norm(g.astype(np.float64)) + EPS)
+        column = np.linalg.norm(x, axis=0 if shape[0] <= shape[1] else 1, keepdims=True)
+        off = np.abs(out.float().cpu().numpy().astype(np.float64) - want)
+        assert (off <= 2.0 ** -8 * np.abs(want) + (1 + 2.0 ** -8) * (min(shape) + 3) * U * 486.0 * column).all()
+
+
 PAIRED = [(512, 1280), (1400, 500), (513, 2000)]         # the first two steps are taken as one
 
 
