@@ -60,7 +60,7 @@ int cce_router_forward(const void* logits, int32_t logits_bf16, const int32_t* l
  * d_logits (of logits' type) for the gradients of weights and losses; counts are constants, as in every balance loss.
  *   indices, lse, counts   in  what the forward pass left; counts may have been summed over the ranks of a job, for losses over
  *               the rows of all ranks.  A row whose first index is negative gets zeros and its logits are not read; another
- *               index outside [0, E) is passed over.
+ *               index outside [0, E) is passed over; the others of a row differ from each other.
  *   d_weights   in  fp32 [N, top_k], may be NULL (0); not read where there is no expert
  *   d_losses    in  fp32 [2] device, may be NULL (0)
  */

@@ -342,6 +342,30 @@ def test_large_matrices(B, shape, count):
         assert torch.equal(out[1], B.cce_orthogonalize_multi(x)[1])
 
 
+@pytest.mark.parametrize("rows,cols", [(16384, 65536), (1 << 24, 64)])
+def test_the_most_values_a_matrix_may_have(B, rows, cols):
+    """2^30.  Two rows of X each share a column and have nothing in common with the others, so that the result is made of 2 x 2 blocks, all alike."""
+    half = min(rows, cols) // 2
+    step = max(rows, cols) // (2 * half)
+    g = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    x = g if rows <= cols else g.t()
+    i = torch.arange(half, device="cuda")
+    p, q = (i * 7919 % half) * step + step // 2, half * step + (i * 104729 % half) * step + step - 1
+    x[i, p], x[half + i, p], x[half + i, q] = 1.0, 0.5, 1.0
+    u, s, v = np.linalg.svd(np.array([[1.0, 0.0], [0.5, 1.0]]))
+    s = s / math.sqrt(half * 2.25)
+    for _ in range(5):
+        s = ABC[0] * s + ABC[1] * s ** 3 + ABC[2] * s ** 5
+    want = (u * s) @ v
+    out, = B.cce_orthogonalize_multi([g], eps=0.0)
+    y = out if rows <= cols else out.t()
+    for row, col, value in ((i, p, want[0, 0]), (i, q, want[0, 1]), (half + i, p, want[1, 0]), (half + i, q, want[1, 1])):
+        # 2^-9 of the operands' rounding, of a block's norm, and bf16's half step
+        assert float((y[row, col].double() - value).abs().max()) <= 2.0 ** -9 * np.linalg.norm(want) + 2.0 ** -8 * abs(value)
+        y[row, col] = 0.0
+    assert int(torch.count_nonzero(out)) == 0
+
+
 def test_refusals(B):
     x = torch.randn(4, 6, device="cuda")
     for bad in ([], [x.half()], [x.t()], [x[0]], [x.cpu()]):
