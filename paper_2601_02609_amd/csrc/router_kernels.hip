@@ -65,6 +65,9 @@ __device__ __forceinline__ uint32_t other_lane(uint32_t x) {
     if (STEP == 16) return (uint32_t)__builtin_amdgcn_ds_swizzle((int)x, 0x401f);
     return (uint32_t)__shfl_xor((int)x, 32);
 }
+// Of the lane in front, of the same 16.
+__device__ __forceinline__ uint32_t lane_before(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false); }
+
 template <int L, int STEP = 1, class Op>
 __device__ __forceinline__ uint32_t over_lanes(uint32_t x, Op op) {
     if constexpr (STEP < L) return over_lanes<L, STEP * 2>(op(x, other_lane<STEP>(x)), op);
@@ -174,6 +177,11 @@ __device__ __forceinline__ void store_values(void* to, int64_t row, int E, int s
     }
 }
 
+// Unsigned numbers in the order of the values that are numbers; -0 as 0.
+__device__ __forceinline__ uint32_t ordered_bits(float x) {
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
 // Unsigned numbers in the order of the values; NaN above all, 0 for -inf.
 __device__ __forceinline__ uint32_t rank_of(float x) {
     const uint32_t u = __float_as_uint(x);
@@ -258,7 +266,7 @@ __global__ __launch_bounds__(64 * router_waves(L, VALUES), wide_lanes(L, VALUES)
     constexpr int kRouterWaves = router_waves(L, VALUES), kRouterThreads = 64 * kRouterWaves;
     constexpr int kSlots = TOP ? 1 : (CCE_ROUTER_MAX_TOP_K + L - 1) / L;      // chosen experts a lane keeps
     constexpr int kColumns = L * VALUES;
-    static_assert(TOP <= L && (TOP == 0 || BF16), "a lane for each chosen expert");
+    static_assert(TOP <= L, "a lane for each chosen expert");
     __shared__ int32_t count[kColumns];
     __shared__ float sums[kRouterWaves][kColumns];
     __shared__ double zs[kRouterWaves];
@@ -310,19 +318,43 @@ __global__ __launch_bounds__(64 * router_waves(L, VALUES), wide_lanes(L, VALUES)
                 uint32_t key[VALUES], list[TOP];
 #pragma unroll
                 for (int j = 0; j < VALUES; ++j) {
-                    const uint32_t pair = raw.ordered(j / 2);
-                    key[j] = (j & 1 ? pair & 0xffff0000u : pair << 16) | (uint32_t)(0xffff - C::of(sub, j));
+                    if constexpr (BF16) {
+                        const uint32_t pair = raw.ordered(j / 2);
+                        key[j] = (j & 1 ? pair & 0xffff0000u : pair << 16) | (uint32_t)(0xffff - C::of(sub, j));
+                    } else {
+                        key[j] = (ordered_bits(x[j]) & ~(uint32_t)(kColumns - 1)) | (uint32_t)(kColumns - 1 - C::of(sub, j));
+                    }
                 }
                 own_largest<TOP, VALUES>(key, list);
                 merge_lanes<TOP, L>(list);
                 uint32_t mine = 0u;
 #pragma unroll
                 for (int i = 0; i < TOP; ++i) mine = sub == i ? list[i] : mine;
-                // 0x8000 - 0x7f80: -inf
-                const bool taken = sub < a.k && (mine >> 16) > 0x80u;
-                const int32_t v = (int32_t)(mine >> 16) - 0x8000, magnitude = v < 0 ? -v : v;
-                index[0] = taken ? (int)(0xffffu - (mine & 0xffffu)) : -1;
-                weight[0] = taken ? __expf(__uint_as_float((uint32_t)magnitude << 16 | (v < 0 ? 0x80000000u : 0u)) - top) : 0.f;
+                float value;
+                bool taken;
+                if constexpr (BF16) {
+                    // 0x8000 - 0x7f80: -inf
+                    taken = sub < a.k && (mine >> 16) > 0x80u;
+                    const int32_t v = (int32_t)(mine >> 16) - 0x8000, magnitude = v < 0 ? -v : v;
+                    value = __uint_as_float((uint32_t)magnitude << 16 | (v < 0 ? 0x80000000u : 0u));
+                    index[0] = taken ? (int)(0xffffu - (mine & 0xffffu)) : -1;
+                } else {
+                    taken = sub < a.k && mine >= 0x00800000u;         // -inf: 0x007fffff
+                    index[0] = taken ? kColumns - 1 - (int)(mine & (uint32_t)(kColumns - 1)) : -1;
+                    value = taken ? ((const float*)a.logits)[row * a.E + index[0]] : -INFINITY;
+                    // The chosen ones are right if they fall in their whole values, and as many of the row's are not below the last one as there are
+                    // chosen ones (which equal values at the border are not).
+                    const float before = __uint_as_float(lane_before(__float_as_uint(value)));
+                    const int index_before = (int)lane_before((uint32_t)index[0]);
+                    const float last = __shfl(value, (lane & ~(L - 1)) + a.k - 1);
+                    uint32_t above = 0u;
+#pragma unroll
+                    for (int j = 0; j < VALUES; ++j) above += x[j] >= last ? 1u : 0u;
+                    above = over_lanes<L>(above, [](uint32_t p, uint32_t q) { return p + q; });
+                    const bool order = !taken || sub == 0 || before > value || (before == value && index_before < index[0]);
+                    rounds = __ballot(!order || (last > -INFINITY && above != (uint32_t)a.k)) != 0;
+                }
+                weight[0] = taken ? __expf(value - top) : 0.f;
                 chosen = lanes_sum<L>(weight[0]);
             }
         }
@@ -687,11 +719,9 @@ int cce_router_forward(const void* logits, int32_t logits_bf16, const int32_t* l
         with_wide_shape(E, [&](auto l, auto values) { run(std::true_type{}, l, values, std::integral_constant<int, 8>{}); });
     } else {
         with_shape(logits_bf16 != 0, E, [&](auto bf16, auto l, auto values) {
-            if constexpr (decltype(bf16)::value) {
-                if (top_k <= 2) return run(bf16, l, values, std::integral_constant<int, 2>{});
-                if (top_k <= 4) return run(bf16, l, values, std::integral_constant<int, 4>{});
-                if (top_k <= 8) return run(bf16, l, values, std::integral_constant<int, 8>{});
-            }
+            if (top_k <= 2) return run(bf16, l, values, std::integral_constant<int, 2>{});
+            if (top_k <= 4) return run(bf16, l, values, std::integral_constant<int, 4>{});
+            if (top_k <= 8) return run(bf16, l, values, std::integral_constant<int, 8>{});
             run(bf16, l, values, std::integral_constant<int, 0>{});
         });
     }

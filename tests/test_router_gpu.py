@@ -132,7 +132,18 @@ def test_ties_and_signed_zeros_go_to_the_lowest_index(B):
             _check_forward(B.cce_router_forward(x.cuda(), k), x, None, k)
 
 
-@pytest.mark.parametrize("E,k,bf16", [(60, 3, False), (64, 4, True), (256, 8, True), (512, 6, True)])
+def test_values_that_differ_in_their_last_bits(B):
+    """More alike than a sorting key with a column in it can tell, in some rows in their first places, in others at the border of the chosen ones."""
+    for E, k in ((8, 2), (60, 4), (128, 8), (256, 7), (500, 8), (1000, 3)):
+        rng = np.random.default_rng(E)
+        near = 1.0 + np.stack([rng.permutation(E) for _ in range(40)]) * 2.0 ** -23
+        far = rng.standard_normal((40, E))
+        x = np.concatenate([near, -near, far, np.where(rng.random((40, E)) < k / E, 3.0 + far, near), np.where(rng.random((40, E)) < 0.5, far, -near)])
+        x = torch.from_numpy(x[rng.permutation(len(x))].astype(np.float32))
+        _check_forward(B.cce_router_forward(x.cuda(), k), x, None, k)
+
+
+@pytest.mark.parametrize("E,k,bf16", [(60, 3, False), (256, 8, False), (64, 4, True), (256, 8, True), (512, 6, True)])
 def test_values_that_are_no_numbers(B, E, k, bf16):
     x = torch.randn(40, E)
     x[3, 7] = math.nan
