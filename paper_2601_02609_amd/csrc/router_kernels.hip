@@ -257,8 +257,10 @@ __device__ __forceinline__ void own_largest(const uint32_t (&key)[VALUES], uint3
     }
 }
 
-// TOP > 0 (bf16, k <= TOP): a logit and its column make one 32-bit key, and the TOP largest of a row come out of sorting networks;
-// 0, and rows that hold a NaN or +inf: k rounds of a maximum over the row.  65536 x 256 bf16, k = 8: rounds 53 us, networks see below.
+// TOP > 0 (k <= TOP): a logit and its column make one 32-bit key, and the TOP largest of a row come out of sorting networks.  Of fp32 logits the
+// column takes the place of the last bits, so that the outcome is checked against the whole values.  0, and rows that hold a NaN or +inf or fail
+// the check: k rounds of a maximum over the row.  The launch alone, 65536 x 256, k = 8, bf16: rounds 53 us, networks 26, with_wide_shape 23; the
+// whole call in fp32: rounds 52.5, networks 43.7.
 template <bool BF16, int L, int VALUES, int TOP>
 __global__ __launch_bounds__(64 * router_waves(L, VALUES), wide_lanes(L, VALUES) ? 2 : 4) void router_forward_kernel(const RouterArgs a) {
     using C = Columns<BF16, L, VALUES>;
@@ -664,7 +666,7 @@ static void with_shape(bool bf16, int64_t E, Launch launch) {
 }
 
 // Half as many lanes a row, each with twice the values: fewer operations, most of them saved in merging the lanes' lists, but fewer
-// wavefronts and longer gathers.  For lists of 8 and whole 16-byte loads; narrow / wide, us: 65536 x 256, k = 8: 34.3 / 31.4, 65536 x 128, k = 8:
+// wavefronts and longer gathers.  For lists of 8 of bf16 keys and whole 16-byte loads (fp32: 43.8 / 42.5, 4096 rows 19.3 / 23.4); narrow / wide, us: 65536 x 256, k = 8: 34.3 / 31.4, 65536 x 128, k = 8:
 // 23.7 / 22.0, 32768 x 512, k = 8: 35.5 / 32.0; 65536 x 160, k = 4: 25.6 / 26.2, 32768 x 511, k = 8: 45.4 / 56.8.
 static bool takes_wide(const RouterArgs& a) { return a.k > 4 && a.E > 64 && a.E <= 512 && a.E % 8 == 0 && ((uintptr_t)a.logits & 15) == 0; }
 template <class Launch>
