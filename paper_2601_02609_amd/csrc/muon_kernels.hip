@@ -956,7 +956,7 @@ __global__ __launch_bounds__(TurnTile::kThreads, 2) void ns_apply_turn_kernel(co
 //   poly    wavefronts share the blocks
 //   apply   each wavefront its own columns, which no other one reads: X stays in its registers
 //
-// The 17 launches of the tiled path take 115 us for 64 x 256 and 199 for 48 matrices of 16 x 896, mostly waiting for each other.
+// The 17 launches of the tiled path take 115 us for 64 x 256, mostly waiting for each other, this 20; 128 x 448 61, 64 x 1024 41.
 // ------------------------------------------------------------------------------------------
 constexpr int kSmallThreads = 512;
 constexpr int kSmallMatrices = 48;

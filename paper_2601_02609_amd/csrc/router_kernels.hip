@@ -643,8 +643,11 @@ static int check_sizes(int64_t N, int64_t E) {
 // Rows that a workgroup of so many wavefronts takes at a time.
 static int64_t rows_of_group(int64_t E, int waves) { return waves * (E <= 64 ? 8 : E <= 256 ? 4 : E <= 512 ? 2 : 1); }
 
+// Workgroups.  One takes two or three trips rather than leaving a join to a second launch, us of the launches without / with it: 256 x 64, k = 4
+// 8.1 / 11.2, 384 x 64 9.9 / 11.1, 512 x 64 11.8 / 11.0, 128 x 128, k = 8 8.7 / 12.1, 192 x 128 10.6 / 12.2 (fp32 13.2 / 12.2), 128 x 256 12.9 / 15.8.
 static int64_t forward_blocks(int64_t N, int64_t E) {
     const int64_t rows = rows_of_group(E, router_waves(E > 512 ? 64 : 8, 1)), want = (N + rows - 1) / rows;
+    if (want <= (E <= 64 ? 3 : 2)) return 1;
     return want < kRouterBlocks ? want : kRouterBlocks;
 }
 

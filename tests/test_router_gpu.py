@@ -21,7 +21,7 @@ U = 2.0 ** -24
 IGN = -100
 # N, E, k
 SIZES = [(1, 1, 1), (1, 8, 2), (3, 2, 1), (5, 7, 7), (4, 64, 4), (33, 8, 2), (100, 16, 3), (65, 17, 5), (257, 60, 4), (130, 61, 6), (70, 128, 8), (33, 129, 9),
-         (41, 256, 8), (19, 255, 32), (9, 300, 12), (7, 512, 8), (6, 513, 32), (5, 1023, 5), (5, 1024, 32), (6, 33, 32), (2100, 8, 1), (200, 96, 6), (150, 200, 8), (90, 264, 5), (400, 512, 7)]
+         (41, 256, 8), (19, 255, 32), (9, 300, 12), (7, 512, 8), (6, 513, 32), (5, 1023, 5), (5, 1024, 32), (6, 33, 32), (2100, 8, 1), (200, 96, 6), (150, 200, 8), (90, 264, 5), (400, 512, 7), (384, 20, 2), (385, 64, 3), (128, 200, 4), (129, 200, 4)]
 
 
 @pytest.fixture(scope="module")
