@@ -9,8 +9,8 @@
  *
  * Products take operands of 16 bits (fp16, power-of-two scales) and add in fp32; the diagonals of A and of b A + c A A
  * and what X loses by its rounding are held beside them, so that the result is within some 2^-9 of the
- * formula's (2-norm of the difference over that of the result): less than bf16's own rounding adds.  Thin matrices (a side of up
- * to 64, the other one beyond 1024 to 2048) take 64-bit products.
+ * formula's (2-norm of the difference over that of the result): less than bf16's own rounding adds.  Matrices with a
+ * side of up to 16, and thin ones (up to 64, the other side beyond 768 to 1024) take 64-bit products.
  *
  * Conventions are those of cce.h: matrix pointers are DEVICE pointers owned by the caller, dense row-major, aligned
  * to their elements; `stream` is a hipStream_t as void*; nothing is allocated, freed or synchronised: the
