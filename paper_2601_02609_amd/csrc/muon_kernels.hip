@@ -148,6 +148,12 @@ __device__ __forceinline__ T* uniform(T* p) {
     return (T*)(uintptr_t)((uint64_t)hi << 32 | lo);
 }
 
+// Between LDS accesses of a wavefront's lanes to each other's places: the LDS keeps their order, and the compiler has to.
+__device__ __forceinline__ void wave_lds_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+}
+
 __device__ __forceinline__ float new_momentum(float m, float g, float mu) { return mu * m + (1.f - mu) * g; }
 __device__ __forceinline__ float direction(float m, float g, float mu, int nesterov) { return nesterov ? mu * m + (1.f - mu) * g : m; }
 
@@ -950,13 +956,19 @@ __global__ __launch_bounds__(TurnTile::kThreads, 2) void ns_apply_turn_kernel(co
 
 // ------------------------------------------------------------------------------------------
 // A matrix of few rows in one workgroup, all steps in one launch: X in fp32 in the accumulators (blocks of 16 x 16 by eight
-// wavefronts, block column j of wavefront w being 8 j + w), its h in LDS for the products.  The linear part a X needs no remainder here.
+// wavefronts, block column j of wavefront w being 8 j + w), its h in LDS for the products.
 //
 //   gram    up to 64 rows each wavefront sums over its own columns; of more rows wavefronts share the blocks of A, each over all columns of h
 //   poly    wavefronts share the blocks
 //   apply   each wavefront its own columns, which no other one reads: X stays in its registers
 //
-// The 17 launches of the tiled path take 115 us for 64 x 256, mostly waiting for each other, this 20; 128 x 448 61, 64 x 1024 41.
+// Rounding.  The roundings of the operands of few rows even out little, and the steps amplify those that are not along a matrix's large
+// directions by up to 485, so that it shows of matrices of low rank.  Up to 64 rows M is multiplied with the next 11 bits of X too, and up to 32
+// all products have their operands' next 11 bits (kWhole).  Largest error (2-norm, of the result's) over spectra of rank 1 to 64, noise and singular
+// values down to 1e-4, without / with: 17 x 17 2.3e-2 / 3e-5, 33 x 33 1.6e-2 / 1.2e-3, 64 x 256 6.7e-3 / 9e-4; us 17 x 17 9.7 / 11.0,
+// 32 x 512 14.5 / 19.2, 64 x 256 19.8 / 21.9, 64 x 1024 45 / 55.
+//
+// The 17 launches of the tiled path take 115 us for 64 x 256, mostly waiting for each other.  128 x 448 62 us.
 // ------------------------------------------------------------------------------------------
 constexpr int kSmallThreads = 512;
 constexpr int kSmallMatrices = 48;
@@ -977,12 +989,13 @@ struct SmallShape {
     static constexpr int RB = RB_, NB = NB_, kRows = 16 * RB_, kColumns = RB_ < 8 ? NB_ * 128 : 448;
     static constexpr int kPitchA = kRows + 8;
     static constexpr bool kOwnSums = RB_ <= 4;           // A from each wavefront's own columns
+    static constexpr bool kWhole = RB_ == 2;             // remainders of X, A and M in all products
     static constexpr int kPairs = RB_ * (RB_ + 1) / 2;   // blocks of A, of each two that mirror each other one
-    static constexpr int kSumBytes = kOwnSums ? 8 * kPairs * 1024 : 0, kMBytes = kOwnSums ? kRows * kPitchA * 2 : 0;
+    static constexpr int kSumBytes = kOwnSums ? 8 * kPairs * 1024 : 0, kSquares = kWhole ? 4 : kOwnSums ? 2 : 1;      // (M in A's place where it has no other)
     static constexpr int kStagePitch = 16 + 1, kStageBytes = kRows * kStagePitch * 4;      // a block column of a wavefront, on its way in or out
     static constexpr int pitch(int c) { return ((c + 63) & ~63) + 8; }
     static constexpr int h_bytes(int c) { return kRows * pitch(c) * 2; }
-    static constexpr int kRest = 64 + kRows * kPitchA * 2 + kMBytes + kRows * 8;
+    static constexpr int kRest = 64 + kSquares * kRows * kPitchA * 2 + kRows * 8;
     // whether the wavefronts' sums have room of their own; else they lie over h, of which none is needed then
     static constexpr bool apart(int c) { return kRest + h_bytes(c) + kSumBytes <= 160 * 1024; }
     static constexpr int h_room(int c) { return apart(c) || h_bytes(c) > kSumBytes ? h_bytes(c) : kSumBytes; }
@@ -998,8 +1011,8 @@ static_assert(Small32::lds(Small32::kColumns) <= 160 * 1024 && Small64::lds(Smal
               Small128::lds(Small128::kColumns) <= 160 * 1024, "160 KB LDS");
 static_assert(Small32::apart(Small32::kColumns) && Small64::apart(448) && !Small64::apart(449), "either form is tested");
 // Columns of the matrices that are taken so; from there on thin ones take three launches, us of a step on 48 matrices in one workgroup each /
-// in three launches: 16 x 512 20 / 22, 16 x 896 27 / 23, 16 x 2048 46 / 26, 32 x 512 25 / 32, 32 x 896 35 / 34, 32 x 2048 67 / 42,
-// 64 x 512 43 / 78, 64 x 1024 71 / 89.
+// in three launches: 16 x 512 20 / 22, 16 x 896 27 / 23, 16 x 2048 46 / 26, 32 x 512 26 / 32, 32 x 768 35 / 34,
+// 64 x 512 48 / 78, 64 x 1024 83 / 85.
 __host__ __device__ constexpr int small_columns(int64_t rows) {
     return rows <= 16 ? 512 : rows <= 32 ? Small32::kColumns : rows <= 64 ? Small64::kColumns : rows <= 128 ? Small128::kColumns : 0;
 }
@@ -1009,6 +1022,13 @@ __device__ __forceinline__ f16x4 half4(const f32x4& x) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) h[e] = (_Float16)x[e];
     return h;
+}
+// What x has beyond its h, of h's scale: the next 11 bits.
+__device__ __forceinline__ f16x4 rest4(const f32x4& x, const f16x4& h) {
+    f16x4 l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) l[e] = (_Float16)(x[e] - (float)h[e]);
+    return l;
 }
 
 // How a wavefront's block columns go in and out.
@@ -1028,8 +1048,11 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
     CCE_LDS double* const red = (CCE_LDS double*)smem;
     CCE_LDS _Float16* const H = (CCE_LDS _Float16*)(smem + 64);
     CCE_LDS _Float16* const A = (CCE_LDS _Float16*)(smem + 64 + S::h_room(c));
-    CCE_LDS _Float16* const M = A + (S::kOwnSums ? S::kRows * S::kPitchA : 0);        // (in A's place where it has no other)
-    CCE_LDS float* const da = (CCE_LDS float*)(M + S::kRows * S::kPitchA);
+    constexpr int kSquare = S::kRows * S::kPitchA;
+    CCE_LDS _Float16* const M = A + (S::kSquares > 1 ? kSquare : 0);
+    CCE_LDS _Float16* const A_rest = A + 2 * kSquare;                                 // (of kWhole)
+    CCE_LDS _Float16* const M_rest = A + 3 * kSquare;
+    CCE_LDS float* const da = (CCE_LDS float*)(A + S::kSquares * kSquare);
     CCE_LDS float* const dm = da + S::kRows;
     const bool apart = S::apart(c);
     CCE_LDS float* const sums = apart ? dm + S::kRows : (CCE_LDS float*)H;
@@ -1147,14 +1170,14 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
     const int bi = wave / kPerRow * BI, bj = wave % kPerRow * BJ;     // this wavefront's blocks of A: from (bi, bj) on
     const bool has_blocks = bi < RB;
     const int frag = l16 * pitch + 8 * quad, frag_a = l16 * S::kPitchA + 8 * quad;
-    // blocks (bi + y, bj + z) += P P^T over columns [0, n) of P, whose fragments lie at p
-    auto blocks_product = [&](f32x4 (&g)[BI][BJ], const CCE_LDS _Float16* p, int pitch_p, int k) {
+    // blocks (bi + y, bj + z) += P Q^T over columns k to k + 31, whose fragments lie at p and q
+    auto blocks_product = [&](f32x4 (&g)[BI][BJ], const CCE_LDS _Float16* p, const CCE_LDS _Float16* q, int pitch_p, int k) {
         f16x8 m[BI];
 #pragma unroll
         for (int y = 0; y < BI; ++y) m[y] = *(const CCE_LDS f16x8*)(p + 16 * (bi + y) * pitch_p + k);
 #pragma unroll
         for (int z = 0; z < BJ; ++z) {
-            const f16x8 n = *(const CCE_LDS f16x8*)(p + 16 * (bj + z) * pitch_p + k);
+            const f16x8 n = *(const CCE_LDS f16x8*)(q + 16 * (bj + z) * pitch_p + k);
 #pragma unroll
             for (int y = 0; y < BI; ++y) g[y][z] = __builtin_amdgcn_mfma_f32_16x16x32_f16(m[y], n, g[y][z], 0, 0, 0);
         }
@@ -1188,17 +1211,24 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
 #pragma unroll
             for (int j = 0; j < NB; j += 2) {
                 if (j >= mine) continue;
-                f16x8 h[RB];
+                f16x8 h[RB], l[RB];
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb) {
                     const f16x4 lo = half4(x[j][rb]), hi = half4(x[j + 1][rb]);
                     h[rb] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    if constexpr (S::kWhole) l[rb] = __builtin_shufflevector(rest4(x[j][rb], lo), rest4(x[j + 1][rb], hi), 0, 1, 2, 3, 4, 5, 6, 7);
                 }
 #pragma unroll
                 for (int y = 0; y < RB; ++y)
 #pragma unroll
-                    for (int z = 0; z <= y; ++z)
-                        part[y * (y + 1) / 2 + z] = __builtin_amdgcn_mfma_f32_16x16x32_f16(h[y], h[z], part[y * (y + 1) / 2 + z], 0, 0, 0);
+                    for (int z = 0; z <= y; ++z) {
+                        f32x4& to = part[y * (y + 1) / 2 + z];
+                        if constexpr (S::kWhole) {
+                            to = __builtin_amdgcn_mfma_f32_16x16x32_f16(h[y], l[z], to, 0, 0, 0);
+                            to = __builtin_amdgcn_mfma_f32_16x16x32_f16(l[y], h[z], to, 0, 0, 0);
+                        }
+                        to = __builtin_amdgcn_mfma_f32_16x16x32_f16(h[y], h[z], to, 0, 0, 0);
+                    }
             }
             if (!apart) __syncthreads();               // h is not needed any more
 #pragma unroll
@@ -1219,23 +1249,28 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
                 for (int w = 0; w < 8; ++w) v[w] = *(const CCE_LDS f32x4*)(sums + (w * S::kPairs + p) * 256 + 4 * lane);
                 const f32x4 sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
                 // element e: column 16 y + 4 quad + e of row 16 z + l16
-                f16x4 of_a;
+                f32x4 beside;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float value = sum[e] * (1.f / (kScaleX * kScaleX));
                     const bool diagonal = y == z && 4 * quad + e == l16;
                     if (diagonal) da[16 * y + l16] = value;
-                    of_a[e] = diagonal ? (_Float16)0.f : (_Float16)(value * kScaleA);
+                    beside[e] = diagonal ? 0.f : value * kScaleA;
                 }
-                *(CCE_LDS f16x4*)(A + (16 * z + l16) * S::kPitchA + 16 * y + 4 * quad) = of_a;
-                if (y != z)
+                auto place = [&](CCE_LDS _Float16* to, const f16x4& v) {
+                    *(CCE_LDS f16x4*)(to + (16 * z + l16) * S::kPitchA + 16 * y + 4 * quad) = v;
+                    if (y != z)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) A[(16 * y + 4 * quad + e) * S::kPitchA + 16 * z + l16] = of_a[e];
+                        for (int e = 0; e < 4; ++e) to[(16 * y + 4 * quad + e) * S::kPitchA + 16 * z + l16] = v[e];
+                };
+                const f16x4 of_a = half4(beside);
+                place(A, of_a);
+                if constexpr (S::kWhole) place(A_rest, rest4(beside, of_a));
             }
         } else if (has_blocks) {
             for (int k = 0; k < columns; k += 64) {
-                blocks_product(g, H + frag, pitch, k);
-                blocks_product(g, H + frag, pitch, k + 32);
+                blocks_product(g, H + frag, H + frag, pitch, k);
+                blocks_product(g, H + frag, H + frag, pitch, k + 32);
             }
             // element e of a block: column 16 (bi + y) + 4 quad + e of row 16 (bj + z) + l16
 #pragma unroll
@@ -1256,7 +1291,13 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
         __syncthreads();
         if (has_blocks) {
 #pragma unroll
-            for (int k = 0; k < S::kRows; k += 32) blocks_product(g, A + frag_a, S::kPitchA, k);
+            for (int k = 0; k < S::kRows; k += 32) {
+                blocks_product(g, A + frag_a, A + frag_a, S::kPitchA, k);
+                if constexpr (S::kWhole) {
+                    blocks_product(g, A + frag_a, A_rest + frag_a, S::kPitchA, k);
+                    blocks_product(g, A_rest + frag_a, A + frag_a, S::kPitchA, k);
+                }
+            }
         }
         if constexpr (S::kOwnSums) write_h();
         else __syncthreads();                          // M takes A's place
@@ -1271,17 +1312,22 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
 #pragma unroll
                 for (int z = 0; z < BJ; ++z) {
                     const float dn = da[16 * (bj + z) + l16];
-                    f16x4 m;
+                    f32x4 beside;
+                    f16x4 rest = {};
+                    if constexpr (S::kWhole) rest = *(const CCE_LDS f16x4*)(A_rest + (16 * (bj + z) + l16) * S::kPitchA + 16 * (bi + y) + 4 * quad);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int col = 16 * (bi + y) + 4 * quad + e;
                         const bool diagonal = col == 16 * (bj + z) + l16;
                         const float p = g[y][z][e] * (cc / (kScaleA * kScaleA));
-                        const float v = (cb + cc * (dn + dc[e])) * ((float)o[y][z][e] * (1.f / kScaleA)) + p;
+                        const float v = (cb + cc * (dn + dc[e])) * (((float)o[y][z][e] + (float)rest[e]) * (1.f / kScaleA)) + p;
                         if (diagonal) dm[col] = cb * dn + (cc * dn * dn + p);
-                        m[e] = diagonal ? (_Float16)0.f : (_Float16)v;
+                        beside[e] = diagonal ? 0.f : v;
                     }
+                    const f16x4 m = half4(beside);
                     *(CCE_LDS f16x4*)(M + (16 * (bj + z) + l16) * S::kPitchA + 16 * (bi + y) + 4 * quad) = m;
+                    if constexpr (S::kWhole)
+                        *(CCE_LDS f16x4*)(M_rest + (16 * (bj + z) + l16) * S::kPitchA + 16 * (bi + y) + 4 * quad) = rest4(beside, m);
                 }
             }
         }
@@ -1290,27 +1336,80 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
         float keep[RB];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) keep[rb] = ca + dm[16 * rb + l16];
+        // 8 rows of a column a lane, from k on, by transpose reads
+        auto column_rows = [&](int j, int k) {
+            const CCE_LDS _Float16* const p = H + (k + 8 * quad + (l16 >> 2)) * pitch + 16 * (8 * j + wave) + 4 * (l16 & 3);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CCE_LDS s16x4*)p);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CCE_LDS s16x4*)(p + 4 * pitch));
+            return __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        if constexpr (S::kOwnSums) {
+            // Products of M with h, and with what X has beyond it, which takes h's place: with h alone the diagonal of M, which acts on X itself, and
+            // the rest of M would not act on the same matrix, and what M leaves of X's smallest directions is the small difference of both.
+            constexpr int KB = S::kRows / 32;
+            f16x8 m[KB][RB], m_rest[KB][RB];
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            if (j >= mine) continue;
+            for (int k = 0; k < KB; ++k)
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) x[j][rb] *= keep[rb];
-        }
+                for (int rb = 0; rb < RB; ++rb) {
+                    m[k][rb] = *(const CCE_LDS f16x8*)(M + 16 * rb * S::kPitchA + frag_a + 32 * k);
+                    if constexpr (S::kWhole) m_rest[k][rb] = *(const CCE_LDS f16x8*)(M_rest + 16 * rb * S::kPitchA + frag_a + 32 * k);
+                }
 #pragma unroll
-        for (int k = 0; k < S::kRows; k += 32) {
-            f16x8 m[RB];
+            for (int j0 = 0; j0 < NB; j0 += 2) {
+                if (j0 >= mine) continue;
+                f16x8 h[2][KB];
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) m[rb] = *(const CCE_LDS f16x8*)(M + 16 * rb * S::kPitchA + frag_a + k);
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int k = 0; k < KB; ++k) h[j][k] = column_rows(j0 + j < mine ? j0 + j : j0, 32 * k);
+                wave_lds_order();
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if (j0 + j >= mine) continue;
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) {
+                        f32x4& v = x[j0 + j][rb];
+                        *(CCE_LDS f16x4*)(H + (16 * rb + l16) * pitch + 16 * (8 * (j0 + j) + wave) + 4 * quad) = rest4(v, half4(v));
+                        v *= keep[rb];
+#pragma unroll
+                        for (int k = 0; k < KB; ++k) {
+                            v = __builtin_amdgcn_mfma_f32_16x16x32_f16(h[j][k], m[k][rb], v, 0, 0, 0);
+                            if constexpr (S::kWhole) v = __builtin_amdgcn_mfma_f32_16x16x32_f16(h[j][k], m_rest[k][rb], v, 0, 0, 0);
+                        }
+                    }
+                }
+            }
+            wave_lds_order();
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
                 if (j >= mine) continue;
-                // transpose reads: 8 rows of a column a lane
-                const CCE_LDS _Float16* const p = H + (k + 8 * quad + (l16 >> 2)) * pitch + 16 * (8 * j + wave) + 4 * (l16 & 3);
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CCE_LDS s16x4*)p);
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CCE_LDS s16x4*)(p + 4 * pitch));
-                const f16x8 h = __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb) x[j][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(h, m[rb], x[j][rb], 0, 0, 0);
+                for (int k = 0; k < KB; ++k) {
+                    const f16x8 l = column_rows(j, 32 * k);
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) x[j][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(l, m[k][rb], x[j][rb], 0, 0, 0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                if (j >= mine) continue;
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) x[j][rb] *= keep[rb];
+            }
+#pragma unroll
+            for (int k = 0; k < S::kRows; k += 32) {
+                f16x8 m[RB];
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) m[rb] = *(const CCE_LDS f16x8*)(M + 16 * rb * S::kPitchA + frag_a + k);
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    if (j >= mine) continue;
+                    const f16x8 h = column_rows(j, k);
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) x[j][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(h, m[rb], x[j][rb], 0, 0, 0);
+                }
             }
         }
     }
