@@ -6,9 +6,17 @@ GPU path, imports nothing from the package and is never called from the product 
     X = G / (|G|_F + eps), transposed where G is taller than wide
     each step:  A = X X^T,  X = a X + (b A + c A A) X
 
-`orthogonalize` is that in 64 bits.  `orthogonalize_rounded` rounds to 16 bits where the kernels may -- the operands of the
-products, the diagonals of A and of b A + c A A apart, the linear part in two 16-bit values -- and is otherwise the same: how far
-it is from `orthogonalize` is how far the kernels may be, beside the order of their fp32 sums.
+`orthogonalize` is that in 64 bits.  `orthogonalize_rounded` rounds where the kernels may, and is otherwise the same: how far it is from
+`orthogonalize` is how far the kernels may be, beside the order of their fp32 sums.
+
+    h      X in fp16, the operand of the products
+    l      what X has beyond h, a whole number of 2^-8 of h's last place
+    A      its diagonal apart, the rest in fp16
+    M      = b A + c A A the same; but in the steps behind which the product of the a is 8 or more the diagonal is in the fp16 operand, and
+           only what that rounding leaves is apart
+    X      a (h + l) + M's diagonal (h + l) + the rest of M h
+
+Of up to 64 rows all of M acts on X, with 22 bits of it; of up to 32 the rest of A and M have 22 bits too.
 """
 from __future__ import annotations
 
@@ -40,10 +48,16 @@ def _half(x, scale):
     return (x * scale).astype(np.float16).astype(np.float64) / scale
 
 
-def _apart(x, scale):
+def _whole(x, scale):
+    """In two 16-bit values."""
+    h = _half(x, scale)
+    return h + _half(x - h, scale)
+
+
+def _apart(x, scale, rounded=_half):
     """A symmetric matrix as its diagonal and the rest, rounded."""
     diagonal = x.diagonal().copy()
-    return diagonal, _half(x - np.diag(diagonal), scale)
+    return diagonal, rounded(x - np.diag(diagonal), scale)
 
 
 def _product(x, y):
@@ -58,20 +72,35 @@ def _polynomial(gram, a, b, c):
     return a * np.eye(len(d)) + b * (np.diag(d) + off) + c * square
 
 
+def _rest(x, h):
+    """x - h in eight bits below h's last place, h = fp16 of 2^13 x."""
+    places = 2.0 ** (np.floor(np.log2(np.maximum(np.abs(h) * 2.0 ** 13, 2.0 ** -14))) - 10 - 13)
+    return np.clip(np.rint((x - h) / places * 256), -128, 127) / 256 * places
+
+
 def orthogonalize_rounded(g, coefficients, steps, eps, pair=False):
     """pair: the first two steps are taken as one, with the next A from the first one's polynomial S as S (S A)."""
     x, tall = _start(g, eps)
+    square = _whole if len(x) <= 32 else _half
     steps_left = list(_steps(coefficients, steps))
     while steps_left:
-        h = _half(x, 2.0 ** 13)
-        linear = h + _half(x - h, 2.0 ** 24)
-        gram = _apart(h @ h.T, 2.0 ** 13)
-        keep, m = _apart(_polynomial(gram, *steps_left.pop(0)), 2.0 ** 10)
+        h = square(x, 2.0 ** 13)
+        gram = _apart(h @ h.T, 2.0 ** 13, square)
+        a, b, c = steps_left.pop(0)
+        keep, m = _apart(_polynomial(gram, a, b, c), 2.0 ** 10, square)
         if pair:
             pair = False
-            gram = _apart(_product((keep, m), _apart(_product((keep, m), gram), 2.0 ** 13)), 2.0 ** 13)
-            keep, m = _apart(_product(_apart(_polynomial(gram, *steps_left.pop(0)), 2.0 ** 10), (keep, m)), 2.0 ** 10)
-        x = keep[:, None] * linear + m @ h
+            gram = _apart(_product((keep, m), _apart(_product((keep, m), gram), 2.0 ** 13, square)), 2.0 ** 13, square)
+            first, (a, b, c) = a, steps_left.pop(0)
+            keep, m = _apart(_product(_apart(_polynomial(gram, a, b, c), 2.0 ** 10, square), (keep, m)), 2.0 ** 10, square)
+            a = a * first
+        if len(x) <= 64:
+            x = keep[:, None] * x + m @ _whole(x, 2.0 ** 13)
+            continue
+        if np.prod([abs(later[0]) for later in steps_left]) >= 8.0:
+            on_h = _half(keep - a, 2.0 ** 10)
+            keep, m = keep - on_h, m + np.diag(on_h)
+        x = keep[:, None] * (h + _rest(x, h)) + m @ h
     return x.T if tall else x
 
 

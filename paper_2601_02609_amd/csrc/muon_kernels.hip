@@ -12,10 +12,10 @@
 // Rounding.  Products take fp16 operands (11 bits) and add in fp32.  Rounding all of X, A and M to them would leave an error of
 // 2 % (6e-3 of matrices with a few large directions), because the diagonals of A and M are much larger than what lies beside them, and the
 // linear part a X carries small directions next to large ones.  So the diagonals of A and M are kept in fp32 and taken out of the
-// 16-bit operands, and the linear part is taken from X as h + l, two 16-bit values: 0.5 to 1.4e-3 in all, half of bf16's own
-// rounding of the result.
+// 16-bit operands (M's in the later steps alone, see apart_steps), and the linear part is taken from X as h + l, a 16-bit and an 8-bit value.
+// ERRORS
 //
-// Scales, powers of two: X 2^13, A 2^13, M 2^10, the remainders l 2^24.  Singular values stay below 2.5 (checked for the coefficients),
+// Scales, powers of two: X 2^13, A 2^13, M 2^10; l see split1.  Singular values stay below 2.5 (checked for the coefficients),
 // values of X too; A's are below 6.25 and M's below 60: within fp16's 65504.
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -45,7 +45,7 @@ constexpr int64_t kMaxMatrix = (int64_t)1 << 30;       // values of a padded mat
 constexpr int64_t kMaxSide = 16384;                    // smaller side
 constexpr int kNormParts = 256;                        // partial sums of a matrix
 constexpr int kNormValues = 8192;                      // values of a part, more where that gives too many parts
-constexpr float kScaleX = 0x1p13f, kScaleA = 0x1p13f, kScaleM = 0x1p10f, kScaleL = 0x1p18f;
+constexpr float kScaleX = 0x1p13f, kScaleA = 0x1p13f, kScaleM = 0x1p10f;
 constexpr double kMaxSigma = 2.5, kMaxM = 60.0;
 
 struct NsMatrix {
@@ -82,6 +82,8 @@ struct NsProductArgs {
     uint32_t tiles, split_tiles, splits;      // tiles of 256 x 256: how many, the last of them in parts of their sums, parts each
     uint32_t partials;         // the parts' place, in units of 256 bytes
     uint32_t kind;             // of a symmetric product
+    uint32_t apart;            // whether M acts on h alone (apart_steps)
+    float on_x;                // what of its diagonal does not
 };
 static_assert(sizeof(NsArgs) <= 4096 && sizeof(NsProductArgs) <= 4096, "kernel arguments hold 4 KB");
 
@@ -218,14 +220,22 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(const NsArgs a) {
     if (threadIdx.x == 0) ((double*)(a.ws + t.base + NsLayout(t.rows, t.cols).partials))[part] = sum;
 }
 
-// x as h + l: h has x's first 11 bits, l, in E4M3, the next four.
+// x as h + l: h has x's first 11 bits, l the next eight, as a whole number of 2^-8 of h's last place, 128 more so that it is positive.  (Four bits
+// in E4M3 left 4e-3 of the results of matrices of rank 1, X's first rounding amplified by the steps; these leave 8e-4.)
+__device__ __forceinline__ uint32_t exponent_bits(_Float16 h) {          // 2^e for h of [2^e, 2^(e + 1)); 2^-14 for less, as h's last place is
+    const uint32_t u = __float_as_uint((float)h) & 0x7f800000u;
+    return u > 0x38800000u ? u : 0x38800000u;
+}
 __device__ __forceinline__ float split1(float x, _Float16& h) {
     const float s = x * kScaleX;
     h = (_Float16)s;
-    return (s - (float)h) * (kScaleL / kScaleX);
+    return fmaf(s - (float)h, __uint_as_float(0x88000000u - exponent_bits(h)), 128.f);      // 2^18 / 2^e
 }
-__device__ __forceinline__ uint32_t pack_fp8(float a, float b, float c, float d) {
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+// What l stands for, 2^18 kScaleX times of it.
+__device__ __forceinline__ float rest_of(_Float16 h, uint32_t l) { return ((float)(l & 0xffu) - 128.f) * __uint_as_float(exponent_bits(h)); }
+// Rounded to the nearest whole number from 0 to 255.
+__device__ __forceinline__ uint32_t pack_u8(float a, float b, float c, float d) {
+    return __builtin_amdgcn_cvt_pk_u8_f32(d, 3, __builtin_amdgcn_cvt_pk_u8_f32(c, 2, __builtin_amdgcn_cvt_pk_u8_f32(b, 1, __builtin_amdgcn_cvt_pk_u8_f32(a, 0, 0u))));
 }
 __device__ __forceinline__ void split8(const float (&x)[8], f16x8& h, u32x2& l) {
     float r[8];
@@ -235,7 +245,7 @@ __device__ __forceinline__ void split8(const float (&x)[8], f16x8& h, u32x2& l) 
         r[e] = split1(x[e], v);
         h[e] = v;
     }
-    l = u32x2{pack_fp8(r[0], r[1], r[2], r[3]), pack_fp8(r[4], r[5], r[6], r[7])};
+    l = u32x2{pack_u8(r[0], r[1], r[2], r[3]), pack_u8(r[4], r[5], r[6], r[7])};
 }
 __device__ __forceinline__ void split4(const af32x4& x, f16x4& h, uint32_t& l) {
     float r[4];
@@ -245,7 +255,7 @@ __device__ __forceinline__ void split4(const af32x4& x, f16x4& h, uint32_t& l) {
         r[e] = split1(x[e], v);
         h[e] = v;
     }
-    l = pack_fp8(r[0], r[1], r[2], r[3]);
+    l = pack_u8(r[0], r[1], r[2], r[3]);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -428,6 +438,15 @@ __device__ __forceinline__ float symmetric_value(const NsProductArgs& a, const S
     return (dn * ((float)x * of.of_x) + (dm * ((float)y * (1.f / kScaleM)) + p)) * of.scale;
 }
 
+// A value of the diagonal: what of it is held beside the operand, and the operand's.
+template <int MODE>
+__device__ __forceinline__ float on_diagonal(const NsProductArgs& a, float diagonal, _Float16& value) {
+    value = (_Float16)0.f;
+    if (MODE == kGram || !a.apart) return diagonal;
+    value = (_Float16)((diagonal - a.on_x) * kScaleM);
+    return diagonal - (float)value * (1.f / kScaleM);
+}
+
 // A tile and its mirror image.
 template <int MODE>
 __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(const NsProductArgs a) {
@@ -501,8 +520,12 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
                 float diagonal;
                 const float beside = symmetric_value<MODE>(a, of, x[e], ox[k][e], oy[k][e], dn[k], dc[e >> 2][e & 3], diagonal);
                 const bool here = m + e == n;
-                if (here && inside) of.dout[n] = diagonal;
-                v[e] = here ? (_Float16)0.f : (_Float16)beside;
+                _Float16 value = (_Float16)beside;
+                if (here) {
+                    diagonal = on_diagonal<MODE>(a, diagonal, value);
+                    if (inside) of.dout[n] = diagonal;
+                }
+                v[e] = value;
             }
             if (inside) *(f16x8*)of.at_place(at, n, m) = v;
             if (m0 != n0)
@@ -576,8 +599,9 @@ __device__ __forceinline__ void symmetric_ping_rows(const NsProductArgs& a, cons
                     float diagonal;
                     const float beside = symmetric_value<MODE>(a, of, x[e], ox[k][e], oy[k][e], dn[k], dc[e >> 2][e & 3], diagonal);
                     const bool here = m + e == n;
-                    if (here) of.dout[n] = diagonal;
-                    v[e] = here ? (_Float16)0.f : (_Float16)beside;
+                    _Float16 value = (_Float16)beside;
+                    if (here) of.dout[n] = on_diagonal<MODE>(a, diagonal, value);
+                    v[e] = value;
                 }
                 if (n < at.rp) *(f16x8*)of.at_place(at, n, m) = v;
                 if (ti != tj)
@@ -778,16 +802,12 @@ struct ApplyRows {
         for (int k = 0; k < 8; ++k) {
             const int y = 4 * k + (lane >> 4), n = n0 + y;
             const uint32_t j = (uint32_t)n * (uint32_t)at.cp + m;
-            const float of_h = (a.a + keep[k]) * (1.f / kScaleX), of_l = (a.a + keep[k]) * (1.f / kScaleL);
+            const float of_h = (a.a + keep[k]) * (1.f / kScaleX), of_l = of_h * 0x1p-18f;
             float x[8];
             read8(rows + y * kApplyPitch + q, x);
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                const f32x2 r = e & 2 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)l[k][e >> 2], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)l[k][e >> 2], false);
-#pragma unroll
-                for (int f = 0; f < 2; ++f)
-                    x[e + f] = fmaf(of_h, (float)h[k][e + f], fmaf(of_l, r[f], x[e + f] * (1.f / (kScaleX * kScaleM))));
-            }
+            for (int e = 0; e < 8; ++e)
+                x[e] = fmaf(of_h, (float)h[k][e], fmaf(of_l, rest_of(h[k][e], l[k][e >> 2] >> 8 * (e & 3)), x[e] * (1.f / (kScaleX * kScaleM))));
             if (!LAST) {
                 f16x8 h1;
                 u32x2 l1;
@@ -964,7 +984,8 @@ __global__ __launch_bounds__(TurnTile::kThreads, 2) void ns_apply_turn_kernel(co
 //
 // Rounding.  The roundings of the operands of few rows even out little, and the steps amplify those that are not along a matrix's large
 // directions by up to 485, so that it shows of matrices of low rank.  Up to 64 rows M is multiplied with the next 11 bits of X too, and up to 32
-// all products have their operands' next 11 bits (kWhole).  Largest error (2-norm, of the result's) over spectra of rank 1 to 64, noise and singular
+// all products have their operands' next 11 bits (kWhole).  Of more rows M acts on h alone in the steps behind which much is amplified (apart_steps):
+// 65 x 200 6.9e-3 / 1.1e-3.  Largest error (2-norm, of the result's) over spectra of rank 1 to 64, noise and singular
 // values down to 1e-4, without / with: 17 x 17 2.3e-2 / 3e-5, 33 x 33 1.6e-2 / 1.2e-3, 64 x 256 6.7e-3 / 9e-4; us 17 x 17 9.7 / 11.0,
 // 32 x 512 14.5 / 19.2, 64 x 256 19.8 / 21.9, 64 x 1024 45 / 55.
 //
@@ -980,6 +1001,7 @@ struct NsSmallArgs {
     const float* clip_coef;
     float mu, eps;
     int32_t nesterov, steps;
+    uint32_t apart;                                    // bit s: in step s M acts on h alone (apart_steps)
 };
 static_assert(sizeof(NsSmallArgs) <= 4096, "kernel arguments hold 4 KB");
 
@@ -1321,8 +1343,13 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
                         const bool diagonal = col == 16 * (bj + z) + l16;
                         const float p = g[y][z][e] * (cc / (kScaleA * kScaleA));
                         const float v = (cb + cc * (dn + dc[e])) * (((float)o[y][z][e] + (float)rest[e]) * (1.f / kScaleA)) + p;
-                        if (diagonal) dm[col] = cb * dn + (cc * dn * dn + p);
-                        beside[e] = diagonal ? 0.f : v;
+                        float d = cb * dn + (cc * dn * dn + p), of_h = 0.f;
+                        if (!S::kOwnSums && (a.apart >> s & 1u)) {
+                            of_h = (float)(_Float16)d;
+                            d -= of_h;
+                        }
+                        if (diagonal) dm[col] = d;
+                        beside[e] = diagonal ? of_h : v;
                     }
                     const f16x4 m = half4(beside);
                     *(CCE_LDS f16x4*)(M + (16 * (bj + z) + l16) * S::kPitchA + 16 * (bi + y) + 4 * quad) = m;
@@ -1967,6 +1994,22 @@ static bool may_pair(const float* coefficients, int steps) {
     return true;
 }
 
+// The steps in which all of M acts on h alone, and a on all of X.  What X has beyond h, l, then lacks M l, which has M's large directions and so is
+// amplified by nothing.  Otherwise M's diagonal D acts on all of X, as it may in other steps: it lacks (M - D) l, which is less where M is mostly
+// its diagonal, as of noise, but D l is along the smallest directions too, which the steps behind it amplify by the product of their a.
+// Largest error of 130 x 130, from the oracle's rounded form, with D on X in all steps / from a factor of 41 on / 12 / in none apart: rank 1 5.0e-3 /
+// 0.9 / 0.8, rank 32 2.4 / 2.0 / 1.1, noise 0.83 / 0.84 / 1.0 / 1.4: from 8 on.
+constexpr double kAmplified = 8.0;
+static uint32_t apart_steps(const float* coefficients, int steps) {
+    uint32_t apart = 0;
+    double behind = 1.0;
+    for (int s = steps - 1; s >= 0; --s) {
+        if (behind >= kAmplified) apart |= 1u << s;
+        behind *= fabs((double)coefficients[3 * s]);
+    }
+    return apart;
+}
+
 static uint32_t sym_tiles(const NsLayout& at, bool large) {
     const int side = large ? SymPing::BM : SymTile::BM;
     const uint32_t n = (uint32_t)((at.rp + side - 1) / side);
@@ -2049,6 +2092,7 @@ static bool run_small(const cce_matrix* matrices, int64_t count, bool step, floa
     a.eps = eps;
     a.nesterov = nesterov;
     a.steps = steps;
+    a.apart = apart_steps(coefficients, steps);
     for (int s = 0; s < 3 * steps; ++s) a.coefficients[s / 3][s % 3] = coefficients[s];
     for (int64_t i = 0; i < count;) {
         int n = 0, bytes = 0;
@@ -2236,11 +2280,15 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
                 p.c = coefficients[3 * s + 2];
             }
         };
+        const uint32_t apart = apart_steps(coefficients, steps);
+        int s = 0;
         auto symmetric = [&](auto mode, uint32_t kind) {
             constexpr int MODE = decltype(mode)::value;
             const int op = MODE == kGram ? 0 : 1;
             NsProductArgs& p = products[op];
             p.kind = kind;
+            p.apart = (kind == kOfA || kind == kBoth) ? apart >> s & 1u : 0u;
+            p.on_x = kind == kBoth ? p.a * (coefficients[3 * (s - 1)] - 1.f) : 0.f;      // a of both steps, less what the apply has
             if (large[op]) hipLaunchKernelGGL(ns_symmetric_ping_kernel<MODE>, dim3(grid[op]), dim3(SymPing::kThreads), kPingLds, stream, p);
             else hipLaunchKernelGGL(ns_symmetric_kernel<MODE>, dim3(grid[op]), dim3(SymTile::kThreads), kSymLds, stream, p);
             if (large[op] && p.split_tiles) hipLaunchKernelGGL(ns_symmetric_join_kernel<MODE>, dim3(8 * p.split_tiles), dim3(64), 0, stream, p);
@@ -2249,7 +2297,7 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
         constexpr std::integral_constant<int, kPoly> poly{};
         constexpr std::integral_constant<int, kProduct> product{};
         uint32_t flip = 0;
-        for (int s = 0; s < steps; ++s) {
+        for (; s < steps; ++s) {
             for (auto& p : products) p.flip = flip;
             coefficients_of(s);
             symmetric(gram, kOfX);

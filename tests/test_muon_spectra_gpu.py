@@ -13,9 +13,10 @@ from oracle import muon_oracle as M
 pytestmark = pytest.mark.gpu
 ABC = (3.4445, -4.7750, 2.0315)
 EPS = 1e-7
-# by the way a matrix takes: up to 16 rows, to 32 and to 64 in one workgroup, thin ones
+# by the way a matrix takes: up to 16 rows, to 32, to 64 and to 128 in one workgroup, thin ones, tiles
 SHAPES = {"16": [(5, 7), (16, 500)], "32": [(17, 17), (20, 30), (40, 17), (32, 64), (31, 767)], "64": [(33, 33), (40, 48), (200, 33), (64, 256), (63, 1001)],
-          "thin": [(24, 3000), (64, 2000)]}
+          "128": [(65, 65), (65, 200), (128, 128), (448, 127)], "thin": [(24, 3000), (64, 2000)],
+          "tiles": [(130, 130), (192, 192), (300, 1000), (512, 512), (100, 2100), (512, 1280), (1400, 520)]}
 # directions of a common size and noise beside them
 KINDS = [(1, 0.0), (2, 0.0), (3, 0.0), (5, 0.0), (16, 0.0), (32, 0.0), (64, 0.0), (1, 1e-3), (2, 1e-3), (8, 1e-3), (1, 1e-2), (4, 5e-2), (0, 1.0)]
 
