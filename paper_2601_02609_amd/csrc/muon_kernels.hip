@@ -151,12 +151,6 @@ __device__ __forceinline__ T* uniform(T* p) {
     return (T*)(uintptr_t)((uint64_t)hi << 32 | lo);
 }
 
-// Between LDS accesses of a wavefront's lanes to each other's places: the LDS keeps their order, and the compiler has to.
-__device__ __forceinline__ void wave_lds_order() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-    __builtin_amdgcn_wave_barrier();
-}
-
 __device__ __forceinline__ float new_momentum(float m, float g, float mu) { return mu * m + (1.f - mu) * g; }
 __device__ __forceinline__ float direction(float m, float g, float mu, int nesterov) { return nesterov ? mu * m + (1.f - mu) * g : m; }
 
@@ -509,7 +503,7 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
             for (int g = 0; g < 4; ++g)
                 *(CCE_LDS f32x4*)(rows + (lane & 31) * kSymPitch + bm * 32 + 8 * g + 4 * (lane >> 5)) =
                     f32x4{acc[bm][bn][4 * g], acc[bm][bn][4 * g + 1], acc[bm][bn][4 * g + 2], acc[bm][bn][4 * g + 3]};
-        __builtin_amdgcn_wave_barrier();
+        wave_lds_order();
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int y = 8 * k + (lane >> 3), n = wn + bn * 32 + y;
@@ -534,7 +528,7 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
 #pragma unroll
                 for (int e = 0; e < 8; ++e) mirror[(q + e) * kSymMirror + bn * 32 + y] = v[e];
         }
-        __builtin_amdgcn_wave_barrier();
+        wave_lds_order();
     }
     if (m0 == n0) return;
 #pragma unroll
@@ -589,7 +583,7 @@ __device__ __forceinline__ void symmetric_ping_rows(const NsProductArgs& a, cons
 #pragma unroll
                 for (int b = 0; b < SymPing::QA; ++b)
                     *(CCE_LDS f32x4*)(rows + (16 * j + (lane & 15)) * kPingPitch + 16 * b + 4 * (lane >> 4)) = acc[part * SymPing::QA + b][4 * side + j];
-            __builtin_amdgcn_wave_barrier();
+            wave_lds_order();
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int y = 16 * k + (lane >> 2), n = nw + 64 * side + y;
@@ -610,7 +604,7 @@ __device__ __forceinline__ void symmetric_ping_rows(const NsProductArgs& a, cons
 #pragma unroll
                     for (int e = 0; e < 8; ++e) mirror[(q + e) * kPingMirror + 64 * side + y] = v[e];
             }
-            __builtin_amdgcn_wave_barrier();
+            wave_lds_order();
         }
         if (ti != tj) {
 #pragma unroll
@@ -619,7 +613,7 @@ __device__ __forceinline__ void symmetric_ping_rows(const NsProductArgs& a, cons
                 const f16x8 v = *(const CCE_LDS f16x8*)(mirror + y * kPingMirror + (lane & 15) * 8);
                 *(f16x8*)of.at_place(at, row, col) = v;
             }
-            __builtin_amdgcn_wave_barrier();
+            wave_lds_order();
         }
     }
 }
@@ -823,7 +817,7 @@ struct ApplyRows {
                 *(CCE_LDS f32x4*)(rows + y * kApplyPitch + q + 4) = f32x4{x[4], x[5], x[6], x[7]};
             }
         }
-        __builtin_amdgcn_wave_barrier();
+        wave_lds_order();
         if constexpr (LAST) {
             // to the caller, four values in a row of their matrix a lane: rows of X, or columns
             const bool tall = t.rows > t.cols, vec = (t.cols & 3) == 0 && aligned(t.param, 16) && aligned(t.out, 8);
@@ -876,7 +870,7 @@ struct ApplyRows {
                         }
                 }
             }
-            __builtin_amdgcn_wave_barrier();
+            wave_lds_order();
         }
     }
 };
@@ -921,7 +915,7 @@ __global__ __launch_bounds__(ApplyTile::kThreads, 2) void ns_apply_kernel(const 
             for (int g = 0; g < 4; ++g)
                 *(CCE_LDS f32x4*)(rows + (lane & 31) * kApplyPitch + bm * 32 + 8 * g + 4 * (lane >> 5)) =
                     f32x4{acc[bm][bn][4 * g], acc[bm][bn][4 * g + 1], acc[bm][bn][4 * g + 2], acc[bm][bn][4 * g + 3]};
-        __builtin_amdgcn_wave_barrier();
+        wave_lds_order();
         of.finish<LAST>(a, t, at, base, wn + bn * 32, wm, rows);
     }
 }
@@ -971,7 +965,7 @@ __global__ __launch_bounds__(TurnTile::kThreads, 2) void ns_apply_turn_kernel(co
 #pragma unroll
             for (int y = 0; y < 2; ++y)
                 *(CCE_LDS f32x4*)(rows + (16 * y + (lane & 15)) * kApplyPitch + 16 * x + 4 * (lane >> 4)) = acc[x][2 * half + y];
-        __builtin_amdgcn_wave_barrier();
+        wave_lds_order();
         of.finish<LAST>(a, t, at, base, wn + half * 32, wm, rows);
     }
 }
@@ -1149,7 +1143,7 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
                 x[j][rb][e] = g;
             }, j);
         } else {
-            __builtin_amdgcn_wave_barrier();
+            wave_lds_order();
             staged(j, [&](int at, CCE_LDS float& to) {
                 float g = grad_value(t.grad, bf16, at);
                 if (t.momentum) {
@@ -1160,7 +1154,7 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
                 }
                 to = g;
             });
-            __builtin_amdgcn_wave_barrier();
+            wave_lds_order();
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
                 const int row = 16 * rb + l16;
@@ -1467,12 +1461,12 @@ __device__ __forceinline__ void small_matrix(const NsSmallArgs& a, const NsMatri
                 if (t.out) t.out[at] = bf16_bits(y);
             }, j);
         } else {
-            __builtin_amdgcn_wave_barrier();
+            wave_lds_order();
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) stage[(16 * rb + l16) * S::kStagePitch + 4 * quad + e] = x[j][rb][e];
-            __builtin_amdgcn_wave_barrier();
+            wave_lds_order();
             staged(j, [&](int at, CCE_LDS float& from) {
                 float y = from;
                 if (t.param) {

@@ -575,6 +575,7 @@ __global__ __launch_bounds__(512, 4) void router_backward_kernel(const RouterGra
         share[j] = C::of(sub, j) < a.E ? beta * (float)a.counts[C::of(sub, j)] : 0.f;
         mine[C::of(sub, j)] = 0.f;
     }
+    wave_lds_order();
     const int64_t step = (int64_t)gridDim.x * kRouterWaves * kRows;
     const int64_t begin = ((int64_t)blockIdx.x * kRouterWaves + wave) * kRows;
     // a trip's first index, by which its loads go, one trip ahead
@@ -616,15 +617,15 @@ __global__ __launch_bounds__(512, 4) void router_backward_kernel(const RouterGra
 #pragma unroll
         for (int q = 0; q < kSlots; ++q)
             if (index[q] >= 0) mine[index[q]] = (dw[q] - mean) * inv;
-        __builtin_amdgcn_wave_barrier();                              // a row's lanes are of one wavefront, whose LDS accesses keep their order
+        wave_lds_order();                                             // a row's lanes are of one wavefront
         float d[VALUES];
 #pragma unroll
         for (int j = 0; j < VALUES; ++j) d[j] = live ? p[j] * (share[j] + mine[C::of(sub, j)] - dot) : 0.f;
-        __builtin_amdgcn_wave_barrier();
+        wave_lds_order();
 #pragma unroll
         for (int q = 0; q < kSlots; ++q)
             if (index[q] >= 0) mine[index[q]] = 0.f;
-        __builtin_amdgcn_wave_barrier();
+        wave_lds_order();
         if (there) store_values<BF16, L, VALUES>(a.d_logits, row, a.E, sub, whole, d);
     }
 }

@@ -1,5 +1,5 @@
 // Device helpers of the kernels that stream their tensors: 16-byte vectors, eight bf16 values to and from
-// fp32, sums over a wavefront.
+// fp32, sums over a wavefront; order of a wavefront's LDS accesses.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -34,6 +34,12 @@ __device__ __forceinline__ float wave_sum(float x) {
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o);
     return x;
+}
+
+// Between LDS accesses of a wavefront's lanes to each other's places: the LDS keeps their order, and the compiler has to.
+__device__ __forceinline__ void wave_lds_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
 }
 
 }  // namespace cce
