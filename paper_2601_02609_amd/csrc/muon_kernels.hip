@@ -2196,6 +2196,9 @@ static bool large_tiles(int op, int n, Length length, Tiles tiles, Layout layout
 
 static int run_groups(const cce_matrix* matrices, int64_t count, bool step, float lr, float mu, int nesterov, const float* coefficients,
                       int steps, float eps, const float* clip_coef, void* workspace, hipStream_t stream) {
+    bool any = false;
+    for (int64_t i = 0; i < count; ++i) any = any || (matrices[i].rows != 0 && matrices[i].cols != 0);
+    if (!any) return CCE_OK;                           // (nothing is asked of the device)
     if (!run_small(matrices, count, step, lr, mu, nesterov, coefficients, steps, eps, clip_coef, stream)) return CCE_ERR_HIP;
     if (!run_thin(matrices, count, step, lr, mu, nesterov, coefficients, steps, eps, clip_coef, workspace, stream)) return CCE_ERR_HIP;
     NsArgs a;
