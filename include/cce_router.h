@@ -23,7 +23,8 @@
  * each other, an input or the workspace; in the backward pass d_logits may be logits' own memory.
  *
  * Sizes: N >= 1 rows (below 2^31), 1 <= top_k <= E; CCE_ERR_UNSUPPORTED for E beyond CCE_ROUTER_MAX_EXPERTS or top_k beyond
- * CCE_ROUTER_MAX_TOP_K.  Results do not depend on the run: sums are taken in an order that the sizes alone decide.
+ * CCE_ROUTER_MAX_TOP_K.  Results do not depend on the run, and a row's own not on the other rows:
+ * sums are taken in an order that the sizes, the type and the alignment of logits decide.
  */
 #ifndef CCE_ROUTER_H_
 #define CCE_ROUTER_H_

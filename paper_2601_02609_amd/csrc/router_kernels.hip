@@ -384,7 +384,7 @@ __global__ __launch_bounds__(64 * router_waves(L, VALUES), wide_lanes(L, VALUES)
                     const uint32_t column = lanes_min<L>(mine);
                     const bool taken = most != 0u;
                     const float w = taken ? __expf(value_of(most) - top) : 0.f;
-                    chosen += w;
+                    if (TOP == 0) chosen += w;
                     if (sub == s) {
                         index[q] = taken ? (int)column : -1;
                         weight[q] = w;
@@ -398,6 +398,7 @@ __global__ __launch_bounds__(64 * router_waves(L, VALUES), wide_lanes(L, VALUES)
                     most = lanes_max<L>(best);
                 }
             }
+            if constexpr (TOP != 0) chosen = lanes_sum<L>(weight[0]);  // (in the networks' order: a row's bits do not depend on its neighbours)
         }
         const float inv = live ? __builtin_amdgcn_rcpf(total) : 0.f;              // (a row that takes no part: p is 0)
         const float lse = live ? top + __logf(total) : 0.f;
