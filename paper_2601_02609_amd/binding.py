@@ -1477,6 +1477,17 @@ def _router_logits(logits: torch.Tensor):
     return N, E
 
 
+def _router_memory(N: int, E: int, k: int, device, out: Optional[RouterOutput], need: int):
+    """Outputs, if none are given, and a workspace of `need` bytes.  Each output is a tensor of its own: some are saved for the backward pass,
+    others summed over ranks in place or kept for a log.  (empty_strided: a decode step is bound by the host, and empty takes a third longer.)"""
+    new = torch.empty_strided
+    if out is None:
+        out = RouterOutput(new((N, k), (k, 1), dtype=torch.int32, device=device), new((N, k), (k, 1), dtype=torch.float32, device=device),
+                           new((N,), (1,), dtype=torch.float32, device=device), new((E + 1,), (1,), dtype=torch.int32, device=device),
+                           new((E,), (1,), dtype=torch.float32, device=device), new((2,), (1,), dtype=torch.float32, device=device))
+    return out, new((need,), (1,), dtype=torch.uint8, device=device) if need else None
+
+
 def cce_router_forward(logits: torch.Tensor, top_k: int, labels: Optional[torch.Tensor] = None, ignore_index: int = -100, *,
                        renormalize: bool = True, out: Optional[RouterOutput] = None, workspace: Optional[torch.Tensor] = None,
                        stream: Optional[torch.cuda.Stream] = None) -> RouterOutput:
@@ -1496,30 +1507,24 @@ def cce_router_forward(logits: torch.Tensor, top_k: int, labels: Optional[torch.
             raise CCEError(CCE_ERR_UNSUPPORTED, "cce_router_workspace_bytes")
     else:
         _check_on(device, workspace, torch.uint8, (workspace.numel(),), "workspace")
+    if out is None or need:
+        if stream is None:
+            new, own = _router_memory(N, E, top_k, device, out, need)
+        else:
+            with torch.cuda.stream(stream):
+                new, own = _router_memory(N, E, top_k, device, out, need)
+        workspace = workspace if own is None else own
     if out is None:
-        # two pieces of memory for all outputs, the fp32 ones behind a small workspace: a decode step is bound by the host
-        front = need // 4 if need <= 4096 else 0
-        ints = _new((N * top_k + E + 1,), torch.int32, device, stream)
-        floats = _new((front + N * top_k + N + E + 2,), torch.float32, device, stream)
-        lse = front + N * top_k
-        out = RouterOutput(ints.as_strided((N, top_k), (top_k, 1)), floats.as_strided((N, top_k), (top_k, 1), front),
-                           floats.as_strided((N,), (1,), lse), ints.as_strided((E + 1,), (1,), N * top_k),
-                           floats.as_strided((E,), (1,), lse + N), floats.as_strided((2,), (1,), lse + N + E))
-        workspace_at = floats.data_ptr() if front else None
+        out = new
     else:
         shapes = (((N, top_k), torch.int32), ((N, top_k), torch.float32), ((N,), torch.float32), ((E + 1,), torch.int32),
                   ((E,), torch.float32), ((2,), torch.float32))
         for name, t, (shape, dtype) in zip(RouterOutput._fields, out, shapes):
             _check_on(device, t, dtype, shape, name)
-        workspace_at = None
-    if workspace_at is None:
-        if workspace is None:
-            workspace = _new((need,), torch.uint8, device, stream)
-        workspace_at, need = workspace.data_ptr(), workspace.numel()
     _call("cce_router_forward", lib().cce_router_forward, device, stream, logits.data_ptr(), 1 if logits.dtype == torch.bfloat16 else 0,
           labels.data_ptr() if labels is not None else None, N, E, top_k, 1 if renormalize else 0, ignore_index,
           out.indices.data_ptr(), out.weights.data_ptr(), out.lse.data_ptr(), out.counts.data_ptr(), out.prob_sums.data_ptr(),
-          out.losses.data_ptr(), workspace_at, need)
+          out.losses.data_ptr(), workspace.data_ptr(), workspace.numel())
     return out
 
 

@@ -1,4 +1,4 @@
-"""What a row of the router gives is that row's alone."""
+"""What a row of the router gives is that row's alone, and what a call gives is tensors of their own."""
 import math
 
 import pytest
@@ -38,3 +38,34 @@ def test_a_rows_bits_do_not_depend_on_its_neighbours(B, E, k, bf16):
         for name in ("indices", "weights", "lse"):
             a, b = getattr(alone, name)[::2], getattr(beside, name)[::2]
             assert torch.equal(a.view(torch.int32), b.view(torch.int32)), name
+
+
+@pytest.mark.parametrize("N,E,k", [(4, 64, 4), (3000, 16, 2)])
+def test_outputs_are_tensors_of_their_own(B, N, E, k):
+    """Counts summed over ranks in place between a forward and a backward pass that saved the others; losses kept for a log."""
+    x = torch.randn(N, E, device="cuda")
+
+    class Route(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, logits):
+            f = B.cce_router_forward(logits, k)
+            ctx.save_for_backward(logits, f.indices, f.lse)
+            ctx.counts = f.counts
+            return f.weights, f.losses
+
+        @staticmethod
+        def backward(ctx, d_weights, d_losses):
+            logits, indices, lse = ctx.saved_tensors
+            return B.cce_router_backward(logits, indices, lse, ctx.counts, d_weights.contiguous(), d_losses.contiguous())
+
+    f = B.cce_router_forward(x, k)
+    assert len({t.untyped_storage().data_ptr() for t in f}) == 6 and f.losses.untyped_storage().nbytes() <= 64
+    before = [t._version for t in f]
+    f.counts.mul_(2)
+    assert [t._version for t in f] == [v + (name == "counts") for name, v in zip(f._fields, before)]
+    leaf = x.clone().requires_grad_()
+    weights, losses = Route.apply(leaf)
+    weights.grad_fn.counts.mul_(2)                                       # as after an all-reduce over two ranks of the same rows
+    (weights.sum() + (losses * torch.tensor([0.1, 0.01], device="cuda")).sum()).backward()
+    want = B.cce_router_backward(x, f.indices, f.lse, f.counts, torch.ones(N, k, device="cuda"), torch.tensor([0.1, 0.01], device="cuda"))
+    assert torch.equal(leaf.grad, want)
