@@ -44,7 +44,7 @@ typedef struct cce_matrix {
     float* momentum;      /* i/o fp32 [rows, cols]  zeros before the first step */
     int64_t rows, cols;
     float lr_scale;       /* this matrix's learning rate is lr * lr_scale */
-    float weight_decay;
+    float weight_decay;   /* param decays by 1 - lr * lr_scale * weight_decay, see cce_muon_multi_step */
     int32_t grad_bf16;    /* 0: grad is fp32, 1: bf16 */
     int32_t reserved;     /* 0 */
 } cce_matrix;
@@ -73,6 +73,9 @@ int cce_orthogonalize_multi(const cce_matrix* matrices, int64_t count, const flo
  *   G        = mu momentum + (1 - mu) g (nesterov != 0) or momentum
  *   param    = (1 - lr lr_scale weight_decay) param - lr lr_scale orthogonalised(G);   out_bf16 = its rounded copy
  *   clip_coef  in fp32 [1] device, may be NULL (= 1);   0 <= mu < 1;   lr, lr_scale, weight_decay >= 0
+ * Decay goes with the matrix's own learning rate, as in cce_optim.h.  The optimizer as published decays every matrix by 1 - lr * wd, its shape's
+ * factor in the update alone: weight_decay = wd / lr_scale is that.  (With wd itself and lr_scale = 0.2 sqrt(max(rows, cols)) a matrix of 14336
+ * rows decays 24 times as fast.)
  * Everything beside the products in fp32; the orthogonalised G goes into param without being rounded to 16 bits.
  */
 int cce_muon_multi_step(const cce_matrix* matrices, int64_t count, float lr, float mu, int32_t nesterov,

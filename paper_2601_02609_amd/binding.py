@@ -1310,7 +1310,9 @@ class MuonTensors(OptimTensors):
     grads         fp32 or bf16, two-dimensional, contiguous; the other lists are parallel to it
     params, momentum   fp32, of the same shapes (momentum: zeros before the first step)
     params_bf16   None, or the bf16 copies to keep (None for a matrix without one)
-    lr_scale, weight_decay   a number, or one for each matrix; lr_scale 0.2 sqrt(max(rows, cols)) makes updates as large as AdamW's"""
+    lr_scale, weight_decay   a number, or one for each matrix; lr_scale 0.2 sqrt(max(rows, cols)) makes updates as large as AdamW's
+    A parameter decays by 1 - lr lr_scale weight_decay.  Muon as published (and torch.optim.Muon) decays by 1 - lr wd whatever the shape: give
+    weight_decay = wd / lr_scale for that, one for each matrix."""
 
     _entry = _Matrix
 
