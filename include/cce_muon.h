@@ -20,6 +20,9 @@
  * made once on the device outside a capture; CCE_OK or a negative CCE_ERR_* code is returned and nothing is
  * enqueued on an error (CCE_ERR_HIP: as in cce.h).
  *
+ * Results do not depend on the run, but in their last bits on the list: the products of a list share their launches, and which tiles they take and
+ * which sums are split goes by all of them.
+ *
  * `matrices` is a HOST array, read before the call returns and not kept.  count >= 1.  A matrix with rows = 0 or
  * cols = 0 takes no part and its pointers are not looked at.  CCE_ERR_UNSUPPORTED: rows * cols, both rounded up to multiples
  * of 64, beyond 2^30, or the smaller side beyond 16384.  The memory of no two entries may overlap, nor the workspace any of it.

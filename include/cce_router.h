@@ -13,7 +13,8 @@
  *
  * A logit of -inf keeps an expert from a row: its p is 0 and it is never chosen; places of a row without an expert get index
  * -1 and weight 0.  A row whose label is ignore_index (padding) or that may use no expert takes no part: indices -1,
- * weights 0, lse 0, a gradient of 0; its logits may hold anything if the label says so.  A NaN ranks before all numbers and +inf
+ * weights 0, lse 0, a gradient of 0; its logits may hold anything if the label says so.  Labels here mark rows that nothing reads: those of
+ * the head's loss will not do where they ignore tokens that later ones attend to, as a prompt's in fine-tuning, which need their experts.  A NaN ranks before all numbers and +inf
  * next; both make NaN of the row's weights and lse, and so of P and both losses.
  *
  * Conventions are those of cce.h: DEVICE pointers owned by the caller, dense row-major, aligned to their elements; `stream`

@@ -1305,7 +1305,9 @@ def cce_adamw_state8_read(codes: torch.Tensor, scales: torch.Tensor, *, second: 
 # ---------------------------------------------------------------- include/cce_muon.h
 
 class MuonTensors(OptimTensors):
-    """The matrices of a Muon step, made once and given to every step, as OptimTensors is for the other tensors of a model.
+    """The matrices of a Muon step, made once and given to every step, as OptimTensors is for the other tensors of a model.  Making it takes the
+    host longer than a small step takes (48 matrices: 140 us, a step 16; set_grads 50), so that a training loop keeps it and its gradients'
+    memory (zero_grad(set_to_none=False)).
 
     grads         fp32 or bf16, two-dimensional, contiguous; the other lists are parallel to it
     params, momentum   fp32, of the same shapes (momentum: zeros before the first step)
@@ -1495,7 +1497,8 @@ def cce_router_forward(logits: torch.Tensor, top_k: int, labels: Optional[torch.
                        stream: Optional[torch.cuda.Stream] = None) -> RouterOutput:
     """The `top_k` experts of each row of `logits` (fp32 or bf16 [N, E]; -inf: not for this row), their softmax weights (of all experts'
     softmax, or with renormalize of the chosen ones'), the experts' counts, the balance loss and the z loss.  Rows whose label is
-    `ignore_index` take no part."""
+    `ignore_index` take no part and have no expert: `labels` marks padding, which no other token reads.  The labels of the loss will not do where
+    they ignore tokens that are read by later ones, as a prompt's in fine-tuning: those have to go through their experts."""
     N, E = _router_logits(logits)
     device = logits.device
     if labels is not None:
