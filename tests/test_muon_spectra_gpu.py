@@ -1,5 +1,6 @@
 """Accuracy of the orthogonalising entry points on matrices of every kind of spectrum, as the header promises it: the 2-norm of the difference
-from the oracle in 64 bits is at most 2^-9 of the result's, before any rounding of the result to bf16.
+from the oracle in 64 bits is at most 2^-9 of the result's, before any rounding of the result to bf16; 2^-13
+where the products' operands have 22 bits or 64.
 
 The five steps amplify what has the smallest singular values by up to 3.4445^5 = 485, so that a matrix of low rank shows every rounding of X
 that is not along its few directions.  The result is read where it is not rounded: a Muon step with lr = 1, no momentum and no decay takes
@@ -55,4 +56,4 @@ def test_result_is_within_the_promised_share(B, way, shape):
         want = M.orthogonalize(g, ABC, 5, EPS)
         off[kind] = float(np.linalg.norm(-p.cpu().numpy().astype(np.float64) - want) / np.linalg.norm(want))
     worst = max(off, key=off.get)
-    assert off[worst] <= 2.0 ** -9, (worst, off[worst], sum(x > 2.0 ** -9 for x in off.values()), len(off))
+    assert off[worst] <= (2.0 ** -13 if way in ("16", "32", "thin") else 2.0 ** -9), (worst, off[worst], len(off))
