@@ -13,7 +13,7 @@ GPU path, imports nothing from the package and is never called from the product 
     l      what X has beyond h, a whole number of 2^-8 of h's last place
     A      its diagonal apart, the rest in fp16
     M      = b A + c A A the same; but in the steps behind which the product of the a is 8 or more the diagonal is in the fp16 operand, and
-           only what that rounding leaves is apart
+           only what that rounding leaves is apart, and what is beyond 60
     X      a (h + l) + M's diagonal (h + l) + the rest of M h
 
 Of up to 64 rows all of M acts on X, with 22 bits of it; of up to 32 the rest of A and M have 22 bits too.
@@ -98,7 +98,7 @@ def orthogonalize_rounded(g, coefficients, steps, eps, pair=False):
             x = keep[:, None] * x + m @ _whole(x, 2.0 ** 13)
             continue
         if np.prod([abs(later[0]) for later in steps_left]) >= 8.0:
-            on_h = _half(keep - a, 2.0 ** 10)
+            on_h = _half(np.clip(keep - a, -60.0, 60.0), 2.0 ** 10)
             keep, m = keep - on_h, m + np.diag(on_h)
         x = keep[:, None] * (h + _rest(x, h)) + m @ h
     return x.T if tall else x

@@ -439,7 +439,8 @@ template <int MODE>
 __device__ __forceinline__ float on_diagonal(const NsProductArgs& a, float diagonal, _Float16& value) {
     value = (_Float16)0.f;
     if (MODE == kGram || !a.apart) return diagonal;
-    value = (_Float16)((diagonal - a.on_x) * kScaleM);
+    // (what is beyond fp16's range stays beside it: S2 S1 less both a may be up to 120)
+    value = (_Float16)__builtin_amdgcn_fmed3f((diagonal - a.on_x) * kScaleM, -61440.f, 61440.f);
     return diagonal - (float)value * (1.f / kScaleM);
 }
 

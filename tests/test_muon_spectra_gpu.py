@@ -57,3 +57,26 @@ def test_result_is_within_the_promised_share(B, way, shape):
         off[kind] = float(np.linalg.norm(-p.cpu().numpy().astype(np.float64) - want) / np.linalg.norm(want))
     worst = max(off, key=off.get)
     assert off[worst] <= (2.0 ** -13 if way in ("16", "32", "thin") else 2.0 ** -9), (worst, off[worst], len(off))
+
+
+def test_diagonal_of_two_steps_beyond_16_bits(B):
+    """Two steps taken as one: a + M is S2 S1, from -60 to 60, and what of it acts on X's 16 bits is that less both a, here 73 off: 2^10 times of it
+    is beyond fp16.  Rows that share no column, with singular values of 3 / 16 and 2 / 16, so that nothing lies beside the diagonals and X is
+    exact: what is left of these two steps are fp32's roundings, 20 of terms of up to 60 in S2 S1, times the value.  The other two steps move that by
+    their slopes, and take A from X's h, which is off by 2^-11 at most: a x + b h^2 x + c h^4 x is off by |2 b x^2 + 4 c x^4| |x| 2^-11.
+    (A first form of this bound, 2^-9 of the values, left the latter out.)"""
+    steps = np.array([[7.826710231582462, -29.774077595899662, 22.84695805183553], [7.653262981373687, -11.938443886507523, 3.712615484762357],
+                      [3.0, -1.2, 0.12], [3.0, -1.2, 0.12]], dtype=np.float32)
+    g = np.zeros((512, 1280), dtype=np.float32)
+    for i in range(29):
+        g[17 * i, 43 * i] = 3.0 if i < 28 else 2.0
+    s = np.array([3.0, 2.0]) / 16.0
+    allowed = 20 * 60 * 2.0 ** -24 * s
+    for k, (a, b, c) in enumerate(steps.astype(np.float64)):
+        if k >= 2:
+            allowed = np.abs(a + 3 * b * s ** 2 + 5 * c * s ** 4) * allowed + np.abs((2 * b * s ** 2 + 4 * c * s ** 4) * s) * 2.0 ** -11 + 2.0 ** -19 * np.abs(s)
+        s = a * s + b * s ** 3 + c * s ** 5
+    grad, param, momentum = torch.from_numpy(g).cuda(), torch.zeros(512, 1280, device="cuda"), torch.zeros(512, 1280, device="cuda")
+    B.cce_muon_multi_step(B.MuonTensors([grad], [param], [momentum]), lr=1.0, momentum=0.0, nesterov=False, steps=4, coefficients=steps, eps=0.0)
+    off = np.abs(-param.cpu().numpy().astype(np.float64) - np.where(g == 3.0, s[0], np.where(g == 2.0, s[1], 0.0)))
+    assert (off <= np.where(g == 3.0, allowed[0], np.where(g == 2.0, allowed[1], 0.0))).all(), (off.max(), allowed)
