@@ -2047,8 +2047,8 @@ static int64_t next_thin_group(const cce_matrix* matrices, int64_t count, int64_
 
 // Whether the first two steps of a matrix are taken as one, X = (S2 S1) X with A = S1 X X^T S1: a product of r c and one of 2 r c are
 // saved for three of r r.  Not in later steps: the first A, whose trace is 1, takes its operands' rounding better than they do (2-norm of the
-// error for 256 x 1024: of a matrix of noise 5.1e-4, 5.1 with the first two, 6.7 with the second and third; with a spectrum down to 1e-3 8.9,
-// 9.1 and 12.5).  us without / with: 32 x 512 x 2048 650 / 620, 8 x 896 x 3584 707 / 653, 16 x 1024 x 4096 1738 / 1580, 4 x 1500 x 4096 955 / 905,
+// error for 256 x 1024: of a matrix of noise 7.2e-4, 7.1 with the first two, 8.7 with the second and third; with a spectrum down to 1e-3 6.8,
+// 6.8 and 9.1).  us without / with: 32 x 512 x 2048 650 / 620, 8 x 896 x 3584 707 / 653, 16 x 1024 x 4096 1738 / 1580, 4 x 1500 x 4096 955 / 905,
 // 3584 x 14336 3290 / 2960, a 24-layer model 7520 / 7130; 512 x 1088 254 / 260, 1024 x 2176 375 / 379: nothing gained below 2.5 columns a row.
 static bool pairs_steps(const cce_matrix& t) {
     const NsLayout at((int)t.rows, (int)t.cols);
