@@ -14,7 +14,8 @@
 // linear part a X carries small directions next to large ones.  So the diagonals of A and M are kept in fp32 and taken out of the
 // 16-bit operands (M's in the later steps alone, see apart_steps), and the linear part is taken from X as h + l, a 16-bit and an 8-bit value.
 // Largest error (2-norm, of the result's) over matrices of rank 1 to 64, with noise and without, of noise, and with singular values down to 1e-4:
-// 1.4e-3 (512 x 1280 of rank 1; others 0.7 to 1.2), of noise 0.6 to 1.2e-3; bf16's rounding of a result adds 1.7e-3.
+// 1.4e-3 (512 x 1280 of rank 1; others 0.7 to 1.2), of noise 0.6 to 1.2e-3; bf16's rounding of a result adds 1.7e-3.  Of ones, or blocks
+// of ones, where all values round alike: up to 8e-3.
 //
 // Scales, powers of two: X 2^13, A 2^13, M 2^10; l see split1.  Singular values stay below 2.5 (checked for the coefficients),
 // values of X too; A's are below 6.25 and M's below 60: within fp16's 65504.

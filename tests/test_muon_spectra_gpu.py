@@ -80,3 +80,22 @@ def test_diagonal_of_two_steps_beyond_16_bits(B):
     B.cce_muon_multi_step(B.MuonTensors([grad], [param], [momentum]), lr=1.0, momentum=0.0, nesterov=False, steps=4, coefficients=steps, eps=0.0)
     off = np.abs(-param.cpu().numpy().astype(np.float64) - np.where(g == 3.0, s[0], np.where(g == 2.0, s[1], 0.0)))
     assert (off <= np.where(g == 3.0, allowed[0], np.where(g == 2.0, allowed[1], 0.0))).all(), (off.max(), allowed)
+
+
+@pytest.mark.parametrize("blocks", [1, 3, 12])
+@pytest.mark.parametrize("shape", [(36, 48), (60, 204), (120, 144), (192, 204), (528, 1320)], ids=lambda s: f"{s[0]}x{s[1]}")
+def test_values_that_round_alike(B, shape, blocks):
+    """Blocks of ones along the diagonal: all singular values are s = blocks^-1/2, all values round the same way, and nothing evens out.  A step's
+    operands are off by 2^-11 each, h twice in A and once in the last product, A and M once: x (2 |b| l + 4 |c| l l + ...) as below, l = s s, with the
+    signs that the terms of one operand have; the steps behind multiply that by their slopes."""
+    m, n = shape
+    g = np.kron(np.eye(blocks), np.ones((m // blocks, n // blocks))).astype(np.float32)
+    s, allowed = blocks ** -0.5, 0.0
+    for a, b, c in np.broadcast_to(np.array(ABC, dtype=np.float32).astype(np.float64), (5, 3)):
+        l = s * s
+        allowed = abs(a + 3 * b * l + 5 * c * l * l) * allowed + s * 2.0 ** -11 * (abs(2 * b * l + 4 * c * l * l) + abs(b * l + 2 * c * l * l) + 2 * abs(b * l + c * l * l))
+        s = a * s + b * s ** 3 + c * s ** 5
+    grad, param, momentum = (torch.from_numpy(x).cuda() for x in (g, 0 * g, 0 * g))
+    B.cce_muon_multi_step(B.MuonTensors([grad], [param], [momentum]), lr=1.0, momentum=0.0, nesterov=False)
+    off = float(np.linalg.norm(-param.cpu().numpy().astype(np.float64) - g * (s * blocks / (m * n) ** 0.5)) / (abs(s) * blocks ** 0.5))
+    assert off <= 1.05 * allowed / abs(s) + 2.0 ** -13                     # (second order; fp32 and the remainder's eight bits)
