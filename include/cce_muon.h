@@ -9,9 +9,10 @@
  *
  * Products take operands of 16 bits (fp16, power-of-two scales) and add in fp32; the diagonals of A and of b A + c A A
  * and what X loses by its rounding are held beside them.  With the coefficients 3.4445, -4.7750, 2.0315 and five steps the result, before it is
- * rounded to bf16, is within 2^-9 of the formula's (2-norm of the difference over that of the result), of low rank too: less than bf16's
- * rounding may add.  (Matrices of a few different values, as one of ones, whose values all round the same way so that nothing evens out: 8e-3
- * at most where it was tried.)  Coefficients and steps that amplify the smallest singular values more than those do (485 times) amplify what is rounded
+ * rounded to bf16, is off by 0.6 to 1.4e-3 of its 2-norm as a rule (what bf16's rounding adds is 1.7e-3), of low rank too, and by less than 2^-9 of it
+ * unless roundings do not even out: where a few rows and columns hold nearly all of a few directions it is up to 2^-7 (5e-3 where it was tried, 6e-3
+ * from 512 rows and 2.5 columns a row on, where two steps are taken as one), and of values that all round the same way, as a matrix of ones, 8e-3.
+ * Coefficients and steps that amplify the smallest singular values more than those do (485 times) amplify what is rounded
  * along them as well.  Matrices with a side of up to 16, and thin ones (up to 64, the other side beyond 768 to 1024) take 64-bit products,
  * those with a side of up to 32 products of 22-bit operands: within 2^-13.
  *

@@ -15,7 +15,8 @@
 // 16-bit operands (M's in the later steps alone, see apart_steps), and the linear part is taken from X as h + l, a 16-bit and an 8-bit value.
 // Largest error (2-norm, of the result's) over matrices of rank 1 to 64, with noise and without, of noise, and with singular values down to 1e-4:
 // 1.4e-3 (512 x 1280 of rank 1; others 0.7 to 1.2), of noise 0.6 to 1.2e-3; bf16's rounding of a result adds 1.7e-3.  Of ones, or blocks
-// of ones, where all values round alike: up to 8e-3.
+// of ones, where all values round alike: up to 8e-3.  Of few directions on a few large rows and columns, where few roundings count: 1.3e-3 in the
+// middle, 2.6e-3 at most (4.8e-3 of 33 to 64 rows); with two steps as one, whose M is four times as large and multiplies h's rounding, 2.1e-3 and 6.2e-3.
 //
 // Scales, powers of two: X 2^13, A 2^13, M 2^10; l see split1.  Singular values stay below 2.5 (checked for the coefficients),
 // values of X too; A's are below 6.25 and M's below 60: within fp16's 65504.
@@ -359,8 +360,11 @@ __device__ __forceinline__ void read8(const CCE_LDS float* p, float (&x)[8]) {
     }
 }
 
-// The symmetric products.  All matrices but X are polynomials of one A: they are symmetric, and any two of them commute.
-enum : int { kGram, kPoly, kProduct };
+// The symmetric products.  All matrices but X are polynomials of one A: they are symmetric, and any two of them commute, up to their rounding.
+// The last product of two steps taken as one is computed in full, T S: a tile's mirror image would be of S T, in which S = 3.4 along the smaller
+// directions multiplies what T's rounding turns the large ones to, where T S has its 0.7 (rank 1, 512 x 1280 0.7e-3 instead of 1.4, with a few large rows
+// and columns 3e-3 instead of 7).
+enum : int { kGram, kPoly, kProduct, kWholeProduct };
 enum SymKind : uint32_t {
     kOfX,                      // A = X X^T
     kOfA,                      // M = b A + c A A
@@ -372,7 +376,7 @@ enum SymKind : uint32_t {
     kBoth                      // a + M = T S
 };
 
-// Operands X, Y and the result with the diagonals that are held beside them.
+// Operands X, Y and the result Y X with the diagonals that are held beside them.
 struct SymBuffers {
     const _Float16* x;
     const _Float16* y;
@@ -400,16 +404,26 @@ struct SymBuffers {
             out = (_Float16*)(base + (last ? at.m : to_t ? at.t : at.s));
             dout = (float*)(base + (last ? at.dm : to_t ? at.dt : at.ds));
             add = last ? 0.f : a.a;
-        } else {
+        } else if (MODE == kProduct) {
             x = (const _Float16*)(base + (to_t ? at.a : at.t));
             y = (const _Float16*)(base + at.s);
             dx = (const float*)(base + (to_t ? at.da : at.dt));
             dy = (const float*)(base + at.ds);
-            out = (_Float16*)(base + (last ? at.m : to_t ? at.t : at.a));
-            dout = (float*)(base + (last ? at.dm : to_t ? at.dt : at.da));
-            of_x = last ? 1.f / kScaleM : 1.f / kScaleA;
-            add = last ? -a.a : 0.f;
-            scale = last ? kScaleM : kScaleA;
+            out = (_Float16*)(base + (to_t ? at.t : at.a));
+            dout = (float*)(base + (to_t ? at.dt : at.da));
+            of_x = 1.f / kScaleA;
+            add = 0.f;
+            scale = kScaleA;
+        } else {
+            x = (const _Float16*)(base + at.s);
+            y = (const _Float16*)(base + at.t);
+            dx = (const float*)(base + at.ds);
+            dy = (const float*)(base + at.dt);
+            out = (_Float16*)(base + at.m);
+            dout = (float*)(base + at.dm);
+            of_x = 1.f / kScaleM;
+            add = -a.a;
+            scale = kScaleM;
         }
         panel = last;
     }
@@ -445,6 +459,14 @@ __device__ __forceinline__ float on_diagonal(const NsProductArgs& a, float diago
     return diagonal - (float)value * (1.f / kScaleM);
 }
 
+// Tile w of a matrix of `side` x `side` tiles.
+template <int MODE>
+__device__ __forceinline__ void tile_of(int w, int side, int& i, int& j) {
+    if (MODE != kWholeProduct) return triangle(w, i, j);
+    i = w / side;
+    j = w - i * side;
+}
+
 // A tile and its mirror image.
 template <int MODE>
 __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(const NsProductArgs a) {
@@ -457,7 +479,7 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
     SymBuffers of;
     of.init<MODE>(a, at, base);
     int ti, tj;
-    triangle((int)(id - (a.first[i] >> 1)), ti, tj);
+    tile_of<MODE>((int)(id - (a.first[i] >> 1)), (at.rp + SymTile::BM - 1) / SymTile::BM, ti, tj);
     const int m0 = __builtin_amdgcn_readfirstlane(ti * SymTile::BM), n0 = __builtin_amdgcn_readfirstlane(tj * SymTile::BN);
     f32x16 acc[SymTile::TM][SymTile::TN];
 #pragma unroll
@@ -477,7 +499,7 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
     const int wm = m0 + wave_m<SymTile>() * 64, wn = n0 + wave_n<SymTile>() * 64;      // this wavefront's corner
     const int q = (lane & 7) * 8;                                                      // this lane's columns
     const int m = wm + q;
-    const bool inside_m = m < at.rp;
+    const bool inside_m = m < at.rp, mirrored = MODE != kWholeProduct && m0 != n0;
     f32x4 dc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
     if (MODE != kGram && inside_m) {
         dc[0] = *(const f32x4*)(of.dx + m);
@@ -495,7 +517,7 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
                 const bool there = inside_m && n < at.rp;
                 const uint32_t place = there ? (uint32_t)n * (uint32_t)at.rp + m : 0u;
                 ox[k] = *(const f16x8*)(of.x + place);
-                if (MODE == kProduct) oy[k] = *(const f16x8*)(of.y + place);
+                if (MODE >= kProduct) oy[k] = *(const f16x8*)(of.y + place);
                 dn[k] = of.dy[there ? n : 0];
             }
         }
@@ -526,13 +548,13 @@ __global__ __launch_bounds__(SymTile::kThreads, 2) void ns_symmetric_kernel(cons
                 v[e] = value;
             }
             if (inside) *(f16x8*)of.at_place(at, n, m) = v;
-            if (m0 != n0)
+            if (mirrored)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) mirror[(q + e) * kSymMirror + bn * 32 + y] = v[e];
         }
         wave_lds_order();
     }
-    if (m0 == n0) return;
+    if (!mirrored) return;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const int y = 8 * k + (lane >> 3), row = wm + y, col = wn + q;                 // of the mirrored tile
@@ -557,6 +579,7 @@ __device__ __forceinline__ void symmetric_ping_rows(const NsProductArgs& a, cons
     CCE_LDS float* const rows = (CCE_LDS float*)smem;
     CCE_LDS _Float16* const mirror = (CCE_LDS _Float16*)(smem + 64 * kPingPitch * 4);
     const int q = (lane & 3) * 8, nw = n0 + wn * SymPing::TNR;
+    const bool mirrored = MODE != kWholeProduct && ti != tj;
 #pragma unroll
     for (int part = 0; part < 2; ++part) {
         const int mw = m0 + part * (SymPing::BM / 2) + wm * 32, m = mw + q;            // 32 columns of the result
@@ -576,7 +599,7 @@ __device__ __forceinline__ void symmetric_ping_rows(const NsProductArgs& a, cons
                     const int n = nw + 64 * side + 16 * k + (lane >> 2);
                     const uint32_t place = n < at.rp ? (uint32_t)n * (uint32_t)at.rp + m : 0u;
                     ox[k] = *(const f16x8*)(of.x + place);
-                    if (MODE == kProduct) oy[k] = *(const f16x8*)(of.y + place);
+                    if (MODE >= kProduct) oy[k] = *(const f16x8*)(of.y + place);
                     dn[k] = of.dy[n < at.rp ? n : 0];
                 }
             }
@@ -602,13 +625,13 @@ __device__ __forceinline__ void symmetric_ping_rows(const NsProductArgs& a, cons
                     v[e] = value;
                 }
                 if (n < at.rp) *(f16x8*)of.at_place(at, n, m) = v;
-                if (ti != tj)
+                if (mirrored)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) mirror[(q + e) * kPingMirror + 64 * side + y] = v[e];
             }
             wave_lds_order();
         }
-        if (ti != tj) {
+        if (mirrored) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const int y = 4 * k + (lane >> 4), row = mw + y, col = nw + (lane & 15) * 8;     // of the mirrored tile
@@ -634,7 +657,7 @@ __global__ __launch_bounds__(SymPing::kThreads, 2) void ns_symmetric_ping_kernel
     SymBuffers of;
     of.init<MODE>(a, at, workspace_of(a, i));
     int ti, tj;
-    triangle((int)(tile - (a.first[i] >> 1)), ti, tj);
+    tile_of<MODE>((int)(tile - (a.first[i] >> 1)), (at.rp + SymPing::BM - 1) / SymPing::BM, ti, tj);
     ti = __builtin_amdgcn_readfirstlane(ti);
     tj = __builtin_amdgcn_readfirstlane(tj);
     const int m0 = ti * SymPing::BM, n0 = tj * SymPing::BN;
@@ -710,7 +733,7 @@ __global__ __launch_bounds__(64) void ns_symmetric_join_kernel(const NsProductAr
     SymBuffers of;
     of.init<MODE>(a, at, workspace_of(a, i));
     int ti, tj;
-    triangle((int)(tile - (a.first[i] >> 1)), ti, tj);
+    tile_of<MODE>((int)(tile - (a.first[i] >> 1)), (at.rp + SymPing::BM - 1) / SymPing::BM, ti, tj);
     const f32x4* from = (const f32x4*)(a.ws + (uint64_t)a.partials * 256) + ((size_t)split * a.splits * 8 + wave) * (SymPing::NA * SymPing::NB * 64) + threadIdx.x;
     f32x4 acc[SymPing::NA][SymPing::NB];
 #pragma unroll
@@ -2008,10 +2031,10 @@ static uint32_t apart_steps(const float* coefficients, int steps) {
     return apart;
 }
 
-static uint32_t sym_tiles(const NsLayout& at, bool large) {
+static uint32_t sym_tiles(const NsLayout& at, bool large, bool whole) {
     const int side = large ? SymPing::BM : SymTile::BM;
     const uint32_t n = (uint32_t)((at.rp + side - 1) / side);
-    return n * (n + 1) / 2;
+    return whole ? n * n : n * (n + 1) / 2;
 }
 static uint32_t apply_tiles(const NsLayout& at, bool large) {
     const int rows = large ? TurnTile::BN : ApplyTile::BN;
@@ -2047,10 +2070,10 @@ static int64_t next_thin_group(const cce_matrix* matrices, int64_t count, int64_
 }
 
 // Whether the first two steps of a matrix are taken as one, X = (S2 S1) X with A = S1 X X^T S1: a product of r c and one of 2 r c are
-// saved for three of r r.  Not in later steps: the first A, whose trace is 1, takes its operands' rounding better than they do (2-norm of the
+// saved for four of r r.  Not in later steps: the first A, whose trace is 1, takes its operands' rounding better than they do (2-norm of the
 // error for 256 x 1024: of a matrix of noise 7.2e-4, 7.1 with the first two, 8.7 with the second and third; with a spectrum down to 1e-3 6.8,
-// 6.8 and 9.1).  us without / with: 32 x 512 x 2048 650 / 620, 8 x 896 x 3584 707 / 653, 16 x 1024 x 4096 1738 / 1580, 4 x 1500 x 4096 955 / 905,
-// 3584 x 14336 3290 / 2960, a 24-layer model 7520 / 7130; 512 x 1088 254 / 260, 1024 x 2176 375 / 379: nothing gained below 2.5 columns a row.
+// 6.8 and 9.1).  What they cost in accuracy is where few roundings count, see the head.  us without / with: 32 x 512 x 2048 655 / 627, 8 x 896 x 3584 730 / 683, 16 x 1024 x 4096 1768 / 1616, 4 x 1500 x 4096 975 / 936,
+// 3584 x 14336 3385 / 3050, a 24-layer model 7657 / 7332; 512 x 1088 254 / 260, 1024 x 2176 375 / 379: nothing gained below 2.5 columns a row.
 static bool pairs_steps(const cce_matrix& t) {
     const NsLayout at((int)t.rows, (int)t.cols);
     return at.rp >= kPairRows && 2 * at.cp >= 5 * at.rp;               // (S and T, and their diagonals, lie in a copy of h)
@@ -2204,7 +2227,7 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
     if (!run_small(matrices, count, step, lr, mu, nesterov, coefficients, steps, eps, clip_coef, stream)) return CCE_ERR_HIP;
     if (!run_thin(matrices, count, step, lr, mu, nesterov, coefficients, steps, eps, clip_coef, workspace, stream)) return CCE_ERR_HIP;
     NsArgs a;
-    NsProductArgs products[3];                         // gram, poly, apply
+    NsProductArgs products[4];                         // gram, poly, apply, whole products
     a.ws = (char*)workspace;
     for (auto& p : products) p.ws = (char*)workspace;
     a.clip_coef = clip_coef;
@@ -2224,8 +2247,10 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
         });
         if (n == 0) continue;
         if (!allow_lds(ns_symmetric_kernel<kGram>, kSymLds) || !allow_lds(ns_symmetric_kernel<kPoly>, kSymLds) ||
-            !allow_lds(ns_symmetric_kernel<kProduct>, kSymLds) || !allow_lds(ns_symmetric_ping_kernel<kGram>, kPingLds) ||
+            !allow_lds(ns_symmetric_kernel<kProduct>, kSymLds) || !allow_lds(ns_symmetric_kernel<kWholeProduct>, kSymLds) ||
+            !allow_lds(ns_symmetric_ping_kernel<kGram>, kPingLds) ||
             !allow_lds(ns_symmetric_ping_kernel<kPoly>, kPingLds) || !allow_lds(ns_symmetric_ping_kernel<kProduct>, kPingLds) ||
+            !allow_lds(ns_symmetric_ping_kernel<kWholeProduct>, kPingLds) ||
             !allow_lds(ns_apply_kernel<false>, ApplyTile::kLdsBytes) || !allow_lds(ns_apply_kernel<true>, ApplyTile::kLdsBytes) ||
             !allow_lds(ns_apply_turn_kernel<false>, kTurnLds) || !allow_lds(ns_apply_turn_kernel<true>, kTurnLds))
             return CCE_ERR_HIP;
@@ -2244,13 +2269,13 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
             }
         };
         // the matrices with the longest sums of a product first: the shorter ones fill what they leave
-        uint32_t grid[3];
-        bool large[3];
-        for (int op = 0; op < 3; ++op) {
+        uint32_t grid[4];
+        bool large[4];
+        for (int op = 0; op < (pairs ? 4 : 3); ++op) {
             NsProductArgs& p = products[op];
             int order[kGroup];
             auto length = [&](int x) { return op == 0 ? layout(x).cp : layout(x).rp; };
-            auto tiles = [&](int x, bool of_256) { return op < 2 ? sym_tiles(layout(x), of_256) : apply_tiles(layout(x), of_256); };
+            auto tiles = [&](int x, bool of_256) { return op == 2 ? apply_tiles(layout(x), of_256) : sym_tiles(layout(x), of_256, op == 3); };
             for (int k = 0; k < n; ++k) {
                 int to = k;
                 for (; to > 0 && length(order[to - 1]) < length(k); --to) order[to] = order[to - 1];
@@ -2285,7 +2310,7 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
         int s = 0;
         auto symmetric = [&](auto mode, uint32_t kind) {
             constexpr int MODE = decltype(mode)::value;
-            const int op = MODE == kGram ? 0 : 1;
+            const int op = MODE == kGram ? 0 : MODE == kWholeProduct ? 3 : 1;
             NsProductArgs& p = products[op];
             p.kind = kind;
             p.apart = (kind == kOfA || kind == kBoth) ? apart >> s & 1u : 0u;
@@ -2297,6 +2322,7 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
         constexpr std::integral_constant<int, kGram> gram{};
         constexpr std::integral_constant<int, kPoly> poly{};
         constexpr std::integral_constant<int, kProduct> product{};
+        constexpr std::integral_constant<int, kWholeProduct> whole{};
         uint32_t flip = 0;
         for (; s < steps; ++s) {
             for (auto& p : products) p.flip = flip;
@@ -2308,7 +2334,7 @@ static int run_groups(const cce_matrix* matrices, int64_t count, bool step, floa
                 symmetric(product, kNextA);
                 coefficients_of(++s);
                 symmetric(poly, kSecond);
-                symmetric(product, kBoth);
+                symmetric(whole, kBoth);
             } else {
                 symmetric(poly, kOfA);
             }

@@ -1,6 +1,5 @@
-"""Accuracy of the orthogonalising entry points on matrices of every kind of spectrum, as the header promises it: the 2-norm of the difference
-from the oracle in 64 bits is at most 2^-9 of the result's, before any rounding of the result to bf16; 2^-13
-where the products' operands have 22 bits or 64.
+"""Accuracy of the orthogonalising entry points on matrices of every kind of spectrum: the 2-norm of the difference from the oracle in 64 bits, before any
+rounding of the result to bf16.  The header promises 2^-9 of the result's, and 2^-13 where the products' operands have 22 bits or 64.
 
 The five steps amplify what has the smallest singular values by up to 3.4445^5 = 485, so that a matrix of low rank shows every rounding of X
 that is not along its few directions.  The result is read where it is not rounded: a Muon step with lr = 1, no momentum and no decay takes
@@ -99,3 +98,22 @@ def test_values_that_round_alike(B, shape, blocks):
     B.cce_muon_multi_step(B.MuonTensors([grad], [param], [momentum]), lr=1.0, momentum=0.0, nesterov=False)
     off = float(np.linalg.norm(-param.cpu().numpy().astype(np.float64) - g * (s * blocks / (m * n) ** 0.5)) / (abs(s) * blocks ** 0.5))
     assert off <= 1.05 * allowed / abs(s) + 2.0 ** -13                     # (second order; fp32 and the remainder's eight bits)
+
+
+@pytest.mark.parametrize("shape", [(50, 255), (79, 1463), (89, 420), (254, 375), (468, 1554), (1554, 470)], ids=lambda s: f"{s[0]}x{s[1]}")
+def test_few_directions_on_few_rows_and_columns(B, shape):
+    """Rank 1, 2 and 9 with most of it in a few rows and columns, so that few roundings count: as far off as the oracle's form that rounds where the
+    kernels do, r, half as much more for what fp32's sums change in later roundings, and 2^-10 over the square root of the smaller side where r is
+    small by chance (as for the matrices of the other tests).  The header's 2^-7 holds as well."""
+    m, n = shape
+    for seed in range(4):
+        rng = np.random.default_rng(1000 * seed + m)
+        for rank, noise in ((1, 0.0), (1, 2e-4), (2, 0.0), (9, 1e-5)):
+            g = rng.standard_normal((m, rank)) @ rng.standard_normal((rank, n)) + noise * rng.standard_normal((m, n))
+            g = (g * np.exp(2.0 * rng.standard_normal((m, 1))) * np.exp(2.0 * rng.standard_normal((1, n)))).astype(np.float32)
+            grad, param, momentum = (torch.from_numpy(x).cuda() for x in (g, 0 * g, 0 * g))
+            B.cce_muon_multi_step(B.MuonTensors([grad], [param], [momentum]), lr=1.0, momentum=0.0, nesterov=False)
+            want = M.orthogonalize(g, ABC, 5, EPS)
+            r = np.linalg.norm(M.orthogonalize_rounded(g, ABC, 5, EPS, min(shape) >= 449 and 2 * max(shape) >= 5 * min(shape)) - want)
+            off, size = float(np.linalg.norm(-param.cpu().numpy().astype(np.float64) - want)), float(np.linalg.norm(want))
+            assert off <= 1.5 * r + 2.0 ** -10 / min(shape) ** 0.5 * size and off <= 2.0 ** -7 * size, (rank, noise, seed, off / size, r / size)
