@@ -16,7 +16,7 @@
 // Largest error (2-norm, of the result's) over matrices of rank 1 to 64, with noise and without, of noise, and with singular values down to 1e-4:
 // 1.4e-3 (512 x 1280 of rank 1; others 0.7 to 1.2), of noise 0.6 to 1.2e-3; bf16's rounding of a result adds 1.7e-3.  Of ones, or blocks
 // of ones, where all values round alike: up to 8e-3.  Of few directions on a few large rows and columns, where few roundings count: 1.3e-3 in the
-// middle, 2.6e-3 at most (4.8e-3 of 33 to 64 rows); with two steps as one, whose M is four times as large and multiplies h's rounding, 2.1e-3 and 6.2e-3.
+// middle, 3.6e-3 at most (4.8e-3 of 33 to 64 rows); with two steps as one, whose M is four times as large and multiplies h's rounding, 2.1e-3 and 6.2e-3.
 //
 // Scales, powers of two: X 2^13, A 2^13, M 2^10; l see split1.  Singular values stay below 2.5 (checked for the coefficients),
 // values of X too; A's are below 6.25 and M's below 60: within fp16's 65504.
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(const NsArgs a) {
 
 // x as h + l: h has x's first 11 bits, l the next eight, as a whole number of 2^-8 of h's last place, 128 more so that it is positive.  (Four bits
 // in E4M3 left 4e-3 of the results of matrices of rank 1, X's first rounding amplified by the steps; these leave 0.7 to 1.4e-3, and cost a
-// tiled call of large matrices 1 %.)
+// tiled call next to nothing.)
 __device__ __forceinline__ uint32_t exponent_bits(_Float16 h) {          // 2^e for h of [2^e, 2^(e + 1)); 2^-14 for less, as h's last place is
     const uint32_t u = __float_as_uint((float)h) & 0x7f800000u;
     return u > 0x38800000u ? u : 0x38800000u;
@@ -450,7 +450,8 @@ __device__ __forceinline__ float symmetric_value(const NsProductArgs& a, const S
 }
 
 // Value n of the diagonal: what of it is held beside the operand, and the operand's where it is not 0.
-// Behind the store of the lane's eight values, which has a 0 in its place: by value inside them a join took 28 us, so 21 (4 x 4096 x 4096).
+// Behind the store of the lane's eight values, which has a 0 in its place: a rounding for each of the
+// eight, where it is needed once a row, took 11 us more of 256 x 256 (179) and 70 of 4 x 4096 x 4096 (5320).
 template <int MODE>
 __device__ __forceinline__ void give_diagonal(const NsProductArgs& a, const SymBuffers& of, const NsLayout& at, int n, float diagonal) {
     if (MODE != kGram && a.apart) {
@@ -2075,7 +2076,7 @@ static int64_t next_thin_group(const cce_matrix* matrices, int64_t count, int64_
 // saved for four of r r.  Not in later steps: the first A, whose trace is 1, takes its operands' rounding better than they do (2-norm of the
 // error for 256 x 1024: of a matrix of noise 7.2e-4, 7.1 with the first two, 8.7 with the second and third; with a spectrum down to 1e-3 6.8,
 // 6.8 and 9.1).  What they cost in accuracy is where few roundings count, see the head.  us without / with: 32 x 512 x 2048 655 / 627, 8 x 896 x 3584 730 / 683, 16 x 1024 x 4096 1768 / 1616, 4 x 1500 x 4096 975 / 936,
-// 3584 x 14336 3385 / 3050, a 24-layer model 7657 / 7332; 512 x 1088 254 / 260, 1024 x 2176 375 / 379: nothing gained below 2.5 columns a row.
+// 3584 x 14336 3385 / 3040, a 24-layer model 7657 / 7290; 512 x 1088 254 / 260, 1024 x 2176 375 / 379: nothing gained below 2.5 columns a row.
 static bool pairs_steps(const cce_matrix& t) {
     const NsLayout at((int)t.rows, (int)t.cols);
     return at.rp >= kPairRows && 2 * at.cp >= 5 * at.rp;               // (S and T, and their diagonals, lie in a copy of h)
