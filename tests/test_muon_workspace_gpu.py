@@ -77,3 +77,15 @@ def test_split_tiles_of_a_few_rows(B):
         _check(o, g)
     again = B.cce_orthogonalize_multi(x)
     assert all(torch.equal(a, b) for a, b in zip(out, again))
+
+
+@pytest.mark.parametrize("shape,count", [((1900, 5000), 5), ((5700, 2048), 5), ((600, 1600), 3), ((1100, 3000), 2)], ids=lambda x: "x".join(map(str, x)) if isinstance(x, tuple) else str(x))
+def test_whole_products_of_two_steps_taken_as_one(B, shape, count):
+    """The last product of the two steps, which is not mirrored: tiles of 256 x 256 with the last ones in parts of their sums, ragged ones among them, and
+    tiles of 128 x 128.  Each matrix of its own values, and the same bits again."""
+    x = _matrices([shape] * count)
+    x = [t * (1.0 + i) for i, t in enumerate(x)]
+    out = B.cce_orthogonalize_multi(x)
+    for o, g in zip(out, x):
+        _check(o, g)
+    assert all(torch.equal(a, b) for a, b in zip(out, B.cce_orthogonalize_multi(x)))
